@@ -1,6 +1,7 @@
 """MI355X (gfx950) RoutePack planner hot path -- Python binding.
 
-A thin ctypes layer over the C-ABI in include/routepack.h (libroutepack.so).
+A thin ctypes layer over the C-ABI in include/routepack.h and, for the
+router's operators, include/routepack/router.h (libroutepack.so).
 It only marshals arguments: torch supplies device memory and the current HIP
 stream, and every step of the path runs in the library's HIP kernels.  There
 is no CPU fallback: importing works without a GPU, but every call raises if
@@ -26,6 +27,9 @@ EXPORTS = ("routepack_aggregate_demand", "routepack_place_experts", "routepack_p
            "routepack_anneal", "routepack_eval_objective", "routepack_select_population",
            "routepack_row_lower_bound", "routepack_fixed_bin_search", "routepack_project_demand",
            "routepack_strerror")
+# the router's operators, declared in include/routepack/router.h
+ROUTER_EXPORTS = ("routepack_route_tokens", "routepack_count_demand", "routepack_balance_workspace",
+                  "routepack_balance_loss", "routepack_route_backward")
 # measurement aid declared in include/routepack_probe.h (not part of the method),
 # built as its own library
 PROBE_EXPORTS = ("routepack_probe_lds_read",)
@@ -55,6 +59,12 @@ class _AnnealParams(C.Structure):
                 ("level_kernel_ms", C.POINTER(C.c_double)), ("level_kernel", C.POINTER(C.c_int32))]
 
 
+class _Rows(C.Structure):
+    """routepack_logits and routepack_ids (the same fields)."""
+    _fields_ = [("data", C.c_void_p), ("type", C.c_int32), ("n_tokens", C.c_int64), ("token_stride", C.c_int64),
+                ("layer_stride", C.c_int64)]
+
+
 _lib = None
 
 
@@ -78,11 +88,20 @@ def load_library():
         lib.routepack_row_lower_bound.argtypes = [P, vp, C.POINTER(C.c_int32), C.POINTER(C.c_int64), vp]
         lib.routepack_fixed_bin_search.argtypes = [P, vp, i32, i64, C.POINTER(C.c_int32), C.POINTER(C.c_int64), vp,
                                                    vp]
+        R, f32 = C.POINTER(_Rows), C.c_float
+        lib.routepack_route_tokens.argtypes = [P, R, R, vp, i32, i32, f32, vp, vp, vp]
+        lib.routepack_count_demand.argtypes = [P, R, vp, vp, vp]
+        lib.routepack_balance_workspace.argtypes = [P, i64, i32]
+        lib.routepack_balance_loss.argtypes = [P, R, i32, vp, vp, i32, i32, vp, vp, vp, i64, vp]
+        lib.routepack_route_backward.argtypes = [P, R, R, vp, i32, f32, i32, vp, vp, i32, vp, i32, vp, vp]
         lib.routepack_strerror.argtypes = [C.c_int]
         lib.routepack_strerror.restype = C.c_char_p
         for f in EXPORTS:
             if f != "routepack_strerror":
                 getattr(lib, f).restype = C.c_int
+        for f in ROUTER_EXPORTS:
+            getattr(lib, f).restype = C.c_int
+        lib.routepack_balance_workspace.restype = C.c_int64
         _lib = lib
     return _lib
 
@@ -345,3 +364,181 @@ def fixed_bin_search(prob: Problem, lengths, n_rows, node_budget):
            lib.routepack_fixed_bin_search(prob.ref, _ptr(t), int(n_rows), int(node_budget), C.byref(st),
                                           C.byref(nodes), _ptr(lay), _stream()))
     return int(st.value), int(nodes.value), (lay if st.value == 1 else None)
+
+
+# -- the router's operators (include/routepack/router.h) ----------------------
+
+SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+def _router_types():
+    import torch
+    return ({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2},
+            {torch.uint8: 3, torch.int16: 4, torch.int32: 5, torch.int64: 6})
+
+
+class _Call:
+    """One call's tensors: checks that they share a GPU, hands out pointers,
+    and runs the call on that GPU's current stream."""
+
+    def __init__(self, fn):
+        self.fn, self.device = fn, None
+
+    def tensor(self, name, x, dtypes, shape=None):
+        torch = _torch()
+        if not isinstance(x, torch.Tensor):
+            raise TypeError(f"{self.fn}: {name} must be a tensor, got {type(x).__name__}")
+        if not x.is_cuda or (self.device is not None and x.device != self.device):
+            raise ValueError(f"{self.fn}: {name} is on {x.device}, expected {self.device or 'a GPU'}")
+        self.device = x.device
+        if x.dtype not in dtypes:
+            raise ValueError(f"{self.fn}: {name} has type {x.dtype}")
+        if shape is not None and tuple(x.shape) != tuple(shape):
+            raise ValueError(f"{self.fn}: {name} has shape {tuple(x.shape)}, expected {tuple(shape)}")
+        return x
+
+    def dense(self, name, x, dtypes, shape):
+        x = self.tensor(name, x, dtypes, shape)
+        if not x.is_contiguous():
+            raise ValueError(f"{self.fn}: {name} must be contiguous")
+        return x
+
+    def rows(self, name, x, dtypes, L, last):
+        """[T][L][last], or [T][last] where L is 1, of any strides but the
+        last: (the tensor, its description for the library)."""
+        x = self.tensor(name, x, dtypes)
+        if x.dim() not in (2, 3) or x.shape[-1] != last or (x.shape[1] != L if x.dim() == 3 else L != 1):
+            raise ValueError(f"{self.fn}: {name} has shape {tuple(x.shape)}, expected [T][{L}][{last}]")
+        if last > 1 and x.stride(-1) != 1 and x.numel() > 0:
+            raise ValueError(f"{self.fn}: the last axis of {name} must be adjacent in memory")
+        return x, _Rows(x.data_ptr(), dtypes[x.dtype], x.shape[0], x.stride(0), x.stride(1) if x.dim() == 3 else 0)
+
+    def run(self, f, *args):
+        torch = _torch()
+        stream = C.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)
+        if self.device.index == torch.cuda.current_device():
+            _check(self.fn, f(*args, stream))
+        else:
+            with torch.cuda.device(self.device):
+                _check(self.fn, f(*args, stream))
+
+
+def _score(fn, score):
+    if score not in SCORES:
+        raise ValueError(f"{fn}: score is {score!r}, expected one of {sorted(SCORES)}")
+    return SCORES[score]
+
+
+def route_tokens(prob: Problem, logits, *, ids=None, bias=None, score="softmax", normalize=True, scale=1.0):
+    """The router's gates: (ids, gates), each [T][L][k] (or [T][k] for logits
+    [T][E]), k = prob.top_k.
+
+    logits [T][L][E] fp32, bf16 or fp16, any strides over tokens and layers.
+    Without `ids` the k experts of largest logit are chosen, or, with `bias`
+    (float32 [L][E]), of largest score + bias; ids are int32, -1 where no
+    expert is available (an expert is masked by a logit of -inf).  With `ids`
+    (uint8, int16, int32 or int64; a replayed record) the gates are those of
+    the recorded experts, and `ids` is returned as it is.  score: "softmax"
+    or "sigmoid"; normalize: divide by the sum over the token's choices."""
+    torch = _torch()
+    lib, call = load_library(), _Call("routepack_route_tokens")
+    floats, ints = _router_types()
+    z, zr = call.rows("logits", logits, floats, prob.n_layers, prob.n_experts)
+    shape = tuple(z.shape[:-1]) + (prob.top_k,)
+    b = None if bias is None else call.dense("bias", bias, (torch.float32,), (prob.n_layers, prob.n_experts))
+    rec = None
+    if ids is not None:
+        out, rec = call.rows("ids", ids, ints, prob.n_layers, prob.top_k)
+        if tuple(out.shape) != shape:
+            raise ValueError(f"{call.fn}: ids has shape {tuple(out.shape)}, expected {shape}")
+    else:
+        out = torch.empty(shape, dtype=torch.int32, device=z.device)
+    gates = torch.empty(shape, dtype=torch.float32, device=z.device)
+    call.run(lib.routepack_route_tokens, prob.ref, C.byref(zr), None if rec is None else C.byref(rec), _ptr(b),
+             _score(call.fn, score), int(bool(normalize)), float(scale), _ptr(out) if rec is None else None,
+             _ptr(gates))
+    return out, gates
+
+
+def count_demand(prob: Problem, ids, offsets):
+    """demand int32 [N][L][E]: how often each sample's tokens chose each
+    expert, the `demand` of aggregate_demand and place_experts.
+
+    ids [T][L][k] (or [T][k] where L is 1) uint8, int16, int32 or int64, any
+    strides over tokens and layers; ids outside [0, E) are not counted.
+    offsets int64 [N + 1], non-decreasing: sample i holds the tokens
+    [offsets[i], offsets[i + 1])."""
+    torch = _torch()
+    lib, call = load_library(), _Call("routepack_count_demand")
+    _, ints = _router_types()
+    x, xr = call.rows("ids", ids, ints, prob.n_layers, prob.top_k)
+    off = call.dense("offsets", offsets, (torch.int64,), (prob.n_samples + 1,))
+    demand = torch.empty((prob.n_samples, prob.n_layers, prob.n_experts), dtype=torch.int32, device=x.device)
+    call.run(lib.routepack_count_demand, prob.ref, C.byref(xr), _ptr(off), _ptr(demand))
+    return demand
+
+
+def _groups(call, prob, counts, offsets):
+    torch = _torch()
+    off = call.tensor("offsets", offsets, (torch.int64,))
+    if off.dim() != 1 or off.shape[0] < 2 or not off.is_contiguous():
+        raise ValueError(f"{call.fn}: offsets has shape {tuple(off.shape)}, expected [G + 1], contiguous, with G >= 1")
+    G = off.shape[0] - 1
+    _, ints = _router_types()
+    n = call.dense("counts", counts, (torch.int32, torch.int64), (G, prob.n_layers, prob.n_experts))
+    return G, off, n, ints[n.dtype]
+
+
+def balance_loss(prob: Problem, logits, counts, offsets, *, score="softmax"):
+    """The balance loss: (loss float32 [L], shares float32 [G][L][E]).
+
+    loss[l] = 1/G sum_g sum_e f[g][l][e] shares[g][l][e] with f the fraction of
+    the counts that expert e has, times E, and shares the mean over the
+    group's tokens of the scores divided by their sum.  counts int32 or int64
+    [G][L][E] (count_demand's result, or aggregate_demand's as [1][L][E] for
+    one group over the window); offsets int64 [G + 1]."""
+    torch = _torch()
+    lib, call = load_library(), _Call("routepack_balance_loss")
+    floats, _ = _router_types()
+    z, zr = call.rows("logits", logits, floats, prob.n_layers, prob.n_experts)
+    G, off, n, n_type = _groups(call, prob, counts, offsets)
+    loss = torch.empty(prob.n_layers, dtype=torch.float32, device=z.device)
+    shares = torch.empty((G, prob.n_layers, prob.n_experts), dtype=torch.float32, device=z.device)
+    size = lib.routepack_balance_workspace(prob.ref, z.shape[0], G)
+    work = torch.empty(max(size, 16), dtype=torch.uint8, device=z.device)
+    call.run(lib.routepack_balance_loss, prob.ref, C.byref(zr), G, _ptr(off), _ptr(n), n_type,
+             _score(call.fn, score), _ptr(loss), _ptr(shares), _ptr(work), work.numel())
+    return loss, shares
+
+
+def route_backward(prob: Problem, logits, *, ids=None, dgates=None, normalize=True, scale=1.0, counts=None,
+                   offsets=None, dloss=None, score="softmax"):
+    """dlogits, of the logits' shape and type, from the gradients of
+    route_tokens' gates (`ids`, `dgates` float32 of their shape, `normalize`,
+    `scale`), of balance_loss' loss (`counts`, `offsets`, `dloss` float32 [L]),
+    or of both in one pass."""
+    torch = _torch()
+    lib, call = load_library(), _Call("routepack_route_backward")
+    floats, ints = _router_types()
+    if (ids is None) != (dgates is None):
+        raise ValueError(f"{call.fn}: ids and dgates go together")
+    if (dloss is None) != (counts is None) or (dloss is None) != (offsets is None):
+        raise ValueError(f"{call.fn}: counts, offsets and dloss go together")
+    if ids is None and dloss is None:
+        raise ValueError(f"{call.fn}: neither dgates nor dloss given")
+    z, zr = call.rows("logits", logits, floats, prob.n_layers, prob.n_experts)
+    rec = dg = off = n = dl = None
+    G = n_type = 0
+    if ids is not None:
+        x, rec = call.rows("ids", ids, ints, prob.n_layers, prob.top_k)
+        if x.shape[:-1] != z.shape[:-1]:
+            raise ValueError(f"{call.fn}: ids has shape {tuple(x.shape)}, logits {tuple(z.shape)}")
+        dg = call.dense("dgates", dgates, (torch.float32,), x.shape)
+    if dloss is not None:
+        G, off, n, n_type = _groups(call, prob, counts, offsets)
+        dl = call.dense("dloss", dloss, (torch.float32,), (prob.n_layers,))
+    dz = torch.empty(z.shape, dtype=z.dtype, device=z.device)
+    call.run(lib.routepack_route_backward, prob.ref, C.byref(zr), None if rec is None else C.byref(rec), _ptr(dg),
+             int(bool(normalize)), float(scale), G, _ptr(off), _ptr(n), n_type, _ptr(dl), _score(call.fn, score),
+             _ptr(dz))
+    return dz
