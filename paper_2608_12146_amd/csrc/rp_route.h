@@ -16,6 +16,22 @@ namespace rp {
 constexpr float kInf = __builtin_inff();
 constexpr int kMaxExperts = 2048, kMaxChoices = 32;
 
+struct RouteArgs {
+    const void *logits;
+    int64_t ts, ls;      // strides of the logits
+    int64_t T;
+    int32_t L, E, k;
+    const void *rec;     // replayed ids, or null
+    int32_t rec_type;
+    int64_t rts, rls;    // their strides
+    const float *bias;
+    int32_t score;
+    bool normalize;
+    float scale;
+    int32_t *ids;
+    float *gates;
+};
+
 template <class T>
 __device__ inline float to_f32(T v) { return (float)v; }
 
@@ -81,6 +97,8 @@ __device__ inline float exp32(float x) {
     return x < -87.0f ? 0.0f : __builtin_fmaf(p * kLn2, lost, p);
 }
 
+__device__ inline float exp_plain(float x) { return __builtin_amdgcn_exp2f(x * 1.44269502f); }
+
 // s = 1 / (1 + e^-z) and 1 - s, without cancellation on either side.
 __device__ inline void logistic(float z, float &s, float &one_less) {
     const float e = exp32(-__builtin_fabsf(z));
@@ -91,24 +109,62 @@ __device__ inline void logistic(float z, float &s, float &one_less) {
     if (z != z) s = one_less = z;
 }
 
-// Reductions over the G lanes of a token; every lane ends with the result.
-template <int G>
-__device__ inline float group_sum(float v) {
-#pragma unroll
-    for (int d = 1; d < G; d <<= 1) v += __shfl_xor(v, d, kWave);
-    return v;
+// The value of the lane at the other side of a group of D lanes' middle (D a
+// power of two in 2..64): lane i of an aligned group sees lane i ^ 1, i ^ 2,
+// 7 - i, 15 - i, i ^ 16 or i ^ 32.  Taken for D = 2, 4, .. G in turn, a
+// symmetric function of both sides reduces a group of G lanes.
+template <int D>
+__device__ inline uint32_t across(uint32_t v) {
+    if constexpr (D == 2) return (uint32_t)dpp32<kDppXor1>((int32_t)v, (int32_t)v);
+    else if constexpr (D == 4) return (uint32_t)dpp32<kDppXor2>((int32_t)v, (int32_t)v);
+    else if constexpr (D == 8) return (uint32_t)dpp32<kDppHalfMirror>((int32_t)v, (int32_t)v);
+    else if constexpr (D == 16) return (uint32_t)dpp32<kDppMirror>((int32_t)v, (int32_t)v);
+    else return (uint32_t)__shfl_xor((int32_t)v, D / 2, kWave);
 }
-template <int G>
+template <int D>
+__device__ inline float across(float v) {
+    return __uint_as_float(across<D>(__float_as_uint(v)));
+}
+template <int D>
+__device__ inline double across(double v) {
+    const uint64_t u = (uint64_t)__double_as_longlong(v);
+    const uint64_t lo = across<D>((uint32_t)u), hi = across<D>((uint32_t)(u >> 32));
+    return __longlong_as_double((long long)(hi << 32 | lo));
+}
+
+// Reductions over the G lanes of a token; every lane ends with the result.
+template <int G, int D = 2>
+__device__ inline float group_sum(float v) {
+    if constexpr (D > G) return v;
+    else return group_sum<G, 2 * D>(v + across<D>(v));
+}
+template <int G, int D = 2>
 __device__ inline float group_max(float v) {
-#pragma unroll
-    for (int d = 1; d < G; d <<= 1) v = __builtin_fmaxf(v, __shfl_xor(v, d, kWave));
-    return v;
+    if constexpr (D > G) return v;
+    else return group_max<G, 2 * D>(__builtin_fmaxf(v, across<D>(v)));
 }
 template <int G>
 __device__ inline int64_t group_sum64(int64_t v) {
 #pragma unroll
     for (int d = 1; d < G; d <<= 1) v += __shfl_xor(v, d, kWave);
     return v;
+}
+
+// A row's maximum m (0 if no expert is available) and 1 / sum e^(z - m) (0
+// then).  The exponentials are the plain 2^(x log2 e): its error, |x| / 2
+// steps, weighs little where e^x is small.
+template <int G, int V>
+__device__ inline void row_sum(const float (&z)[V], float &m, float &inv) {
+    m = z[0];
+#pragma unroll
+    for (int v = 1; v < V; ++v) m = __builtin_fmaxf(m, z[v]);
+    m = group_max<G>(m);
+    m = m == -kInf ? 0.0f : m;
+    float sum = 0.0f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) sum += exp_plain(z[v] - m);
+    sum = group_sum<G>(sum);
+    inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 }
 
 // Softmax of a row, in place: z becomes p.  A row without an available
@@ -198,6 +254,191 @@ __device__ inline void choice_gates(const float (&zc)[S], const bool (&on)[S], i
     for (int s = 0; s < S; ++s) w[s] *= by;
 }
 
+// ---------------------------------------------------------------------------
+// Selection of the largest of many values, lowest index first among equals,
+// on keys that hold a value's order and the complement of its index: then a
+// larger key precedes, no two keys are equal, and a compare and exchange is
+// one maximum and one minimum.  The key 0 (and any below `least`) stands for
+// an unavailable expert: -inf, NaN, or none.  -0 equals +0.
+
+constexpr uint32_t kIndexMask = 2047;  // an index below 2048 (kMaxExperts)
+
+// A float's order as an unsigned number; -inf is 0x007FFFFF, NaN too.
+__device__ inline uint32_t order32(float z) {
+    const uint32_t u = __float_as_uint(__builtin_fmaxf(z + 0.0f, -kInf));
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ inline float value32(uint32_t o) {
+    return __uint_as_float(o >> 31 ? o ^ 0x80000000u : ~o);
+}
+
+// 16-bit logits: their 32-bit form has at most 19 significant leading bits
+// (bf16 16, fp16 1 + 8 + 10), so 21 bits of order and 11 of index are one
+// 32-bit word.
+struct Key16 {
+    using Word = uint32_t;
+    static constexpr Word least = 0x00800000u;
+    static __device__ Word make(float z, uint32_t inv) { return (order32(z) & ~kIndexMask) | inv; }
+    static __device__ bool available(Word k) { return k >= least; }
+    // (a negative number's order ends in ones, which the index took)
+    static __device__ float value(Word k) { return value32(k >> 31 ? k & ~kIndexMask : k | kIndexMask); }
+    static __device__ uint32_t index(Word k) { return ~k & kIndexMask; }
+    static __device__ Word max(Word a, Word b) { return a > b ? a : b; }
+    static __device__ Word min(Word a, Word b) { return a < b ? a : b; }
+};
+
+// 32-bit logits: the 32 bits of order and the index as the bits of a normal
+// positive double (its order is that of its bits), which has a maximum and a
+// minimum instruction where 64-bit integers have none.  The instructions are
+// written out: the compiler would first quiet each operand.
+struct Key32 {
+    using Word = double;
+    static __device__ Word make(float z, uint32_t inv) {
+        const uint32_t o = order32(z);
+        return __hiloint2double((int)((o >> 2) + 0x00100000u), (int)(o << 30 | inv));
+    }
+    static __device__ uint32_t order(Word k) {
+        return ((uint32_t)__double2hiint(k) - 0x00100000u) << 2 | (uint32_t)__double2loint(k) >> 30;
+    }
+    static __device__ bool available(Word k) {
+        return (uint32_t)__double2hiint(k) >= (0x00800000u >> 2) + 0x00100000u;
+    }
+    static __device__ float value(Word k) { return value32(order(k)); }
+    static __device__ uint32_t index(Word k) { return ~(uint32_t)__double2loint(k) & kIndexMask; }
+    static __device__ Word max(Word a, Word b) {
+        Word d;
+        asm("v_max_f64 %0, %1, %2" : "=v"(d) : "v"(a), "v"(b));
+        return d;
+    }
+    static __device__ Word min(Word a, Word b) {
+        Word d;
+        asm("v_min_f64 %0, %1, %2" : "=v"(d) : "v"(a), "v"(b));
+        return d;
+    }
+};
+
+template <class T> struct KeyOf { using type = Key16; };
+template <> struct KeyOf<float> { using type = Key32; };
+
+template <class Key, int A, int B, int N>
+__device__ inline void order_pair(typename Key::Word (&a)[N]) {
+    const typename Key::Word x = a[A], y = a[B];
+    a[A] = Key::max(x, y);
+    a[B] = Key::min(x, y);
+}
+
+// Batcher's odd-even merge sort of a[LO .. LO + M), largest first.
+template <class Key, int LO, int M, int R, int I, int N>
+__device__ inline void odd_even_pairs(typename Key::Word (&a)[N]) {
+    if constexpr (I + R < LO + M) {
+        order_pair<Key, I, I + R>(a);
+        odd_even_pairs<Key, LO, M, R, I + 2 * R>(a);
+    }
+}
+template <class Key, int LO, int M, int R, int N>
+__device__ inline void odd_even_merge(typename Key::Word (&a)[N]) {
+    if constexpr (2 * R < M) {
+        odd_even_merge<Key, LO, M, 2 * R>(a);
+        odd_even_merge<Key, LO + R, M, 2 * R>(a);
+        odd_even_pairs<Key, LO, M, R, LO + R>(a);
+    } else {
+        order_pair<Key, LO, LO + R>(a);
+    }
+}
+template <class Key, int LO, int M, int N>
+__device__ inline void sort_keys(typename Key::Word (&a)[N]) {
+    if constexpr (M > 1) {
+        sort_keys<Key, LO, M / 2>(a);
+        sort_keys<Key, LO + M / 2, M / 2>(a);
+        odd_even_merge<Key, LO, M, 1>(a);
+    }
+}
+
+// Sorts a bitonic sequence a[LO .. LO + M), largest first.
+template <class Key, int LO, int M, int I, int N>
+__device__ inline void bitonic_pairs(typename Key::Word (&a)[N]) {
+    if constexpr (I < M / 2) {
+        order_pair<Key, LO + I, LO + I + M / 2>(a);
+        bitonic_pairs<Key, LO, M, I + 1>(a);
+    }
+}
+template <class Key, int LO, int M, int N>
+__device__ inline void bitonic_sort(typename Key::Word (&a)[N]) {
+    if constexpr (M > 1) {
+        bitonic_pairs<Key, LO, M, 0>(a);
+        bitonic_sort<Key, LO, M / 2>(a);
+        bitonic_sort<Key, LO + M / 2, M / 2>(a);
+    }
+}
+
+// The K largest of two sorted lists of K: the larger of each a[i], b[K-1-i]
+// is among them, and these form a bitonic sequence.
+template <class Key, int K>
+__device__ inline void merge_top(typename Key::Word (&a)[K], const typename Key::Word (&b)[K]) {
+#pragma unroll
+    for (int i = 0; i < K; ++i) a[i] = Key::max(a[i], b[K - 1 - i]);
+    bitonic_sort<Key, 0, K>(a);
+}
+
+// The K largest of a lane's M keys (powers of two), sorted.
+template <class Key, int K, int M>
+__device__ inline void lane_top(const typename Key::Word (&x)[M], typename Key::Word (&top)[K]) {
+    constexpr int B = M < K ? M : K;
+#pragma unroll
+    for (int i = 0; i < K; ++i) top[i] = i < B ? x[i] : typename Key::Word(0);
+    sort_keys<Key, 0, B>(top);
+    if constexpr (M > K) {
+#pragma unroll
+        for (int b = 1; b < M / K; ++b) {
+            typename Key::Word y[K];
+#pragma unroll
+            for (int i = 0; i < K; ++i) y[i] = x[b * K + i];
+            sort_keys<Key, 0, K>(y);
+            merge_top<Key, K>(top, y);
+        }
+    }
+}
+
+// The K largest of G lanes' lists, in every one of them.
+template <class Key, int K, int G, int D = 2>
+__device__ inline void group_top(typename Key::Word (&top)[K]) {
+    if constexpr (D <= G) {
+        typename Key::Word y[K];
+#pragma unroll
+        for (int i = 0; i < K; ++i) y[i] = across<D>(top[i]);
+        merge_top<Key, K>(top, y);
+        group_top<Key, K, G, 2 * D>(top);
+    }
+}
+
+// The token and layer of a group of G lanes in a workgroup of 256 threads;
+// groups past the last item repeat it and are not live.
+struct Item {
+    int64_t at, t;
+    int32_t l;
+    bool live;
+};
+template <int G>
+__device__ inline Item item_of(int64_t T, int32_t L) {
+    Item it;
+    const int64_t n = T * L;
+    it.at = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (256 / G) + threadIdx.x / G;
+    it.live = it.at < n;
+    it.at = it.live ? it.at : n - 1;
+    if (L == 1) {
+        it.t = it.at;
+        it.l = 0;
+    } else if (n <= UINT32_MAX) {
+        const uint32_t t = (uint32_t)it.at / (uint32_t)L;
+        it.t = t;
+        it.l = (int32_t)((uint32_t)it.at - t * (uint32_t)L);
+    } else {
+        it.t = it.at / L;
+        it.l = (int32_t)(it.at - it.t * L);
+    }
+    return it;
+}
+
 // One recorded id, as an expert or -1.
 __device__ inline int32_t load_id(const void *data, int type, int64_t at, int32_t E) {
     int64_t v;
@@ -227,6 +468,29 @@ inline int check_ids(const routepack_problem *p, const routepack_ids *r, int64_t
     if (r->n_tokens != n_tokens || r->token_stride < 0 || r->layer_stride < 0) return ROUTEPACK_E_INVALID;
     if (!r->data && n_tokens > 0 && p->n_layers > 0) return ROUTEPACK_E_INVALID;
     return ROUTEPACK_OK;
+}
+
+template <int N>
+struct Int {
+    static constexpr int value = N;
+};
+
+// Calls f with the lanes of a token and the vectors of a lane for rows of E
+// logits: 4 lanes of 1, 2 .. MOST vectors, or more lanes of MOST.
+template <class T, int MOST, class F>
+int by_geometry(int32_t E, F &&f) {
+    const int32_t n = (E * (int32_t)sizeof(T) + 15) / 16;
+    if (n <= 4) return f(Int<4>(), Int<1>());
+    if constexpr (MOST >= 4)
+        if (n <= 8) return f(Int<4>(), Int<2>());
+    if constexpr (MOST >= 8)
+        if (n <= 16) return f(Int<4>(), Int<4>());
+    if (n <= 4 * MOST) return f(Int<4>(), Int<MOST>());
+    if (n <= 8 * MOST) return f(Int<8>(), Int<MOST>());
+    if (n <= 16 * MOST) return f(Int<16>(), Int<MOST>());
+    if (n <= 32 * MOST) return f(Int<32>(), Int<MOST>());
+    if constexpr (32 * MOST * 16 / (int)sizeof(T) < kMaxExperts) return f(Int<64>(), Int<MOST>());
+    else return ROUTEPACK_E_UNSUPPORTED;
 }
 
 // Calls f with a value of the logits' type.

@@ -7,113 +7,53 @@
 
 namespace rp {
 
-struct RouteArgs {
-    const void *logits;
-    int64_t ts, ls;      // strides of the logits
-    int64_t T;
-    int32_t L, E, k;
-    const void *rec;     // replayed ids, or null
-    int32_t rec_type;
-    int64_t rts, rls;    // their strides
-    const float *bias;
-    int32_t score;
-    bool normalize;
-    float scale;
-    int32_t *ids;
-    float *gates;
-};
+// The choices of logits of one type (rp_route_choose.h, a translation unit
+// for each type).
+int choose_f32(const RouteArgs &a, hipStream_t stream);
+int choose_bf16(const RouteArgs &a, hipStream_t stream);
+int choose_f16(const RouteArgs &a, hipStream_t stream);
 
-// A double's order as an unsigned number (-0 equals +0); 0 stands for "not
-// available".
-__device__ inline uint64_t order64(double x) {
-    const uint64_t u = (uint64_t)__double_as_longlong(x + 0.0);
-    return u >> 63 ? ~u : u | (uint64_t)1 << 63;
+// Gates of recorded experts that need no more of a row than the experts'
+// logits: a group of G >= k lanes a token, a choice a lane.
+template <class T, int G>
+__global__ void __launch_bounds__(256) k_replay_chosen(RouteArgs a) {
+    const int c = threadIdx.x & (G - 1);
+    const Item it = item_of<G>(a.T, a.L);
+    const T *row = static_cast<const T *>(a.logits) + it.t * a.ts + it.l * a.ls;
+    int32_t id = -1;
+    if (c < a.k) id = load_id(a.rec, a.rec_type, it.t * a.rts + it.l * a.rls + c, a.E);
+    const float zc[1] = {id >= 0 ? to_f32(row[id]) : 0.0f};
+    const bool on[1] = {id >= 0};
+    float w[1], less[1];
+    choice_gates<G, 1>(zc, on, a.score, a.normalize, 0.0f, 0.0f, w, less);
+    if (it.live && c < a.k) a.gates[it.at * a.k + c] = a.scale * w[0];
 }
 
-// A wave per token and layer, the row in its lanes; the choices by k rounds
-// of a maximum over (key, -index).
-template <class T, int V>
-__global__ void __launch_bounds__(256) k_route(RouteArgs a) {
-    const int64_t item = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + wave_id();
-    if (item >= a.T * a.L) return;
-    const int64_t t = item / a.L;
-    const int32_t l = (int32_t)(item - t * a.L);
-    const int c = lane_id();
-    const T *row = static_cast<const T *>(a.logits) + t * a.ts + l * a.ls;
-    float z[V];
-    load_row<T, kWave, V>(row, a.E, c, z);
-    float m = 0.0f, inv = 0.0f;
-    if (a.score == ROUTEPACK_SOFTMAX) {
-        float p[V], top = -kInf, sum = 0.0f;
+// Unnormalised softmax gates of recorded experts: the row's sum, then its k
+// choices, S of them a lane.
+template <class T, int G, int NV>
+__global__ void __launch_bounds__(256) k_replay_row(RouteArgs a) {
+    constexpr int V = NV * (16 / sizeof(T)), S = kMaxChoices / G > 0 ? kMaxChoices / G : 1;
+    const int c = threadIdx.x & (G - 1);
+    const Item it = item_of<G>(a.T, a.L);
+    const T *row = static_cast<const T *>(a.logits) + it.t * a.ts + it.l * a.ls;
+    float z[V], zc[S], w[S], less[S];
+    bool on[S];
+    load_row<T, G, V>(row, a.E, c, z);
 #pragma unroll
-        for (int v = 0; v < V; ++v) top = __builtin_fmaxf(top, z[v]);
-        top = group_max<kWave>(top);
-        m = top == -kInf ? 0.0f : top;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            p[v] = exp32(z[v] - m);
-            sum += p[v];
-        }
-        sum = group_sum<kWave>(sum);
-        inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    for (int s = 0; s < S; ++s) {
+        const int j = s * G + c;
+        int32_t id = -1;
+        if (j < a.k) id = load_id(a.rec, a.rec_type, it.t * a.rts + it.l * a.rls + j, a.E);
+        on[s] = id >= 0;
+        zc[s] = on[s] ? to_f32(row[id]) : 0.0f;
     }
-    const int64_t out = item * a.k;
-    int32_t mine = -1;
-    if (a.rec) {
-        if (c < a.k) mine = load_id(a.rec, a.rec_type, t * a.rts + l * a.rls + c, a.E);
-    } else {
-        uint64_t key[V];
-        double sum = 0.0;
-        if (a.bias && a.score == ROUTEPACK_SOFTMAX) {
+    float m, inv;
+    row_sum<G, V>(z, m, inv);
+    choice_gates<G, S>(zc, on, ROUTEPACK_SOFTMAX, false, m, inv, w, less);
 #pragma unroll
-            for (int v = 0; v < V; ++v) sum += z[v] > -kInf ? exp((double)z[v] - (double)m) : 0.0;
-#pragma unroll
-            for (int d = 1; d < kWave; d <<= 1) sum += __shfl_xor(sum, d, kWave);
-        }
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            double x = z[v];
-            const int e = elem_of<T, kWave>(v, c);
-            bool ok = z[v] > -kInf;
-            if (a.bias && e < a.E) {
-                x = a.score == ROUTEPACK_SOFTMAX ? exp(x - (double)m) / sum : 1.0 / (1.0 + exp(-x));
-                x += (double)a.bias[(int64_t)l * a.E + e];
-                ok = ok && x > -__builtin_inf();
-            }
-            key[v] = ok ? order64(x) : 0;
-        }
-        for (int j = 0; j < a.k; ++j) {
-            uint64_t best = 0;
-            int32_t at = INT32_MAX;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int32_t e = elem_of<T, kWave>(v, c);
-                if (key[v] > best || (key[v] == best && key[v] && e < at)) {
-                    best = key[v];
-                    at = e;
-                }
-            }
-#pragma unroll
-            for (int d = 1; d < kWave; d <<= 1) {
-                const uint64_t ob = (uint64_t)__shfl_xor((long long)best, d, kWave);
-                const int32_t oa = __shfl_xor(at, d, kWave);
-                if (ob > best || (ob == best && oa < at)) {
-                    best = ob;
-                    at = oa;
-                }
-            }
-            if (best == 0) break;
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (elem_of<T, kWave>(v, c) == at) key[v] = 0;
-            if (c == j) mine = at;
-        }
-        if (c < a.k) a.ids[out + c] = mine;
-    }
-    float zc[1] = {mine >= 0 ? to_f32(row[mine]) : 0.0f}, w[1], less[1];
-    const bool on[1] = {mine >= 0};
-    choice_gates<kWave, 1>(zc, on, a.score, a.normalize, m, inv, w, less);
-    if (c < a.k) a.gates[out + c] = a.scale * w[0];
+    for (int s = 0; s < S; ++s)
+        if (it.live && s * G + c < a.k) a.gates[it.at * a.k + s * G + c] = a.scale * w[s];
 }
 
 struct BackArgs {
@@ -272,12 +212,27 @@ extern "C" int routepack_route_tokens(const routepack_problem *prob, const route
                    prob->n_experts, prob->top_k, replay ? replay->data : nullptr, replay ? replay->type : 0,
                    replay ? replay->token_stride : 0, replay ? replay->layer_stride : 0, bias, score, normalize != 0,
                    scale, ids, gates};
+    if (!replay) {
+        switch (logits->type) {
+            case ROUTEPACK_F32: return choose_f32(a, stream);
+            case ROUTEPACK_BF16: return choose_bf16(a, stream);
+            default: return choose_f16(a, stream);
+        }
+    }
     return by_type(logits->type, [&](auto tag) -> int {
         using T = decltype(tag);
-        const dim3 grid = grid_of((items + 3) / 4);
-        if (a.E <= 512) hipLaunchKernelGGL((k_route<T, 8>), grid, dim3(256), 0, stream, a);
-        else hipLaunchKernelGGL((k_route<T, 32>), grid, dim3(256), 0, stream, a);
-        return hipGetLastError() == hipSuccess ? ROUTEPACK_OK : ROUTEPACK_E_DEVICE;
+        auto go = [&](auto kern, int g) {
+            hipLaunchKernelGGL(kern, grid_of((items + 256 / g - 1) / (256 / g)), dim3(256), 0, stream, a);
+            return hipGetLastError() == hipSuccess ? ROUTEPACK_OK : ROUTEPACK_E_DEVICE;
+        };
+        if (score == ROUTEPACK_SOFTMAX && !normalize)
+            return by_geometry<T, 2 * sizeof(T)>(a.E, [&](auto g, auto nv) {
+                return go(k_replay_row<T, g.value, nv.value>, g.value);
+            });
+        if (a.k <= 4) return go(k_replay_chosen<T, 4>, 4);
+        if (a.k <= 8) return go(k_replay_chosen<T, 8>, 8);
+        if (a.k <= 16) return go(k_replay_chosen<T, 16>, 16);
+        return go(k_replay_chosen<T, 32>, 32);
     });
 }
 
