@@ -371,26 +371,36 @@ def fixed_bin_search(prob: Problem, lengths, n_rows, node_budget):
 SCORES = {"softmax": 0, "sigmoid": 1}
 
 
-def _router_types():
-    import torch
-    return ({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2},
-            {torch.uint8: 3, torch.int16: 4, torch.int32: 5, torch.int64: 6})
+_ROUTER = None
+
+
+def _router():
+    """(the library, torch, types of logits, types of ids), looked up once:
+    the smallest calls take a few microseconds."""
+    global _ROUTER
+    if _ROUTER is None:
+        lib, torch = load_library(), _torch()
+        _ROUTER = (lib, torch, {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2},
+                   {torch.uint8: 3, torch.int16: 4, torch.int32: 5, torch.int64: 6})
+    return _ROUTER
 
 
 class _Call:
     """One call's tensors: checks that they share a GPU, hands out pointers,
     and runs the call on that GPU's current stream."""
 
-    def __init__(self, fn):
-        self.fn, self.device = fn, None
+    __slots__ = ("fn", "torch", "device")
+
+    def __init__(self, fn, torch):
+        self.fn, self.torch, self.device = fn, torch, None
 
     def tensor(self, name, x, dtypes, shape=None):
-        torch = _torch()
-        if not isinstance(x, torch.Tensor):
+        if not isinstance(x, self.torch.Tensor):
             raise TypeError(f"{self.fn}: {name} must be a tensor, got {type(x).__name__}")
         if not x.is_cuda or (self.device is not None and x.device != self.device):
             raise ValueError(f"{self.fn}: {name} is on {x.device}, expected {self.device or 'a GPU'}")
-        self.device = x.device
+        if self.device is None:
+            self.device = x.device
         if x.dtype not in dtypes:
             raise ValueError(f"{self.fn}: {name} has type {x.dtype}")
         if shape is not None and tuple(x.shape) != tuple(shape):
@@ -405,22 +415,26 @@ class _Call:
 
     def rows(self, name, x, dtypes, L, last):
         """[T][L][last], or [T][last] where L is 1, of any strides but the
-        last: (the tensor, its description for the library)."""
-        x = self.tensor(name, x, dtypes)
-        if x.dim() not in (2, 3) or x.shape[-1] != last or (x.shape[1] != L if x.dim() == 3 else L != 1):
-            raise ValueError(f"{self.fn}: {name} has shape {tuple(x.shape)}, expected [T][{L}][{last}]")
-        if last > 1 and x.stride(-1) != 1 and x.numel() > 0:
+        last: (the tensor's shape, its description for the library)."""
+        self.tensor(name, x, dtypes)
+        shape, stride = x.shape, x.stride()
+        three = len(shape) == 3
+        if not (three and shape[1] == L or len(shape) == 2 and L == 1) or shape[-1] != last:
+            raise ValueError(f"{self.fn}: {name} has shape {tuple(shape)}, expected [T][{L}][{last}]")
+        if last > 1 and stride[-1] != 1 and shape[0] > 0:
             raise ValueError(f"{self.fn}: the last axis of {name} must be adjacent in memory")
-        return x, _Rows(x.data_ptr(), dtypes[x.dtype], x.shape[0], x.stride(0), x.stride(1) if x.dim() == 3 else 0)
+        return shape, _Rows(x.data_ptr(), dtypes[x.dtype], shape[0], stride[0], stride[1] if three else 0)
 
     def run(self, f, *args):
-        torch = _torch()
-        stream = C.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)
-        if self.device.index == torch.cuda.current_device():
-            _check(self.fn, f(*args, stream))
+        cuda = self.torch.cuda
+        stream = cuda.current_stream(self.device).cuda_stream
+        if self.device.index == cuda.current_device():
+            rc = f(*args, stream)
         else:
-            with torch.cuda.device(self.device):
-                _check(self.fn, f(*args, stream))
+            with cuda.device(self.device):
+                rc = f(*args, stream)
+        if rc != 0:
+            raise RoutepackError(self.fn, rc)
 
 
 def _score(fn, score):
@@ -440,23 +454,24 @@ def route_tokens(prob: Problem, logits, *, ids=None, bias=None, score="softmax",
     (uint8, int16, int32 or int64; a replayed record) the gates are those of
     the recorded experts, and `ids` is returned as it is.  score: "softmax"
     or "sigmoid"; normalize: divide by the sum over the token's choices."""
-    torch = _torch()
-    lib, call = load_library(), _Call("routepack_route_tokens")
-    floats, ints = _router_types()
-    z, zr = call.rows("logits", logits, floats, prob.n_layers, prob.n_experts)
-    shape = tuple(z.shape[:-1]) + (prob.top_k,)
-    b = None if bias is None else call.dense("bias", bias, (torch.float32,), (prob.n_layers, prob.n_experts))
-    rec = None
+    lib, torch, floats, ints = _router()
+    call = _Call("routepack_route_tokens", torch)
+    shape, z = call.rows("logits", logits, floats, prob.n_layers, prob.n_experts)
+    shape = (*shape[:-1], prob.top_k)
+    b = bias
+    if bias is not None:
+        b = call.dense("bias", bias, (torch.float32,), (prob.n_layers, prob.n_experts)).data_ptr()
+    out, rec = ids, None
     if ids is not None:
-        out, rec = call.rows("ids", ids, ints, prob.n_layers, prob.top_k)
-        if tuple(out.shape) != shape:
-            raise ValueError(f"{call.fn}: ids has shape {tuple(out.shape)}, expected {shape}")
+        got, rec = call.rows("ids", ids, ints, prob.n_layers, prob.top_k)
+        if tuple(got) != shape:
+            raise ValueError(f"{call.fn}: ids has shape {tuple(got)}, expected {shape}")
+        rec = C.byref(rec)
     else:
-        out = torch.empty(shape, dtype=torch.int32, device=z.device)
-    gates = torch.empty(shape, dtype=torch.float32, device=z.device)
-    call.run(lib.routepack_route_tokens, prob.ref, C.byref(zr), None if rec is None else C.byref(rec), _ptr(b),
-             _score(call.fn, score), int(bool(normalize)), float(scale), _ptr(out) if rec is None else None,
-             _ptr(gates))
+        out = torch.empty(shape, dtype=torch.int32, device=call.device)
+    gates = torch.empty(shape, dtype=torch.float32, device=call.device)
+    call.run(lib.routepack_route_tokens, prob.ref, C.byref(z), rec, b, _score(call.fn, score), 1 if normalize else 0,
+             scale, out.data_ptr() if ids is None else None, gates.data_ptr())
     return out, gates
 
 
@@ -468,25 +483,23 @@ def count_demand(prob: Problem, ids, offsets):
     strides over tokens and layers; ids outside [0, E) are not counted.
     offsets int64 [N + 1], non-decreasing: sample i holds the tokens
     [offsets[i], offsets[i + 1])."""
-    torch = _torch()
-    lib, call = load_library(), _Call("routepack_count_demand")
-    _, ints = _router_types()
-    x, xr = call.rows("ids", ids, ints, prob.n_layers, prob.top_k)
+    lib, torch, _, ints = _router()
+    call = _Call("routepack_count_demand", torch)
+    _, x = call.rows("ids", ids, ints, prob.n_layers, prob.top_k)
     off = call.dense("offsets", offsets, (torch.int64,), (prob.n_samples + 1,))
-    demand = torch.empty((prob.n_samples, prob.n_layers, prob.n_experts), dtype=torch.int32, device=x.device)
-    call.run(lib.routepack_count_demand, prob.ref, C.byref(xr), _ptr(off), _ptr(demand))
+    demand = torch.empty((prob.n_samples, prob.n_layers, prob.n_experts), dtype=torch.int32, device=call.device)
+    call.run(lib.routepack_count_demand, prob.ref, C.byref(x), off.data_ptr(), demand.data_ptr())
     return demand
 
 
 def _groups(call, prob, counts, offsets):
-    torch = _torch()
+    _, torch, _, ints = _router()
     off = call.tensor("offsets", offsets, (torch.int64,))
     if off.dim() != 1 or off.shape[0] < 2 or not off.is_contiguous():
         raise ValueError(f"{call.fn}: offsets has shape {tuple(off.shape)}, expected [G + 1], contiguous, with G >= 1")
     G = off.shape[0] - 1
-    _, ints = _router_types()
     n = call.dense("counts", counts, (torch.int32, torch.int64), (G, prob.n_layers, prob.n_experts))
-    return G, off, n, ints[n.dtype]
+    return G, off.data_ptr(), n.data_ptr(), ints[n.dtype]
 
 
 def balance_loss(prob: Problem, logits, counts, offsets, *, score="softmax"):
@@ -497,17 +510,17 @@ def balance_loss(prob: Problem, logits, counts, offsets, *, score="softmax"):
     group's tokens of the scores divided by their sum.  counts int32 or int64
     [G][L][E] (count_demand's result, or aggregate_demand's as [1][L][E] for
     one group over the window); offsets int64 [G + 1]."""
-    torch = _torch()
-    lib, call = load_library(), _Call("routepack_balance_loss")
-    floats, _ = _router_types()
-    z, zr = call.rows("logits", logits, floats, prob.n_layers, prob.n_experts)
+    lib, torch, floats, _ = _router()
+    call = _Call("routepack_balance_loss", torch)
+    shape, z = call.rows("logits", logits, floats, prob.n_layers, prob.n_experts)
     G, off, n, n_type = _groups(call, prob, counts, offsets)
-    loss = torch.empty(prob.n_layers, dtype=torch.float32, device=z.device)
-    shares = torch.empty((G, prob.n_layers, prob.n_experts), dtype=torch.float32, device=z.device)
-    size = lib.routepack_balance_workspace(prob.ref, z.shape[0], G)
-    work = torch.empty(max(size, 16), dtype=torch.uint8, device=z.device)
-    call.run(lib.routepack_balance_loss, prob.ref, C.byref(zr), G, _ptr(off), _ptr(n), n_type,
-             _score(call.fn, score), _ptr(loss), _ptr(shares), _ptr(work), work.numel())
+    L, E, at = prob.n_layers, prob.n_experts, call.device
+    loss = torch.empty(L, dtype=torch.float32, device=at)
+    shares = torch.empty((G, L, E), dtype=torch.float32, device=at)
+    size = lib.routepack_balance_workspace(prob.ref, shape[0], G)
+    work = torch.empty(max(size, 16), dtype=torch.uint8, device=at)
+    call.run(lib.routepack_balance_loss, prob.ref, C.byref(z), G, off, n, n_type, _score(call.fn, score),
+             loss.data_ptr(), shares.data_ptr(), work.data_ptr(), size)
     return loss, shares
 
 
@@ -517,28 +530,27 @@ def route_backward(prob: Problem, logits, *, ids=None, dgates=None, normalize=Tr
     route_tokens' gates (`ids`, `dgates` float32 of their shape, `normalize`,
     `scale`), of balance_loss' loss (`counts`, `offsets`, `dloss` float32 [L]),
     or of both in one pass."""
-    torch = _torch()
-    lib, call = load_library(), _Call("routepack_route_backward")
-    floats, ints = _router_types()
+    lib, torch, floats, ints = _router()
+    call = _Call("routepack_route_backward", torch)
     if (ids is None) != (dgates is None):
         raise ValueError(f"{call.fn}: ids and dgates go together")
     if (dloss is None) != (counts is None) or (dloss is None) != (offsets is None):
         raise ValueError(f"{call.fn}: counts, offsets and dloss go together")
     if ids is None and dloss is None:
         raise ValueError(f"{call.fn}: neither dgates nor dloss given")
-    z, zr = call.rows("logits", logits, floats, prob.n_layers, prob.n_experts)
+    shape, z = call.rows("logits", logits, floats, prob.n_layers, prob.n_experts)
     rec = dg = off = n = dl = None
     G = n_type = 0
     if ids is not None:
-        x, rec = call.rows("ids", ids, ints, prob.n_layers, prob.top_k)
-        if x.shape[:-1] != z.shape[:-1]:
-            raise ValueError(f"{call.fn}: ids has shape {tuple(x.shape)}, logits {tuple(z.shape)}")
-        dg = call.dense("dgates", dgates, (torch.float32,), x.shape)
+        got, rec = call.rows("ids", ids, ints, prob.n_layers, prob.top_k)
+        if got[:-1] != shape[:-1]:
+            raise ValueError(f"{call.fn}: ids has shape {tuple(got)}, logits {tuple(shape)}")
+        dg = call.dense("dgates", dgates, (torch.float32,), got).data_ptr()
+        rec = C.byref(rec)
     if dloss is not None:
         G, off, n, n_type = _groups(call, prob, counts, offsets)
-        dl = call.dense("dloss", dloss, (torch.float32,), (prob.n_layers,))
-    dz = torch.empty(z.shape, dtype=z.dtype, device=z.device)
-    call.run(lib.routepack_route_backward, prob.ref, C.byref(zr), None if rec is None else C.byref(rec), _ptr(dg),
-             int(bool(normalize)), float(scale), G, _ptr(off), _ptr(n), n_type, _ptr(dl), _score(call.fn, score),
-             _ptr(dz))
+        dl = call.dense("dloss", dloss, (torch.float32,), (prob.n_layers,)).data_ptr()
+    dz = torch.empty(shape, dtype=logits.dtype, device=call.device)
+    call.run(lib.routepack_route_backward, prob.ref, C.byref(z), rec, dg, 1 if normalize else 0, scale, G, off, n,
+             n_type, dl, _score(call.fn, score), dz.data_ptr())
     return dz

@@ -1,9 +1,13 @@
 // Expert demand from recorded ids (Eq. routing-replay-input), on gfx950.
 //
-// The tokens are cut into chunks of equal length; a workgroup takes one chunk
-// of one layer and counts each sample that meets it in LDS.  A sample that
-// lies within one chunk is written by plain stores; the parts of one that
-// spans chunks are added with integer atomics to a row cleared before.
+// Reading the ids once is the floor.  The tokens are cut into chunks of equal
+// length and the layers into groups whose counters fit the LDS; a workgroup
+// counts one chunk of one group, sample by sample, with LDS atomics, and reads
+// the ids as vectors of 16 bytes.  A thread keeps its place in the row of a
+// token (or of several short ones), so the layers that its ids belong to are
+// worked out once.  A sample that lies within one chunk is written by plain
+// stores; the parts of one that spans chunks are added with integer atomics to
+// a row cleared before (integer sums do not depend on their order).
 #include "rp_internal.h"
 #include "rp_route.h"
 
@@ -11,10 +15,19 @@ namespace rp {
 
 struct CountArgs {
     const void *ids;
-    int64_t ts, ls, T, chunk, n_chunks;
-    int32_t type, N, L, E, k;
+    int64_t ts, ls;         // strides of tokens and layers
+    int64_t T, n_chunks;
+    int32_t shift;          // a chunk holds 2^shift tokens
+    int32_t N, L, E, k;
     const int64_t *offsets;
     int32_t *demand;
+    int32_t group;          // layers of a workgroup
+    // A row is `join` tokens of one workgroup's layers; its threads stand at
+    // `cols` places of it, `slots` rows abreast.
+    int32_t join, cols, slots;
+    int64_t row_stride;
+    bool one_layer;         // the row holds ids of one layer only
+    int32_t pitch, copies;  // words between layers' counters, and copies of them
 };
 
 // A sample's tokens and the first and last chunk that it meets (an empty
@@ -27,60 +40,219 @@ __device__ inline Span span_of(const CountArgs &a, int32_t i) {
     const int64_t b = a.offsets[i], e = a.offsets[i + 1];
     s.b = b < 0 ? 0 : (b > a.T ? a.T : b);
     s.e = e < s.b ? s.b : (e > a.T ? a.T : e);
-    s.first = s.b / a.chunk;
+    s.first = s.b >> a.shift;
     s.first = s.first < a.n_chunks ? s.first : a.n_chunks - 1;
-    s.last = s.e > s.b ? (s.e - 1) / a.chunk : s.first;
+    s.last = s.e > s.b ? (s.e - 1) >> a.shift : s.first;
     return s;
 }
 
-// Clears the rows of samples that span chunks (a workgroup per sample).
+// Clears the rows of samples that span chunks.
 __global__ void __launch_bounds__(256) k_count_clear(CountArgs a) {
-    for (int64_t i = (int64_t)blockIdx.x; i < a.N; i += gridDim.x) {
+    const int64_t row_len = (int64_t)a.L * a.E;
+    for (int64_t i = blockIdx.x; i < a.N; i += gridDim.x) {
         const Span s = span_of(a, (int32_t)i);
         if (s.first == s.last) continue;
-        int32_t *row = a.demand + i * a.L * a.E;
-        for (int64_t x = threadIdx.x; x < (int64_t)a.L * a.E; x += 256) row[x] = 0;
+        int32_t *row = a.demand + i * row_len;
+        for (int64_t x = (int64_t)blockIdx.y * 256 + threadIdx.x; x < row_len; x += (int64_t)gridDim.y * 256) row[x] = 0;
     }
 }
 
+// The i-th id of a vector.
+template <class I>
+__device__ inline uint32_t id_at(const uint32_t (&w)[4], int i) {
+    if constexpr (sizeof(I) == 1) return w[i / 4] >> (8 * (i % 4)) & 0xFF;
+    else if constexpr (sizeof(I) == 2) return (uint32_t)(int32_t)(int16_t)(w[i / 2] >> (16 * (i % 2)));
+    else if constexpr (sizeof(I) == 4) return w[i];
+    else return w[2 * i + 1] ? UINT32_MAX : w[2 * i];  // (a high word is 0 for an expert)
+}
+template <class I>
+__device__ inline uint32_t id_of(I x) {
+    if constexpr (sizeof(I) == 8) return (uint64_t)x >> 32 ? UINT32_MAX : (uint32_t)x;
+    else return (uint32_t)(int32_t)x;
+}
+
+// W ids a thread (16 bytes; where the row is not of one piece, W = 1).
+template <class I, int W>
 __global__ void __launch_bounds__(256) k_count(CountArgs a) {
-    extern __shared__ int32_t hist[];  // [E]
+    extern __shared__ int32_t hist[];  // [copies][group][pitch], then a word a thread for what is not counted
+    const int tid = threadIdx.x, lane = lane_id();
     const int64_t ch = blockIdx.x;
-    const int32_t l = (int32_t)blockIdx.y;
-    int32_t lo = 0, hi = a.N;  // the first sample whose last chunk is ch or later
+    const int32_t l0 = (int32_t)blockIdx.y * a.group;
+    const int32_t nl = a.group < a.L - l0 ? a.group : a.L - l0;
+    // the first sample whose last chunk is ch or later: 64 probes a round
+    int32_t lo = 0, hi = a.N;
     while (lo < hi) {
-        const int32_t mid = lo + (hi - lo) / 2;
-        if (span_of(a, mid).last >= ch) hi = mid;
-        else lo = mid + 1;
+        const int32_t step = (hi - lo + kWave - 1) / kWave;
+        const int64_t p = lo + (int64_t)lane * step;
+        const uint64_t yes = __ballot(p >= hi || span_of(a, (int32_t)p).last >= ch);
+        const int f = yes ? first_lane(yes) : kWave;
+        const int64_t past = lo + (int64_t)f * step;
+        const int64_t from = f > 0 ? lo + (int64_t)(f - 1) * step + 1 : lo;
+        hi = past < hi ? (int32_t)past : hi;
+        lo = from < hi ? (int32_t)from : hi;
     }
-    const int64_t t0 = ch * a.chunk, t1 = t0 + a.chunk;
+    const int32_t words = a.copies * a.group * a.pitch;
+    for (int x = tid; x < words; x += 256) hist[x] = 0;
+    const int64_t t0 = ch << a.shift, t1 = t0 + ((int64_t)1 << a.shift);
+    const int32_t piece = nl * a.k;        // ids of one token
+    const int32_t len = a.join * piece;    // of a row
+    const int col = tid % a.cols, slot = tid / a.cols;
+    // the thread's ids are at .. at + W of its rows, less those that the place
+    // before holds already (the last place is moved back into the row)
+    const int32_t want = col * W;
+    const int32_t at = want + W <= len || len < W ? want : len - W;
+    uint32_t base[W];  // byte offset of the id's layer in the LDS, or none
+    const uint32_t none = (uint32_t)words * 4 + 4 * tid;
+    bool mine[W];
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        const int32_t x = at + w;
+        mine[w] = x >= want && x < len && slot < a.slots;
+        const int32_t l = a.one_layer ? 0 : x % piece / a.k;
+        base[w] = (uint32_t)((lane % a.copies) * a.group + l) * (uint32_t)a.pitch * 4;
+    }
+    const I *ids = static_cast<const I *>(a.ids) + (int64_t)l0 * a.ls;
+    // (where the row is not of one piece, W is 1: the thread's layer and choice)
+    const int64_t place = W == 1 && !a.one_layer ? (int64_t)(at % piece / a.k) * a.ls + at % a.k : at;
+    const uint32_t limit = (uint32_t)a.E;
+    auto add = [&](uint32_t id, int w) {
+        const uint32_t to = id < limit && mine[w] ? base[w] + id * 4 : none;
+        atomicAdd(reinterpret_cast<int32_t *>(reinterpret_cast<char *>(hist) + to), 1);
+    };
     for (int32_t i = lo; i < a.N; ++i) {
         const Span s = span_of(a, i);
         if (s.first > ch) break;
         if (s.last < ch) continue;
         const int64_t b = s.b > t0 ? s.b : t0, e = s.e < t1 ? s.e : t1;
+        const int32_t rows = (int32_t)((e - b + a.join - 1) / a.join);
+        const I *p = ids + b * a.ts + place;
+        const int64_t left = (e - b) * piece;  // ids of the sample here (rows of one piece)
         __syncthreads();
-        for (int x = threadIdx.x; x < a.E; x += 256) hist[x] = 0;
-        __syncthreads();
-        const int64_t n = (e - b) * a.k;
-        for (int64_t x = threadIdx.x; x < n; x += 256) {
-            const int64_t t = b + x / a.k, j = x % a.k;
-            const int32_t id = load_id(a.ids, a.type, t * a.ts + l * a.ls + j, a.E);
-            if (id >= 0) atomicAdd(&hist[id], 1);
+        if (slot < a.slots) {
+            int32_t r = slot;
+            if constexpr (W == 1) {
+                for (; r < rows; r += a.slots) add(id_of<I>(p[r * a.row_stride]), 0);
+            } else {
+                constexpr int U = 4;
+                const int32_t whole = a.join == 1 ? (len < W ? 0 : rows) : (int32_t)(left / len);
+                for (; r + (U - 1) * a.slots < whole; r += U * a.slots) {
+                    Words16 v[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+                        v[u] = *reinterpret_cast<const Words16 *>(p + (int64_t)(r + u * a.slots) * a.row_stride);
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const uint32_t w4[4] = {v[u].w[0], v[u].w[1], v[u].w[2], v[u].w[3]};
+#pragma unroll
+                        for (int w = 0; w < W; ++w) add(id_at<I>(w4, w), w);
+                    }
+                }
+                for (; r < whole; r += a.slots) {
+                    const Words16 v = *reinterpret_cast<const Words16 *>(p + (int64_t)r * a.row_stride);
+                    const uint32_t w4[4] = {v.w[0], v.w[1], v.w[2], v.w[3]};
+#pragma unroll
+                    for (int w = 0; w < W; ++w) add(id_at<I>(w4, w), w);
+                }
+                // the last row where its tokens are fewer than `join`, or rows
+                // shorter than a vector
+                for (; r < rows; r += a.slots) {
+                    const I *q = p + (int64_t)r * a.row_stride;
+                    const int64_t end = a.join == 1 ? len : left - (int64_t)r * len;
+#pragma unroll
+                    for (int w = 0; w < W; ++w)
+                        if (at + w < end) add(id_of<I>(q[w]), w);
+                }
+            }
         }
         __syncthreads();
-        int32_t *row = a.demand + ((int64_t)i * a.L + l) * a.E;
-        if (s.first == s.last)
-            for (int x = threadIdx.x; x < a.E; x += 256) row[x] = hist[x];
-        else
-            for (int x = threadIdx.x; x < a.E; x += 256)
-                if (hist[x]) atomicAdd(&row[x], hist[x]);
+        int32_t *row = a.demand + ((int64_t)i * a.L + l0) * a.E;
+        const bool alone = s.first == s.last;
+        for (int32_t x = tid; x < nl * a.E; x += 256) {
+            const int32_t l = x / a.E, h = l * a.pitch + (x - l * a.E);
+            int32_t n = 0;
+            for (int32_t y = 0; y < a.copies; ++y) {
+                n += hist[y * a.group * a.pitch + h];
+                hist[y * a.group * a.pitch + h] = 0;
+            }
+            if (alone) row[x] = n;
+            else if (n) atomicAdd(&row[x], n);
+        }
     }
 }
 
 }  // namespace rp
 
 using namespace rp;
+
+namespace {
+
+int32_t gcd_of(int32_t a, int32_t b) { return b ? gcd_of(b, a % b) : a; }
+
+template <class I>
+int count(CountArgs &a, bool layer_runs, bool token_rows, hipStream_t stream) {
+    constexpr int W = 16 / sizeof(I);
+    constexpr int32_t kWords = 8192;  // 32 KiB of counters: four workgroups a CU and more
+    a.pitch = a.E | 1;  // (odd: equal experts of several layers stand in different banks)
+    // Layers of a workgroup: as many as fit; where that is not all of them, such
+    // that a token's piece is whole lines of 128 bytes, or whole vectors.
+    int32_t fit = kWords / a.pitch;
+    fit = fit < 1 ? 1 : fit;
+    a.group = layer_runs ? 1 : (fit < a.L ? fit : a.L);
+    if (a.group < a.L && token_rows) {
+        const int32_t line = 128 / gcd_of(128, a.k * (int32_t)sizeof(I)), vec = W / gcd_of(W, a.k);
+        if (a.group >= line) a.group -= a.group % line;
+        else if (a.group >= vec) a.group -= a.group % vec;
+    }
+    bool pieces = token_rows || layer_runs;
+    // at most 256 places in a row
+    while (!layer_runs && (a.group * a.k + W - 1) / W > 256 && a.group > 1) a.group = (a.group + 1) / 2;
+    if (!layer_runs && (a.group * a.k + W - 1) / W > 256) return ROUTEPACK_E_UNSUPPORTED;
+    if (!pieces && a.group * a.k > 256) a.group = 256 / a.k;
+    if (a.group < 1) return ROUTEPACK_E_UNSUPPORTED;
+    a.join = 1;
+    a.one_layer = a.group == 1 && pieces;
+    const int32_t piece = a.group * a.k;
+    if (pieces) {
+        // tokens that follow each other without a gap form one row of whole vectors
+        const bool dense = a.ts == piece && (layer_runs || a.group == a.L);
+        if (dense) a.join = W / gcd_of(W, piece);
+        if (dense && a.join * piece / W > 256) a.join = 1;
+    }
+    a.row_stride = a.join * a.ts;
+    a.cols = pieces ? (a.join * piece + W - 1) / W : piece;
+    if (a.cols > 256) return ROUTEPACK_E_UNSUPPORTED;
+    a.slots = 256 / a.cols;
+    a.copies = 1;
+    while (a.copies < 16 && 2 * a.copies * a.group * a.pitch <= kWords / 2) a.copies *= 2;
+    // chunks: about 2048 workgroups, but 64 tokens and more, and enough ids to
+    // outweigh the counters that each workgroup clears and hands over
+    const int64_t n_groups = (a.L + a.group - 1) / a.group;
+    a.shift = 6;
+    while (a.shift < 20 && (((a.T * n_groups) >> a.shift) > 2048 || ((int64_t)a.k << a.shift) < 4 * a.E) &&
+           ((int64_t)1 << a.shift) < a.T)
+        ++a.shift;
+    a.n_chunks = a.T > 0 ? (a.T + ((int64_t)1 << a.shift) - 1) >> a.shift : 1;
+    if (n_groups > 65535) return ROUTEPACK_E_UNSUPPORTED;
+    if (a.n_chunks > 1) {
+        const int64_t row_len = (int64_t)a.L * a.E;
+        const int64_t gx = a.N < 65536 ? a.N : 65536;
+        int64_t gy = (row_len + 1023) / 1024;
+        gy = gy > 16 ? 16 : gy;
+        hipLaunchKernelGGL(k_count_clear, dim3((unsigned)gx, (unsigned)gy), dim3(256), 0, stream, a);
+    }
+    const size_t lds = 4 * ((size_t)a.copies * a.group * a.pitch + 256);
+    auto go = [&](auto kern) -> int {
+        if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(kern),
+                                                   hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
+            return ROUTEPACK_E_DEVICE;
+        hipLaunchKernelGGL(kern, dim3((unsigned)a.n_chunks, (unsigned)n_groups), dim3(256), lds, stream, a);
+        return hipGetLastError() == hipSuccess ? ROUTEPACK_OK : ROUTEPACK_E_DEVICE;
+    };
+    if (pieces) return go(k_count<I, W>);
+    return go(k_count<I, 1>);
+}
+
+}  // namespace
 
 extern "C" int routepack_count_demand(const routepack_problem *prob, const routepack_ids *ids,
                                       const int64_t *offsets, int32_t *demand, hipStream_t stream) {
@@ -89,20 +261,26 @@ extern "C" int routepack_count_demand(const routepack_problem *prob, const route
     const int32_t L = prob->n_layers, E = prob->n_experts, k = prob->top_k;
     if (N < 0 || L < 0 || E < 1 || k < 1 || T < 0) return ROUTEPACK_E_INVALID;
     RP_TRY(check_ids(prob, ids, T));
-    if (E > 32768 || L > 65535 || T > INT32_MAX / k) return ROUTEPACK_E_UNSUPPORTED;
+    if (E > 32768 || k > 256 || T > INT32_MAX / k) return ROUTEPACK_E_UNSUPPORTED;
     if (N == 0 || L == 0) return ROUTEPACK_OK;
     if (!offsets || !demand) return ROUTEPACK_E_INVALID;
-    int64_t chunk = T * L / 4096;
-    chunk = chunk < 256 ? 256 : (chunk > 8192 ? 8192 : chunk);
-    const int64_t n_chunks = T > 0 ? (T + chunk - 1) / chunk : 1;
-    const CountArgs a = {ids->data, ids->token_stride, ids->layer_stride, T, chunk, n_chunks, ids->type, (int32_t)N, L,
-                         E, k, offsets, demand};
-    if (n_chunks > 1)
-        hipLaunchKernelGGL(k_count_clear, dim3((unsigned)(N < 65536 ? N : 65536)), dim3(256), 0, stream, a);
-    const size_t lds = (size_t)4 * E;
-    if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(k_count),
-                                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
-        return ROUTEPACK_E_DEVICE;
-    hipLaunchKernelGGL(k_count, dim3((unsigned)n_chunks, (unsigned)L), dim3(256), lds, stream, a);
-    return hipGetLastError() == hipSuccess ? ROUTEPACK_OK : ROUTEPACK_E_DEVICE;
+    CountArgs a = {};
+    a.ids = ids->data;
+    a.ts = ids->token_stride;
+    a.ls = ids->layer_stride;
+    a.T = T;
+    a.N = (int32_t)N;
+    a.L = L;
+    a.E = E;
+    a.k = k;
+    a.offsets = offsets;
+    a.demand = demand;
+    const bool token_rows = L == 1 || a.ls == k;   // a token's layers are adjacent
+    const bool layer_runs = !token_rows && a.ts == k;  // a layer's tokens are
+    switch (ids->type) {
+        case ROUTEPACK_U8: return count<uint8_t>(a, layer_runs, token_rows, stream);
+        case ROUTEPACK_I16: return count<int16_t>(a, layer_runs, token_rows, stream);
+        case ROUTEPACK_I32: return count<int32_t>(a, layer_runs, token_rows, stream);
+        default: return count<int64_t>(a, layer_runs, token_rows, stream);
+    }
 }

@@ -35,45 +35,122 @@ struct RouteArgs {
 template <class T>
 __device__ inline float to_f32(T v) { return (float)v; }
 
+// A vector of 16 bytes of logits, as four words; it may start at any element
+// (global memory takes unaligned accesses of any width).
 template <class T>
-struct __attribute__((packed, aligned(sizeof(T)))) Vec16 {
-    T v[16 / sizeof(T)];
+struct Vec {
+    static constexpr int W = 16 / sizeof(T);
+    uint32_t w[4];
+    __device__ float at(int i) const;
+    __device__ void set(const float (&x)[W]);
 };
+struct __attribute__((packed, aligned(2))) Words16 {
+    uint32_t w[4];
+};
+template <> __device__ inline float Vec<float>::at(int i) const { return __uint_as_float(w[i]); }
+template <> __device__ inline float Vec<__bf16>::at(int i) const {
+    return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+}
+template <> __device__ inline float Vec<_Float16>::at(int i) const {
+    typedef _Float16 half2_ __attribute__((ext_vector_type(2)));
+    return (float)__builtin_bit_cast(half2_, w[i / 2])[i & 1];
+}
+template <> __device__ inline void Vec<float>::set(const float (&x)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(x[i]);
+}
+template <> __device__ inline void Vec<__bf16>::set(const float (&x)[8]) {
+    typedef __bf16 two __attribute__((ext_vector_type(2)));
+    typedef float two32 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const two32 y = {x[2 * i], x[2 * i + 1]};
+        w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, two));
+    }
+}
+template <> __device__ inline void Vec<_Float16>::set(const float (&x)[8]) {
+    typedef _Float16 two __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const two y = {(_Float16)x[2 * i], (_Float16)x[2 * i + 1]};
+        w[i] = __builtin_bit_cast(uint32_t, y);
+    }
+}
 
-// The row's part of one lane; elements past the row are -inf (no score).
-template <class T, int G, int V>
-__device__ inline void load_row(const T *row, int E, int c, float (&z)[V]) {
-    constexpr int W = 16 / sizeof(T);
-    static_assert(V % W == 0, "whole vectors");
-#pragma unroll
-    for (int i = 0; i < V / W; ++i) {
-        const int e0 = (i * G + c) * W;
+template <class T>
+__device__ inline uint32_t bits_of(const T *p) {
+    if constexpr (sizeof(T) == 4) return *reinterpret_cast<const uint32_t *>(p);
+    else return *reinterpret_cast<const uint16_t *>(p);
+}
+
+// A row of E elements by vectors; those past its end are -inf.
+template <class T>
+struct Row {
+    static constexpr int W = Vec<T>::W;
+    const T *data;
+    int32_t E;
+    __device__ Vec<T> vec(int v) const {
+        constexpr uint32_t kLow = sizeof(T) == 4 ? 0xFF800000u : (__is_same(T, __bf16) ? 0xFF80u : 0xFC00u);
+        const int e0 = v * W;
+        Vec<T> x;
         if (e0 + W <= E) {
-            const Vec16<T> w = *reinterpret_cast<const Vec16<T> *>(row + e0);
+            const Words16 y = *reinterpret_cast<const Words16 *>(data + e0);
 #pragma unroll
-            for (int x = 0; x < W; ++x) z[i * W + x] = to_f32(w.v[x]);
+            for (int i = 0; i < 4; ++i) x.w[i] = y.w[i];
         } else {
 #pragma unroll
-            for (int x = 0; x < W; ++x) z[i * W + x] = e0 + x < E ? to_f32(row[e0 + x]) : -kInf;
+            for (int i = 0; i < 4; ++i) x.w[i] = sizeof(T) == 4 ? kLow : kLow << 16 | kLow;
+            // (one vector of the row at most is cut: a loop, not W branches)
+            for (int i = 0; e0 + i < E; ++i) {
+                const uint32_t b = bits_of(data + e0 + i);
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    if constexpr (sizeof(T) == 4) {
+                        x.w[n] = n == i ? b : x.w[n];
+                    } else {
+                        x.w[n] = 2 * n == i ? (x.w[n] & 0xFFFF0000u) | b : x.w[n];
+                        x.w[n] = 2 * n + 1 == i ? (x.w[n] & 0xFFFFu) | b << 16 : x.w[n];
+                    }
+                }
+            }
         }
+        return x;
     }
+};
+
+// The row's part of one lane.
+template <class T, int G, int V>
+__device__ inline void load_row(const T *row, int E, int c, float (&z)[V]) {
+    constexpr int W = Vec<T>::W;
+    static_assert(V % W == 0, "whole vectors");
+    const Row<T> r = {row, E};
+    Vec<T> x[V / W];
+#pragma unroll
+    for (int i = 0; i < V / W; ++i) x[i] = r.vec(i * G + c);
+#pragma unroll
+    for (int v = 0; v < V; ++v) z[v] = x[v / W].at(v % W);
 }
 
 template <class T, int G, int V>
 __device__ inline void store_row(T *row, int E, int c, const float (&z)[V]) {
-    constexpr int W = 16 / sizeof(T);
+    constexpr int W = Vec<T>::W;
 #pragma unroll
     for (int i = 0; i < V / W; ++i) {
         const int e0 = (i * G + c) * W;
-        if (e0 + W <= E) {
-            Vec16<T> w;
+        float y[W];
 #pragma unroll
-            for (int x = 0; x < W; ++x) w.v[x] = (T)z[i * W + x];
-            *reinterpret_cast<Vec16<T> *>(row + e0) = w;
+        for (int x = 0; x < W; ++x) y[x] = z[i * W + x];
+        if (e0 + W <= E) {
+            Vec<T> w;
+            w.set(y);
+            Words16 b;
+#pragma unroll
+            for (int n = 0; n < 4; ++n) b.w[n] = w.w[n];
+            *reinterpret_cast<Words16 *>(row + e0) = b;
         } else {
 #pragma unroll
             for (int x = 0; x < W; ++x)
-                if (e0 + x < E) row[e0 + x] = (T)z[i * W + x];
+                if (e0 + x < E) row[e0 + x] = (T)y[x];
         }
     }
 }

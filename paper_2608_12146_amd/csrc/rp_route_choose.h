@@ -29,22 +29,6 @@ __device__ inline float most_of(const float (&x)[8]) {
     return max3(max3(max3(x[0], x[1], x[2]), x[3], x[4]), max3(x[5], x[6], x[7]), x[7]);
 }
 
-template <class T>
-struct Row {
-    static constexpr int W = 16 / sizeof(T);
-    const T *data;
-    int32_t E;
-    // vector v of the row; elements past its end are -inf
-    __device__ Vec16<T> vec(int v) const {
-        const int e0 = v * W;
-        if (e0 + W <= E) return *reinterpret_cast<const Vec16<T> *>(data + e0);
-        Vec16<T> x;
-#pragma unroll
-        for (int i = 0; i < W; ++i) x.v[i] = e0 + i < E ? data[e0 + i] : (T)(-kInf);
-        return x;
-    }
-};
-
 template <class T, int G, int NV, int K>
 __global__ void __launch_bounds__(256) k_route(RouteArgs a) {
     using Key = typename KeyOf<T>::type;
@@ -53,7 +37,7 @@ __global__ void __launch_bounds__(256) k_route(RouteArgs a) {
     const int c = threadIdx.x & (G - 1);
     const Item it = item_of<G>(a.T, a.L);
     const Row<T> row = {static_cast<const T *>(a.logits) + it.t * a.ts + it.l * a.ls, a.E};
-    Vec16<T> raw[NV];
+    Vec<T> raw[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) raw[i] = row.vec(i * G + c);
     // the k vectors of largest maximum
@@ -63,7 +47,7 @@ __global__ void __launch_bounds__(256) k_route(RouteArgs a) {
     for (int i = 0; i < NV; ++i) {
         float x[W];
 #pragma unroll
-        for (int w = 0; w < W; ++w) x[w] = to_f32(raw[i].v[w]);
+        for (int w = 0; w < W; ++w) x[w] = raw[i].at(w);
         mx[i] = most_of(x);
         odd = odd || mx[i] != mx[i];
     }
@@ -72,7 +56,7 @@ __global__ void __launch_bounds__(256) k_route(RouteArgs a) {
         for (int i = 0; i < NV; ++i) {
             mx[i] = -kInf;
 #pragma unroll
-            for (int w = 0; w < W; ++w) mx[i] = __builtin_fmaxf(mx[i], to_f32(raw[i].v[w]) + 0.0f);
+            for (int w = 0; w < W; ++w) mx[i] = __builtin_fmaxf(mx[i], raw[i].at(w) + 0.0f);
         }
     }
     Word vk[NV], first[K];
@@ -87,7 +71,7 @@ __global__ void __launch_bounds__(256) k_route(RouteArgs a) {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int w = 0; w < W; ++w) sum += exp_plain(to_f32(raw[i].v[w]) - m);
+            for (int w = 0; w < W; ++w) sum += exp_plain(raw[i].at(w) - m);
         sum = group_sum<G>(sum);
         inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     }
@@ -103,10 +87,10 @@ __global__ void __launch_bounds__(256) k_route(RouteArgs a) {
 #pragma unroll
         for (int w = 0; w < W; ++w) x[s * W + w] = Word(0);
         if (ok) {
-            const Vec16<T> y = row.vec((int)v);
+            const Vec<T> y = row.vec((int)v);
             const uint32_t inv0 = kIndexMask ^ (v * W);
 #pragma unroll
-            for (int w = 0; w < W; ++w) x[s * W + w] = Key::make(to_f32(y.v[w]), inv0 ^ (uint32_t)w);
+            for (int w = 0; w < W; ++w) x[s * W + w] = Key::make(y.at(w), inv0 ^ (uint32_t)w);
         }
     }
     lane_top<Key, K, S * W>(x, top);
@@ -154,17 +138,25 @@ __device__ inline void group_first(uint64_t &key, uint32_t &at) {
     }
 }
 
-// The choices by score + bias.  The two selections run on keys in 32 bits,
-// which are off by at most (64 + 2 |key|) 2^-24 (see below).  Where that
-// leaves the order of the k choices, or the last of them against the rest,
-// open (two keys within twice that), the wave repeats the selection on keys in
-// 64 bits, by k rounds of a maximum over the row: about one wave in a hundred
-// with random logits; exact ties always.
+template <class T, int N>
+__device__ inline void shift_down(T (&a)[N]) {
+#pragma unroll
+    for (int i = 0; i + 1 < N; ++i) a[i] = a[i + 1];
+}
+
+// The choices by score + bias.  The two selections run on keys in 32 bits.
+// Where their error leaves the order of the k choices, or the last of them
+// against the rest, open, the wave orders the elements of the vectors in
+// question (the chosen ones and, in a second batch, the next K) by keys in 64
+// bits, or the whole row where even the second batch does not hold every
+// candidate.  With random logits about one token in 500 is open and none needs
+// the whole row; tokens with equal keys always are.  That part is loops of
+// little code: few waves run it, each would wait for all of its instructions.
 //
-// A score's error in 32 bits, in steps u = 2^-24: logistic, 8 s u
-// (exponential 4 u, the sum, the inverse and the product 4 u); softmax,
-// p (|z - m| + 54) u with p |z - m| < 0.37, so at most 55 u.  The
-// sum with the bias is rounded once: |key| u.
+// A score's error in 32 bits, in steps u = 2^-24: logistic, 8 u s <= 8 u (the
+// exponential 4, the sum, the inverse and the product 4); softmax,
+// p (|z - m| + 54) u with p |z - m| < 0.5 and p <= inv, the inverse of the
+// row's sum.  The sum with the bias is rounded once: |key| u.
 template <class T, int G, int NV, int K>
 __global__ void __launch_bounds__(256) k_route_bias(RouteArgs a) {
     using Key = Key32;
@@ -175,33 +167,29 @@ __global__ void __launch_bounds__(256) k_route_bias(RouteArgs a) {
     const Row<T> row = {static_cast<const T *>(a.logits) + it.t * a.ts + it.l * a.ls, a.E};
     const float *bias = a.bias + (int64_t)it.l * a.E;
     const bool softmax = a.score == ROUTEPACK_SOFTMAX;
-    Vec16<T> raw[NV];
+    Vec<T> raw[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) raw[i] = row.vec(i * G + c);
     float m = 0.0f, inv = 0.0f;
     if (softmax) {
         float z[NV * W];
 #pragma unroll
-        for (int v = 0; v < NV * W; ++v) z[v] = to_f32(raw[v / W].v[v % W]);
+        for (int v = 0; v < NV * W; ++v) z[v] = raw[v / W].at(v % W);
         row_sum<G, NV * W>(z, m, inv);
     }
     // a vector's keys in 32 bits; -inf where the expert is not available
-    auto keys_of = [&](const Vec16<T> &r, int v, float (&y)[W]) {
-        float b[W];
-        if (v * W + W <= a.E) {
+    const Row<float> bias_row = {bias, a.E};
+    auto keys_of = [&](const Vec<T> &r, int v, float (&y)[W]) {
+        Vec<float> b[W / 4];
 #pragma unroll
-            for (int w = 0; w < W; ++w) b[w] = bias[v * W + w];
-        } else {
-#pragma unroll
-            for (int w = 0; w < W; ++w) b[w] = v * W + w < a.E ? bias[v * W + w] : -kInf;
-        }
+        for (int n = 0; n < W / 4; ++n) b[n] = bias_row.vec(v * (W / 4) + n);
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-            const float z = to_f32(r.v[w]);
+            const float z = r.at(w);
             float s, less;
             if (softmax) s = exp32(z - m) * inv;
             else logistic(z, s, less);
-            const float key = s + b[w];
+            const float key = s + b[w / 4].at(w % 4);
             y[w] = z > -kInf && key > -kInf ? key : -kInf;
         }
     };
@@ -246,35 +234,32 @@ __global__ void __launch_bounds__(256) k_route_bias(RouteArgs a) {
     }
     lane_top<Key, K, S * W>(x, top);
     group_top<Key, K, M>(top);
-    // is the order beyond doubt?
+    // is the order beyond doubt?  Two keys further apart than `slack` are in order.
+    const float err = softmax ? 0.5f + 54.0f * inv : 8.0f;
+    auto slack = [&](float key) { return (err + 2.0f * __builtin_fabsf(key)) * 0x1p-23f; };
     bool open = false;
-    float last = 0.0f;
-    bool full = false;  // k experts are available
+    float edge = -kInf;  // a key below it is not among the k largest
 #pragma unroll
     for (int j = 0; j < K; ++j) {
         if (j >= a.k || !Key::available(top[j])) continue;
         const float v = Key::value(top[j]);
         if (j > 0) {
             const float u = Key::value(top[j > 0 ? j - 1 : 0]);
-            const float slack = (128.0f + 4.0f * __builtin_fmaxf(__builtin_fabsf(u), __builtin_fabsf(v))) * 0x1p-24f;
-            open = open || !(u - v > slack);
+            open = open || !(u - v > slack(u) && u - v > slack(v));
         }
-        if (j == a.k - 1) {
-            last = v;
-            full = true;
-        }
+        if (j == a.k - 1) edge = v - slack(v);
     }
-    if (full) {
-        const float edge = last - (128.0f + 8.0f * __builtin_fabsf(last)) * 0x1p-24f;
-        float over = 0.0f;  // elements at or over the edge, besides the choices, and vectors not taken
+    // from the edge on: elements of the chosen vectors, and other vectors
+    float over = 0.0f, more = 0.0f;
 #pragma unroll
-        for (int n = 0; n < S * W; ++n) over += near_[n] >= edge && near_[n] > -kInf ? 1.0f : 0.0f;
+    for (int n = 0; n < S * W; ++n) over += near_[n] >= edge && near_[n] > -kInf ? 1.0f : 0.0f;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) over += mx[i] >= edge && mx[i] > -kInf ? 1.0f : 0.0f;
+    for (int i = 0; i < NV; ++i) more += mx[i] >= edge && mx[i] > -kInf ? 1.0f : 0.0f;
 #pragma unroll
-        for (int s = 0; s < S; ++s) over -= most[s] >= edge && most[s] > -kInf ? 1.0f : 0.0f;
-        open = open || !(group_sum<G>(over) == (float)a.k) || !(edge == edge);
-    }
+    for (int s = 0; s < S; ++s) more -= most[s] >= edge && most[s] > -kInf ? 1.0f : 0.0f;
+    over = group_sum<G>(over);
+    more = group_sum<G>(more);
+    open = open || (edge > -kInf && (over != (float)a.k || more != 0.0f)) || edge != edge;
     float zc[S], g[S], less[S];
     bool on[S];
     int32_t id[S];
@@ -286,47 +271,113 @@ __global__ void __launch_bounds__(256) k_route_bias(RouteArgs a) {
         id[s] = s * M + c < a.k && Key::available(mine) ? (int32_t)Key::index(mine) : -1;
     }
     if (__any(open)) {
-        uint64_t key[NV * W];
         double sum = 0.0;
         if (softmax) {
+#pragma unroll 1
+            for (int i = 0; i < NV; ++i) {
+                float z[W];
+                const Vec<T> y = row.vec(i * G + c);
 #pragma unroll
-            for (int v = 0; v < NV * W; ++v) {
-                const float z = to_f32(raw[v / W].v[v % W]);
-                sum += z > -kInf ? exp((double)z - (double)m) : 0.0;
+                for (int w = 0; w < W; ++w) z[w] = y.at(w);
+#pragma unroll 1
+                for (int w = 0; w < W; ++w) {
+                    sum += z[0] > -kInf ? exp((double)z[0] - (double)m) : 0.0;
+                    shift_down(z);
+                }
             }
 #pragma unroll
             for (int d = 1; d < G; d <<= 1) sum += __shfl_xor(sum, d, kWave);
         }
+        Word next[K];
 #pragma unroll
-        for (int v = 0; v < NV * W; ++v) {
-            const float z = to_f32(raw[v / W].v[v % W]);
-            const int e = elem_of<T, G>(v, c);
-            key[v] = 0;
-            if (z > -kInf && e < a.E) {
-                double s = softmax ? exp((double)z - (double)m) / sum : 1.0 / (1.0 + exp(-(double)z));
-                s += (double)bias[e];
-                if (s > -__builtin_inf()) key[v] = order64(s);
+        for (int j = 0; j < K; ++j) next[j] = Word(0);
+        const bool second = __any(more > 0.0f);
+        bool deep = false;
+        if (second) {  // the vectors after the first k
+            Word kth = Word(0);
+#pragma unroll
+            for (int j = 0; j < K; ++j) kth = j == a.k - 1 ? first[j] : kth;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) vk[i] = Key::available(kth) && vk[i] < kth ? vk[i] : Word(0);
+            lane_top<Key, K, NV>(vk, next);
+            group_top<Key, K, G>(next);
+            deep = __any(Key::available(next[K - 1]) && Key::value(next[K - 1]) >= edge);
+        }
+        int at[2 * S];  // this lane's vectors of both batches
+#pragma unroll
+        for (int s = 0; s < 2 * S; ++s) {
+            Word mine = Word(0);
+#pragma unroll
+            for (int j = 0; j < M; ++j) {
+                const Word w = s < S ? first[s % S * M + j] : next[s % S * M + j];
+                mine = c == j ? w : mine;
+            }
+            const bool ok = c < M && (s >= S || s * M + c < a.k) && Key::available(mine);
+            at[s] = ok ? (int)Key::index(mine) : kMaxExperts;
+        }
+        // a lane's K largest candidates, sorted by insertion
+        uint64_t best[K];
+        uint32_t who[K];
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            best[j] = 0;
+            who[j] = UINT32_MAX;
+        }
+#pragma unroll 1
+        for (int i = 0; i < (deep ? NV : second ? 2 * S : S); ++i) {
+            int v = i * G + c;
+            if (!deep) {
+                v = at[0];
+                shift_down(at);
+            }
+            if (v * W >= a.E) continue;
+            float z[W], b[W];
+            const Vec<T> y = row.vec(v);
+            Vec<float> bv[W / 4];
+#pragma unroll
+            for (int n = 0; n < W / 4; ++n) bv[n] = bias_row.vec(v * (W / 4) + n);
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                z[w] = y.at(w);
+                b[w] = bv[w / 4].at(w % 4);
+            }
+#pragma unroll 1
+            for (int w = 0; w < W; ++w) {
+                const double x = (double)z[0];
+                double key = softmax ? exp(x - (double)m) / sum : 1.0 / (1.0 + exp(-x));
+                key += (double)b[0];
+                uint64_t k0 = z[0] > -kInf && key > -__builtin_inf() ? order64(key) : 0;
+                uint32_t e0 = (uint32_t)(v * W + w);
+                shift_down(z);
+                shift_down(b);
+#pragma unroll
+                for (int j = 0; j < K; ++j) {
+                    const bool before = k0 > best[j] || (k0 == best[j] && e0 < who[j]);
+                    const uint64_t k1 = best[j];
+                    const uint32_t e1 = who[j];
+                    best[j] = before ? k0 : k1;
+                    who[j] = before ? e0 : e1;
+                    k0 = before ? k1 : k0;
+                    e0 = before ? e1 : e0;
+                }
             }
         }
 #pragma unroll
         for (int s = 0; s < S; ++s) id[s] = -1;
+#pragma unroll 1
         for (int j = 0; j < a.k; ++j) {
-            uint64_t best = 0;
-            uint32_t at = UINT32_MAX;
-#pragma unroll
-            for (int v = 0; v < NV * W; ++v) {  // (a lane's elements ascend)
-                if (key[v] > best) {
-                    best = key[v];
-                    at = (uint32_t)elem_of<T, G>(v, c);
-                }
+            uint64_t k0 = best[0];
+            uint32_t e0 = who[0];
+            group_first<G>(k0, e0);
+            if (who[0] == e0) {
+                shift_down(best);
+                shift_down(who);
+                best[K - 1] = 0;
+                who[K - 1] = UINT32_MAX;
             }
-            group_first<G>(best, at);
-#pragma unroll
-            for (int v = 0; v < NV * W; ++v)
-                if ((uint32_t)elem_of<T, G>(v, c) == at) key[v] = 0;
 #pragma unroll
             for (int s = 0; s < S; ++s)
-                if (j == s * M + c && best) id[s] = (int32_t)at;
+                if (j == s * M + c && k0) id[s] = (int32_t)e0;
         }
     }
 #pragma unroll
@@ -355,6 +406,7 @@ int choose(const RouteArgs &a, hipStream_t stream) {
     if (a.bias)
         return by_geometry<T, 2 * sizeof(T)>(a.E, [&](auto g, auto nv) {
             if (a.k <= 8) return go(k_route_bias<T, g.value, nv.value, 8>, g.value);
+            if (a.k <= 16) return go(k_route_bias<T, g.value, nv.value, 16>, g.value);
             return go(k_route_bias<T, g.value, nv.value, 32>, g.value);
         });
     return by_geometry<T, 8>(a.E, [&](auto g, auto nv) {
