@@ -96,7 +96,7 @@ int routepack_route_tokens(const routepack_problem *prob, const routepack_logits
  *   offsets  int64 [N + 1]
  *   demand   int32 [N][L][E] out
  * E_INVALID on null pointers, a negative size or stride, k < 1 or an unknown
- * type; E_UNSUPPORTED when E > 32768, k > 256 or T k >= 2^31 (a count would not
+ * type; E_UNSUPPORTED when E > 16384, k > 256 or T k >= 2^31 (a count would not
  * fit). */
 int routepack_count_demand(const routepack_problem *prob, const routepack_ids *ids,
                            const int64_t *offsets, int32_t *demand, hipStream_t stream);

@@ -1,12 +1,15 @@
 // The balance loss over expert counts (shares of the router's scores against
 // the fractions of its choices), on gfx950.
 //
-// The tokens are cut into chunks of equal length; a workgroup takes one chunk
-// of one layer and sums the shares of each group that meets it into a row of
-// its own (group g's part of chunk c is row c + g: both only grow along the
-// tokens, so no two parts share a row).  A second kernel adds every group's
-// rows in their order and forms its part of the loss, a third one adds the
-// groups.  No atomics: the result does not depend on the launch.
+// Reading the logits once is the floor.  The tokens are cut into chunks of
+// equal length; a workgroup takes one chunk of one layer, keeps running sums of
+// the shares in registers (a group of lanes a token) and writes one row of sums
+// for each group of the loss that meets its chunk: group g's part of chunk c is
+// row c + g (both only grow along the tokens, so no two parts share a row).  A
+// second kernel adds every group's rows in their order, a slab of 64 experts a
+// workgroup, and forms the slab's part of the loss; the last workgroup of a
+// layer to arrive adds those parts, again in their order.  No floating-point
+// atomics: the result does not depend on the launch.
 #include "rp_internal.h"
 #include "rp_route.h"
 
@@ -14,106 +17,180 @@ namespace rp {
 
 struct ShareArgs {
     const void *logits;
-    int64_t ts, ls, T, chunk;
-    int32_t L, E, n_groups, score;
+    int64_t ts, ls, T, n_chunks;
+    int32_t chunk, L, E, n_groups;
     const int64_t *offsets;
-    float *rows;  // [n_chunks + n_groups][L][E]
+    float *rows;        // [n_chunks + n_groups][L][E]
+    uint32_t *arrived;  // [L], cleared here
 };
 
 __device__ inline int64_t clamp64(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : (x > hi ? hi : x); }
 
-template <class T, int V>
+template <class T, int G, int NV, bool SOFTMAX>
 __global__ void __launch_bounds__(256) k_share_chunks(ShareArgs a) {
-    extern __shared__ float part[];  // [4][E]
-    const int64_t ch = blockIdx.x;
-    const int32_t l = (int32_t)blockIdx.y;
-    const int c = lane_id(), wv = wave_id();
+    constexpr int W = 16 / sizeof(T), V = NV * W, SLOTS = 256 / G, EP = G * V;
+    __shared__ __align__(16) float part[SLOTS * EP];
+    const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    const int64_t ch = a.L == 1 ? block : block / a.L;
+    const int32_t l = a.L == 1 ? 0 : (int32_t)(block - ch * a.L);
+    const int tid = threadIdx.x, c = tid & (G - 1), slot = tid / G, lane = lane_id();
+    if (ch == 0 && tid == 0) a.arrived[l] = 0;
+    if (ch >= a.n_chunks) return;
     const int64_t t0 = ch * a.chunk, t1 = t0 + a.chunk < a.T ? t0 + a.chunk : a.T;
-    // the first group that ends behind t0
+    // the first group that ends behind t0: 64 probes a round
     int32_t lo = 0, hi = a.n_groups;
     while (lo < hi) {
-        const int32_t mid = lo + (hi - lo) / 2;
-        if (a.offsets[mid + 1] > t0) hi = mid;
-        else lo = mid + 1;
+        const int32_t step = (hi - lo + kWave - 1) / kWave;
+        const int64_t p = lo + (int64_t)lane * step;
+        const uint64_t yes = __ballot(p >= hi || a.offsets[(p < hi ? p : lo) + 1] > t0);
+        const int f = yes ? first_lane(yes) : kWave;
+        const int64_t past = lo + (int64_t)f * step;
+        const int64_t from = f > 0 ? lo + (int64_t)(f - 1) * step + 1 : lo;
+        hi = past < hi ? (int32_t)past : hi;
+        lo = from < hi ? (int32_t)from : hi;
     }
     for (int32_t g = lo; g < a.n_groups; ++g) {
-        const int64_t b = clamp64(a.offsets[g], t0, t1), e = clamp64(a.offsets[g + 1], t0, t1);
-        if (a.offsets[g] >= t1) break;
+        const int64_t from = a.offsets[g];
+        if (from >= t1) break;
+        const int64_t b = clamp64(from, t0, t1), e = clamp64(a.offsets[g + 1], t0, t1);
         if (b >= e) continue;
         float acc[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) acc[v] = 0.0f;
-        for (int64_t t = b + wv; t < e; t += 4) {
-            float z[V], less[V];
-            load_row<T, kWave, V>(static_cast<const T *>(a.logits) + t * a.ts + l * a.ls, a.E, c, z);
-            if (a.score == ROUTEPACK_SOFTMAX) softmax_row<kWave, V>(z);
-            else logistic_row<kWave, V>(z, less);
+        for (int64_t t = b + slot; t < e; t += SLOTS) {
+            float z[V];
+            load_row<T, G, V>(static_cast<const T *>(a.logits) + t * a.ts + l * a.ls, a.E, c, z);
+            if constexpr (SOFTMAX) {
+                float m, inv;
+                softmax_row<G, V>(z, m, inv);
+            } else {
+                float less[V];
+                logistic_row<G, V>(z, less);
+            }
 #pragma unroll
             for (int v = 0; v < V; ++v) acc[v] += z[v];
         }
         __syncthreads();
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int x = elem_of<T, kWave>(v, c);
-            if (x < a.E) part[wv * a.E + x] = acc[v];
-        }
+        for (int v = 0; v < V; v += 4)
+            *reinterpret_cast<float4 *>(part + slot * EP + elem_of<T, G>(v, c)) =
+                make_float4(acc[v], acc[v + 1], acc[v + 2], acc[v + 3]);
         __syncthreads();
         float *dst = a.rows + ((ch + g) * a.L + l) * a.E;
-        for (int x = threadIdx.x; x < a.E; x += 256)
-            dst[x] = (part[x] + part[a.E + x]) + (part[2 * a.E + x] + part[3 * a.E + x]);
+        if constexpr (EP >= 256) {
+            for (int x = tid; x < a.E; x += 256) {
+                float s = 0.0f;
+#pragma unroll 8
+                for (int y = 0; y < SLOTS; ++y) s += part[y * EP + x];
+                dst[x] = s;
+            }
+        } else {
+            constexpr int P = 256 / EP;
+            const int x = tid & (EP - 1), y0 = tid / EP;
+            float s = 0.0f;
+#pragma unroll 8
+            for (int y = y0; y < SLOTS; y += P) s += part[y * EP + x];
+            __syncthreads();
+            part[tid] = s;
+            __syncthreads();
+            if (tid < a.E) {
+                s = part[tid];
+#pragma unroll
+                for (int y = 1; y < P; ++y) s += part[y * EP + tid];
+                dst[tid] = s;
+            }
+        }
     }
 }
 
 struct LossArgs {
     const float *rows;
-    int64_t T, chunk;
-    int32_t L, E, n_groups, counts_type;
+    int64_t T;
+    int32_t chunk, L, E, n_groups, n_slabs, counts_type;
     const int64_t *offsets;
     const void *counts;
-    float *shares;
-    double *parts;  // [L][n_groups]
+    float *loss, *shares;
+    double *parts;  // [L][n_groups][n_slabs][2]
+    uint32_t *arrived;
 };
 
-__device__ inline double block_sum(double v, double *red) {
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) v += __shfl_xor(v, d, kWave);
-    __syncthreads();
-    if (lane_id() == 0) red[wave_id()] = v;
-    __syncthreads();
-    return (red[0] + red[1]) + (red[2] + red[3]);
-}
-
-__global__ void __launch_bounds__(256) k_group_loss(LossArgs a) {
-    __shared__ double red[4];
+// R rows abreast of 64 experts.
+template <int R>
+__global__ void __launch_bounds__(64 * R) k_group_loss(LossArgs a) {
+    __shared__ double red[R][kWave];
+    __shared__ bool last;
+    const int64_t n_items = (int64_t)a.n_groups * a.L * a.n_slabs;
     const int64_t item = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-    if (item >= (int64_t)a.n_groups * a.L) return;
-    const int32_t g = (int32_t)(item / a.L), l = (int32_t)(item - (int64_t)g * a.L);
+    if (item >= n_items) return;
+    const int32_t slab = (int32_t)(item % a.n_slabs);
+    const int64_t gl = item / a.n_slabs;
+    const int32_t g = (int32_t)(gl / a.L), l = (int32_t)(gl - (int64_t)g * a.L);
+    const int lane = lane_id(), r = wave_id();
+    const int32_t x = slab * kWave + lane;
     const int64_t b = clamp64(a.offsets[g], 0, a.T), e = clamp64(a.offsets[g + 1], 0, a.T);
-    const int64_t at = item * a.E;
-    double dot = 0.0, sum = 0.0;
-    for (int x = threadIdx.x; x < a.E; x += 256) {
-        double s = 0.0;
-        if (b < e) {
-            for (int64_t ch = b / a.chunk; ch <= (e - 1) / a.chunk; ++ch) s += a.rows[((ch + g) * a.L + l) * a.E + x];
-            s /= (double)(e - b);
-        }
-        const double n = (double)(a.counts_type == ROUTEPACK_I32 ? static_cast<const int32_t *>(a.counts)[at + x]
-                                                                 : static_cast<const int64_t *>(a.counts)[at + x]);
-        a.shares[at + x] = (float)s;
-        dot += n * s;
-        sum += n;
-    }
-    dot = block_sum(dot, red);
-    sum = block_sum(sum, red);
-    if (threadIdx.x == 0) a.parts[(int64_t)l * a.n_groups + g] = sum > 0.0 ? a.E * dot / sum : 0.0;
-}
-
-__global__ void __launch_bounds__(256) k_sum_loss(const double *parts, int32_t n_groups, float *loss) {
-    __shared__ double red[4];
     double s = 0.0;
-    for (int32_t g = threadIdx.x; g < n_groups; g += 256) s += parts[(int64_t)blockIdx.x * n_groups + g];
-    s = block_sum(s, red);
-    if (threadIdx.x == 0) loss[blockIdx.x] = (float)(s / n_groups);
+    if (b < e && x < a.E) {
+        const int64_t c1 = (e - 1) / a.chunk;
+        const int64_t pitch = (int64_t)a.L * a.E;
+        const float *p = a.rows + (int64_t)g * pitch + (int64_t)l * a.E + x;
+        int64_t ch = b / a.chunk + r;
+        for (; ch + 3 * R <= c1; ch += 4 * R) {
+            const float y0 = p[ch * pitch], y1 = p[(ch + R) * pitch], y2 = p[(ch + 2 * R) * pitch],
+                        y3 = p[(ch + 3 * R) * pitch];
+            s += ((double)y0 + (double)y1) + ((double)y2 + (double)y3);
+        }
+        for (; ch <= c1; ch += R) s += (double)p[ch * pitch];
+    }
+    red[r][lane] = s;
+    __syncthreads();
+    if (r == 0) {
+#pragma unroll
+        for (int y = 1; y < R; ++y) s += red[y][lane];
+        double dot = 0.0, sum = 0.0;
+        if (x < a.E) {
+            const int64_t at = gl * a.E + x;
+            s = b < e ? s / (double)(e - b) : 0.0;
+            const double n = (double)(a.counts_type == ROUTEPACK_I32 ? static_cast<const int32_t *>(a.counts)[at]
+                                                                     : static_cast<const int64_t *>(a.counts)[at]);
+            a.shares[at] = (float)s;
+            dot = n * s;
+            sum = n;
+        }
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) {
+            dot += __shfl_xor(dot, d, kWave);
+            sum += __shfl_xor(sum, d, kWave);
+        }
+        if (lane == 0) {
+            double *part = a.parts + (((int64_t)l * a.n_groups + g) * a.n_slabs + slab) * 2;
+            __hip_atomic_store(part, dot, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_store(part + 1, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            const uint32_t before = __hip_atomic_fetch_add(a.arrived + l, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+            last = before == (uint32_t)a.n_groups * (uint32_t)a.n_slabs - 1;
+        }
+    }
+    __syncthreads();
+    if (!last) return;
+    // the layer's parts, all there
+    double total = 0.0;
+    for (int32_t y = threadIdx.x; y < a.n_groups; y += 64 * R) {
+        double *part = a.parts + ((int64_t)l * a.n_groups + y) * a.n_slabs * 2;
+        double dot = 0.0, sum = 0.0;
+        for (int32_t z = 0; z < a.n_slabs; ++z) {
+            dot += __hip_atomic_load(part + 2 * z, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            sum += __hip_atomic_load(part + 2 * z + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        total += sum > 0.0 ? a.E * dot / sum : 0.0;
+    }
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) total += __shfl_xor(total, d, kWave);
+    __syncthreads();
+    if (lane == 0) red[0][r] = total;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int y = 1; y < R; ++y) total += red[0][y];
+        a.loss[l] = (float)(total / a.n_groups);
+    }
 }
 
 }  // namespace rp
@@ -122,21 +199,22 @@ using namespace rp;
 
 namespace {
 
-int64_t chunk_of(int64_t T, int32_t L) {
-    int64_t c = T * L / 2048;
-    return c < 16 ? 16 : (c > 1024 ? 1024 : c);
-}
-
-// The workspace: the chunks' rows, then the groups' parts of the loss.
+// The workspace: the chunks' rows, the groups' parts of the loss, and a count
+// of arrivals a layer.
 struct Workspace {
-    int64_t chunk, n_chunks, parts_at, bytes;
+    int64_t n_chunks, parts_at, arrived_at, bytes;
+    int32_t chunk;
 };
 Workspace workspace_of(int64_t T, int32_t L, int32_t E, int32_t n_groups) {
     Workspace w;
-    w.chunk = chunk_of(T, L);
-    w.n_chunks = (T + w.chunk - 1) / w.chunk;
+    // about 1024 workgroups of 32 tokens and more
+    int64_t c = 32;
+    while (c < 1024 && T * L > c * 1024) c *= 2;
+    w.chunk = (int32_t)c;
+    w.n_chunks = (T + c - 1) / c;
     w.parts_at = ((w.n_chunks + n_groups) * L * E * 4 + 15) & ~(int64_t)15;
-    w.bytes = w.parts_at + (int64_t)8 * L * n_groups;
+    w.arrived_at = w.parts_at + (int64_t)16 * L * n_groups * ((E + kWave - 1) / kWave);
+    w.bytes = w.arrived_at + (int64_t)4 * L;
     return w;
 }
 
@@ -158,22 +236,29 @@ extern "C" int routepack_balance_loss(const routepack_problem *prob, const route
     if (!offsets || !counts || !loss || !shares || !workspace || (uintptr_t)workspace % 16) return ROUTEPACK_E_INVALID;
     const Workspace w = workspace_of(logits->n_tokens, L, E, n_groups);
     if (workspace_bytes < w.bytes) return ROUTEPACK_E_INVALID;
-    if (L > 65535 || w.n_chunks > (1 << 23)) return ROUTEPACK_E_UNSUPPORTED;
     float *rows = static_cast<float *>(workspace);
     double *parts = reinterpret_cast<double *>(static_cast<char *>(workspace) + w.parts_at);
-    if (w.n_chunks > 0) {
-        const ShareArgs a = {logits->data, logits->token_stride, logits->layer_stride, logits->n_tokens, w.chunk,
-                             L, E, n_groups, score, offsets, rows};
-        by_type(logits->type, [&](auto tag) {
-            using T = decltype(tag);
-            const dim3 grid((unsigned)w.n_chunks, (unsigned)L);
-            if (E <= 512) hipLaunchKernelGGL((k_share_chunks<T, 8>), grid, dim3(256), (size_t)16 * E, stream, a);
-            else hipLaunchKernelGGL((k_share_chunks<T, 32>), grid, dim3(256), (size_t)16 * E, stream, a);
-            return 0;
+    uint32_t *arrived = reinterpret_cast<uint32_t *>(static_cast<char *>(workspace) + w.arrived_at);
+    const ShareArgs a = {logits->data, logits->token_stride, logits->layer_stride, logits->n_tokens, w.n_chunks,
+                         w.chunk, L, E, n_groups, offsets, rows, arrived};
+    const dim3 grid = grid_of((w.n_chunks > 0 ? w.n_chunks : 1) * L);
+    RP_TRY(by_type(logits->type, [&](auto tag) {
+        using T = decltype(tag);
+        return by_geometry<T, 2 * sizeof(T)>(E, [&](auto g, auto nv) {
+            if (score == ROUTEPACK_SOFTMAX)
+                hipLaunchKernelGGL((k_share_chunks<T, g.value, nv.value, true>), grid, dim3(256), 0, stream, a);
+            else
+                hipLaunchKernelGGL((k_share_chunks<T, g.value, nv.value, false>), grid, dim3(256), 0, stream, a);
+            return ROUTEPACK_OK;
         });
-    }
-    const LossArgs b = {rows, logits->n_tokens, w.chunk, L, E, n_groups, counts_type, offsets, counts, shares, parts};
-    hipLaunchKernelGGL(k_group_loss, grid_of((int64_t)n_groups * L), dim3(256), 0, stream, b);
-    hipLaunchKernelGGL(k_sum_loss, dim3((unsigned)L), dim3(256), 0, stream, parts, n_groups, loss);
+    }));
+    const int32_t slabs = (E + kWave - 1) / kWave;
+    const LossArgs b = {rows, logits->n_tokens, w.chunk, L, E, n_groups, slabs, counts_type, offsets, counts, loss,
+                        shares, parts, arrived};
+    const dim3 grid2 = grid_of((int64_t)n_groups * L * slabs);
+    const int64_t each = w.n_chunks / n_groups;  // rows of a group, about
+    if (each >= 64) hipLaunchKernelGGL(k_group_loss<16>, grid2, dim3(1024), 0, stream, b);
+    else if (each >= 8) hipLaunchKernelGGL(k_group_loss<4>, grid2, dim3(256), 0, stream, b);
+    else hipLaunchKernelGGL(k_group_loss<1>, grid2, dim3(64), 0, stream, b);
     return hipGetLastError() == hipSuccess ? ROUTEPACK_OK : ROUTEPACK_E_DEVICE;
 }

@@ -74,7 +74,7 @@ __device__ inline uint32_t id_of(I x) {
 // W ids a thread (16 bytes; where the row is not of one piece, W = 1).
 template <class I, int W>
 __global__ void __launch_bounds__(256) k_count(CountArgs a) {
-    extern __shared__ int32_t hist[];  // [copies][group][pitch], then a word a thread for what is not counted
+    extern __shared__ int32_t hist[];  // [copies][group][pitch], then [pitch] for what is not this thread's to count
     const int tid = threadIdx.x, lane = lane_id();
     const int64_t ch = blockIdx.x;
     const int32_t l0 = (int32_t)blockIdx.y * a.group;
@@ -101,24 +101,19 @@ __global__ void __launch_bounds__(256) k_count(CountArgs a) {
     // before holds already (the last place is moved back into the row)
     const int32_t want = col * W;
     const int32_t at = want + W <= len || len < W ? want : len - W;
-    uint32_t base[W];  // byte offset of the id's layer in the LDS, or none
-    const uint32_t none = (uint32_t)words * 4 + 4 * tid;
-    bool mine[W];
+    int32_t *to[W];  // the counters of each id's layer
 #pragma unroll
     for (int w = 0; w < W; ++w) {
         const int32_t x = at + w;
-        mine[w] = x >= want && x < len && slot < a.slots;
         const int32_t l = a.one_layer ? 0 : x % piece / a.k;
-        base[w] = (uint32_t)((lane % a.copies) * a.group + l) * (uint32_t)a.pitch * 4;
+        to[w] = x >= want && x < len ? hist + ((lane % a.copies) * a.group + l) * a.pitch : hist + words;
     }
     const I *ids = static_cast<const I *>(a.ids) + (int64_t)l0 * a.ls;
     // (where the row is not of one piece, W is 1: the thread's layer and choice)
     const int64_t place = W == 1 && !a.one_layer ? (int64_t)(at % piece / a.k) * a.ls + at % a.k : at;
+    // an id that is no expert's goes to the word behind the last expert's
     const uint32_t limit = (uint32_t)a.E;
-    auto add = [&](uint32_t id, int w) {
-        const uint32_t to = id < limit && mine[w] ? base[w] + id * 4 : none;
-        atomicAdd(reinterpret_cast<int32_t *>(reinterpret_cast<char *>(hist) + to), 1);
-    };
+    auto add = [&](uint32_t id, int w) { atomicAdd(to[w] + (id < limit ? id : limit), 1); };
     for (int32_t i = lo; i < a.N; ++i) {
         const Span s = span_of(a, i);
         if (s.first > ch) break;
@@ -167,16 +162,16 @@ __global__ void __launch_bounds__(256) k_count(CountArgs a) {
         __syncthreads();
         int32_t *row = a.demand + ((int64_t)i * a.L + l0) * a.E;
         const bool alone = s.first == s.last;
-        for (int32_t x = tid; x < nl * a.E; x += 256) {
-            const int32_t l = x / a.E, h = l * a.pitch + (x - l * a.E);
-            int32_t n = 0;
-            for (int32_t y = 0; y < a.copies; ++y) {
-                n += hist[y * a.group * a.pitch + h];
-                hist[y * a.group * a.pitch + h] = 0;
+        for (int32_t l = wave_id(); l < nl; l += 4)
+            for (int32_t x = lane; x < a.E; x += kWave) {
+                int32_t n = 0, *h = hist + l * a.pitch + x;
+                for (int32_t y = 0; y < a.copies; ++y, h += a.group * a.pitch) {
+                    n += *h;
+                    *h = 0;
+                }
+                if (alone) row[l * a.E + x] = n;
+                else if (n) atomicAdd(&row[l * a.E + x], n);
             }
-            if (alone) row[x] = n;
-            else if (n) atomicAdd(&row[x], n);
-        }
     }
 }
 
@@ -192,7 +187,7 @@ template <class I>
 int count(CountArgs &a, bool layer_runs, bool token_rows, hipStream_t stream) {
     constexpr int W = 16 / sizeof(I);
     constexpr int32_t kWords = 8192;  // 32 KiB of counters: four workgroups a CU and more
-    a.pitch = a.E | 1;  // (odd: equal experts of several layers stand in different banks)
+    a.pitch = (a.E + 1) | 1;  // (odd: equal experts of several layers stand in different banks)
     // Layers of a workgroup: as many as fit; where that is not all of them, such
     // that a token's piece is whole lines of 128 bytes, or whole vectors.
     int32_t fit = kWords / a.pitch;
@@ -224,11 +219,11 @@ int count(CountArgs &a, bool layer_runs, bool token_rows, hipStream_t stream) {
     a.slots = 256 / a.cols;
     a.copies = 1;
     while (a.copies < 16 && 2 * a.copies * a.group * a.pitch <= kWords / 2) a.copies *= 2;
-    // chunks: about 2048 workgroups, but 64 tokens and more, and enough ids to
+    // chunks: about 4096 workgroups, but 64 tokens and more, and enough ids to
     // outweigh the counters that each workgroup clears and hands over
     const int64_t n_groups = (a.L + a.group - 1) / a.group;
     a.shift = 6;
-    while (a.shift < 20 && (((a.T * n_groups) >> a.shift) > 2048 || ((int64_t)a.k << a.shift) < 4 * a.E) &&
+    while (a.shift < 20 && (((a.T * n_groups) >> a.shift) > 4096 || ((int64_t)a.k << a.shift) < 4 * a.E) &&
            ((int64_t)1 << a.shift) < a.T)
         ++a.shift;
     a.n_chunks = a.T > 0 ? (a.T + ((int64_t)1 << a.shift) - 1) >> a.shift : 1;
@@ -240,7 +235,7 @@ int count(CountArgs &a, bool layer_runs, bool token_rows, hipStream_t stream) {
         gy = gy > 16 ? 16 : gy;
         hipLaunchKernelGGL(k_count_clear, dim3((unsigned)gx, (unsigned)gy), dim3(256), 0, stream, a);
     }
-    const size_t lds = 4 * ((size_t)a.copies * a.group * a.pitch + 256);
+    const size_t lds = 4 * ((size_t)a.copies * a.group + 1) * a.pitch;
     auto go = [&](auto kern) -> int {
         if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(kern),
                                                    hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
@@ -261,7 +256,7 @@ extern "C" int routepack_count_demand(const routepack_problem *prob, const route
     const int32_t L = prob->n_layers, E = prob->n_experts, k = prob->top_k;
     if (N < 0 || L < 0 || E < 1 || k < 1 || T < 0) return ROUTEPACK_E_INVALID;
     RP_TRY(check_ids(prob, ids, T));
-    if (E > 32768 || k > 256 || T > INT32_MAX / k) return ROUTEPACK_E_UNSUPPORTED;
+    if (E > 16384 || k > 256 || T > INT32_MAX / k) return ROUTEPACK_E_UNSUPPORTED;
     if (N == 0 || L == 0) return ROUTEPACK_OK;
     if (!offsets || !demand) return ROUTEPACK_E_INVALID;
     CountArgs a = {};

@@ -32,6 +32,27 @@ struct RouteArgs {
     float *gates;
 };
 
+struct BackArgs {
+    const void *logits;
+    int64_t ts, ls;
+    int64_t T;
+    int32_t L, E, k;
+    const void *ids;  // null: no gates
+    int32_t id_type;
+    int64_t its, ils;
+    const float *dgates;
+    bool normalize;
+    float scale;
+    int32_t n_groups;
+    const int64_t *offsets;
+    const void *counts;
+    int32_t counts_type;
+    const float *dloss;  // null: no balance loss
+    int32_t score;
+    void *dlogits;
+};
+
+
 template <class T>
 __device__ inline float to_f32(T v) { return (float)v; }
 
@@ -247,8 +268,8 @@ __device__ inline void row_sum(const float (&z)[V], float &m, float &inv) {
 // Softmax of a row, in place: z becomes p.  A row without an available
 // expert becomes 0; a NaN or +inf in it makes it NaN.
 template <int G, int V>
-__device__ inline void softmax_row(float (&z)[V]) {
-    float m = z[0];
+__device__ inline void softmax_row(float (&z)[V], float &m, float &inv) {
+    m = z[0];
 #pragma unroll
     for (int v = 1; v < V; ++v) m = __builtin_fmaxf(m, z[v]);
     m = group_max<G>(m);
@@ -260,7 +281,7 @@ __device__ inline void softmax_row(float (&z)[V]) {
         sum += z[v];
     }
     sum = group_sum<G>(sum);
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
     for (int v = 0; v < V; ++v) z[v] *= inv;
 }

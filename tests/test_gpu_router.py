@@ -243,7 +243,7 @@ COUNTS = [  # lengths, rows past, L, E, k
     ([1], 0, 1, 1, 1), ([5], 3, 1, 16, 2), ([0], 4, 2, 8, 2), ([0, 0, 3, 0, 1, 0], 0, 3, 7, 3),
     ([16, 300, 1, 512, 77], 9, 4, 16, 2), ([2000, 1, 3000, 0, 17, 513], 100, 3, 60, 6),
     ([256] * 9 + [0] * 3, 0, 2, 64, 8), ([70000, 1, 0, 60001], 33, 2, 256, 8), ([9] * 1000, 5, 2, 33, 10),
-    ([40, 0, 900], 0, 24, 512, 8), ([123, 456], 0, 5, 5000, 3), ([64, 1], 0, 64, 130, 1), ([700], 0, 1, 30000, 40),
+    ([40, 0, 900], 0, 24, 512, 8), ([123, 456], 0, 5, 5000, 3), ([64, 1], 0, 64, 130, 1), ([700], 0, 1, 16384, 40),
 ]
 
 

@@ -71,7 +71,7 @@ def test_count_refusals():
     assert call(_problem(), I, off=None) == -1 and call(_problem(), I, out=None) == -1
     assert call(_problem(k=0), I) == -1 and call(_problem(E=0), I) == -1
     assert call(_problem(N=-1), I) == -1 and call(_problem(L=-1), I) == -1
-    assert call(_problem(E=32769), I) == -8 and call(_problem(), _rows(5, T=1 << 30)) == -8
+    assert call(_problem(E=16385), I) == -8 and call(_problem(), _rows(5, T=1 << 30)) == -8
     assert call(_problem(k=257), I) == -8
     assert call(_problem(N=0), I, None, None) == 0 and call(_problem(L=0), I, None, None) == 0
 
