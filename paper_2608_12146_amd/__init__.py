@@ -385,6 +385,14 @@ def _router():
     return _ROUTER
 
 
+def _raw_stream(device):
+    """The current stream's handle (without a torch.cuda.Stream object where
+    torch offers that)."""
+    torch = _ROUTER[1]
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device.index) if raw is not None else torch.cuda.current_stream(device).cuda_stream
+
+
 class _Call:
     """One call's tensors: checks that they share a GPU, hands out pointers,
     and runs the call on that GPU's current stream."""
@@ -427,7 +435,7 @@ class _Call:
 
     def run(self, f, *args):
         cuda = self.torch.cuda
-        stream = cuda.current_stream(self.device).cuda_stream
+        stream = _raw_stream(self.device)
         if self.device.index == cuda.current_device():
             rc = f(*args, stream)
         else:

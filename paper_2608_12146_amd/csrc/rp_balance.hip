@@ -60,15 +60,15 @@ __global__ void __launch_bounds__(256) k_share_chunks(ShareArgs a) {
         for (int64_t t = b + slot; t < e; t += SLOTS) {
             float z[V];
             load_row<T, G, V>(static_cast<const T *>(a.logits) + t * a.ts + l * a.ls, a.E, c, z);
+            float m, inv;
             if constexpr (SOFTMAX) {
-                float m, inv;
-                softmax_row<G, V>(z, m, inv);
+                softmax_row<false, G, V>(z, m, inv);
             } else {
                 float less[V];
-                logistic_row<G, V>(z, less);
+                logistic_row<false, G, V>(z, less, inv);
             }
 #pragma unroll
-            for (int v = 0; v < V; ++v) acc[v] += z[v];
+            for (int v = 0; v < V; ++v) acc[v] = __builtin_fmaf(z[v], inv, acc[v]);
         }
         __syncthreads();
 #pragma unroll

@@ -152,27 +152,21 @@ __device__ inline void load_row(const T *row, int E, int c, float (&z)[V]) {
     for (int v = 0; v < V; ++v) z[v] = x[v / W].at(v % W);
 }
 
-template <class T, int G, int V>
-__device__ inline void store_row(T *row, int E, int c, const float (&z)[V]) {
+// Elements e0 .. e0 + W of a row of E.
+template <class T>
+__device__ inline void store_vec(T *row, int E, int e0, const float (&y)[Vec<T>::W]) {
     constexpr int W = Vec<T>::W;
+    if (e0 + W <= E) {
+        Vec<T> w;
+        w.set(y);
+        Words16 b;
 #pragma unroll
-    for (int i = 0; i < V / W; ++i) {
-        const int e0 = (i * G + c) * W;
-        float y[W];
+        for (int n = 0; n < 4; ++n) b.w[n] = w.w[n];
+        *reinterpret_cast<Words16 *>(row + e0) = b;
+    } else {
 #pragma unroll
-        for (int x = 0; x < W; ++x) y[x] = z[i * W + x];
-        if (e0 + W <= E) {
-            Vec<T> w;
-            w.set(y);
-            Words16 b;
-#pragma unroll
-            for (int n = 0; n < 4; ++n) b.w[n] = w.w[n];
-            *reinterpret_cast<Words16 *>(row + e0) = b;
-        } else {
-#pragma unroll
-            for (int x = 0; x < W; ++x)
-                if (e0 + x < E) row[e0 + x] = (T)y[x];
-        }
+        for (int x = 0; x < W; ++x)
+            if (e0 + x < E) row[e0 + x] = (T)y[x];
     }
 }
 
@@ -195,16 +189,23 @@ __device__ inline float exp32(float x) {
     return x < -87.0f ? 0.0f : __builtin_fmaf(p * kLn2, lost, p);
 }
 
+// 2^(x log2 e) without that correction: a relative error of about 1.2 |x| + 2
+// steps, in two instructions instead of eight.  It serves where it is lost in
+// a sum or a mean of scores (the terms with large |x| are the small ones), or
+// in the rounding of the result to 16 bits.  -inf gives 0, NaN gives NaN.
 __device__ inline float exp_plain(float x) { return __builtin_amdgcn_exp2f(x * 1.44269502f); }
 
+template <bool FINE>
+__device__ inline float exp_of(float x) { return FINE ? exp32(x) : exp_plain(x); }
+
 // s = 1 / (1 + e^-z) and 1 - s, without cancellation on either side.
+template <bool FINE>
 __device__ inline void logistic(float z, float &s, float &one_less) {
-    const float e = exp32(-__builtin_fabsf(z));
+    const float e = exp_of<FINE>(-__builtin_fabsf(z));
     const float r = __builtin_amdgcn_rcpf(1.0f + e);
     const float q = e * r;
     s = z >= 0.0f ? r : q;
     one_less = z >= 0.0f ? q : r;
-    if (z != z) s = one_less = z;
 }
 
 // The value of the lane at the other side of a group of D lanes' middle (D a
@@ -248,68 +249,69 @@ __device__ inline int64_t group_sum64(int64_t v) {
     return v;
 }
 
-// A row's maximum m (0 if no expert is available) and 1 / sum e^(z - m) (0
-// then).  The exponentials are the plain 2^(x log2 e): its error, |x| / 2
-// steps, weighs little where e^x is small.
 template <int G, int V>
-__device__ inline void row_sum(const float (&z)[V], float &m, float &inv) {
-    m = z[0];
+__device__ inline float row_max(const float (&z)[V]) {
+    float m = z[0];
 #pragma unroll
     for (int v = 1; v < V; ++v) m = __builtin_fmaxf(m, z[v]);
-    m = group_max<G>(m);
-    m = m == -kInf ? 0.0f : m;
-    float sum = 0.0f;
-#pragma unroll
-    for (int v = 0; v < V; ++v) sum += exp_plain(z[v] - m);
-    sum = group_sum<G>(sum);
-    inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    return group_max<G>(m);
 }
 
-// Softmax of a row, in place: z becomes p.  A row without an available
-// expert becomes 0; a NaN or +inf in it makes it NaN.
-template <int G, int V>
+// Softmax of a row in place, but for the factor `inv`, the inverse of the sum:
+// z becomes e^(z - m), m the row's maximum.  A row without an available expert
+// becomes 0 (m and inv too); a NaN or +inf in it makes inv NaN.
+template <bool FINE, int G, int V>
 __device__ inline void softmax_row(float (&z)[V], float &m, float &inv) {
-    m = z[0];
-#pragma unroll
-    for (int v = 1; v < V; ++v) m = __builtin_fmaxf(m, z[v]);
-    m = group_max<G>(m);
+    m = row_max<G, V>(z);
     m = m == -kInf ? 0.0f : m;
     float sum = 0.0f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        z[v] = exp32(z[v] - m);
+        z[v] = exp_of<FINE>(z[v] - m);
         sum += z[v];
     }
     sum = group_sum<G>(sum);
     inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-#pragma unroll
-    for (int v = 0; v < V; ++v) z[v] *= inv;
 }
 
-// Logistic shares of a row, in place: z becomes s / sum s, and `less` 1 - s.
-// Where every logit is below 0 the scores may leave the range of 32 bits, but
-// their ratios do not: with a maximum m < 0 all are taken times e^-m.
+// A row's m and inv alone.
 template <int G, int V>
-__device__ inline void logistic_row(float (&z)[V], float (&less)[V]) {
-    float m = z[0];
+__device__ inline void row_sum(const float (&z)[V], float &m, float &inv) {
+    float e[V];
 #pragma unroll
-    for (int v = 1; v < V; ++v) m = __builtin_fmaxf(m, z[v]);
-    m = group_max<G>(m);
+    for (int v = 0; v < V; ++v) e[v] = z[v];
+    softmax_row<false, G, V>(e, m, inv);
+}
+
+// Logistic scores of a row in place, but for the factor `inv`, the inverse of
+// their sum, and 1 - s in `less`.  Where every logit is below 0 the scores may
+// leave the range of 32 bits, but their ratios do not: with a maximum m < 0
+// all are taken times e^-m.
+template <bool FINE, int G, int V>
+__device__ inline void logistic_row(float (&z)[V], float (&less)[V], float &inv) {
+    const float m = row_max<G, V>(z);
     const bool low = m < 0.0f && m > -kInf;
     float sum = 0.0f;
+    if (__any(low)) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        float s;
-        const float x = z[v];
-        logistic(x, s, less[v]);
-        if (low) s = exp32(x - m) * less[v];  // e^x / (1 + e^x) and 1 / (1 + e^x)
-        z[v] = s;
-        sum += s;
+        for (int v = 0; v < V; ++v) {
+            float s;
+            logistic<FINE>(z[v], s, less[v]);
+            // e^x / (1 + e^x), and less is 1 / (1 + e^x)
+            z[v] = low ? exp_of<FINE>(z[v] - m) * less[v] : s;
+            sum += z[v];
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            float s;
+            logistic<FINE>(z[v], s, less[v]);
+            z[v] = s;
+            sum += s;
+        }
     }
     sum = group_sum<G>(sum);
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-#pragma unroll
-    for (int v = 0; v < V; ++v) z[v] *= inv;
+    inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 }
 
 // The gates, divided by scale, of a token's choices, S of them a lane (slot s
@@ -327,7 +329,7 @@ __device__ inline void choice_gates(const float (&zc)[S], const bool (&on)[S], i
     if (score == ROUTEPACK_SIGMOID) {
 #pragma unroll
         for (int s = 0; s < S; ++s) {
-            logistic(zc[s], w[s], less[s]);
+            logistic<true>(zc[s], w[s], less[s]);
             w[s] = on[s] ? w[s] : 0.0f;
         }
         if (!normalize) return;

@@ -74,6 +74,7 @@ __device__ inline void load_weights(const BackArgs &a, int32_t g, int32_t l, int
 template <class T, int G, int NV, int K, bool SOFTMAX>
 __global__ void __launch_bounds__(256) k_route_back(BackArgs a, int32_t iters) {
     constexpr int W = 16 / sizeof(T), V = NV * W, S = K > G ? K / G : 1, SLOTS = 256 / G;
+    constexpr bool FINE = sizeof(T) == 4;  // (else the result's rounding hides the plain exponential's error)
     __shared__ __align__(16) float direct_rows[SLOTS][G * V];
     const int c = threadIdx.x & (G - 1), slot = threadIdx.x / G;
     const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
@@ -98,7 +99,7 @@ __global__ void __launch_bounds__(256) k_route_back(BackArgs a, int32_t iters) {
         const bool live = t < a.T;
         t = live ? t : a.T - 1;
         const T *row = static_cast<const T *>(a.logits) + t * a.ts + l * a.ls;
-        float z[V], less[SOFTMAX ? 1 : V], out[V];
+        float z[V], less[SOFTMAX ? 1 : V];
         int32_t id[S];
         float zc[S], dg[S];
         bool on[S];
@@ -129,8 +130,8 @@ __global__ void __launch_bounds__(256) k_route_back(BackArgs a, int32_t iters) {
         }
         float m = 0.0f, inv = 0.0f, drop = 0.0f;
         if (whole) {
-            if constexpr (SOFTMAX) softmax_row<G, V>(z, m, inv);
-            else logistic_row<G, V>(z, less);
+            if constexpr (SOFTMAX) softmax_row<FINE, G, V>(z, m, inv);
+            else logistic_row<FINE, G, V>(z, less, inv);
         }
         if (gates) {
             float w[S], sl[S], d[S];
@@ -179,38 +180,52 @@ __global__ void __launch_bounds__(256) k_route_back(BackArgs a, int32_t iters) {
                 wave_sync();
             }
         }
+        float mean = 0.0f;
         if (whole) {
+            // (z holds the scores before the factor inv)
             float dot = 0.0f;
             if (loss) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) dot += z[v] * f[v];
-                dot = group_sum<G>(dot);
+                for (int v = 0; v < V; ++v) dot = __builtin_fmaf(z[v], f[v], dot);
+                dot = group_sum<G>(dot) * inv;
             }
+            mean = -(dot + drop) * inv;
+        }
+        T *to = static_cast<T *>(a.dlogits) + (t * a.L + l) * a.E;
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                if constexpr (SOFTMAX) out[v] = z[v] * (f[v] - dot - drop);
-                else out[v] = z[v] * (f[v] - dot) * less[v];
+        for (int i = 0; i < NV; ++i) {
+            float y[W];
+            const int e0 = (i * G + c) * W;
+#pragma unroll
+            for (int w = 0; w < W; ++w) y[w] = 0.0f;
+            if (gates) {
+#pragma unroll
+                for (int w = 0; w < W; w += 4) {
+                    const float4 x = *reinterpret_cast<const float4 *>(direct + e0 + w);
+                    y[w] = x.x;
+                    y[w + 1] = x.y;
+                    y[w + 2] = x.z;
+                    y[w + 3] = x.w;
+                }
             }
-        } else {
+            if (whole) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) out[v] = 0.0f;
+                for (int w = 0; w < W; ++w) {
+                    const int v = i * W + w;
+                    const float rel = __builtin_fmaf(f[v], inv, mean);
+                    if constexpr (SOFTMAX) y[w] = __builtin_fmaf(z[v], rel, y[w]);
+                    else y[w] = __builtin_fmaf(z[v] * less[v], rel, y[w]);
+                }
+            }
+            if (live) store_vec<T>(to, a.E, e0, y);
         }
         if (gates) {
-#pragma unroll
-            for (int v = 0; v < V; v += 4) {
-                const float4 x = *reinterpret_cast<const float4 *>(direct + elem_of<T, G>(v, c));
-                out[v] += x.x;
-                out[v + 1] += x.y;
-                out[v + 2] += x.z;
-                out[v + 3] += x.w;
-            }
             wave_sync();
 #pragma unroll
             for (int s = 0; s < S; ++s)
                 if (on[s]) direct[id[s]] = 0.0f;
             wave_sync();
         }
-        if (live) store_row<T, G, V>(static_cast<T *>(a.dlogits) + (t * a.L + l) * a.E, a.E, c, out);
     }
 }
 

@@ -188,7 +188,7 @@ __global__ void __launch_bounds__(256) k_route_bias(RouteArgs a) {
             const float z = r.at(w);
             float s, less;
             if (softmax) s = exp32(z - m) * inv;
-            else logistic(z, s, less);
+            else logistic<true>(z, s, less);
             const float key = s + b[w / 4].at(w % 4);
             y[w] = z > -kInf && key > -kInf ? key : -kInf;
         }
