@@ -104,8 +104,9 @@ __device__ inline uint32_t bits_of(const T *p) {
     else return *reinterpret_cast<const uint16_t *>(p);
 }
 
-// A row of E elements by vectors; those past its end are -inf.
-template <class T>
+// A row of E elements by vectors; those past its end are -inf.  WHOLE: the
+// caller asks for none that reaches past it.
+template <class T, bool WHOLE = false>
 struct Row {
     static constexpr int W = Vec<T>::W;
     const T *data;
@@ -114,7 +115,7 @@ struct Row {
         constexpr uint32_t kLow = sizeof(T) == 4 ? 0xFF800000u : (__is_same(T, __bf16) ? 0xFF80u : 0xFC00u);
         const int e0 = v * W;
         Vec<T> x;
-        if (e0 + W <= E) {
+        if (WHOLE || e0 + W <= E) {
             const Words16 y = *reinterpret_cast<const Words16 *>(data + e0);
 #pragma unroll
             for (int i = 0; i < 4; ++i) x.w[i] = y.w[i];
@@ -140,11 +141,11 @@ struct Row {
 };
 
 // The row's part of one lane.
-template <class T, int G, int V>
+template <class T, int G, int V, bool WHOLE = false>
 __device__ inline void load_row(const T *row, int E, int c, float (&z)[V]) {
     constexpr int W = Vec<T>::W;
     static_assert(V % W == 0, "whole vectors");
-    const Row<T> r = {row, E};
+    const Row<T, WHOLE> r = {row, E};
     Vec<T> x[V / W];
 #pragma unroll
     for (int i = 0; i < V / W; ++i) x[i] = r.vec(i * G + c);
@@ -153,10 +154,10 @@ __device__ inline void load_row(const T *row, int E, int c, float (&z)[V]) {
 }
 
 // Elements e0 .. e0 + W of a row of E.
-template <class T>
+template <class T, bool WHOLE>
 __device__ inline void store_vec(T *row, int E, int e0, const float (&y)[Vec<T>::W]) {
     constexpr int W = Vec<T>::W;
-    if (e0 + W <= E) {
+    if (WHOLE || e0 + W <= E) {
         Vec<T> w;
         w.set(y);
         Words16 b;
@@ -292,23 +293,13 @@ __device__ inline void logistic_row(float (&z)[V], float (&less)[V], float &inv)
     const float m = row_max<G, V>(z);
     const bool low = m < 0.0f && m > -kInf;
     float sum = 0.0f;
-    if (__any(low)) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            float s;
-            logistic<FINE>(z[v], s, less[v]);
-            // e^x / (1 + e^x), and less is 1 / (1 + e^x)
-            z[v] = low ? exp_of<FINE>(z[v] - m) * less[v] : s;
-            sum += z[v];
-        }
-    } else {
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            float s;
-            logistic<FINE>(z[v], s, less[v]);
-            z[v] = s;
-            sum += s;
-        }
+    for (int v = 0; v < V; ++v) {
+        const float x = z[v];
+        logistic<FINE>(x, z[v], less[v]);
+        // e^x / (1 + e^x), and less is 1 / (1 + e^x)
+        if (__any(low)) z[v] = low ? exp_of<FINE>(x - m) * less[v] : z[v];
+        sum += z[v];
     }
     sum = group_sum<G>(sum);
     inv = sum == 0.0f ? 0.0f : 1.0f / sum;
@@ -589,8 +580,9 @@ int by_geometry(int32_t E, F &&f) {
     if (n <= 8 * MOST) return f(Int<8>(), Int<MOST>());
     if (n <= 16 * MOST) return f(Int<16>(), Int<MOST>());
     if (n <= 32 * MOST) return f(Int<32>(), Int<MOST>());
-    if constexpr (32 * MOST * 16 / (int)sizeof(T) < kMaxExperts) return f(Int<64>(), Int<MOST>());
-    else return ROUTEPACK_E_UNSUPPORTED;
+    if constexpr (32 * MOST * 16 / (int)sizeof(T) < kMaxExperts)
+        if (n <= 64 * MOST) return f(Int<64>(), Int<MOST>());
+    return ROUTEPACK_E_UNSUPPORTED;
 }
 
 // Calls f with a value of the logits' type.

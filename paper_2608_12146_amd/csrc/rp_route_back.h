@@ -39,19 +39,19 @@ __device__ inline int32_t find_group(const int64_t *offsets, int32_t n, int64_t 
 }
 
 // f of one group: E counts / sum counts, times dloss / (groups tokens).
-template <class T, int G, int V>
+template <class T, int G, int V, bool WHOLE>
 __device__ inline void load_weights(const BackArgs &a, int32_t g, int32_t l, int64_t len, int c, float (&f)[V]) {
     const int64_t at = ((int64_t)g * a.L + l) * a.E;
     int64_t sum = 0;
     if (a.counts_type == ROUTEPACK_I32) {
-        const Row<float> row = {static_cast<const float *>(a.counts) + at, a.E};  // (words of 32 bits)
+        const Row<float, WHOLE> row = {static_cast<const float *>(a.counts) + at, a.E};  // (words of 32 bits)
 #pragma unroll
         for (int v = 0; v < V; v += 4) {
             const int e0 = elem_of<T, G>(v, c);
             const Vec<float> x = row.vec(e0 / 4);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int32_t n = e0 + i < a.E ? (int32_t)x.w[i] : 0;
+                const int32_t n = WHOLE || e0 + i < a.E ? (int32_t)x.w[i] : 0;
                 sum += n;
                 f[v + i] = (float)n;
             }
@@ -60,9 +60,9 @@ __device__ inline void load_weights(const BackArgs &a, int32_t g, int32_t l, int
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int e = elem_of<T, G>(v, c);
-            const int64_t n = e < a.E ? static_cast<const int64_t *>(a.counts)[at + e] : 0;
+            const int64_t n = WHOLE || e < a.E ? static_cast<const int64_t *>(a.counts)[at + e] : 0;
             sum += n;
-            f[v] = (float)n;
+            f[v] = __builtin_fmaf((float)(int32_t)(n >> 32), 0x1p32f, (float)(uint32_t)n);
         }
     }
     sum = group_sum64<G>(sum);
@@ -71,7 +71,7 @@ __device__ inline void load_weights(const BackArgs &a, int32_t g, int32_t l, int
     for (int v = 0; v < V; ++v) f[v] *= by;
 }
 
-template <class T, int G, int NV, int K, bool SOFTMAX>
+template <class T, int G, int NV, int K, bool SOFTMAX, bool WHOLE>
 __global__ void __launch_bounds__(256) k_route_back(BackArgs a, int32_t iters) {
     constexpr int W = 16 / sizeof(T), V = NV * W, S = K > G ? K / G : 1, SLOTS = 256 / G;
     constexpr bool FINE = sizeof(T) == 4;  // (else the result's rounding hides the plain exponential's error)
@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(256) k_route_back(BackArgs a, int32_t iters) {
         int32_t id[S];
         float zc[S], dg[S];
         bool on[S];
-        if (whole) load_row<T, G, V>(row, a.E, c, z);
+        if (whole) load_row<T, G, V, WHOLE>(row, a.E, c, z);
         if (gates) {
 #pragma unroll
             for (int s = 0; s < S; ++s) {
@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(256) k_route_back(BackArgs a, int32_t iters) {
             const int32_t g = find_group<G>(a.offsets, a.n_groups, t, begin, end);
             known = g >= 0;
             if (g >= 0) {
-                load_weights<T, G, V>(a, g, l, end - begin, c, f);
+                load_weights<T, G, V, WHOLE>(a, g, l, end - begin, c, f);
             } else {
 #pragma unroll
                 for (int v = 0; v < V; ++v) f[v] = 0.0f;
@@ -217,7 +217,7 @@ __global__ void __launch_bounds__(256) k_route_back(BackArgs a, int32_t iters) {
                     else y[w] = __builtin_fmaf(z[v] * less[v], rel, y[w]);
                 }
             }
-            if (live) store_vec<T>(to, a.E, e0, y);
+            if (live) store_vec<T, WHOLE>(to, a.E, e0, y);
         }
         if (gates) {
             wave_sync();
@@ -229,25 +229,36 @@ __global__ void __launch_bounds__(256) k_route_back(BackArgs a, int32_t iters) {
     }
 }
 
+template <class T, bool SOFTMAX, int G, int NV>
+int launch_back(const BackArgs &a, hipStream_t stream) {
+    const int64_t slots = 256 / G, n = (a.T + slots - 1) / slots;
+    // several tokens a group of lanes where that leaves 2048 workgroups
+    int64_t iters = n * a.L / 2048;
+    iters = iters < 1 ? 1 : (iters > 8 ? 8 : iters);
+    auto go = [&](auto kern) {
+        hipLaunchKernelGGL(kern, grid_of((n + iters - 1) / iters * a.L), dim3(256), 0, stream, a, (int32_t)iters);
+        return hipGetLastError() == hipSuccess ? ROUTEPACK_OK : ROUTEPACK_E_DEVICE;
+    };
+    // Up to 8 choices, and rows that fill the lanes exactly (E a power of two,
+    // mostly), take kernels without the further slots and the checks of every
+    // vector: at 131072 x 512 bf16 63 us and 71 us with the checks.
+    const bool few = !a.ids || a.k <= 8, fills = a.E == G * NV * (16 / (int)sizeof(T));
+    if (few && fills) return go(k_route_back<T, G, NV, 8, SOFTMAX, true>);
+    if (few) return go(k_route_back<T, G, NV, 8, SOFTMAX, false>);
+    return go(k_route_back<T, G, NV, 32, SOFTMAX, false>);
+}
+
 template <class T>
 int route_back(const BackArgs &a, hipStream_t stream) {
-    return by_geometry<T, 2 * sizeof(T)>(a.E, [&](auto g, auto nv) {
-        const int64_t slots = 256 / g.value, n = (a.T + slots - 1) / slots;
-        // several tokens a group of lanes where that leaves 2048 workgroups
-        int64_t iters = n * a.L / 2048;
-        iters = iters < 1 ? 1 : (iters > 8 ? 8 : iters);
-        const dim3 grid = grid_of((n + iters - 1) / iters * a.L);
-        auto go = [&](auto kern) {
-            hipLaunchKernelGGL(kern, grid, dim3(256), 0, stream, a, (int32_t)iters);
-            return hipGetLastError() == hipSuccess ? ROUTEPACK_OK : ROUTEPACK_E_DEVICE;
-        };
-        const bool few = !a.ids || a.k <= 8;
-        if (a.score == ROUTEPACK_SOFTMAX) {
-            if (few) return go(k_route_back<T, g.value, nv.value, 8, true>);
-            return go(k_route_back<T, g.value, nv.value, 32, true>);
-        }
-        if (few) return go(k_route_back<T, g.value, nv.value, 8, false>);
-        return go(k_route_back<T, g.value, nv.value, 32, false>);
+    constexpr int kMost = 2 * sizeof(T);  // 32 values a lane
+    if (a.score == ROUTEPACK_SOFTMAX)
+        return by_geometry<T, kMost>(a.E, [&](auto g, auto nv) {
+            return launch_back<T, true, g.value, nv.value>(a, stream);
+        });
+    // logistic rows keep 1 - s too: 16 values a lane while the wave holds the row
+    if (a.E > 1024) return launch_back<T, false, kWave, kMost>(a, stream);
+    return by_geometry<T, kMost / 2>(a.E, [&](auto g, auto nv) {
+        return launch_back<T, false, g.value, nv.value>(a, stream);
     });
 }
 
