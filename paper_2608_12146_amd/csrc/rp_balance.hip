@@ -33,22 +33,12 @@ __global__ void __launch_bounds__(256) k_share_chunks(ShareArgs a) {
     const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     const int64_t ch = a.L == 1 ? block : block / a.L;
     const int32_t l = a.L == 1 ? 0 : (int32_t)(block - ch * a.L);
-    const int tid = threadIdx.x, c = tid & (G - 1), slot = tid / G, lane = lane_id();
+    const int tid = threadIdx.x, c = tid & (G - 1), slot = tid / G;
     if (ch == 0 && tid == 0) a.arrived[l] = 0;
     if (ch >= a.n_chunks) return;
     const int64_t t0 = ch * a.chunk, t1 = t0 + a.chunk < a.T ? t0 + a.chunk : a.T;
-    // the first group that ends behind t0: 64 probes a round
-    int32_t lo = 0, hi = a.n_groups;
-    while (lo < hi) {
-        const int32_t step = (hi - lo + kWave - 1) / kWave;
-        const int64_t p = lo + (int64_t)lane * step;
-        const uint64_t yes = __ballot(p >= hi || a.offsets[(p < hi ? p : lo) + 1] > t0);
-        const int f = yes ? first_lane(yes) : kWave;
-        const int64_t past = lo + (int64_t)f * step;
-        const int64_t from = f > 0 ? lo + (int64_t)(f - 1) * step + 1 : lo;
-        hi = past < hi ? (int32_t)past : hi;
-        lo = from < hi ? (int32_t)from : hi;
-    }
+    // the first group that ends behind t0
+    const int32_t lo = first_where(a.n_groups, [&](int32_t g) { return a.offsets[g + 1] > t0; });
     for (int32_t g = lo; g < a.n_groups; ++g) {
         const int64_t from = a.offsets[g];
         if (from >= t1) break;

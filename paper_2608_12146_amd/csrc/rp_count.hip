@@ -21,13 +21,14 @@ struct CountArgs {
     int32_t N, L, E, k;
     const int64_t *offsets;
     int32_t *demand;
-    int32_t group;          // layers of a workgroup
+    int32_t group, n_groups;  // layers of a workgroup, and such groups
     // A row is `join` tokens of one workgroup's layers; its threads stand at
     // `cols` places of it, `slots` rows abreast.
     int32_t join, cols, slots;
     int64_t row_stride;
     bool one_layer;         // the row holds ids of one layer only
-    int32_t pitch, copies;  // words between layers' counters, and copies of them
+    int32_t pitch, copies;  // words between layers' counters, and copies of them (a power of two)
+    bool per_sample;        // one chunk, and a workgroup for each sample
 };
 
 // A sample's tokens and the first and last chunk that it meets (an empty
@@ -76,21 +77,19 @@ template <class I, int W>
 __global__ void __launch_bounds__(256) k_count(CountArgs a) {
     extern __shared__ int32_t hist[];  // [copies][group][pitch], then [pitch] for what is not this thread's to count
     const int tid = threadIdx.x, lane = lane_id();
-    const int64_t ch = blockIdx.x;
-    const int32_t l0 = (int32_t)blockIdx.y * a.group;
+    // Workgroups go to the 8 XCDs in turn: 8 chunks abreast, and behind them
+    // the same chunks' other groups of layers, which share lines in their L2.
+    const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    const int64_t turn = block >> 3;
+    const int32_t grp = (int32_t)(a.per_sample ? block % a.n_groups : turn % a.n_groups);
+    const int64_t x0 = a.per_sample ? block / a.n_groups : turn / a.n_groups * 8 + (block & 7);
+    if (x0 >= (a.per_sample ? a.N : a.n_chunks)) return;
+    const int64_t ch = a.per_sample ? 0 : x0;
+    const int32_t l0 = grp * a.group;
     const int32_t nl = a.group < a.L - l0 ? a.group : a.L - l0;
-    // the first sample whose last chunk is ch or later: 64 probes a round
-    int32_t lo = 0, hi = a.N;
-    while (lo < hi) {
-        const int32_t step = (hi - lo + kWave - 1) / kWave;
-        const int64_t p = lo + (int64_t)lane * step;
-        const uint64_t yes = __ballot(p >= hi || span_of(a, (int32_t)p).last >= ch);
-        const int f = yes ? first_lane(yes) : kWave;
-        const int64_t past = lo + (int64_t)f * step;
-        const int64_t from = f > 0 ? lo + (int64_t)(f - 1) * step + 1 : lo;
-        hi = past < hi ? (int32_t)past : hi;
-        lo = from < hi ? (int32_t)from : hi;
-    }
+    // the first sample whose last chunk is ch or later
+    const int32_t lo = a.per_sample ? (int32_t)x0
+                                    : first_where(a.N, [&](int32_t i) { return span_of(a, i).last >= ch; });
     const int32_t words = a.copies * a.group * a.pitch;
     for (int x = tid; x < words; x += 256) hist[x] = 0;
     const int64_t t0 = ch << a.shift, t1 = t0 + ((int64_t)1 << a.shift);
@@ -102,19 +101,27 @@ __global__ void __launch_bounds__(256) k_count(CountArgs a) {
     const int32_t want = col * W;
     const int32_t at = want + W <= len || len < W ? want : len - W;
     int32_t *to[W];  // the counters of each id's layer
+    const int32_t first = at % piece;
+    int32_t l = a.one_layer ? 0 : first / a.k, j = first - l * a.k;
+    const int32_t l_first = l, j_first = j;
+    int32_t *const mine = hist + (lane & (a.copies - 1)) * a.group * a.pitch;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
         const int32_t x = at + w;
-        const int32_t l = a.one_layer ? 0 : x % piece / a.k;
-        to[w] = x >= want && x < len ? hist + ((lane % a.copies) * a.group + l) * a.pitch : hist + words;
+        to[w] = x >= want && x < len ? mine + l * a.pitch : hist + words;
+        if (!a.one_layer && ++j == a.k) {
+            j = 0;
+            l = l + 1 == nl ? 0 : l + 1;
+        }
     }
     const I *ids = static_cast<const I *>(a.ids) + (int64_t)l0 * a.ls;
     // (where the row is not of one piece, W is 1: the thread's layer and choice)
-    const int64_t place = W == 1 && !a.one_layer ? (int64_t)(at % piece / a.k) * a.ls + at % a.k : at;
+    const int64_t place = W == 1 ? (int64_t)l_first * a.ls + j_first : at;
     // an id that is no expert's goes to the word behind the last expert's
     const uint32_t limit = (uint32_t)a.E;
     auto add = [&](uint32_t id, int w) { atomicAdd(to[w] + (id < limit ? id : limit), 1); };
-    for (int32_t i = lo; i < a.N; ++i) {
+    const int32_t stop = a.per_sample ? lo + 1 : a.N;
+    for (int32_t i = lo; i < stop; ++i) {
         const Span s = span_of(a, i);
         if (s.first > ch) break;
         if (s.last < ch) continue;
@@ -131,22 +138,20 @@ __global__ void __launch_bounds__(256) k_count(CountArgs a) {
                 constexpr int U = 4;
                 const int32_t whole = a.join == 1 ? (len < W ? 0 : rows) : (int32_t)(left / len);
                 for (; r + (U - 1) * a.slots < whole; r += U * a.slots) {
-                    Words16 v[U];
+                    uint32_t v[U][4];
 #pragma unroll
                     for (int u = 0; u < U; ++u)
-                        v[u] = *reinterpret_cast<const Words16 *>(p + (int64_t)(r + u * a.slots) * a.row_stride);
+                        load16<true>(p + (int64_t)(r + u * a.slots) * a.row_stride, v[u]);
 #pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        const uint32_t w4[4] = {v[u].w[0], v[u].w[1], v[u].w[2], v[u].w[3]};
+                    for (int u = 0; u < U; ++u)
 #pragma unroll
-                        for (int w = 0; w < W; ++w) add(id_at<I>(w4, w), w);
-                    }
+                        for (int w = 0; w < W; ++w) add(id_at<I>(v[u], w), w);
                 }
                 for (; r < whole; r += a.slots) {
-                    const Words16 v = *reinterpret_cast<const Words16 *>(p + (int64_t)r * a.row_stride);
-                    const uint32_t w4[4] = {v.w[0], v.w[1], v.w[2], v.w[3]};
+                    uint32_t v[4];
+                    load16<true>(p + (int64_t)r * a.row_stride, v);
 #pragma unroll
-                    for (int w = 0; w < W; ++w) add(id_at<I>(w4, w), w);
+                    for (int w = 0; w < W; ++w) add(id_at<I>(v, w), w);
                 }
                 // the last row where its tokens are fewer than `join`, or rows
                 // shorter than a vector
@@ -188,46 +193,58 @@ int count(CountArgs &a, bool layer_runs, bool token_rows, hipStream_t stream) {
     constexpr int W = 16 / sizeof(I);
     constexpr int32_t kWords = 8192;  // 32 KiB of counters: four workgroups a CU and more
     a.pitch = (a.E + 1) | 1;  // (odd: equal experts of several layers stand in different banks)
-    // Layers of a workgroup: as many as fit; where that is not all of them, such
-    // that a token's piece is whole lines of 128 bytes, or whole vectors.
-    int32_t fit = kWords / a.pitch;
-    fit = fit < 1 ? 1 : fit;
-    a.group = layer_runs ? 1 : (fit < a.L ? fit : a.L);
+    const bool pieces = token_rows || layer_runs;
+    // Layers of a workgroup: as many as fit the counters and 256 places of a
+    // row, but fewer where the chunks of 64 tokens (or the samples, if they are
+    // more) would leave less than 512 workgroups; where that is not all of
+    // them, such that a token's piece is whole lines of 128 bytes, or whole
+    // vectors.
+    const int32_t fit = kWords / a.pitch < 1 ? 1 : kWords / a.pitch;
+    const int32_t places = 256 * (pieces ? W : 1) / a.k;  // (k <= 256)
+    a.group = fit < a.L ? fit : a.L;
+    a.group = places < a.group ? places : a.group;
+    const int64_t along = a.T / 64 > a.N ? a.T / 64 : a.N;
+    while (a.group > 1 && a.group * a.k * (int32_t)sizeof(I) > 64 && along * ((a.L + a.group - 1) / a.group) < 512)
+        a.group = (a.group + 1) / 2;
+    if (layer_runs) a.group = 1;
     if (a.group < a.L && token_rows) {
         const int32_t line = 128 / gcd_of(128, a.k * (int32_t)sizeof(I)), vec = W / gcd_of(W, a.k);
         if (a.group >= line) a.group -= a.group % line;
         else if (a.group >= vec) a.group -= a.group % vec;
     }
-    bool pieces = token_rows || layer_runs;
-    // at most 256 places in a row
-    while (!layer_runs && (a.group * a.k + W - 1) / W > 256 && a.group > 1) a.group = (a.group + 1) / 2;
-    if (!layer_runs && (a.group * a.k + W - 1) / W > 256) return ROUTEPACK_E_UNSUPPORTED;
-    if (!pieces && a.group * a.k > 256) a.group = 256 / a.k;
-    if (a.group < 1) return ROUTEPACK_E_UNSUPPORTED;
-    a.join = 1;
+    a.n_groups = (a.L + a.group - 1) / a.group;
     a.one_layer = a.group == 1 && pieces;
+    // tokens that follow each other without a gap form one row of whole vectors
     const int32_t piece = a.group * a.k;
-    if (pieces) {
-        // tokens that follow each other without a gap form one row of whole vectors
-        const bool dense = a.ts == piece && (layer_runs || a.group == a.L);
-        if (dense) a.join = W / gcd_of(W, piece);
-        if (dense && a.join * piece / W > 256) a.join = 1;
-    }
+    a.join = 1;
+    if (pieces && a.ts == piece && (layer_runs || a.group == a.L)) a.join = W / gcd_of(W, piece);
+    if (a.join * piece / W > 256) a.join = 1;
     a.row_stride = a.join * a.ts;
     a.cols = pieces ? (a.join * piece + W - 1) / W : piece;
-    if (a.cols > 256) return ROUTEPACK_E_UNSUPPORTED;
+    if (a.cols > 256) return ROUTEPACK_E_INTERNAL;  // (never: `places`)
     a.slots = 256 / a.cols;
     a.copies = 1;
     while (a.copies < 16 && 2 * a.copies * a.group * a.pitch <= kWords / 2) a.copies *= 2;
-    // chunks: about 4096 workgroups, but 64 tokens and more, and enough ids to
-    // outweigh the counters that each workgroup clears and hands over
-    const int64_t n_groups = (a.L + a.group - 1) / a.group;
+    // Chunks of 64 tokens and more: up to two samples of the mean length (a
+    // workgroup takes the samples of its chunk one after the other), about 4096
+    // workgroups, and, where 512 are left, enough ids to outweigh the counters
+    // that a workgroup clears and hands over.
     a.shift = 6;
-    while (a.shift < 20 && (((a.T * n_groups) >> a.shift) > 4096 || ((int64_t)a.k << a.shift) < 4 * a.E) &&
-           ((int64_t)1 << a.shift) < a.T)
+    while (a.shift < 20 && ((int64_t)a.N << a.shift) < 2 * a.T) {
+        const int64_t n = (a.T * a.n_groups) >> a.shift;
+        if (!(n > 4096 || (n > 512 && ((int64_t)a.k << a.shift) < 4 * a.E))) break;
         ++a.shift;
+    }
     a.n_chunks = a.T > 0 ? (a.T + ((int64_t)1 << a.shift) - 1) >> a.shift : 1;
-    if (n_groups > 65535) return ROUTEPACK_E_UNSUPPORTED;
+    // Few ids: a workgroup counts its sample alone, however long it is, in one
+    // launch and without a search (64 samples of 16896 tokens, 4 layers of 2
+    // byte ids: 9.6 us, and 12.3 us by chunks; one sample of 128 KiB of ids
+    // for a workgroup, about even).
+    a.per_sample = a.N <= 65536 && a.T * piece * (int64_t)sizeof(I) <= 128 * 1024;
+    if (a.per_sample) {
+        a.shift = 31;
+        a.n_chunks = 1;
+    }
     if (a.n_chunks > 1) {
         const int64_t row_len = (int64_t)a.L * a.E;
         const int64_t gx = a.N < 65536 ? a.N : 65536;
@@ -236,11 +253,12 @@ int count(CountArgs &a, bool layer_runs, bool token_rows, hipStream_t stream) {
         hipLaunchKernelGGL(k_count_clear, dim3((unsigned)gx, (unsigned)gy), dim3(256), 0, stream, a);
     }
     const size_t lds = 4 * ((size_t)a.copies * a.group + 1) * a.pitch;
+    const int64_t along_x = a.per_sample ? a.N : (a.n_chunks + 7) / 8 * 8;
     auto go = [&](auto kern) -> int {
         if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(kern),
                                                    hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
             return ROUTEPACK_E_DEVICE;
-        hipLaunchKernelGGL(kern, dim3((unsigned)a.n_chunks, (unsigned)n_groups), dim3(256), lds, stream, a);
+        hipLaunchKernelGGL(kern, grid_of(along_x * a.n_groups), dim3(256), lds, stream, a);
         return hipGetLastError() == hipSuccess ? ROUTEPACK_OK : ROUTEPACK_E_DEVICE;
     };
     if (pieces) return go(k_count<I, W>);

@@ -68,6 +68,17 @@ struct Vec {
 struct __attribute__((packed, aligned(2))) Words16 {
     uint32_t w[4];
 };
+// 16 bytes at any address; ONCE: that nothing reads again (a hint that keeps
+// them from displacing others in the caches: counting 300007 x 24 x 8 ids takes
+// 55 us without and 50 us with it).
+template <bool ONCE>
+__device__ inline void load16(const void *p, uint32_t (&w)[4]) {
+    typedef uint32_t four __attribute__((ext_vector_type(4), aligned(1)));
+    const four *q = static_cast<const four *>(p);
+    const four x = ONCE ? __builtin_nontemporal_load(q) : *q;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = x[i];
+}
 template <> __device__ inline float Vec<float>::at(int i) const { return __uint_as_float(w[i]); }
 template <> __device__ inline float Vec<__bf16>::at(int i) const {
     return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
@@ -116,9 +127,7 @@ struct Row {
         const int e0 = v * W;
         Vec<T> x;
         if (WHOLE || e0 + W <= E) {
-            const Words16 y = *reinterpret_cast<const Words16 *>(data + e0);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x.w[i] = y.w[i];
+            load16<false>(data + e0, x.w);
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) x.w[i] = sizeof(T) == 4 ? kLow : kLow << 16 | kLow;
@@ -528,6 +537,24 @@ __device__ inline Item item_of(int64_t T, int32_t L) {
         it.l = (int32_t)(it.at - it.t * L);
     }
     return it;
+}
+
+// The first of n places where `yes` holds, which holds for all after it (n if
+// for none): the lanes of a wave probe 64 places a round.
+template <class F>
+__device__ inline int32_t first_where(int32_t n, F &&yes) {
+    int32_t lo = 0;
+    while (n > 0) {  // the answer is in [lo, lo + n]
+        const int32_t step = (n - 1) / kWave + 1, at = lane_id() * step;
+        const uint64_t mask = __ballot(at < n ? (bool)yes(lo + at) : true);
+        const int32_t f = mask ? first_lane(mask) : kWave;
+        if (f == 0) break;
+        // behind probe f - 1, up to probe f or the end
+        const int32_t past = (f - 1) * step + 1;
+        n = __builtin_elementwise_min(n, f * step) - past;
+        lo += past;
+    }
+    return lo;
 }
 
 // One recorded id, as an expert or -1.

@@ -249,6 +249,7 @@ __global__ void __launch_bounds__(256) k_route_bias(RouteArgs a) {
         }
         if (j == a.k - 1) edge = v - slack(v);
     }
+    edge = group_max<G>(edge);  // (lanes from M on hold no list)
     // from the edge on: elements of the chosen vectors, and other vectors
     float over = 0.0f, more = 0.0f;
 #pragma unroll

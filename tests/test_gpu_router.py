@@ -275,6 +275,38 @@ def test_count_demand(idtype):
 
 
 @gpu
+def test_many_samples():
+    """Numbers of samples about and past multiples of a wave's lanes, with
+    empty ones at the front, between others and at the end: counts, shares and
+    gradients find every sample's tokens."""
+    import torch
+    import paper_2608_12146_amd as rp
+    L, E, k = 2, 9, 2
+    for N in (63, 64, 65, 66, 127, 129, 1000, 4095, 4097, 5000):
+        rng = np.random.default_rng(N)
+        for low, high in ((0, 3), (1, 40), (9, 10)):
+            lengths = rng.integers(low, high, size=N)
+            lengths[rng.random(N) < 0.2] *= low > 0
+            T = int(lengths.sum()) + 3
+            _log((N, low, high, T))
+            prob = _problem(N, L, E, k)
+            off = _offsets(lengths, 1)
+            ids = _ids(N, T, L, E, k, "u8")
+            demand = rp.count_demand(prob, ids, off)
+            assert np.array_equal(_host(demand), O.count(_host(ids), _host(off), E)), N
+            z = _logits(N, T, L, E, "fp32")
+            zh = _host(z)
+            rel = (2 * _range(zh) + 310) * U
+            _, shares = rp.balance_loss(prob, z, demand, off)
+            want = O.balance(zh, _host(demand), _host(off), "softmax")[1]
+            _close(shares, want, rel * want + TINY, N)
+            dl = torch.full((L,), float(N * E), device="cuda")
+            got = rp.route_backward(prob, z, counts=demand, offsets=off, dloss=dl)
+            want, mag = O.backward(zh, "softmax", counts=_host(demand), offsets=_host(off), dloss=_host(dl))
+            _close(got, want, (2 * _range(zh) + 110) * U * mag + TINY * (1 + mag.max()), N)
+
+
+@gpu
 def test_hot_experts_and_broadcast_records():
     """Every choice on one expert, and a record that repeats one token's."""
     import torch
