@@ -7,9 +7,10 @@
 // for each group of the loss that meets its chunk: group g's part of chunk c is
 // row c + g (both only grow along the tokens, so no two parts share a row).  A
 // second kernel adds every group's rows in their order, a slab of 64 experts a
-// workgroup, and forms the slab's part of the loss; the last workgroup of a
-// layer to arrive adds those parts, again in their order.  No floating-point
-// atomics: the result does not depend on the launch.
+// workgroup, and forms the slab's part of the loss.  The parts are added in
+// their order too, by the last workgroup of a layer to arrive where these are
+// few, or by a third kernel.  No floating-point atomics: the result does not
+// depend on the launch.
 #include "rp_internal.h"
 #include "rp_route.h"
 
@@ -26,7 +27,7 @@ struct ShareArgs {
 
 __device__ inline int64_t clamp64(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : (x > hi ? hi : x); }
 
-template <class T, int G, int NV, bool SOFTMAX>
+template <class T, int G, int NV, bool SOFTMAX, bool WHOLE>
 __global__ void __launch_bounds__(256) k_share_chunks(ShareArgs a) {
     constexpr int W = 16 / sizeof(T), V = NV * W, SLOTS = 256 / G, EP = G * V;
     __shared__ __align__(16) float part[SLOTS * EP];
@@ -49,7 +50,7 @@ __global__ void __launch_bounds__(256) k_share_chunks(ShareArgs a) {
         for (int v = 0; v < V; ++v) acc[v] = 0.0f;
         for (int64_t t = b + slot; t < e; t += SLOTS) {
             float z[V];
-            load_row<T, G, V>(static_cast<const T *>(a.logits) + t * a.ts + l * a.ls, a.E, c, z);
+            load_row<T, G, V, WHOLE>(static_cast<const T *>(a.logits) + t * a.ts + l * a.ls, a.E, c, z);
             float m, inv;
             if constexpr (SOFTMAX) {
                 softmax_row<false, G, V>(z, m, inv);
@@ -104,8 +105,38 @@ struct LossArgs {
     uint32_t *arrived;
 };
 
-// R rows abreast of 64 experts.
-template <int R>
+// A layer's loss from its parts, by a whole workgroup; `load` reads one.
+template <class F>
+__device__ inline void add_parts(const LossArgs &a, int32_t l, double *red, F &&load) {
+    double total = 0.0;
+    for (int32_t y = threadIdx.x; y < a.n_groups; y += blockDim.x) {
+        double *part = a.parts + ((int64_t)l * a.n_groups + y) * a.n_slabs * 2;
+        double dot = 0.0, sum = 0.0;
+        for (int32_t z = 0; z < a.n_slabs; ++z) {
+            dot += load(part + 2 * z);
+            sum += load(part + 2 * z + 1);
+        }
+        total += sum > 0.0 ? a.E * dot / sum : 0.0;
+    }
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) total += __shfl_xor(total, d, kWave);
+    __syncthreads();
+    if (lane_id() == 0) red[wave_id()] = total;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int y = 1; y < (int)blockDim.x / kWave; ++y) total += red[y];
+        a.loss[l] = (float)(total / a.n_groups);
+    }
+}
+
+__global__ void __launch_bounds__(1024) k_sum_loss(LossArgs a) {
+    __shared__ double red[16];
+    add_parts(a, (int32_t)blockIdx.x, red, [](double *p) { return *p; });
+}
+
+// R rows abreast of 64 experts.  LAST: the last workgroup of a layer adds its
+// parts.
+template <int R, bool LAST>
 __global__ void __launch_bounds__(64 * R) k_group_loss(LossArgs a) {
     __shared__ double red[R][kWave];
     __shared__ bool last;
@@ -124,10 +155,13 @@ __global__ void __launch_bounds__(64 * R) k_group_loss(LossArgs a) {
         const int64_t pitch = (int64_t)a.L * a.E;
         const float *p = a.rows + (int64_t)g * pitch + (int64_t)l * a.E + x;
         int64_t ch = b / a.chunk + r;
-        for (; ch + 3 * R <= c1; ch += 4 * R) {
-            const float y0 = p[ch * pitch], y1 = p[(ch + R) * pitch], y2 = p[(ch + 2 * R) * pitch],
-                        y3 = p[(ch + 3 * R) * pitch];
-            s += ((double)y0 + (double)y1) + ((double)y2 + (double)y3);
+        constexpr int U = 8;
+        for (; ch + (U - 1) * R <= c1; ch += U * R) {
+            float y[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) y[u] = p[(ch + u * R) * pitch];
+#pragma unroll
+            for (int u = 0; u < U; ++u) s += (double)y[u];
         }
         for (; ch <= c1; ch += R) s += (double)p[ch * pitch];
     }
@@ -153,33 +187,24 @@ __global__ void __launch_bounds__(64 * R) k_group_loss(LossArgs a) {
         }
         if (lane == 0) {
             double *part = a.parts + (((int64_t)l * a.n_groups + g) * a.n_slabs + slab) * 2;
-            __hip_atomic_store(part, dot, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            __hip_atomic_store(part + 1, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            const uint32_t before = __hip_atomic_fetch_add(a.arrived + l, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-            last = before == (uint32_t)a.n_groups * (uint32_t)a.n_slabs - 1;
+            if constexpr (LAST) {
+                __hip_atomic_store(part, dot, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                __hip_atomic_store(part + 1, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                const uint32_t before =
+                    __hip_atomic_fetch_add(a.arrived + l, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+                last = before == (uint32_t)(a.n_groups * a.n_slabs) - 1;
+            } else {
+                part[0] = dot;
+                part[1] = sum;
+            }
         }
     }
-    __syncthreads();
-    if (!last) return;
-    // the layer's parts, all there
-    double total = 0.0;
-    for (int32_t y = threadIdx.x; y < a.n_groups; y += 64 * R) {
-        double *part = a.parts + ((int64_t)l * a.n_groups + y) * a.n_slabs * 2;
-        double dot = 0.0, sum = 0.0;
-        for (int32_t z = 0; z < a.n_slabs; ++z) {
-            dot += __hip_atomic_load(part + 2 * z, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            sum += __hip_atomic_load(part + 2 * z + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-        total += sum > 0.0 ? a.E * dot / sum : 0.0;
-    }
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) total += __shfl_xor(total, d, kWave);
-    __syncthreads();
-    if (lane == 0) red[0][r] = total;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int y = 1; y < R; ++y) total += red[0][y];
-        a.loss[l] = (float)(total / a.n_groups);
+    if constexpr (LAST) {
+        __syncthreads();
+        if (last)  // the layer's parts are all there
+            add_parts(a, l, &red[0][0], [](double *q) {
+                return __hip_atomic_load(q, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            });
     }
 }
 
@@ -234,12 +259,25 @@ extern "C" int routepack_balance_loss(const routepack_problem *prob, const route
     const dim3 grid = grid_of((w.n_chunks > 0 ? w.n_chunks : 1) * L);
     RP_TRY(by_type(logits->type, [&](auto tag) {
         using T = decltype(tag);
-        return by_geometry<T, 2 * sizeof(T)>(E, [&](auto g, auto nv) {
-            if (score == ROUTEPACK_SOFTMAX)
-                hipLaunchKernelGGL((k_share_chunks<T, g.value, nv.value, true>), grid, dim3(256), 0, stream, a);
-            else
-                hipLaunchKernelGGL((k_share_chunks<T, g.value, nv.value, false>), grid, dim3(256), 0, stream, a);
+        constexpr int kMost = 2 * sizeof(T);  // 32 values a lane
+        // rows that fill the lanes exactly go without the checks of every vector
+        auto go = [&](auto checked, auto whole, int32_t lanes_hold) {
+            hipLaunchKernelGGL(E == lanes_hold ? whole : checked, grid, dim3(256), 0, stream, a);
             return ROUTEPACK_OK;
+        };
+        if (score == ROUTEPACK_SOFTMAX)
+            return by_geometry<T, kMost>(E, [&](auto g, auto nv) {
+                return go(k_share_chunks<T, g.value, nv.value, true, false>,
+                          k_share_chunks<T, g.value, nv.value, true, true>, g.value * nv.value * Vec<T>::W);
+            });
+        // logistic rows keep 1 - s too: 16 values a lane while the wave holds the
+        // row (131072 x 512 bf16: 63 us, 81 us with 32)
+        if (E > 1024)
+            return go(k_share_chunks<T, kWave, kMost, false, false>, k_share_chunks<T, kWave, kMost, false, true>,
+                      kMaxExperts);
+        return by_geometry<T, kMost / 2>(E, [&](auto g, auto nv) {
+            return go(k_share_chunks<T, g.value, nv.value, false, false>,
+                      k_share_chunks<T, g.value, nv.value, false, true>, g.value * nv.value * Vec<T>::W);
         });
     }));
     const int32_t slabs = (E + kWave - 1) / kWave;
@@ -247,8 +285,21 @@ extern "C" int routepack_balance_loss(const routepack_problem *prob, const route
                         shares, parts, arrived};
     const dim3 grid2 = grid_of((int64_t)n_groups * L * slabs);
     const int64_t each = w.n_chunks / n_groups;  // rows of a group, about
-    if (each >= 64) hipLaunchKernelGGL(k_group_loss<16>, grid2, dim3(1024), 0, stream, b);
-    else if (each >= 8) hipLaunchKernelGGL(k_group_loss<4>, grid2, dim3(256), 0, stream, b);
-    else hipLaunchKernelGGL(k_group_loss<1>, grid2, dim3(64), 0, stream, b);
+    // A workgroup that counts its arrival waits for its stores to reach memory,
+    // and the counts of a layer follow one another: up to 64 parts (1000 groups
+    // x 4 slabs of 131072 x 256: 116 us, 31 us with the third kernel; 5 x 4 of
+    // 8192 x 256: 15.6 us, 17.9 us).
+    const bool last = (int64_t)n_groups * slabs <= 64;
+    auto go = [&](auto kern, int threads) { hipLaunchKernelGGL(kern, grid2, dim3(threads), 0, stream, b); };
+    if (last) {
+        if (each >= 64) go(k_group_loss<16, true>, 1024);
+        else if (each >= 8) go(k_group_loss<4, true>, 256);
+        else go(k_group_loss<1, true>, 64);
+    } else {
+        if (each >= 64) go(k_group_loss<16, false>, 1024);
+        else if (each >= 8) go(k_group_loss<4, false>, 256);
+        else go(k_group_loss<1, false>, 64);
+        hipLaunchKernelGGL(k_sum_loss, dim3((unsigned)L), dim3(n_groups > 256 ? 1024 : 256), 0, stream, b);
+    }
     return hipGetLastError() == hipSuccess ? ROUTEPACK_OK : ROUTEPACK_E_DEVICE;
 }

@@ -28,6 +28,7 @@ struct CountArgs {
     int64_t row_stride;
     bool one_layer;         // the row holds ids of one layer only
     int32_t pitch, copies;  // words between layers' counters, and copies of them (a power of two)
+    int32_t lanes;          // log2 of the lanes that hand over a layer's counters
     bool per_sample;        // one chunk, and a workgroup for each sample
 };
 
@@ -167,8 +168,9 @@ __global__ void __launch_bounds__(256) k_count(CountArgs a) {
         __syncthreads();
         int32_t *row = a.demand + ((int64_t)i * a.L + l0) * a.E;
         const bool alone = s.first == s.last;
-        for (int32_t l = wave_id(); l < nl; l += 4)
-            for (int32_t x = lane; x < a.E; x += kWave) {
+        // (few experts: several layers a wave)
+        for (int32_t l = (tid >> a.lanes); l < nl; l += 256 >> a.lanes)
+            for (int32_t x = tid & ((1 << a.lanes) - 1); x < a.E; x += 1 << a.lanes) {
                 int32_t n = 0, *h = hist + l * a.pitch + x;
                 for (int32_t y = 0; y < a.copies; ++y, h += a.group * a.pitch) {
                     n += *h;
@@ -209,10 +211,13 @@ int count(CountArgs &a, bool layer_runs, bool token_rows, hipStream_t stream) {
     if (layer_runs) a.group = 1;
     if (a.group < a.L && token_rows) {
         const int32_t line = 128 / gcd_of(128, a.k * (int32_t)sizeof(I)), vec = W / gcd_of(W, a.k);
-        if (a.group >= line) a.group -= a.group % line;
-        else if (a.group >= vec) a.group -= a.group % vec;
+        const int32_t unit = a.group >= line ? line : (a.group >= vec ? vec : 1);
+        const int32_t most = a.group - a.group % unit, n = (a.L + most - 1) / most;
+        a.group = ((a.L + n - 1) / n + unit - 1) / unit * unit;  // (the groups about equal)
     }
     a.n_groups = (a.L + a.group - 1) / a.group;
+    a.lanes = 0;
+    while (a.lanes < 6 && (1 << a.lanes) < a.E) ++a.lanes;
     a.one_layer = a.group == 1 && pieces;
     // tokens that follow each other without a gap form one row of whole vectors
     const int32_t piece = a.group * a.k;
@@ -227,20 +232,22 @@ int count(CountArgs &a, bool layer_runs, bool token_rows, hipStream_t stream) {
     while (a.copies < 16 && 2 * a.copies * a.group * a.pitch <= kWords / 2) a.copies *= 2;
     // Chunks of 64 tokens and more: up to two samples of the mean length (a
     // workgroup takes the samples of its chunk one after the other), about 4096
-    // workgroups, and, where 512 are left, enough ids to outweigh the counters
-    // that a workgroup clears and hands over.
+    // workgroups, and, where 512 are left, 16 ids for each counter that a
+    // workgroup hands over, mostly with atomics (262144 tokens x 8 int32 in one
+    // sample: 17 us, 45 us with 4 ids; 144230 x 26 x 8 int64, 400 experts: 63
+    // and 60 us).
     a.shift = 6;
     while (a.shift < 20 && ((int64_t)a.N << a.shift) < 2 * a.T) {
         const int64_t n = (a.T * a.n_groups) >> a.shift;
-        if (!(n > 4096 || (n > 512 && ((int64_t)a.k << a.shift) < 4 * a.E))) break;
+        if (!(n > 4096 || (n > 512 && ((int64_t)a.k << a.shift) < 16 * a.E))) break;
         ++a.shift;
     }
     a.n_chunks = a.T > 0 ? (a.T + ((int64_t)1 << a.shift) - 1) >> a.shift : 1;
     // Few ids: a workgroup counts its sample alone, however long it is, in one
     // launch and without a search (64 samples of 16896 tokens, 4 layers of 2
-    // byte ids: 9.6 us, and 12.3 us by chunks; one sample of 128 KiB of ids
-    // for a workgroup, about even).
-    a.per_sample = a.N <= 65536 && a.T * piece * (int64_t)sizeof(I) <= 128 * 1024;
+    // byte ids: 8.7 us, and 12.7 us by chunks; at worst, one sample of 256 KiB
+    // of ids for one workgroup, 12.2 and 11.2 us).
+    a.per_sample = a.N <= 65536 && a.T * piece * (int64_t)sizeof(I) <= 256 * 1024;
     if (a.per_sample) {
         a.shift = 31;
         a.n_chunks = 1;
