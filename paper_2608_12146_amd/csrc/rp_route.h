@@ -199,7 +199,7 @@ __device__ inline float exp32(float x) {
     return x < -87.0f ? 0.0f : __builtin_fmaf(p * kLn2, lost, p);
 }
 
-// 2^(x log2 e) without that correction: a relative error of about 1.2 |x| + 2
+// 2^(x log2 e) without that correction: a relative error of up to 1.3 |x| + 2
 // steps, in two instructions instead of eight.  It serves where it is lost in
 // a sum or a mean of scores (the terms with large |x| are the small ones), or
 // in the rounding of the result to 16 bits.  -inf gives 0, NaN gives NaN.

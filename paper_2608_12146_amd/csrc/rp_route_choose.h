@@ -153,10 +153,14 @@ __device__ inline void shift_down(T (&a)[N]) {
 // the whole row; tokens with equal keys always are.  That part is loops of
 // little code: few waves run it, each would wait for all of its instructions.
 //
-// A score's error in 32 bits, in steps u = 2^-24: logistic, 8 u s <= 8 u (the
-// exponential 4, the sum, the inverse and the product 4); softmax,
-// p (|z - m| + 54) u with p |z - m| < 0.5 and p <= inv, the inverse of the
-// row's sum.  The sum with the bias is rounded once: |key| u.
+// A score's error in 32 bits, in steps u = 2^-24 (the plain exponential e^x is
+// off by (1.3 |x| + 2) u, and z - m is rounded once):
+// - logistic: s (1 - s) (1.3 |z| + 2) u, at most 0.8 u as s (1 - s) |z| < 0.23,
+//   and 4 u of the sum, the inverse and the product: below 8 u;
+// - softmax: p (2.3 |z - m| + 2) u with p |z - m| < 0.37, and of p the row sum's
+//   error: 38 additions, 2.3 times the mean of |z - m| (at most ln 2048) and 7
+//   more: at most (1 + 66 p) u, and p is at most inv, the inverse of the sum.
+// The sum with the bias is rounded once: |key| u.
 template <class T, int G, int NV, int K>
 __global__ void __launch_bounds__(256) k_route_bias(RouteArgs a) {
     using Key = Key32;
@@ -187,8 +191,8 @@ __global__ void __launch_bounds__(256) k_route_bias(RouteArgs a) {
         for (int w = 0; w < W; ++w) {
             const float z = r.at(w);
             float s, less;
-            if (softmax) s = exp32(z - m) * inv;
-            else logistic<true>(z, s, less);
+            if (softmax) s = exp_plain(z - m) * inv;
+            else logistic<false>(z, s, less);
             const float key = s + b[w / 4].at(w % 4);
             y[w] = z > -kInf && key > -kInf ? key : -kInf;
         }
@@ -235,7 +239,7 @@ __global__ void __launch_bounds__(256) k_route_bias(RouteArgs a) {
     lane_top<Key, K, S * W>(x, top);
     group_top<Key, K, M>(top);
     // is the order beyond doubt?  Two keys further apart than `slack` are in order.
-    const float err = softmax ? 0.5f + 54.0f * inv : 8.0f;
+    const float err = softmax ? 1.0f + 66.0f * inv : 8.0f;
     auto slack = [&](float key) { return (err + 2.0f * __builtin_fabsf(key)) * 0x1p-23f; };
     bool open = false;
     float edge = -kInf;  // a key below it is not among the k largest
