@@ -22,9 +22,7 @@ struct CountArgs {
     const int64_t *offsets;
     int32_t *demand;
     int32_t group, n_groups;  // layers of a workgroup, and such groups
-    // A row is `join` tokens of one workgroup's layers; its threads stand at
-    // `cols` places of it, `slots` rows abreast.
-    int32_t join, cols, slots;
+    int32_t join;           // a row is that many tokens of one workgroup's layers
     int64_t row_stride;
     bool one_layer;         // the row holds ids of one layer only
     int32_t pitch, copies;  // words between layers' counters, and copies of them (a power of two)
@@ -94,9 +92,12 @@ __global__ void __launch_bounds__(256) k_count(CountArgs a) {
     const int32_t words = a.copies * a.group * a.pitch;
     for (int x = tid; x < words; x += 256) hist[x] = 0;
     const int64_t t0 = ch << a.shift, t1 = t0 + ((int64_t)1 << a.shift);
+    constexpr bool pieces = W > 1;         // (where the row is not of one piece, W is 1)
     const int32_t piece = nl * a.k;        // ids of one token
     const int32_t len = a.join * piece;    // of a row
-    const int col = tid % a.cols, slot = tid / a.cols;
+    // its places, and the rows that the threads stand on abreast
+    const int cols = pieces ? (len + W - 1) / W : len, slots = 256 / cols;
+    const int col = tid % cols, slot = tid / cols;
     // the thread's ids are at .. at + W of its rows, less those that the place
     // before holds already (the last place is moved back into the row)
     const int32_t want = col * W;
@@ -131,24 +132,24 @@ __global__ void __launch_bounds__(256) k_count(CountArgs a) {
         const I *p = ids + b * a.ts + place;
         const int64_t left = (e - b) * piece;  // ids of the sample here (rows of one piece)
         __syncthreads();
-        if (slot < a.slots) {
+        if (slot < slots) {
             int32_t r = slot;
             if constexpr (W == 1) {
-                for (; r < rows; r += a.slots) add(id_of<I>(p[r * a.row_stride]), 0);
+                for (; r < rows; r += slots) add(id_of<I>(p[r * a.row_stride]), 0);
             } else {
                 constexpr int U = 4;
                 const int32_t whole = a.join == 1 ? (len < W ? 0 : rows) : (int32_t)(left / len);
-                for (; r + (U - 1) * a.slots < whole; r += U * a.slots) {
+                for (; r + (U - 1) * slots < whole; r += U * slots) {
                     uint32_t v[U][4];
 #pragma unroll
                     for (int u = 0; u < U; ++u)
-                        load16<true>(p + (int64_t)(r + u * a.slots) * a.row_stride, v[u]);
+                        load16<true>(p + (int64_t)(r + u * slots) * a.row_stride, v[u]);
 #pragma unroll
                     for (int u = 0; u < U; ++u)
 #pragma unroll
                         for (int w = 0; w < W; ++w) add(id_at<I>(v[u], w), w);
                 }
-                for (; r < whole; r += a.slots) {
+                for (; r < whole; r += slots) {
                     uint32_t v[4];
                     load16<true>(p + (int64_t)r * a.row_stride, v);
 #pragma unroll
@@ -156,7 +157,7 @@ __global__ void __launch_bounds__(256) k_count(CountArgs a) {
                 }
                 // the last row where its tokens are fewer than `join`, or rows
                 // shorter than a vector
-                for (; r < rows; r += a.slots) {
+                for (; r < rows; r += slots) {
                     const I *q = p + (int64_t)r * a.row_stride;
                     const int64_t end = a.join == 1 ? len : left - (int64_t)r * len;
 #pragma unroll
@@ -225,9 +226,7 @@ int count(CountArgs &a, bool layer_runs, bool token_rows, hipStream_t stream) {
     if (pieces && a.ts == piece && (layer_runs || a.group == a.L)) a.join = W / gcd_of(W, piece);
     if (a.join * piece / W > 256) a.join = 1;
     a.row_stride = a.join * a.ts;
-    a.cols = pieces ? (a.join * piece + W - 1) / W : piece;
-    if (a.cols > 256) return ROUTEPACK_E_INTERNAL;  // (never: `places`)
-    a.slots = 256 / a.cols;
+    if ((pieces ? (a.join * piece + W - 1) / W : piece) > 256) return ROUTEPACK_E_INTERNAL;  // (never: `places`)
     a.copies = 1;
     while (a.copies < 16 && 2 * a.copies * a.group * a.pitch <= kWords / 2) a.copies *= 2;
     // Chunks of 64 tokens and more: up to two samples of the mean length (a
