@@ -2,12 +2,15 @@
 //
 // Reading the ids once is the floor.  The tokens are cut into chunks of equal
 // length and the layers into groups whose counters fit the LDS; a workgroup
-// counts one chunk of one group, sample by sample, with LDS atomics, and reads
-// the ids as vectors of 16 bytes.  A thread keeps its place in the row of a
+// counts what one sample has in one chunk, for one group, with LDS atomics,
+// and reads the ids as vectors of 16 bytes.  A thread keeps its place in the row of a
 // token (or of several short ones), so the layers that its ids belong to are
 // worked out once.  A sample that lies within one chunk is written by plain
 // stores; the parts of one that spans chunks are added with integer atomics to
 // a row cleared before (integer sums do not depend on their order).
+//
+// Sample i's part of chunk c is part i + c: both only grow along the tokens,
+// so the parts i + (its first chunk) on are its own, up to the next sample's.
 #include "rp_internal.h"
 #include "rp_route.h"
 
@@ -22,12 +25,11 @@ struct CountArgs {
     const int64_t *offsets;
     int32_t *demand;
     int32_t group, n_groups;  // layers of a workgroup, and such groups
-    int32_t join;           // a row is that many tokens of one workgroup's layers
+    int32_t join;           // a row is that many tokens (of one workgroup's layers, or of one layer)
     int64_t row_stride;
-    bool one_layer;         // the row holds ids of one layer only
+    bool layer_runs;        // a row holds ids of one layer only
     int32_t pitch, copies;  // words between layers' counters, and copies of them (a power of two)
     int32_t lanes;          // log2 of the lanes that hand over a layer's counters
-    bool per_sample;        // one chunk, and a workgroup for each sample
 };
 
 // A sample's tokens and the first and last chunk that it meets (an empty
@@ -76,27 +78,30 @@ template <class I, int W>
 __global__ void __launch_bounds__(256) k_count(CountArgs a) {
     extern __shared__ int32_t hist[];  // [copies][group][pitch], then [pitch] for what is not this thread's to count
     const int tid = threadIdx.x, lane = lane_id();
-    // Workgroups go to the 8 XCDs in turn: 8 chunks abreast, and behind them
-    // the same chunks' other groups of layers, which share lines in their L2.
+    // Workgroups go to the 8 XCDs in turn: 8 parts abreast, and behind them the
+    // same parts' other groups of layers, which share lines in their L2.
     const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     const int64_t turn = block >> 3;
-    const int32_t grp = (int32_t)(a.per_sample ? block % a.n_groups : turn % a.n_groups);
-    const int64_t x0 = a.per_sample ? block / a.n_groups : turn / a.n_groups * 8 + (block & 7);
-    if (x0 >= (a.per_sample ? a.N : a.n_chunks)) return;
-    const int64_t ch = a.per_sample ? 0 : x0;
+    const int32_t grp = (int32_t)(turn % a.n_groups);
+    const int64_t part = turn / a.n_groups * 8 + (block & 7);
+    if (part >= a.n_chunks + a.N) return;
     const int32_t l0 = grp * a.group;
     const int32_t nl = a.group < a.L - l0 ? a.group : a.L - l0;
-    // the first sample whose last chunk is ch or later
-    const int32_t lo = a.per_sample ? (int32_t)x0
-                                    : first_where(a.N, [&](int32_t i) { return span_of(a, i).last >= ch; });
+    // the sample whose part it is: the last one with first part <= part
+    const int32_t i = first_where(a.N, [&](int32_t x) { return x + span_of(a, x).first > part; }) - 1;
+    if (i < 0) return;
+    const Span s = span_of(a, i);
+    const int64_t ch = part - i;
+    if (ch > s.last) return;
     const int32_t words = a.copies * a.group * a.pitch;
     for (int x = tid; x < words; x += 256) hist[x] = 0;
     const int64_t t0 = ch << a.shift, t1 = t0 + ((int64_t)1 << a.shift);
+    const int64_t b = s.b > t0 ? s.b : t0, e = s.e < t1 ? s.e : t1;
     constexpr bool pieces = W > 1;         // (where the row is not of one piece, W is 1)
-    const int32_t piece = nl * a.k;        // ids of one token
+    const int32_t piece = a.layer_runs ? a.k : nl * a.k;  // ids of one token in a row
     const int32_t len = a.join * piece;    // of a row
     // its places, and the rows that the threads stand on abreast
-    const int cols = pieces ? (len + W - 1) / W : len, slots = 256 / cols;
+    const int32_t cols = pieces ? (len + W - 1) / W : len, slots = 256 / cols;
     const int col = tid % cols, slot = tid / cols;
     // the thread's ids are at .. at + W of its rows, less those that the place
     // before holds already (the last place is moved back into the row)
@@ -104,14 +109,14 @@ __global__ void __launch_bounds__(256) k_count(CountArgs a) {
     const int32_t at = want + W <= len || len < W ? want : len - W;
     int32_t *to[W];  // the counters of each id's layer
     const int32_t first = at % piece;
-    int32_t l = a.one_layer ? 0 : first / a.k, j = first - l * a.k;
+    int32_t l = a.layer_runs ? 0 : first / a.k, j = first - l * a.k;
     const int32_t l_first = l, j_first = j;
     int32_t *const mine = hist + (lane & (a.copies - 1)) * a.group * a.pitch;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
         const int32_t x = at + w;
         to[w] = x >= want && x < len ? mine + l * a.pitch : hist + words;
-        if (!a.one_layer && ++j == a.k) {
+        if (!a.layer_runs && ++j == a.k) {
             j = 0;
             l = l + 1 == nl ? 0 : l + 1;
         }
@@ -121,66 +126,57 @@ __global__ void __launch_bounds__(256) k_count(CountArgs a) {
     const int64_t place = W == 1 ? (int64_t)l_first * a.ls + j_first : at;
     // an id that is no expert's goes to the word behind the last expert's
     const uint32_t limit = (uint32_t)a.E;
-    auto add = [&](uint32_t id, int w) { atomicAdd(to[w] + (id < limit ? id : limit), 1); };
-    const int32_t stop = a.per_sample ? lo + 1 : a.N;
-    for (int32_t i = lo; i < stop; ++i) {
-        const Span s = span_of(a, i);
-        if (s.first > ch) break;
-        if (s.last < ch) continue;
-        const int64_t b = s.b > t0 ? s.b : t0, e = s.e < t1 ? s.e : t1;
-        const int32_t rows = (int32_t)((e - b + a.join - 1) / a.join);
-        const I *p = ids + b * a.ts + place;
-        const int64_t left = (e - b) * piece;  // ids of the sample here (rows of one piece)
-        __syncthreads();
-        if (slot < slots) {
-            int32_t r = slot;
-            if constexpr (W == 1) {
-                for (; r < rows; r += slots) add(id_of<I>(p[r * a.row_stride]), 0);
-            } else {
-                constexpr int U = 4;
-                const int32_t whole = a.join == 1 ? (len < W ? 0 : rows) : (int32_t)(left / len);
-                for (; r + (U - 1) * slots < whole; r += U * slots) {
-                    uint32_t v[U][4];
+    const int32_t rows = (int32_t)((e - b + a.join - 1) / a.join);
+    const int64_t left = (e - b) * piece;  // ids of the part in rows of one piece
+    __syncthreads();
+    for (int32_t q = 0; q < (a.layer_runs ? nl : 1); ++q) {
+        const I *p = ids + b * a.ts + q * a.ls + place;
+        const int32_t up = q * a.pitch;  // (rows of one layer are whole vectors: all places are the thread's)
+        auto add = [&](uint32_t id, int w) { atomicAdd(to[w] + (up + (id < limit ? id : limit)), 1); };
+        int32_t r = slot < slots ? slot : rows;
+        if constexpr (W == 1) {
+            for (; r < rows; r += slots) add(id_of<I>(p[r * a.row_stride]), 0);
+        } else {
+            constexpr int U = 4;
+            const int32_t whole = a.join == 1 ? (len < W ? 0 : rows) : (int32_t)(left / len);
+            for (; r + (U - 1) * slots < whole; r += U * slots) {
+                uint32_t v[U][4];
 #pragma unroll
-                    for (int u = 0; u < U; ++u)
-                        load16<true>(p + (int64_t)(r + u * slots) * a.row_stride, v[u]);
+                for (int u = 0; u < U; ++u) load16<true>(p + (int64_t)(r + u * slots) * a.row_stride, v[u]);
 #pragma unroll
-                    for (int u = 0; u < U; ++u)
+                for (int u = 0; u < U; ++u)
 #pragma unroll
-                        for (int w = 0; w < W; ++w) add(id_at<I>(v[u], w), w);
-                }
-                for (; r < whole; r += slots) {
-                    uint32_t v[4];
-                    load16<true>(p + (int64_t)r * a.row_stride, v);
+                    for (int w = 0; w < W; ++w) add(id_at<I>(v[u], w), w);
+            }
+            for (; r < whole; r += slots) {
+                uint32_t v[4];
+                load16<true>(p + (int64_t)r * a.row_stride, v);
 #pragma unroll
-                    for (int w = 0; w < W; ++w) add(id_at<I>(v, w), w);
-                }
-                // the last row where its tokens are fewer than `join`, or rows
-                // shorter than a vector
-                for (; r < rows; r += slots) {
-                    const I *q = p + (int64_t)r * a.row_stride;
-                    const int64_t end = a.join == 1 ? len : left - (int64_t)r * len;
+                for (int w = 0; w < W; ++w) add(id_at<I>(v, w), w);
+            }
+            // the last row where its tokens are fewer than `join`, or rows
+            // shorter than a vector
+            for (; r < rows; r += slots) {
+                const I *x = p + (int64_t)r * a.row_stride;
+                const int64_t end = a.join == 1 ? len : left - (int64_t)r * len;
 #pragma unroll
-                    for (int w = 0; w < W; ++w)
-                        if (at + w < end) add(id_of<I>(q[w]), w);
-                }
+                for (int w = 0; w < W; ++w)
+                    if (at + w < end) add(id_of<I>(x[w]), w);
             }
         }
-        __syncthreads();
-        int32_t *row = a.demand + ((int64_t)i * a.L + l0) * a.E;
-        const bool alone = s.first == s.last;
-        // (few experts: several layers a wave)
-        for (int32_t l = (tid >> a.lanes); l < nl; l += 256 >> a.lanes)
-            for (int32_t x = tid & ((1 << a.lanes) - 1); x < a.E; x += 1 << a.lanes) {
-                int32_t n = 0, *h = hist + l * a.pitch + x;
-                for (int32_t y = 0; y < a.copies; ++y, h += a.group * a.pitch) {
-                    n += *h;
-                    *h = 0;
-                }
-                if (alone) row[l * a.E + x] = n;
-                else if (n) atomicAdd(&row[l * a.E + x], n);
-            }
     }
+    __syncthreads();
+    int32_t *row = a.demand + ((int64_t)i * a.L + l0) * a.E;
+    const bool alone = s.first == s.last;
+    // (few experts: several layers a wave)
+    for (int32_t y = tid >> a.lanes; y < nl; y += 256 >> a.lanes)
+        for (int32_t x = tid & ((1 << a.lanes) - 1); x < a.E; x += 1 << a.lanes) {
+            int32_t n = 0;
+            const int32_t *h = hist + y * a.pitch + x;
+            for (int32_t z = 0; z < a.copies; ++z, h += a.group * a.pitch) n += *h;
+            if (alone) row[y * a.E + x] = n;
+            else if (n) atomicAdd(&row[y * a.E + x], n);
+        }
 }
 
 }  // namespace rp
@@ -202,14 +198,21 @@ int count(CountArgs &a, bool layer_runs, bool token_rows, hipStream_t stream) {
     // more) would leave less than 512 workgroups; where that is not all of
     // them, such that a token's piece is whole lines of 128 bytes, or whole
     // vectors.
-    const int32_t fit = kWords / a.pitch < 1 ? 1 : kWords / a.pitch;
+    // Where a layer's tokens follow each other the threads stand on one layer at
+    // a time: one layer and copies of its counters, or several layers where a
+    // sample has less than 16 KiB in one (300007 x 24 x 8 int32, 71 samples: 48 us
+    // by one layer, 61 by seven; 88222 x 27 x 8, 467 samples: 45 and 32 us).
+    const int64_t each = a.T / a.N * a.k * (int64_t)sizeof(I);
+    int32_t fit = (layer_runs ? kWords / 4 : kWords) / a.pitch;
+    if (layer_runs && each > 0) fit = each >= 16384 ? 1 : (fit < 32768 / each ? fit : (int32_t)(32768 / each));
+    fit = fit < 1 ? 1 : fit;
     const int32_t places = 256 * (pieces ? W : 1) / a.k;  // (k <= 256)
     a.group = fit < a.L ? fit : a.L;
     a.group = places < a.group ? places : a.group;
     const int64_t along = a.T / 64 > a.N ? a.T / 64 : a.N;
-    while (a.group > 1 && a.group * a.k * (int32_t)sizeof(I) > 64 && along * ((a.L + a.group - 1) / a.group) < 512)
-        a.group = (a.group + 1) / 2;
-    if (layer_runs) a.group = 1;
+    while (a.group > 1 && (layer_runs || a.group * a.k * (int32_t)sizeof(I) > 64) &&
+           along * ((a.L + a.group - 1) / a.group) < (layer_runs ? 2048 : 512))
+        a.group = (a.group + 1) / 2;  // (layers one after the other: 289 x 27, 9 samples, 50 us by 27)
     if (a.group < a.L && token_rows) {
         const int32_t line = 128 / gcd_of(128, a.k * (int32_t)sizeof(I)), vec = W / gcd_of(W, a.k);
         const int32_t unit = a.group >= line ? line : (a.group >= vec ? vec : 1);
@@ -219,38 +222,34 @@ int count(CountArgs &a, bool layer_runs, bool token_rows, hipStream_t stream) {
     a.n_groups = (a.L + a.group - 1) / a.group;
     a.lanes = 0;
     while (a.lanes < 6 && (1 << a.lanes) < a.E) ++a.lanes;
-    a.one_layer = a.group == 1 && pieces;
+    a.layer_runs = layer_runs;
     // tokens that follow each other without a gap form one row of whole vectors
-    const int32_t piece = a.group * a.k;
+    const int32_t piece = layer_runs ? a.k : a.group * a.k;
     a.join = 1;
     if (pieces && a.ts == piece && (layer_runs || a.group == a.L)) a.join = W / gcd_of(W, piece);
     if (a.join * piece / W > 256) a.join = 1;
     a.row_stride = a.join * a.ts;
     if ((pieces ? (a.join * piece + W - 1) / W : piece) > 256) return ROUTEPACK_E_INTERNAL;  // (never: `places`)
     a.copies = 1;
-    while (a.copies < 16 && 2 * a.copies * a.group * a.pitch <= kWords / 2) a.copies *= 2;
-    // Chunks of 64 tokens and more: up to two samples of the mean length (a
-    // workgroup takes the samples of its chunk one after the other), about 4096
-    // workgroups, and, where 512 are left, 16 ids for each counter that a
-    // workgroup hands over, mostly with atomics (262144 tokens x 8 int32 in one
-    // sample: 17 us, 45 us with 4 ids; 144230 x 26 x 8 int64, 400 experts: 63
-    // and 60 us).
+    while (a.copies < 16 && 2 * a.copies * a.group * a.pitch <= (layer_runs ? kWords : kWords / 2)) a.copies *= 2;
+    // Chunks of 64 tokens and more: about 4096 of them, but, where 512 are left,
+    // 16 ids for each counter that a workgroup hands over (262144 tokens x 8
+    // int32 in one sample: 17 us, 45 us with 4 ids), and 8 samples of the mean
+    // length where these are short, since a sample that spans two chunks is
+    // cleared and added.
     a.shift = 6;
-    while (a.shift < 20 && ((int64_t)a.N << a.shift) < 2 * a.T) {
+    while (a.shift < 20) {
         const int64_t n = (a.T * a.n_groups) >> a.shift;
-        if (!(n > 4096 || (n > 512 && ((int64_t)a.k << a.shift) < 16 * a.E))) break;
+        const bool many = n > 4096, thin = n > 512 && ((int64_t)a.k << a.shift) < 16 * a.E;
+        const bool cut = a.shift < 9 && (int64_t)a.N * a.n_groups > 512 && ((int64_t)a.N << a.shift) < 8 * a.T;
+        if (!many && !thin && !cut) break;
         ++a.shift;
     }
+    // Few ids: one chunk, so no row to clear (64 samples of 16896 tokens, 4
+    // layers of 2 byte ids: 8.7 us, and 12.7 us by chunks; at worst, one sample of
+    // 256 KiB of ids for one workgroup, 12.2 and 11.2 us).
+    if (a.T * piece * (layer_runs ? a.group : 1) * (int64_t)sizeof(I) <= 256 * 1024) a.shift = 31;
     a.n_chunks = a.T > 0 ? (a.T + ((int64_t)1 << a.shift) - 1) >> a.shift : 1;
-    // Few ids: a workgroup counts its sample alone, however long it is, in one
-    // launch and without a search (64 samples of 16896 tokens, 4 layers of 2
-    // byte ids: 8.7 us, and 12.7 us by chunks; at worst, one sample of 256 KiB
-    // of ids for one workgroup, 12.2 and 11.2 us).
-    a.per_sample = a.N <= 65536 && a.T * piece * (int64_t)sizeof(I) <= 256 * 1024;
-    if (a.per_sample) {
-        a.shift = 31;
-        a.n_chunks = 1;
-    }
     if (a.n_chunks > 1) {
         const int64_t row_len = (int64_t)a.L * a.E;
         const int64_t gx = a.N < 65536 ? a.N : 65536;
@@ -259,12 +258,12 @@ int count(CountArgs &a, bool layer_runs, bool token_rows, hipStream_t stream) {
         hipLaunchKernelGGL(k_count_clear, dim3((unsigned)gx, (unsigned)gy), dim3(256), 0, stream, a);
     }
     const size_t lds = 4 * ((size_t)a.copies * a.group + 1) * a.pitch;
-    const int64_t along_x = a.per_sample ? a.N : (a.n_chunks + 7) / 8 * 8;
+    const int64_t parts = (a.n_chunks + a.N + 7) / 8 * 8;
     auto go = [&](auto kern) -> int {
         if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(kern),
                                                    hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
             return ROUTEPACK_E_DEVICE;
-        hipLaunchKernelGGL(kern, grid_of(along_x * a.n_groups), dim3(256), lds, stream, a);
+        hipLaunchKernelGGL(kern, grid_of(parts * a.n_groups), dim3(256), lds, stream, a);
         return hipGetLastError() == hipSuccess ? ROUTEPACK_OK : ROUTEPACK_E_DEVICE;
     };
     if (pieces) return go(k_count<I, W>);

@@ -31,9 +31,9 @@ __global__ void __launch_bounds__(256) k_replay_chosen(RouteArgs a) {
 
 // Unnormalised softmax gates of recorded experts: the row's sum, then its k
 // choices, S of them a lane.
-template <class T, int G, int NV>
+template <class T, int G, int NV, int K>
 __global__ void __launch_bounds__(256) k_replay_row(RouteArgs a) {
-    constexpr int V = NV * (16 / sizeof(T)), S = kMaxChoices / G > 0 ? kMaxChoices / G : 1;
+    constexpr int V = NV * (16 / sizeof(T)), S = K > G ? K / G : 1;
     const int c = threadIdx.x & (G - 1);
     const Item it = item_of<G>(a.T, a.L);
     const T *row = static_cast<const T *>(a.logits) + it.t * a.ts + it.l * a.ls;
@@ -97,7 +97,8 @@ extern "C" int routepack_route_tokens(const routepack_problem *prob, const route
         };
         if (score == ROUTEPACK_SOFTMAX && !normalize)
             return by_geometry<T, 2 * sizeof(T)>(a.E, [&](auto g, auto nv) {
-                return go(k_replay_row<T, g.value, nv.value>, g.value);
+                if (a.k <= 8) return go(k_replay_row<T, g.value, nv.value, 8>, g.value);
+                return go(k_replay_row<T, g.value, nv.value, kMaxChoices>, g.value);
             });
         if (a.k <= 4) return go(k_replay_chosen<T, 4>, 4);
         if (a.k <= 8) return go(k_replay_chosen<T, 8>, 8);
