@@ -472,6 +472,33 @@ def test_infinities_and_nan():
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_nan_of_every_kind_is_never_chosen(dtype):
+    """Quiet and signalling NaN of both signs among the logits, at every place
+    of a vector, leave the order of the others."""
+    import torch
+    import paper_2608_12146_amd as rp
+    kinds = {"fp32": (torch.int32, [0x7FC00000, 0x7F800001, -0x400000, -0x7FFFFF]),
+             "bf16": (torch.int16, [0x7FC0, 0x7F81, -0x40, -0x7F]),
+             "fp16": (torch.int16, [0x7E00, 0x7C01, -0x200, -0x3FF])}
+    itype, bits = kinds[dtype]
+    for E, k in ((8, 4), (61, 8), (256, 8), (512, 16)):
+        z = _logits(E, 64, 1, E, dtype).cpu()
+        raw = z.view(itype)
+        for t in range(64):
+            for n, b in enumerate(bits[:1 + t % 4]):
+                raw[t, 0, (t * 5 + n * 3) % E] = b
+        assert torch.isnan(z).any(dim=2).all()
+        zh = _host(z)
+        for bias in (None, torch.linspace(-0.2, 0.2, E).view(1, E)):
+            ids, gates = rp.route_tokens(_problem(1, 1, E, k), z.cuda(), bias=None if bias is None else bias.cuda(),
+                                         score="sigmoid")
+            want = O.choose(zh, k, None if bias is None else bias.double().numpy(), "sigmoid")
+            assert np.array_equal(_host(ids), want), (dtype, E, bias is None)
+            assert torch.isfinite(gates).all()
+
+
+@gpu
 def test_scores_below_the_range_of_32_bits():
     """Logistic scores of very low logits vanish in 32 bits; their ratios
     (normalised gates and shares) do not."""
