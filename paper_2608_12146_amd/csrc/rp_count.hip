@@ -9,6 +9,11 @@
 // stores; the parts of one that spans chunks are added with integer atomics to
 // a row cleared before (integer sums do not depend on their order).
 //
+// 300007 x 24 x 8 int32: 45 us, 5.2 TB/s.  Byte ids are bound by the LDS:
+// 1000000 x 48 x 8 of them, 384 MB, take 101 us, 3.8 TB/s, at 64 atomics in
+// about 7 cycles (4.8 of them lost to lanes that meet in a bank, the mean of
+// random ones).  Two vector instructions an id.
+//
 // Sample i's part of chunk c is part i + c: both only grow along the tokens,
 // so the parts i + (its first chunk) on are its own, up to the next sample's.
 #include "rp_internal.h"
@@ -126,8 +131,8 @@ __global__ void __launch_bounds__(256) k_count(CountArgs a) {
     const int64_t place = W == 1 ? (int64_t)l_first * a.ls + j_first : at;
     // an id that is no expert's goes to the word behind the last expert's
     const uint32_t limit = (uint32_t)a.E;
-    const int32_t rows = (int32_t)((e - b + a.join - 1) / a.join);
-    const int64_t left = (e - b) * piece;  // ids of the part in rows of one piece
+    const int32_t tokens = (int32_t)(e > b ? e - b : 0), full = tokens / a.join;
+    const int32_t rows = full + (full * a.join < tokens ? 1 : 0);
     __syncthreads();
     for (int32_t q = 0; q < (a.layer_runs ? nl : 1); ++q) {
         const I *p = ids + b * a.ts + q * a.ls + place;
@@ -138,7 +143,7 @@ __global__ void __launch_bounds__(256) k_count(CountArgs a) {
             for (; r < rows; r += slots) add(id_of<I>(p[r * a.row_stride]), 0);
         } else {
             constexpr int U = 4;
-            const int32_t whole = a.join == 1 ? (len < W ? 0 : rows) : (int32_t)(left / len);
+            const int32_t whole = len < W ? 0 : full;  // (join is 1 where len < W)
             for (; r + (U - 1) * slots < whole; r += U * slots) {
                 uint32_t v[U][4];
 #pragma unroll
@@ -158,7 +163,7 @@ __global__ void __launch_bounds__(256) k_count(CountArgs a) {
             // shorter than a vector
             for (; r < rows; r += slots) {
                 const I *x = p + (int64_t)r * a.row_stride;
-                const int64_t end = a.join == 1 ? len : left - (int64_t)r * len;
+                const int64_t end = a.join == 1 ? len : (int64_t)(tokens - r * a.join) * piece;
 #pragma unroll
                 for (int w = 0; w < W; ++w)
                     if (at + w < end) add(id_of<I>(x[w]), w);

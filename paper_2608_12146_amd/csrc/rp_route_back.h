@@ -10,6 +10,11 @@
 // D goes through a row of LDS, zero but for the choices, to the lanes that hold
 // their experts: that costs an eighth of the LDS reads that comparing every
 // element with every choice would cost in instructions.
+//
+// 131072 x 512 bf16, both parts: 58 us, 4.7 TB/s read and written, where a
+// large copy reaches 4.9 to 5.4; what is left is the exponentials (a quarter of
+// the rate of other instructions) under 4 waves a SIMD.  Logistic rows, two
+// quarter-rate instructions an element and twice the registers, take 94 us.
 #pragma once
 
 #include "rp_route.h"
