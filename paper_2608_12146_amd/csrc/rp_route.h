@@ -302,13 +302,21 @@ __device__ inline void logistic_row(float (&z)[V], float (&less)[V], float &inv)
     const float m = row_max<G, V>(z);
     const bool low = m < 0.0f && m > -kInf;
     float sum = 0.0f;
+    if (__any(low)) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const float x = z[v];
-        logistic<FINE>(x, z[v], less[v]);
-        // e^x / (1 + e^x), and less is 1 / (1 + e^x)
-        if (__any(low)) z[v] = low ? exp_of<FINE>(x - m) * less[v] : z[v];
-        sum += z[v];
+        for (int v = 0; v < V; ++v) {
+            const float x = z[v];
+            logistic<FINE>(x, z[v], less[v]);
+            // e^x / (1 + e^x), and less is 1 / (1 + e^x)
+            z[v] = low ? exp_of<FINE>(x - m) * less[v] : z[v];
+            sum += z[v];
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            logistic<FINE>(z[v], z[v], less[v]);
+            sum += z[v];
+        }
     }
     sum = group_sum<G>(sum);
     inv = sum == 0.0f ? 0.0f : 1.0f / sum;

@@ -14,7 +14,7 @@
 // 131072 x 512 bf16, both parts: 58 us, 4.7 TB/s read and written, where a
 // large copy reaches 4.9 to 5.4; what is left is the exponentials (a quarter of
 // the rate of other instructions) under 4 waves a SIMD.  Logistic rows, two
-// quarter-rate instructions an element and twice the registers, take 94 us.
+// quarter-rate instructions an element and twice the registers, take 86 us.
 #pragma once
 
 #include "rp_route.h"
