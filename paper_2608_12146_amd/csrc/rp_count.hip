@@ -33,6 +33,7 @@ struct CountArgs {
     int32_t join;           // a row is that many tokens (of one workgroup's layers, or of one layer)
     int64_t row_stride;
     bool layer_runs;        // a row holds ids of one layer only
+    int32_t team;           // threads that count one layer then, or all 256
     int32_t pitch, copies;  // words between layers' counters, and copies of them (a power of two)
     int32_t lanes;          // log2 of the lanes that hand over a layer's counters
 };
@@ -106,8 +107,8 @@ __global__ void __launch_bounds__(256) k_count(CountArgs a) {
     const int32_t piece = a.layer_runs ? a.k : nl * a.k;  // ids of one token in a row
     const int32_t len = a.join * piece;    // of a row
     // its places, and the rows that the threads stand on abreast
-    const int32_t cols = pieces ? (len + W - 1) / W : len, slots = 256 / cols;
-    const int col = tid % cols, slot = tid / cols;
+    const int32_t cols = pieces ? (len + W - 1) / W : len, slots = a.team / cols;
+    const int me = tid & (a.team - 1), col = me % cols, slot = me / cols;
     // the thread's ids are at .. at + W of its rows, less those that the place
     // before holds already (the last place is moved back into the row)
     const int32_t want = col * W;
@@ -132,18 +133,17 @@ __global__ void __launch_bounds__(256) k_count(CountArgs a) {
     // an id that is no expert's goes to the word behind the last expert's
     const uint32_t limit = (uint32_t)a.E;
     const int32_t tokens = (int32_t)(e > b ? e - b : 0), full = tokens / a.join;
-    const int32_t rows = full + (full * a.join < tokens ? 1 : 0);
     __syncthreads();
-    for (int32_t q = 0; q < (a.layer_runs ? nl : 1); ++q) {
+    for (int32_t q = tid / a.team; q < (a.layer_runs ? nl : 1); q += 256 / a.team) {
         const I *p = ids + b * a.ts + q * a.ls + place;
         const int32_t up = q * a.pitch;  // (rows of one layer are whole vectors: all places are the thread's)
         auto add = [&](uint32_t id, int w) { atomicAdd(to[w] + (up + (id < limit ? id : limit)), 1); };
-        int32_t r = slot < slots ? slot : rows;
+        int32_t r = slot < slots ? slot : full;
         if constexpr (W == 1) {
-            for (; r < rows; r += slots) add(id_of<I>(p[r * a.row_stride]), 0);
+            for (; r < full; r += slots) add(id_of<I>(p[r * a.row_stride]), 0);  // (join is 1)
         } else {
             constexpr int U = 4;
-            const int32_t whole = len < W ? 0 : full;  // (join is 1 where len < W)
+            const int32_t whole = len < W ? 0 : full;
             for (; r + (U - 1) * slots < whole; r += U * slots) {
                 uint32_t v[U][4];
 #pragma unroll
@@ -159,14 +159,20 @@ __global__ void __launch_bounds__(256) k_count(CountArgs a) {
 #pragma unroll
                 for (int w = 0; w < W; ++w) add(id_at<I>(v, w), w);
             }
-            // the last row where its tokens are fewer than `join`, or rows
-            // shorter than a vector
-            for (; r < rows; r += slots) {
-                const I *x = p + (int64_t)r * a.row_stride;
-                const int64_t end = a.join == 1 ? len : (int64_t)(tokens - r * a.join) * piece;
-#pragma unroll
-                for (int w = 0; w < W; ++w)
-                    if (at + w < end) add(id_of<I>(x[w]), w);
+            // what is left, an id a thread: the tokens behind the last row of
+            // `join`, or all of a small last group, whose row is shorter than a
+            // vector
+            const int32_t done = whole * a.join;
+            const I *x = ids + (b + done) * a.ts + q * a.ls;
+            auto one = [&](int32_t t, int32_t y) {
+                const uint32_t id = id_of<I>(x[t * a.ts + y]);
+                const int32_t l = a.layer_runs ? q : y / a.k;
+                atomicAdd(mine + l * a.pitch + (id < limit ? id : limit), 1);
+            };
+            if (len >= W) {
+                for (int32_t y = me; y < (tokens - done) * piece; y += a.team) one(y / piece, y % piece);
+            } else {
+                for (int32_t t = me / piece; t < tokens && me < 256 / piece * piece; t += 256 / piece) one(t, me % piece);
             }
         }
     }
@@ -234,7 +240,12 @@ int count(CountArgs &a, bool layer_runs, bool token_rows, hipStream_t stream) {
     if (pieces && a.ts == piece && (layer_runs || a.group == a.L)) a.join = W / gcd_of(W, piece);
     if (a.join * piece / W > 256) a.join = 1;
     a.row_stride = a.join * a.ts;
-    if ((pieces ? (a.join * piece + W - 1) / W : piece) > 256) return ROUTEPACK_E_INTERNAL;  // (never: `places`)
+    const bool vectors = pieces && a.join * piece >= W;  // (else an id a thread)
+    const int32_t cols = vectors ? (a.join * piece + W - 1) / W : piece;
+    if (cols > 256) return ROUTEPACK_E_INTERNAL;  // (never: `places`)
+    // several layers: a wave each (131233 x 64 x 3 bytes by layers, 2863 samples:
+    // 75 us, 484 with the workgroup on one layer and its odd ids by few threads)
+    a.team = layer_runs && a.group > 1 && cols <= kWave ? kWave : 256;
     a.copies = 1;
     while (a.copies < 16 && 2 * a.copies * a.group * a.pitch <= (layer_runs ? kWords : kWords / 2)) a.copies *= 2;
     // Chunks of 64 tokens and more: about 4096 of them, but, where 512 are left,
@@ -271,7 +282,7 @@ int count(CountArgs &a, bool layer_runs, bool token_rows, hipStream_t stream) {
         hipLaunchKernelGGL(kern, grid_of(parts * a.n_groups), dim3(256), lds, stream, a);
         return hipGetLastError() == hipSuccess ? ROUTEPACK_OK : ROUTEPACK_E_DEVICE;
     };
-    if (pieces) return go(k_count<I, W>);
+    if (vectors) return go(k_count<I, W>);
     return go(k_count<I, 1>);
 }
 
