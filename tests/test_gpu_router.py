@@ -768,3 +768,65 @@ def test_refused_tensors():
                  lambda: rp.route_tokens(_problem(1, 1, 2, 3), torch.zeros((1, 1, 2), device="cuda"))):
         with pytest.raises(rp.RoutepackError):
             call()
+
+
+def _close_or_nan(got, want, tol, what):
+    """_close, where `want` has no NaN; NaN where it has."""
+    got = _host(got)
+    nan = np.isnan(want)
+    assert np.array_equal(np.isnan(got), nan), (what, np.argwhere(np.isnan(got) != nan)[:4].tolist())
+    bad = ~(np.abs(got - want) <= tol) & ~nan
+    assert not bad.any(), (what, int(bad.sum()), got[bad][:4], want[bad][:4])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("terms", ["gates", "balance", "both"])
+def test_gradient_of_padding_that_holds_anything(dtype, score, terms):
+    """Rows before the first offset, behind the last one and of no sample get
+    the gates' part alone whatever they hold: NaN, +inf and rows without an
+    expert reach it where the gates' scores do, and nowhere else."""
+    import torch
+    import paper_2608_12146_amd as rp
+    for T, L, E, k in ((40, 1, 60, 6), (41, 2, 64, 8), (29, 1, 256, 8), (30, 1, 7, 2), (33, 1, 512, 9), (31, 1, 1500, 4)):
+        first, lengths = 9, [T - 25, 0, 5]
+        z, dg, counts, dl = _gradient_case(E, T, L, E, k, dtype, 0.0, lengths)
+        off = _offsets(lengths, first)
+        ids = _ids(E, T, L, E, k, "i32", 0.2)
+        pad = list(range(first)) + list(range(int(off[-1]), T))
+        for n, t in enumerate(pad):
+            kind = n % 6
+            if kind == 0:
+                z[t] = float("nan")
+            elif kind == 1:
+                z[t, :, n % E] = float("nan")
+            elif kind == 2:
+                z[t, :, n % E] = float("inf")
+            elif kind == 3:
+                z[t] = float("-inf")
+            elif kind == 4:
+                ids[t] = -1
+                z[t] = float("nan")
+        zh = _host(z)
+        for normalize in (True, False):
+            what = (dtype, score, terms, T, L, E, k, normalize)
+            _log(what)
+            a, w = {}, {}
+            if terms != "balance":
+                a.update(ids=ids, dgates=dg.cuda(), normalize=normalize, scale=1.5)
+                w.update(ids=_host(ids), dgates=dg.double().numpy(), normalize=normalize, scale=1.5)
+            if terms != "gates":
+                a.update(counts=counts.cuda(), offsets=off, dloss=dl.cuda())
+                w.update(counts=counts.numpy(), offsets=_host(off), dloss=dl.double().numpy())
+            got = rp.route_backward(_problem(1, L, E, k), z, score=score, **a)
+            with np.errstate(invalid="ignore"):
+                want, mag = O.backward(zh, score, **w)
+            if terms == "balance":
+                assert not want[pad].any()
+            info = torch.finfo(_type(dtype))
+            mag = np.nan_to_num(mag)
+            far = _range(zh[[t for t in range(T) if np.isfinite(zh[t]).all()]])
+            tol = (9.2 * far + 214) * U * mag
+            tol = tol + info.eps / 2 * (np.abs(want) + tol) + info.tiny * info.eps / 2 + TINY * (1 + mag.max())
+            _close_or_nan(got, want, tol, what)
