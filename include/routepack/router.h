@@ -71,7 +71,9 @@ typedef struct routepack_ids {
 /* The gates of every token's k experts.
  * With replay == NULL the experts are chosen: the k available ones of largest
  * logit, or, given a bias, of largest score + bias (compared in 64 bits; the
- * bias takes no part in the gates, and -inf or NaN there bars its expert);
+ * bias takes no part in the gates, and -inf or NaN there bars its expert; a
+ * NaN logit takes no part in the softmax scores that a bias is added to, and
+ * experts of +inf share those alone, in equal parts);
  * ties go to the lowest index, largest first, and -1 stands where none is
  * left.  With replay the experts are those of the record (a repeated expert
  * has a gate for each mention).  Gates: scale times the chosen experts'

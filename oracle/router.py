@@ -39,7 +39,12 @@ def shares(z, score):
 
 
 def choose(z, k, bias=None, score="softmax"):
-    key = z if bias is None else (_softmax(z) if score == "softmax" else _sigmoid(z)[0]) + bias
+    if bias is not None and score == "softmax":
+        # a NaN takes no part, and experts of +inf share the scores alone
+        key = _softmax(np.where(np.isnan(z), -np.inf, np.where((z == np.inf).any(axis=-1, keepdims=True),
+                                                               np.where(z == np.inf, 0.0, -np.inf), z))) + bias
+    else:
+        key = z if bias is None else _sigmoid(z)[0] + bias
     key = np.where(np.isneginf(z) | np.isnan(z) | np.isnan(key), -np.inf, key)
     ids = np.argsort(-key, axis=-1, kind="stable")[..., :k]
     return np.where(np.isneginf(np.take_along_axis(key, ids, -1)), -1, ids)

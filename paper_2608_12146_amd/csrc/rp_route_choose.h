@@ -273,6 +273,9 @@ __global__ void __launch_bounds__(256) k_route_bias(RouteArgs a) {
     over = group_sum<G>(over);
     more = group_sum<G>(more);
     open = open || (edge > -kInf && (over != (float)a.k || more != 0.0f)) || edge != edge;
+    // a softmax row with NaN or +inf has no keys in 32 bits
+    const bool odd = inv != inv;
+    open = open || odd;
     float zc[S], g[S], less[S];
     bool on[S];
     int32_t id[S];
@@ -284,6 +287,20 @@ __global__ void __launch_bounds__(256) k_route_bias(RouteArgs a) {
         id[s] = s * M + c < a.k && Key::available(mine) ? (int32_t)Key::index(mine) : -1;
     }
     if (__any(open)) {
+        const bool any_odd = __any(odd);
+        float base = m;  // the largest logit that is no NaN
+        if (any_odd) {
+            base = -kInf;
+#pragma unroll 1
+            for (int i = 0; i < NV; ++i) {
+                const Vec<T> y = row.vec(i * G + c);
+#pragma unroll
+                for (int w = 0; w < W; ++w) base = y.at(w) > base ? y.at(w) : base;
+            }
+            base = group_max<G>(base);
+        }
+        // e^(z - base) in 64 bits; the minimum makes inf - inf a 0
+        auto part = [&](float z) { return exp(__builtin_fmin((double)z - (double)base, 0.0)); };
         double sum = 0.0;
         if (softmax) {
 #pragma unroll 1
@@ -294,7 +311,7 @@ __global__ void __launch_bounds__(256) k_route_bias(RouteArgs a) {
                 for (int w = 0; w < W; ++w) z[w] = y.at(w);
 #pragma unroll 1
                 for (int w = 0; w < W; ++w) {
-                    sum += z[0] > -kInf ? exp((double)z[0] - (double)m) : 0.0;
+                    sum += z[0] > -kInf ? part(z[0]) : 0.0;
                     shift_down(z);
                 }
             }
@@ -305,7 +322,7 @@ __global__ void __launch_bounds__(256) k_route_bias(RouteArgs a) {
 #pragma unroll
         for (int j = 0; j < K; ++j) next[j] = Word(0);
         const bool second = __any(more > 0.0f);
-        bool deep = false;
+        bool deep = any_odd;
         if (second) {  // the vectors after the first k
             Word kth = Word(0);
 #pragma unroll
@@ -314,7 +331,7 @@ __global__ void __launch_bounds__(256) k_route_bias(RouteArgs a) {
             for (int i = 0; i < NV; ++i) vk[i] = Key::available(kth) && vk[i] < kth ? vk[i] : Word(0);
             lane_top<Key, K, NV>(vk, next);
             group_top<Key, K, G>(next);
-            deep = __any(Key::available(next[K - 1]) && Key::value(next[K - 1]) >= edge);
+            deep = deep || __any(Key::available(next[K - 1]) && Key::value(next[K - 1]) >= edge);
         }
         int at[2 * S];  // this lane's vectors of both batches
 #pragma unroll
@@ -356,8 +373,7 @@ __global__ void __launch_bounds__(256) k_route_bias(RouteArgs a) {
             }
 #pragma unroll 1
             for (int w = 0; w < W; ++w) {
-                const double x = (double)z[0];
-                double key = softmax ? exp(x - (double)m) / sum : 1.0 / (1.0 + exp(-x));
+                double key = softmax ? part(z[0]) / sum : 1.0 / (1.0 + exp(-(double)z[0]));
                 key += (double)b[0];
                 uint64_t k0 = z[0] > -kInf && key > -__builtin_inf() ? order64(key) : 0;
                 uint32_t e0 = (uint32_t)(v * W + w);

@@ -830,3 +830,55 @@ def test_gradient_of_padding_that_holds_anything(dtype, score, terms):
             tol = (9.2 * far + 214) * U * mag
             tol = tol + info.eps / 2 * (np.abs(want) + tol) + info.tiny * info.eps / 2 + TINY * (1 + mag.max())
             _close_or_nan(got, want, tol, what)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_bias_over_nan_and_infinities(dtype, score):
+    """NaN and +inf logits with a selection bias: the available experts are
+    chosen all the same, the gates show the NaN where its score enters, and a
+    token's result does not depend on the tokens beside it (rows of equal
+    logits, whose order is found in 64 bits, among them)."""
+    import torch
+    import paper_2608_12146_amd as rp
+    signalling = {"fp32": (torch.int32, 0x7F800001), "bf16": (torch.int16, 0x7F81), "fp16": (torch.int16, 0x7C01)}
+    for E, k in ((256, 8), (7, 3), (61, 6), (512, 16), (40, 32), (2048, 8)):
+        T = 19
+        z = _logits(E, T, 1, E, dtype).cpu()
+        z[0, 0, 3] = float("nan")
+        z[1] = 0.5
+        z[2, 0, 5] = float("inf")
+        z[4, 0, [1, E - 1]] = float("inf")
+        z[5] = float("nan")
+        itype, bits = signalling[dtype]
+        z[6].view(itype)[0, E // 2] = bits
+        z[7, 0, 0], z[7, 0, 2] = float("nan"), float("inf")
+        z[8] = float("-inf")
+        z[9, 0, 4:] = float("-inf")
+        z[9, 0, 2] = float("nan")
+        z[10] = -0.5
+        z[11, 0, ::2] = float("nan")
+        z[12] = float("inf")
+        z[13] = 2.0
+        z[13, 0, E - 2] = float("nan")
+        zh = _host(z)
+        prob = _problem(1, 1, E, k)
+        g = torch.Generator().manual_seed(E)
+        for bias in (torch.zeros((1, E)), torch.randn((1, E), generator=g) * 0.3,
+                     torch.where(torch.rand((1, E), generator=g) < 0.3, -np.inf, 0.25)):
+            with np.errstate(invalid="ignore"):
+                want = O.choose(zh, k, bias.double().numpy(), score)
+            for normalize in (True, False):
+                what = (dtype, score, E, k, normalize)
+                _log(what)
+                ids, gates = rp.route_tokens(prob, z.cuda(), bias=bias.cuda(), score=score, normalize=normalize)
+                assert np.array_equal(_host(ids), want), (what, np.argwhere((_host(ids) != want).any(-1)).tolist())
+                with np.errstate(invalid="ignore"):
+                    wg = O.gates(zh, want, score, normalize, 1.0)
+                far = _range(np.where(np.isfinite(zh), zh, -np.inf))
+                _close_or_nan(gates, wg, (3.3 * far + 80) * U * np.abs(wg) + TINY, what)
+                for t in range(T):
+                    one = rp.route_tokens(prob, z[t:t + 1].cuda(), bias=bias.cuda(), score=score, normalize=normalize)
+                    assert torch.equal(one[0], ids[t:t + 1]), (what, t)
+                    assert np.array_equal(_host(one[1]), _host(gates[t:t + 1]), equal_nan=True), (what, t)

@@ -175,3 +175,21 @@ def test_oracle_gradient(score, normalize):
 def test_oracle_counts():
     ids = np.array([[[0, 1]], [[1, 1]], [[-1, 9]], [[2, 0]]])
     assert O.count(ids, np.array([0, 2, 2, 3]), 3).tolist() == [[[1, 3, 0]], [[0, 0, 0]], [[0, 0, 0]]]
+
+
+def test_oracle_biased_choices_over_nan_and_infinities():
+    """Under a softmax a NaN logit takes no part in the scores that a bias is
+    added to, and experts of +inf share them alone."""
+    z = np.array([[[1.0, 3.0, 3.0, -np.inf, np.nan]], [[1.0, np.inf, 0.0, np.inf, np.nan]]])
+    none = np.zeros((1, 5))
+    with np.errstate(invalid="ignore"):
+        ids = O.choose(z, 5, none, "softmax")
+        assert ids.tolist() == [[[1, 2, 0, -1, -1]], [[1, 3, 0, 2, -1]]]
+        some = np.array([[0.6, 0.0, 0.4, 0.0, 9.0]])
+        assert O.choose(z[1:], 3, some, "softmax").tolist() == [[[0, 1, 3]]]
+        assert O.choose(z[:1], 2, np.array([[-np.inf, 0.0, np.nan, 9.0, 9.0]]), "softmax").tolist() == [[[1, -1]]]
+        # the gates: NaN where such a score enters
+        g = O.gates(z, ids, "softmax", True, 1.0)
+        assert np.isfinite(g[0]).all() and np.isnan(g[1, 0, :4]).all()
+        g = O.gates(z, ids, "softmax", False, 1.0)
+        assert np.isnan(g[0, 0, :3]).all() and np.isnan(g[1, 0, :4]).all() and not g[:, 0, 4].any()
