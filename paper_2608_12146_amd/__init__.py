@@ -2,8 +2,8 @@
 
 A thin ctypes layer over the C-ABI in include/routepack.h and, for the
 router's operators, include/routepack/router.h (libroutepack.so).
-It only marshals arguments: torch supplies device memory and the current HIP
-stream, and every step of the path runs in the library's HIP kernels.  There
+It only marshals arguments (and lets autograd record the router's gates and
+loss): torch supplies device memory and the current HIP stream, and every step of the path runs in the library's HIP kernels.  There
 is no CPU fallback: importing works without a GPU, but every call raises if
 the library or a GPU is missing.
 """
@@ -451,6 +451,65 @@ def _score(fn, score):
     return SCORES[score]
 
 
+_FUNCTIONS = None
+
+
+def _functions():
+    """(gates, loss) as functions that autograd records: route_tokens and
+    balance_loss go through them, and they (with recording off) through these,
+    where the logits require a gradient.  Their backward passes are
+    route_backward's; ids and counts are constants."""
+    global _FUNCTIONS
+    if _FUNCTIONS is not None:
+        return _FUNCTIONS
+    torch = _router()[1]
+    once_differentiable = torch.autograd.function.once_differentiable
+
+    class Gates(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, logits, prob, ids, bias, score, normalize, scale):
+            out, gates = route_tokens(prob, logits, ids=ids, bias=bias, score=score, normalize=normalize, scale=scale)
+            ctx.save_for_backward(logits, out)
+            ctx.set_materialize_grads(False)
+            ctx.args = prob, dict(score=score, normalize=normalize, scale=scale)
+            if ids is not None:
+                return gates
+            ctx.mark_non_differentiable(out)
+            return out, gates
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, *grads):
+            dz = None
+            if grads[-1] is not None:
+                (logits, ids), (prob, how) = ctx.saved_tensors, ctx.args
+                dz = route_backward(prob, logits, ids=ids, dgates=grads[-1].contiguous(), **how)
+            return dz, None, None, None, None, None, None
+
+    class Loss(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, logits, prob, counts, offsets, score):
+            ctx.save_for_backward(logits, counts, offsets)
+            ctx.set_materialize_grads(False)
+            ctx.args = prob, score
+            return balance_loss(prob, logits, counts, offsets, score=score)
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, dloss, dshares):
+            if dshares is not None:
+                raise NotImplementedError("routepack_balance_loss: the shares have no gradient, only the loss has")
+            dz = None
+            if dloss is not None:
+                (logits, counts, offsets), (prob, score) = ctx.saved_tensors, ctx.args
+                dz = route_backward(prob, logits, counts=counts, offsets=offsets, dloss=dloss.contiguous(),
+                                    score=score)
+            return dz, None, None, None, None
+
+    _FUNCTIONS = Gates, Loss
+    return _FUNCTIONS
+
+
 def route_tokens(prob: Problem, logits, *, ids=None, bias=None, score="softmax", normalize=True, scale=1.0):
     """The router's gates: (ids, gates), each [T][L][k] (or [T][k] for logits
     [T][E]), k = prob.top_k.
@@ -461,10 +520,21 @@ def route_tokens(prob: Problem, logits, *, ids=None, bias=None, score="softmax",
     expert is available (an expert is masked by a logit of -inf).  With `ids`
     (uint8, int16, int32 or int64; a replayed record) the gates are those of
     the recorded experts, and `ids` is returned as it is.  score: "softmax"
-    or "sigmoid"; normalize: divide by the sum over the token's choices."""
+    or "sigmoid"; normalize: divide by the sum over the token's choices.
+
+    Where the logits require a gradient, autograd records the gates: their
+    backward pass is route_backward's with the ids as constants (none reaches
+    the bias, which takes no part in the gates).  A trainer that has the
+    gradients of gates and loss at hand saves a pass by calling route_backward
+    itself, under torch.no_grad().  (As for all that autograd records: before a
+    backward pass is captured into a graph, results recorded eagerly from the
+    same leaves are to be released.)"""
     lib, torch, floats, ints = _router()
     call = _Call("routepack_route_tokens", torch)
     shape, z = call.rows("logits", logits, floats, prob.n_layers, prob.n_experts)
+    if logits.requires_grad and torch.is_grad_enabled():
+        out = _functions()[0].apply(logits, prob, ids, bias, score, normalize, scale)
+        return out if ids is None else (ids, out)
     shape = (*shape[:-1], prob.top_k)
     b = bias
     if bias is not None:
@@ -517,10 +587,16 @@ def balance_loss(prob: Problem, logits, counts, offsets, *, score="softmax"):
     the counts that expert e has, times E, and shares the mean over the
     group's tokens of the scores divided by their sum.  counts int32 or int64
     [G][L][E] (count_demand's result, or aggregate_demand's as [1][L][E] for
-    one group over the window); offsets int64 [G + 1]."""
+    one group over the window); offsets int64 [G + 1].
+
+    Where the logits require a gradient, autograd records the loss: its
+    backward pass is route_backward's with the counts as constants.  The
+    shares' own gradient is not formed; a backward pass through them raises."""
     lib, torch, floats, _ = _router()
     call = _Call("routepack_balance_loss", torch)
     shape, z = call.rows("logits", logits, floats, prob.n_layers, prob.n_experts)
+    if logits.requires_grad and torch.is_grad_enabled():
+        return _functions()[1].apply(logits, prob, counts, offsets, score)
     G, off, n, n_type = _groups(call, prob, counts, offsets)
     L, E, at = prob.n_layers, prob.n_experts, call.device
     loss = torch.empty(L, dtype=torch.float32, device=at)
@@ -537,7 +613,7 @@ def route_backward(prob: Problem, logits, *, ids=None, dgates=None, normalize=Tr
     """dlogits, of the logits' shape and type, from the gradients of
     route_tokens' gates (`ids`, `dgates` float32 of their shape, `normalize`,
     `scale`), of balance_loss' loss (`counts`, `offsets`, `dloss` float32 [L]),
-    or of both in one pass."""
+    or of both in one pass.  The result itself carries no gradient."""
     lib, torch, floats, ints = _router()
     call = _Call("routepack_route_backward", torch)
     if (ids is None) != (dgates is None):

@@ -882,3 +882,137 @@ def test_bias_over_nan_and_infinities(dtype, score):
                     one = rp.route_tokens(prob, z[t:t + 1].cuda(), bias=bias.cuda(), score=score, normalize=normalize)
                     assert torch.equal(one[0], ids[t:t + 1]), (what, t)
                     assert np.array_equal(_host(one[1]), _host(gates[t:t + 1]), equal_nan=True), (what, t)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_autograd_takes_route_backward(dtype, score):
+    """Logits that require a gradient get route_backward's, bit for bit, from
+    the gates and from the loss; logits that do not, or under no_grad, record
+    nothing."""
+    import torch
+    import paper_2608_12146_amd as rp
+    for T, L, E, k in ((33, 2, 60, 6), (1, 1, 8, 2), (40, 1, 256, 8)):
+        prob = _problem(2, L, E, k)
+        off = _offsets([T // 2, T - T // 2])
+        z = _logits(11, T, L, E, dtype)
+        rec = _ids(12, T, L, E, k, "i16", 0.1)
+        w = torch.randn((T, L, k), device="cuda")
+        v = torch.rand(L, device="cuda")
+        for normalize in (True, False):
+            how = dict(score=score, normalize=normalize, scale=1.5)
+            for ids in (None, rec):
+                leaf = z.clone().requires_grad_()
+                got, gates = rp.route_tokens(prob, leaf, ids=ids, **how)
+                plain = rp.route_tokens(prob, z, ids=ids, **how)
+                assert torch.equal(got, plain[0]) and torch.equal(gates, plain[1])
+                assert gates.requires_grad and not got.requires_grad and (ids is None or got is ids)
+                assert not plain[1].requires_grad
+                (gates * w).sum().backward()
+                assert torch.equal(leaf.grad, rp.route_backward(prob, z, ids=got, dgates=w, **how))
+                # a gradient that is one number in every place, and one with other strides
+                d1, = torch.autograd.grad(rp.route_tokens(prob, leaf, ids=ids, **how)[1].sum(), leaf)
+                assert torch.equal(d1, rp.route_backward(prob, z, ids=got, dgates=torch.ones_like(w), **how))
+                turned = w.permute(2, 1, 0).contiguous().permute(2, 1, 0)
+                d2, = torch.autograd.grad(rp.route_tokens(prob, leaf, ids=ids, **how)[1], leaf, turned)
+                assert torch.equal(d2, leaf.grad)
+                with torch.no_grad():
+                    assert not rp.route_tokens(prob, leaf, ids=ids, **how)[1].requires_grad
+        counts = rp.count_demand(prob, rec, off)
+        leaf = z.clone().requires_grad_()
+        loss, shares = rp.balance_loss(prob, leaf, counts, off, score=score)
+        plain = rp.balance_loss(prob, z, counts, off, score=score)
+        assert torch.equal(loss, plain[0]) and torch.equal(shares, plain[1]) and not plain[0].requires_grad
+        (loss * v).sum().backward()
+        assert torch.equal(leaf.grad, rp.route_backward(prob, z, counts=counts, offsets=off, dloss=v, score=score))
+        d, = torch.autograd.grad(rp.balance_loss(prob, leaf, counts, off, score=score)[0].sum(), leaf)
+        ones = torch.ones(L, device="cuda")
+        assert torch.equal(d, rp.route_backward(prob, z, counts=counts, offsets=off, dloss=ones, score=score))
+
+
+@gpu
+def test_autograd_of_broadcast_and_narrow_logits():
+    """One row of logits for all tokens, [T][E] logits of one layer and a
+    slice of a wider projection: gradients arrive where the values came from."""
+    import torch
+    import paper_2608_12146_amd as rp
+    T, E, k = 12, 16, 3
+    prob = _problem(1, 1, E, k)
+    w = torch.randn((T, k), device="cuda")
+    ids = _ids(1, T, 1, E, k)[:, 0]
+    row = _logits(2, 1, 1, E, "fp32")[0].requires_grad_()
+    _, gates = rp.route_tokens(prob, row.expand(T, E), ids=ids)
+    (gates * w).sum().backward()
+    want, mag = O.backward(_host(row.detach().expand(T, E))[:, None], "softmax", _host(ids)[:, None],
+                           _host(w)[:, None], True, 1.0)
+    _close(row.grad, want.sum(axis=0), (9.2 * _range(_host(row)) + 214 + T) * U * mag.sum(axis=0) + TINY * T, "row")
+    wide = _logits(3, T, 1, E + 5, "fp32")[:, 0].requires_grad_()
+    _, gates = rp.route_tokens(prob, wide[:, 2:2 + E], ids=ids)
+    (gates * w).sum().backward()
+    inner = wide.detach()[:, 2:2 + E]
+    assert torch.equal(wide.grad[:, 2:2 + E], rp.route_backward(prob, inner, ids=ids, dgates=w))
+    assert not wide.grad[:, :2].any() and not wide.grad[:, 2 + E:].any()
+
+
+@gpu
+def test_autograd_refusals():
+    """No silent gradients: the shares' raises, so do a second derivative and
+    a backward pass over logits or ids that were written since."""
+    import torch
+    import paper_2608_12146_amd as rp
+    T, L, E, k = 9, 2, 16, 2
+    prob = _problem(1, L, E, k)
+    off = _offsets([T])
+    ids = _ids(1, T, L, E, k)
+    counts = rp.count_demand(prob, ids, off)
+    leaf = _logits(2, T, L, E, "fp32").requires_grad_()
+    loss, shares = rp.balance_loss(prob, leaf, counts, off)
+    with pytest.raises(NotImplementedError):
+        (loss.sum() + shares[0, 0, 0]).backward()
+    _, gates = rp.route_tokens(prob, leaf)
+    d, = torch.autograd.grad(gates.square().sum(), leaf, create_graph=True)
+    with pytest.raises(RuntimeError):
+        d.sum().backward()
+    for write in (lambda: z.add_(1.0), lambda: ids.add_(1)):
+        z = leaf * 1.0
+        _, gates = rp.route_tokens(prob, z, ids=ids)
+        write()
+        with pytest.raises(RuntimeError):
+            gates.sum().backward()
+
+
+@gpu
+def test_autograd_on_streams_and_in_graphs():
+    """A pass forward and back on a side stream, and captured and replayed on
+    other inputs between eager work, gives the eager gradient."""
+    import torch
+    import paper_2608_12146_amd as rp
+    T, L, E, k = 3000, 2, 64, 6
+    prob = _problem(3, L, E, k)
+    off = _offsets([1000, 1500, 500])
+    w, v = torch.randn((T, L, k), device="cuda"), torch.rand(L, device="cuda") * T
+    x = _logits(0, T, L, E, "fp32").requires_grad_()
+
+    def step():
+        ids, gates = rp.route_tokens(prob, x)
+        loss, _ = rp.balance_loss(prob, x, rp.count_demand(prob, ids, off), off)
+        return torch.autograd.grad((gates * w).sum() + (loss * v).sum(), x)[0]
+    want = step()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(3):
+            assert torch.equal(step(), want)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = step()
+    for r in range(4):
+        with torch.no_grad():
+            x.copy_(_logits(20 + r, T, L, E, "fp32"))
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, step()), r
+        torch.cuda.synchronize()
