@@ -25,6 +25,8 @@
  *   an ordinary, very low logit.
  * - Ids outside [0, E) mark a choice that was not made: such a choice counts
  *   nowhere and its gate and gate gradient are 0.
+ * - Calls whose logits have 2^59 elements and more (broadcast ones can) give
+ *   E_UNSUPPORTED.
  * - Scores, sums and gradients are formed in 32 bits or more and rounded
  *   once, to the output's type.  Results do not depend on the launch: no
  *   floating-point atomics.
@@ -105,7 +107,8 @@ int routepack_count_demand(const routepack_problem *prob, const routepack_ids *i
                            const int64_t *offsets, int32_t *demand, hipStream_t stream);
 
 /* Bytes of workspace that routepack_balance_loss needs for n_tokens tokens
- * in n_groups groups, or ROUTEPACK_E_INVALID. */
+ * in n_groups groups, or ROUTEPACK_E_INVALID (E_UNSUPPORTED where that number
+ * does not fit 64 bits). */
 int64_t routepack_balance_workspace(const routepack_problem *prob, int64_t n_tokens, int32_t n_groups);
 
 /* The balance loss of every layer, a mean over groups of tokens (the samples

@@ -219,7 +219,7 @@ using namespace rp;
 namespace {
 
 // The workspace: the chunks' rows, the groups' parts of the loss, and a count
-// of arrivals a layer.
+// of arrivals a layer (or in `bytes` the error where these do not fit 64 bits).
 struct Workspace {
     int64_t n_chunks, parts_at, arrived_at, bytes;
     int32_t chunk;
@@ -228,11 +228,17 @@ Workspace workspace_of(int64_t T, int32_t L, int32_t E, int32_t n_groups) {
     Workspace w;
     // about 1024 workgroups of 32 tokens and more
     int64_t c = 32;
-    while (c < 1024 && T * L > c * 1024) c *= 2;
+    while (c < 1024 && (__int128)T * L > c * 1024) c *= 2;
     w.chunk = (int32_t)c;
-    w.n_chunks = (T + c - 1) / c;
-    w.parts_at = ((w.n_chunks + n_groups) * L * E * 4 + 15) & ~(int64_t)15;
-    w.arrived_at = w.parts_at + (int64_t)16 * L * n_groups * ((E + kWave - 1) / kWave);
+    w.n_chunks = T / c + (T % c != 0);
+    const __int128 rows = ((__int128)w.n_chunks + n_groups) * L * E * 4 + 15;
+    const __int128 parts = (__int128)16 * L * n_groups * ((E - 1) / kWave + 1);
+    if (rows + parts + (int64_t)4 * L > INT64_MAX) {  // (each addend is below 2^127)
+        w.bytes = ROUTEPACK_E_UNSUPPORTED;
+        return w;
+    }
+    w.parts_at = (int64_t)rows & ~(int64_t)15;
+    w.arrived_at = w.parts_at + (int64_t)parts;
     w.bytes = w.arrived_at + (int64_t)4 * L;
     return w;
 }
@@ -254,6 +260,7 @@ extern "C" int routepack_balance_loss(const routepack_problem *prob, const route
     if (L == 0) return ROUTEPACK_OK;
     if (!offsets || !counts || !loss || !shares || !workspace || (uintptr_t)workspace % 16) return ROUTEPACK_E_INVALID;
     const Workspace w = workspace_of(logits->n_tokens, L, E, n_groups);
+    if (w.bytes < 0) return (int)w.bytes;
     if (workspace_bytes < w.bytes) return ROUTEPACK_E_INVALID;
     float *rows = static_cast<float *>(workspace);
     double *parts = reinterpret_cast<double *>(static_cast<char *>(workspace) + w.parts_at);

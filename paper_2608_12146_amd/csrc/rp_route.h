@@ -586,6 +586,9 @@ inline int check_logits(const routepack_problem *p, const routepack_logits *z, i
     if (!z->data && z->n_tokens > 0 && p->n_layers > 0) return ROUTEPACK_E_INVALID;
     if (score != ROUTEPACK_SOFTMAX && score != ROUTEPACK_SIGMOID) return ROUTEPACK_E_INVALID;
     if (p->n_experts > kMaxExperts) return ROUTEPACK_E_UNSUPPORTED;
+    // (all products of tokens, layers and experts, in bytes, fit 64 bits)
+    if (p->n_layers > 0 && z->n_tokens > INT64_MAX / 16 / ((int64_t)p->n_layers * p->n_experts))
+        return ROUTEPACK_E_UNSUPPORTED;
     return ROUTEPACK_OK;
 }
 

@@ -193,3 +193,26 @@ def test_oracle_biased_choices_over_nan_and_infinities():
         assert np.isfinite(g[0]).all() and np.isnan(g[1, 0, :4]).all()
         g = O.gates(z, ids, "softmax", False, 1.0)
         assert np.isnan(g[0, 0, :3]).all() and np.isnan(g[1, 0, :4]).all() and not g[:, 0, 4].any()
+
+
+def test_sizes_past_64_bits_are_refused():
+    """Numbers of tokens, layers and groups whose products leave 64 bits (of
+    broadcast logits, say) give an error, no size that wrapped around."""
+    import paper_2608_12146_amd as rp
+    lib = rp.load_library()
+    most = 2 ** 31 - 1
+    for T, L, E, G in ((4, 1 << 20, 2048, most), (4, most, 2048, 1 << 20), (1 << 62, 1 << 10, 64, 2), (4, most, most, most)):
+        assert lib.routepack_balance_workspace(_problem(L=L, E=E).ref, T, G) == -8, (T, L, E, G)
+    exact = lib.routepack_balance_workspace(_problem(L=most, E=2048).ref, 4, 1 << 16)
+    assert exact >= (1 + (1 << 16)) * most * 2048 * 4 + 16 * most * (1 << 16) * 32
+
+    def loss(L, T, G):
+        z = _rows(0, T=T, ts=0, ls=0)
+        return lib.routepack_balance_loss(_problem(L=L, E=2048).ref, C.byref(z), G, SOME, SOME, 5, 0, SOME, SOME, SOME,
+                                          2 ** 62, None)
+    assert loss(1 << 20, 4, most) == -8 and loss(1 << 10, 1 << 53, 2) == -8
+    for T, L in ((1 << 62, 4), (1 << 40, 1 << 20)):
+        z, rec = _rows(0, T=T, ts=0, ls=0), _rows(5, T=T, ts=0, ls=0)
+        assert _route(_problem(L=L, E=2048), z) == -8 and _route(_problem(L=L, E=2048), z, rec) == -8
+        assert lib.routepack_route_backward(_problem(L=L, E=2048).ref, C.byref(z), C.byref(rec), SOME, 1, 1.0, 0, None,
+                                            None, 0, None, 0, SOME, None) == -8
