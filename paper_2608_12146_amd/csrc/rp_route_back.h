@@ -129,14 +129,8 @@ __global__ void __launch_bounds__(256) k_route_back(BackArgs a, int32_t iters) {
             if (g >= 0) {
                 load_weights<T, G, V, WHOLE>(a, g, l, end - begin, c, f);
             } else {
-                // padding may hold anything, NaN among it: where the gates do not
-                // need the row it is taken as zeros, whose part of the loss is 0
-                const bool needed = gates && SOFTMAX && !a.normalize;
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    f[v] = 0.0f;
-                    z[v] = needed ? z[v] : 0.0f;
-                }
+                for (int v = 0; v < V; ++v) f[v] = 0.0f;
             }
         }
         float m = 0.0f, inv = 0.0f, drop = 0.0f;
@@ -202,6 +196,9 @@ __global__ void __launch_bounds__(256) k_route_back(BackArgs a, int32_t iters) {
             }
             mean = -(dot + drop) * inv;
         }
+        // padding may hold anything, NaN among it: where the gates do not need the
+        // row, nothing of it reaches the gradient
+        const bool part = whole && (known || !loss || (gates && SOFTMAX && !a.normalize));
         T *to = static_cast<T *>(a.dlogits) + (t * a.L + l) * a.E;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -219,7 +216,7 @@ __global__ void __launch_bounds__(256) k_route_back(BackArgs a, int32_t iters) {
                     y[w + 3] = x.w;
                 }
             }
-            if (whole) {
+            if (part) {
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
                     const int v = i * W + w;
