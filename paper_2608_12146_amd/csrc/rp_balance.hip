@@ -48,7 +48,10 @@ __global__ void __launch_bounds__(256) k_share_chunks(ShareArgs a) {
         const int64_t from = a.offsets[g];
         if (from >= t1) break;
         const int64_t b = clamp64(from, t0, t1), e = clamp64(a.offsets[g + 1], t0, t1);
-        if (b >= e) continue;
+        if (__builtin_expect(b >= e, false)) {  // empty: on to the next group that is not (there may be many)
+            g += first_where(a.n_groups - 1 - g, [&](int32_t x) { return a.offsets[g + 2 + (int64_t)x] > e; });
+            continue;
+        }
         float acc[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) acc[v] = 0.0f;

@@ -1016,3 +1016,27 @@ def test_autograd_on_streams_and_in_graphs():
         torch.cuda.synchronize()
         assert torch.equal(out, step()), r
         torch.cuda.synchronize()
+
+
+@gpu
+def test_many_empty_groups_between_tokens():
+    """Millions of empty groups before, between and behind the tokens of one
+    chunk: the shares' kernel steps over them."""
+    import torch
+    import paper_2608_12146_amd as rp
+    G, T, E = 1 << 22, 40, 4
+    prob = _problem(1, 1, E, 1)
+    at = [G // 3, G // 2, G // 2 + 1, G // 2 + 70, G - G // 5]
+    lengths = torch.zeros(G, dtype=torch.int64)
+    lengths[at] = torch.tensor([3, 1, 20, 9, 6])
+    off = torch.cat([torch.zeros(1, dtype=torch.int64), lengths.cumsum(0)]).cuda()
+    counts = torch.zeros((G, 1, E), dtype=torch.int32)
+    counts[at] = torch.arange(5 * E, dtype=torch.int32).view(5, 1, E) % 7
+    z = _logits(1, T, 1, E, "fp32")
+    loss, shares = rp.balance_loss(prob, z, counts.cuda(), off)
+    few = np.array([0, 3, 4, 24, 33, 39])
+    wl, ws = O.balance(_host(z), _host(counts[at]), few, "softmax")
+    rel = (4.6 * _range(_host(z)) + 340) * U
+    _close(shares[at], ws, rel * ws + TINY, "shares")
+    assert int(torch.count_nonzero(shares)) == 5 * E
+    _close(loss * (G / 5), wl, (rel + 2 * U) * wl, "loss")
