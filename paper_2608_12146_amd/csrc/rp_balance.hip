@@ -116,7 +116,7 @@ struct LossArgs {
 template <class F>
 __device__ inline void add_parts(const LossArgs &a, int32_t l, double *red, F &&load) {
     double total = 0.0;
-    for (int32_t y = threadIdx.x; y < a.n_groups; y += blockDim.x) {
+    for (int64_t y = threadIdx.x; y < a.n_groups; y += blockDim.x) {
         double *part = a.parts + ((int64_t)l * a.n_groups + y) * a.n_slabs * 2;
         double dot = 0.0, sum = 0.0;
         for (int32_t z = 0; z < a.n_slabs; ++z) {

@@ -557,9 +557,9 @@ __device__ inline int32_t first_where(int32_t n, F &&yes) {
         const uint64_t mask = __ballot(at < n ? (bool)yes(lo + at) : true);
         const int32_t f = mask ? first_lane(mask) : kWave;
         if (f == 0) break;
-        // behind probe f - 1, up to probe f or the end
+        // behind probe f - 1, up to probe f or the end (64 steps may be 2^31)
         const int32_t past = (f - 1) * step + 1;
-        n = __builtin_elementwise_min(n, f * step) - past;
+        n = (int32_t)__builtin_elementwise_min((uint32_t)n, (uint32_t)f * (uint32_t)step) - past;
         lo += past;
     }
     return lo;

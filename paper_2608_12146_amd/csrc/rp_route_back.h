@@ -30,7 +30,7 @@ __device__ inline int32_t find_group(const int64_t *offsets, int32_t n, int64_t 
     const int base = lane_id() & ~(G - 1);
     int32_t lo = 0, hi = n;
     while (__any(hi - lo > 1)) {
-        const int32_t step = (hi - lo + G) / (G + 1);
+        const int32_t step = (hi - lo - 1) / (G + 1) + 1;  // (of any n up to 2^31 - 1)
         const int64_t p = lo + (int64_t)(c + 1) * step;
         const uint64_t yes = __ballot(p < hi && offsets[p < hi ? p : lo] <= t);
         const int cnt = __popcll(yes >> base & low_lanes(G));

@@ -1040,3 +1040,37 @@ def test_many_empty_groups_between_tokens():
     _close(shares[at], ws, rel * ws + TINY, "shares")
     assert int(torch.count_nonzero(shares)) == 5 * E
     _close(loss * (G / 5), wl, (rel + 2 * U) * wl, "loss")
+
+
+@gpu
+def test_groups_up_to_the_end_of_32_bits():
+    """2^31 - 1 groups of the loss, all but two of them empty: the searches
+    stay within the arrays."""
+    import torch
+    import paper_2608_12146_amd as rp
+    G, T, E = 2 ** 31 - 1, 5, 2
+    prob = _problem(1, 1, E, 1)
+    off = torch.zeros(G + 1, dtype=torch.int64, device="cuda")
+    off[G // 2:] = 2  # (tokens 0 and 1 in a group of the middle, 2 .. 4 in the last one)
+    off[G] = T
+    counts = torch.zeros((G, 1, E), dtype=torch.int32, device="cuda")
+    counts[G // 2 - 1] = torch.tensor([3, 1], dtype=torch.int32)
+    counts[G - 1] = torch.tensor([1, 4], dtype=torch.int32)
+    z = _logits(1, T, 1, E, "fp32")
+    dl = torch.full((1,), float(G), device="cuda")
+    few = np.array([0, 2, T])
+    fc = np.array([[[3, 1]], [[1, 4]]])
+    for score in ("softmax", "sigmoid"):
+        _log(("back", score))
+        got = rp.route_backward(prob, z, counts=counts, offsets=off, dloss=dl, score=score)
+        want, mag = O.backward(_host(z), score, counts=fc, offsets=few, dloss=np.array([2.0]))
+        _close(got, want, (9.2 * _range(_host(z)) + 214) * U * mag + TINY, score)
+    _log("balance")
+    loss, shares = rp.balance_loss(prob, z, counts, off)
+    wl, ws = O.balance(_host(z), fc, few, "softmax")
+    rel = (4.6 * _range(_host(z)) + 340) * U
+    _close(shares[[G // 2 - 1, G - 1]], ws, rel * ws + TINY, "shares")
+    _close(loss * (G / 2), wl, (rel + 2 * U) * wl, "loss")
+    _log("done")
+    del shares, counts, off
+    torch.cuda.empty_cache()
