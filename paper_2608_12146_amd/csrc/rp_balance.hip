@@ -138,7 +138,8 @@ __device__ inline void add_parts(const LossArgs &a, int32_t l, double *red, F &&
 
 __global__ void __launch_bounds__(1024) k_sum_loss(LossArgs a) {
     __shared__ double red[16];
-    add_parts(a, (int32_t)blockIdx.x, red, [](double *p) { return *p; });
+    const int64_t l = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    if (l < a.L) add_parts(a, (int32_t)l, red, [](double *p) { return *p; });
 }
 
 // R rows abreast of 64 experts.  LAST: the last workgroup of a layer adds its
@@ -297,23 +298,25 @@ extern "C" int routepack_balance_loss(const routepack_problem *prob, const route
     const int32_t slabs = (E + kWave - 1) / kWave;
     const LossArgs b = {rows, logits->n_tokens, w.chunk, L, E, n_groups, slabs, counts_type, offsets, counts, loss,
                         shares, parts, arrived};
-    const dim3 grid2 = grid_of((int64_t)n_groups * L * slabs);
     const int64_t each = w.n_chunks / n_groups;  // rows of a group, about
     // A workgroup that counts its arrival waits for its stores to reach memory,
     // and the counts of a layer follow one another: up to 64 parts (1000 groups
     // x 4 slabs of 131072 x 256: 116 us, 31 us with the third kernel; 5 x 4 of
     // 8192 x 256: 15.6 us, 17.9 us).
     const bool last = (int64_t)n_groups * slabs <= 64;
-    auto go = [&](auto kern, int threads) { hipLaunchKernelGGL(kern, grid2, dim3(threads), 0, stream, b); };
+    auto go = [&](auto kern, int threads, int64_t n) {
+        hipLaunchKernelGGL(kern, grid_of(n, threads), dim3(threads), 0, stream, b);
+    };
+    const int64_t parts_n = (int64_t)n_groups * L * slabs;
     if (last) {
-        if (each >= 64) go(k_group_loss<16, true>, 1024);
-        else if (each >= 8) go(k_group_loss<4, true>, 256);
-        else go(k_group_loss<1, true>, 64);
+        if (each >= 64) go(k_group_loss<16, true>, 1024, parts_n);
+        else if (each >= 8) go(k_group_loss<4, true>, 256, parts_n);
+        else go(k_group_loss<1, true>, 64, parts_n);
     } else {
-        if (each >= 64) go(k_group_loss<16, false>, 1024);
-        else if (each >= 8) go(k_group_loss<4, false>, 256);
-        else go(k_group_loss<1, false>, 64);
-        hipLaunchKernelGGL(k_sum_loss, dim3((unsigned)L), dim3(n_groups > 256 ? 1024 : 256), 0, stream, b);
+        if (each >= 64) go(k_group_loss<16, false>, 1024, parts_n);
+        else if (each >= 8) go(k_group_loss<4, false>, 256, parts_n);
+        else go(k_group_loss<1, false>, 64, parts_n);
+        go(k_sum_loss, n_groups > 256 ? 1024 : 256, L);
     }
     return hipGetLastError() == hipSuccess ? ROUTEPACK_OK : ROUTEPACK_E_DEVICE;
 }

@@ -1074,3 +1074,23 @@ def test_groups_up_to_the_end_of_32_bits():
     _log("done")
     del shares, counts, off
     torch.cuda.empty_cache()
+
+
+@gpu
+def test_more_layers_than_one_grid_row_holds():
+    """Layers times threads past 2^32 in the sum over a layer's groups."""
+    import torch
+    import paper_2608_12146_amd as rp
+    G, L = 257, (1 << 22) + 5
+    prob = _problem(1, L, 1, 1)
+    z = torch.zeros((2, L, 1), device="cuda")
+    off = torch.zeros(G + 1, dtype=torch.int64, device="cuda")
+    off[101:] = 1
+    off[G] = 2  # (token 0 in group 100, token 1 in the last one)
+    counts = torch.ones((G, L, 1), dtype=torch.int32, device="cuda")
+    _log("loss")
+    loss, shares = rp.balance_loss(prob, z, counts, off)
+    assert (loss == torch.tensor(2 / G, dtype=torch.float32)).all()  # (2 / G rounded once, from 64 bits)
+    assert (shares[[100, G - 1]] == 1.0).all() and int(torch.count_nonzero(shares)) == 2 * L
+    del shares, counts
+    torch.cuda.empty_cache()
