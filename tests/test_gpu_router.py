@@ -1094,3 +1094,109 @@ def test_more_layers_than_one_grid_row_holds():
     assert (shares[[100, G - 1]] == 1.0).all() and int(torch.count_nonzero(shares)) == 2 * L
     del shares, counts
     torch.cuda.empty_cache()
+
+
+@gpu
+@pytest.mark.parametrize("idtype", ["u8", "i16", "i32", "i64"])
+def test_count_layers_of_short_samples(idtype):
+    """Recordings by layers of a few thousand short and empty samples: several
+    layers a workgroup, a wave or all its threads on one, the last group of
+    layers smaller than the others, ids behind the last whole vector."""
+    import torch
+    import paper_2608_12146_amd as rp
+    rng = np.random.default_rng(4)
+    for N, low, high, L, E, k in ((2500, 0, 90, 7, 16, 1), (2500, 0, 90, 64, 16, 3), (2863, 1, 90, 64, 130, 8),
+                                  (2100, 0, 200, 23, 16, 8), (700, 5, 300, 37, 130, 3), (2200, 0, 9, 64, 16, 3),
+                                  (2050, 1, 30, 5, 40, 250), (2050, 1, 60, 3, 9, 96)):
+        lengths = rng.integers(low, high, size=N)
+        for start, past in ((0, 0), (3, 17)):
+            T = start + int(lengths.sum()) + past
+            ids = _ids(N + L, T, L, E, k, idtype, 0.1)
+            off = _offsets(lengths, start)
+            # (the oracle's count, all samples and layers at once)
+            row = np.searchsorted(_host(off), np.arange(T), side="right") - 1
+            cell = (row[:, None, None] * L + np.arange(L)[:, None]) * E + _host(ids)
+            cell = cell[(row >= 0)[:, None, None] & (row < N)[:, None, None] & (_host(ids) >= 0) & (_host(ids) < E)]
+            want = np.bincount(cell, minlength=N * L * E).reshape(N, L, E)
+            prob = _problem(N, L, E, k)
+            by_layer = ids.transpose(0, 1).contiguous().transpose(0, 1)
+            gap = torch.full((L, T * k + 5), 1, dtype=ids.dtype, device="cuda")  # (layers off a vector's start)
+            apart = gap[:, 1:1 + T * k].view(L, T, k).transpose(0, 1)
+            apart.copy_(ids)
+            for name, view in (("layers", by_layer), ("apart", apart), ("tokens", ids)):
+                _log((idtype, N, T, L, E, k, start, name))
+                assert np.array_equal(_host(rp.count_demand(prob, view, off)), want), (idtype, N, L, E, k, start, name)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_gradient_of_several_tokens_a_group_of_lanes(dtype, score):
+    """Enough tokens that a group of lanes takes several: the row of choices
+    and the weights of the loss go from one token to the next."""
+    import torch
+    import paper_2608_12146_amd as rp
+    # (from 2048 workgroups on two tokens and more each; a layer alone has fewer)
+    for T, L, E, k in ((40000, 4, 60, 6), (9000, 9, 250, 9), (9000, 9, 256, 20), (100000, 2, 16, 2), (3000, 4, 1100, 5)):
+        lengths = [T // 3, 0, 1, T // 2, T - T // 3 - T // 2 - 30]
+        z, dg, counts, dl = _gradient_case(7, T, L, E, k, dtype, 0.2 if k == 9 else 0.0, lengths)
+        off = _offsets(lengths, 11)
+        ids = _ids(8, T, L, E, k, "i16", 0.2, same=k in (6, 20))
+        dg, counts, dl = dg.cuda(), counts.cuda(), dl.cuda()
+        rows = np.arange(5, T, T // 300)
+        far = _range(_host(z[rows]))
+        info = torch.finfo(_type(dtype))
+        for terms in ("both", "gates"):
+            for normalize in (True, False):
+                what = (dtype, score, T, L, E, k, terms, normalize)
+                _log(what)
+                how = dict(normalize=normalize, scale=1.5)
+                loss = dict(counts=counts, offsets=off, dloss=dl) if terms == "both" else {}
+                got = rp.route_backward(_problem(1, L, E, k), z, ids=ids, dgates=dg, score=score, **how, **loss)
+                # every row as a call of its layer alone has it
+                for l in range(L):
+                    if loss:
+                        loss = dict(counts=counts[:, l:l + 1].contiguous(), offsets=off, dloss=dl[l:l + 1])
+                    one = rp.route_backward(_problem(1, 1, E, k), z[:, l:l + 1], ids=ids[:, l:l + 1],
+                                            dgates=dg[:, l:l + 1].contiguous(), score=score, **how, **loss)
+                    assert torch.equal(got[:, l:l + 1], one), (what, l)
+                # and some against the formulas, group by group (n of its m rows)
+                zh = _host(z[rows])
+                want, mag = O.backward(zh, score, _host(ids[rows]), _host(dg[rows]), normalize, 1.5)
+                if terms == "both":
+                    o, G = _host(off), len(lengths)
+                    for g in range(G):
+                        at = (rows >= o[g]) & (rows < o[g + 1])
+                        n, m = int(at.sum()), int(o[g + 1] - o[g])
+                        if n:
+                            w, x = O.backward(zh[at], score, counts=_host(counts[g:g + 1]), offsets=np.array([0, n]),
+                                              dloss=_host(dl) * n / (m * G))
+                            want[at] += w
+                            mag[at] += x
+                tol = (9.2 * far + 214) * U * mag
+                tol = tol + info.eps / 2 * (np.abs(want) + tol) + info.tiny * info.eps / 2 + TINY * (1 + mag.max())
+                _close(got[rows], want, tol, what)
+
+
+@gpu
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_balance_of_many_groups_of_many_chunks(score):
+    """More than 64 parts of a layer's loss, with 8 and with 64 chunks a group
+    and more: the third kernel behind each shape of the second."""
+    import torch
+    import paper_2608_12146_amd as rp
+    for G, each, L, E, dtype in ((65, 300, 1, 8, "fp32"), (70, 530, 2, 100, "bf16"), (3, 2100, 1, 2048, "fp16"),
+                                 (66, 2100, 1, 40, "bf16")):
+        rng = np.random.default_rng(G)
+        lengths = rng.integers(each, each + 60, size=G)
+        lengths[G // 2] = 0
+        T = int(lengths.sum()) + 40
+        z = _logits(G, T, L, E, dtype, 0.2)
+        off = _offsets(lengths, 7)
+        counts = torch.randint(0, 50, (G, L, E), generator=torch.Generator().manual_seed(G)).to(torch.int32)
+        _log((score, G, T, L, E, dtype))
+        loss, shares = rp.balance_loss(_problem(1, L, E, 1), z, counts.cuda(), off, score=score)
+        want, ws = O.balance(_host(z), counts.numpy(), _host(off), score)
+        rel = (4.6 * _range(_host(z)) + 340) * U
+        _close(shares, ws, rel * ws + TINY, (G, E))
+        _close(loss, want, rel * want + TINY * E, (G, E))
