@@ -28,8 +28,12 @@
  * - Calls whose logits have 2^59 elements and more (broadcast ones can) give
  *   E_UNSUPPORTED.
  * - Scores, sums and gradients are formed in 32 bits or more and rounded
- *   once, to the output's type.  Results do not depend on the launch: no
- *   floating-point atomics.
+ *   once, to the output's type.  An exponential e^(z - m) of a chosen expert's
+ *   gate, and of fp32 logits' gradient, is good to 4 steps of 32 bits beside
+ *   the rounding of z - m; one that enters a row's sum in the forward call, a
+ *   share, or the gradient of 16-bit logits is off by up to 1.3 |z - m| + 2
+ *   steps of itself.  Results do not depend on the launch: no floating-point
+ *   atomics.
  */
 #ifndef ROUTEPACK_ROUTER_H
 #define ROUTEPACK_ROUTER_H
@@ -116,7 +120,8 @@ int64_t routepack_balance_workspace(const routepack_problem *prob, int64_t n_tok
  *   f[g][l][e]      = E counts[g][l][e] / sum_e' counts[g][l][e'] (0 where the sum is 0)
  *   shares[g][l][e] = mean over the group's tokens of s_e / sum_e' s_e' with
  *                     the scores s of the token (0 for an empty group, and a
- *                     token with no available expert adds 0)
+ *                     token with no available expert adds 0; a NaN score,
+ *                     or +inf under a softmax, makes its group's NaN)
  *   loss[l]         = 1/G sum_g sum_e f[g][l][e] shares[g][l][e].
  * The counts are constants to the loss (they may be summed over ranks).
  *   offsets    int64 [G + 1], G = n_groups
@@ -145,7 +150,8 @@ int routepack_balance_loss(const routepack_problem *prob, const routepack_logits
  *   dloss      float [L] or NULL
  *   dlogits    [T][L][E] out, of the logits' type, not overlapping them; rows
  *              that are padding get the gates' part alone, and unavailable
- *              experts 0
+ *              experts 0 (NaN where a NaN logit, or +inf under a softmax,
+ *              enters the sum over the row or over the choices)
  * Errors as routepack_route_tokens and routepack_balance_loss. */
 int routepack_route_backward(const routepack_problem *prob, const routepack_logits *logits,
                              const routepack_ids *ids, const float *dgates, int32_t normalize,

@@ -3,9 +3,10 @@
 A thin ctypes layer over the C-ABI in include/routepack.h and, for the
 router's operators, include/routepack/router.h (libroutepack.so).
 It only marshals arguments (and lets autograd record the router's gates and
-loss): torch supplies device memory and the current HIP stream, and every step of the path runs in the library's HIP kernels.  There
-is no CPU fallback: importing works without a GPU, but every call raises if
-the library or a GPU is missing.
+loss): torch supplies device memory and the current HIP stream, and every step
+of the path runs in the library's HIP kernels.  There is no CPU fallback:
+importing works without a GPU, but every call raises if the library or a GPU
+is missing.
 """
 from __future__ import annotations
 

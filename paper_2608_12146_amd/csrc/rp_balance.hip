@@ -12,9 +12,11 @@
 // few, or by a third kernel.  No floating-point atomics: the result does not
 // depend on the launch.
 //
-// 32768 x 16 x 64 fp32: 23 us for the shares (5.8 TB/s) and 7 us for the loss,
-// which waits for four reads in a row (offsets, rows, counts, parts).
-// 131072 x 512 bf16: 25 and 10 us.
+// 32768 x 16 x 64 fp32: 22 us for the shares (6 TB/s, part of it from the
+// last-level cache) and 7 to 8 us for the loss, which waits for four reads in a
+// row (offsets, rows, counts, parts).  131072 x 512 bf16: 24 and 10.5 us;
+// logistic scores 40 us for the shares, about 37 of them the issue of 16 vector
+// instructions an element, two of a quarter of the others' rate.
 #include "rp_internal.h"
 #include "rp_route.h"
 
@@ -286,7 +288,7 @@ extern "C" int routepack_balance_loss(const routepack_problem *prob, const route
                           k_share_chunks<T, g.value, nv.value, true, true>, g.value * nv.value * Vec<T>::W);
             });
         // logistic rows keep 1 - s too: 16 values a lane while the wave holds the
-        // row (131072 x 512 bf16: 63 us, 81 us with 32)
+        // row (131072 x 512 bf16 took 1.3 times as long with 32)
         if (E > 1024)
             return go(k_share_chunks<T, kWave, kMost, false, false>, k_share_chunks<T, kWave, kMost, false, true>,
                       kMaxExperts);

@@ -69,8 +69,8 @@ struct __attribute__((packed, aligned(2))) Words16 {
     uint32_t w[4];
 };
 // 16 bytes at any address; ONCE: that nothing reads again (a hint that keeps
-// them from displacing others in the caches: counting 300007 x 24 x 8 ids takes
-// 55 us without and 50 us with it).
+// them from displacing others in the caches: it took counting 300007 x 24 x 8
+// ids from 55 to 50 us).
 template <bool ONCE>
 __device__ inline void load16(const void *p, uint32_t (&w)[4]) {
     typedef uint32_t four __attribute__((ext_vector_type(4), aligned(1)));
@@ -548,7 +548,11 @@ __device__ inline Item item_of(int64_t T, int32_t L) {
 }
 
 // The first of n places where `yes` holds, which holds for all after it (n if
-// for none): the lanes of a wave probe 64 places a round.
+// for none): the lanes of a wave probe 64 places a round.  In 32 bits and with
+// a minimum, not with uniform 64-bit selects behind the ballot: a build of such
+// a search counted some of 1000 samples of 9 tokens as empty, and its assembly
+// had a select on the condition of the compare before its own.  (Builds of the
+// same source about it did not show that; the tests count 63 to 5000 samples.)
 template <class F>
 __device__ inline int32_t first_where(int32_t n, F &&yes) {
     int32_t lo = 0;

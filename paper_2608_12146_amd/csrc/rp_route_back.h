@@ -12,9 +12,10 @@
 // element with every choice would cost in instructions.
 //
 // 131072 x 512 bf16, both parts: 58 us, 4.7 TB/s read and written, where a
-// large copy reaches 4.9 to 5.4; what is left is the exponentials (a quarter of
-// the rate of other instructions) under 4 waves a SIMD.  Logistic rows, two
-// quarter-rate instructions an element and twice the registers, take 86 us.
+// large copy reaches 4.9 to 5.4; its 16 vector instructions an element, one of
+// them an exponential, would take 32 us alone.  Logistic rows take 86 us, about
+// 73 of them the issue of 37 vector instructions an element, two of a quarter of
+// the others' rate.
 #pragma once
 
 #include "rp_route.h"
@@ -242,7 +243,8 @@ int launch_back(const BackArgs &a, hipStream_t stream) {
     const int64_t slots = 256 / G, n = (a.T + slots - 1) / slots;
     // Several tokens a group of lanes, which loads the weights of a group of the
     // loss once for them, where that leaves 1024 workgroups (131072 x 512 bf16
-    // at 8 tokens: 59 us, 61 at 4, 95 at 1; 1797 x 23 x 432 at 2: 33.5 us, 40 at 1).
+    // takes 1.03 times as long at 4 tokens as at 8, and 1.6 times at 1; 1797 x 23
+    // x 432 1.2 times at 1 as at 2).
     int64_t iters = n * a.L / 1024;
     iters = iters < 1 ? 1 : (iters > 8 ? 8 : iters);
     auto go = [&](auto kern) {
@@ -251,8 +253,8 @@ int launch_back(const BackArgs &a, hipStream_t stream) {
     };
     // Up to 8 choices, and rows that fill the lanes exactly (E a power of two,
     // mostly), take kernels without the further slots and the checks of every
-    // vector: at 131072 x 512 bf16 63 us and 71 us with the checks; 9 choices of
-    // 110325 x 5 x 28 fp32 101 us with 16 slots and 130 us with 32.
+    // vector (131072 x 512 bf16 takes 1.13 times as long with the checks, 9 choices
+    // of 110325 x 5 x 28 fp32 1.3 times with 32 slots as with 16).
     const bool few = !a.ids || a.k <= 8, fills = a.E == G * NV * (16 / (int)sizeof(T));
     if (few && fills) return go(k_route_back<T, G, NV, 8, SOFTMAX, true>);
     if (few) return go(k_route_back<T, G, NV, 8, SOFTMAX, false>);
