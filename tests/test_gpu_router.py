@@ -1200,3 +1200,51 @@ def test_balance_of_many_groups_of_many_chunks(score):
         rel = (4.6 * _range(_host(z)) + 340) * U
         _close(shares, ws, rel * ws + TINY, (G, E))
         _close(loss, want, rel * want + TINY * E, (G, E))
+
+
+@gpu
+def test_more_rows_than_32_bits_count():
+    """2^32 and more rows of logits (one token's, broadcast): every row of
+    every result is the first token's."""
+    import torch
+    import paper_2608_12146_amd as rp
+    T, L, E, k = (1 << 22) + 3, 1024, 4, 1
+    prob = _problem(1, L, E, k)
+    z = _logits(1, 1, L, E, "bf16").expand(T, L, E)
+    bias = torch.zeros((L, E), device="cuda")
+
+    def same(x, what):
+        for a in range(0, T, 1 << 19):
+            assert bool((x[a:a + (1 << 19)] == x[:1]).all()), (what, a)
+    ids = rp.route_tokens(prob, z, bias=bias, normalize=False)[0]
+    _log("biased")
+    same(ids, "biased")
+    ids, gates = rp.route_tokens(prob, z, normalize=False)
+    _log("chosen")
+    same(ids, "ids")
+    same(gates, "gates")
+    want = O.choose(_host(z[:1]), k)
+    assert np.array_equal(_host(ids[:1]), want)
+    _check_gates(gates[:1], _host(z[:1]), want, "softmax", False, 1.0, "gates")
+    again = rp.route_tokens(prob, z, ids=ids, normalize=False)[1]
+    _log("replayed")
+    assert torch.equal(again, gates)
+    off = _offsets([T])
+    counts = rp.count_demand(prob, ids, off)
+    _log("counted")
+    assert (counts.sum(dim=2) == T).all() and (counts.amax(dim=2) == T).all()
+    loss, _ = rp.balance_loss(prob, z, counts, off)
+    wl, _ = O.balance(_host(z[:1]), _host(counts), np.array([0, 1]), "softmax")
+    # (1024 tokens a chunk, 64 rows of 4 lanes: 16 additions and 64 rows)
+    _close(loss, wl, (4.6 * _range(_host(z[:1])) + 340) * U * wl, "loss")
+    dl = torch.full((L,), float(T), device="cuda")
+    del again
+    dz = rp.route_backward(prob, z, ids=ids, dgates=gates, normalize=False, counts=counts, offsets=off, dloss=dl)
+    _log("back")
+    same(dz, "dz")
+    w, mag = O.backward(_host(z[:1]), "softmax", want, _host(gates[:1]), False, 1.0, _host(counts), np.array([0, 1]),
+                        np.ones(L))
+    tol = (9.2 * _range(_host(z[:1])) + 214) * U * mag
+    _close(dz[:1], w, tol + 2.0 ** -8 * (np.abs(w) + tol) + TINY, "dz")
+    del ids, gates, dz
+    torch.cuda.empty_cache()
