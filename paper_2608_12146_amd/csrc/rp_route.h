@@ -551,8 +551,8 @@ __device__ inline Item item_of(int64_t T, int32_t L) {
 // for none): the lanes of a wave probe 64 places a round.  In 32 bits and with
 // a minimum, not with uniform 64-bit selects behind the ballot: a build of such
 // a search counted some of 1000 samples of 9 tokens as empty, and its assembly
-// had a select on the condition of the compare before its own.  (Builds of the
-// same source about it did not show that; the tests count 63 to 5000 samples.)
+// had a select on the condition of the compare before its own.  (No build of
+// the other forms that were looked at does; the tests count 63 to 5000 samples.)
 template <class F>
 __device__ inline int32_t first_where(int32_t n, F &&yes) {
     int32_t lo = 0;
