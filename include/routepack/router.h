@@ -100,6 +100,24 @@ int routepack_route_tokens(const routepack_problem *prob, const routepack_logits
                            int32_t normalize, float scale, int32_t *ids, float *gates,
                            hipStream_t stream);
 
+/* routepack_route_tokens, choosing among a few groups of experts: n_groups
+ * groups of E / n_groups adjacent experts, of which each token keeps the `keep`
+ * of largest sum of their group_top largest keys (of the available ones; a
+ * group without any is not kept; ties go to the lowest group).  The keys are
+ * score + bias, or the scores without a bias, compared in 64 bits; with
+ * group_top = 1 and no bias they are compared as logits.  The gates are
+ * routepack_route_tokens': an unnormalised softmax is over all experts.
+ *   bias     float [L][E] or NULL, as there
+ *   ids      int32 [T][L][k] out
+ *   gates    float [T][L][k] out
+ * Errors as there, and E_INVALID when n_groups < 1 does not divide E, keep is
+ * outside [1, n_groups], group_top is neither 1 nor 2, or k exceeds the experts
+ * of `keep` groups; E_UNSUPPORTED when E > 1024 or n_groups > 64. */
+int routepack_route_grouped(const routepack_problem *prob, const routepack_logits *logits, const float *bias,
+                            int32_t n_groups, int32_t keep, int32_t group_top, int32_t score,
+                            int32_t normalize, float scale, int32_t *ids, float *gates,
+                            hipStream_t stream);
+
 /* The demand of routepack.h from recorded ids:
  *   demand[i][l][e] = #{(t, j): t in sample i, ids[t][l][j] = e}.
  *   offsets  int64 [N + 1]

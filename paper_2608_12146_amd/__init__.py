@@ -1,9 +1,9 @@
 """MI355X (gfx950) RoutePack planner hot path -- Python binding.
 
 A thin ctypes layer over the C-ABI in include/routepack.h and, for the
-router's operators, include/routepack/router.h (libroutepack.so).
-It only marshals arguments (and lets autograd record the router's gates and
-loss): torch supplies device memory and the current HIP stream, and every step
+router's and the experts' operators, include/routepack/router.h and experts.h
+(libroutepack.so).  It only marshals arguments (and lets autograd record the
+router's gates and loss, the experts' products and their sums): torch supplies device memory and the current HIP stream, and every step
 of the path runs in the library's HIP kernels.  There is no CPU fallback:
 importing works without a GPU, but every call raises if the library or a GPU
 is missing.
@@ -29,8 +29,12 @@ EXPORTS = ("routepack_aggregate_demand", "routepack_place_experts", "routepack_p
            "routepack_row_lower_bound", "routepack_fixed_bin_search", "routepack_project_demand",
            "routepack_strerror")
 # the router's operators, declared in include/routepack/router.h
-ROUTER_EXPORTS = ("routepack_route_tokens", "routepack_count_demand", "routepack_balance_workspace",
+ROUTER_EXPORTS = ("routepack_route_tokens", "routepack_route_grouped", "routepack_count_demand", "routepack_balance_workspace",
                   "routepack_balance_loss", "routepack_route_backward")
+# the experts' operators, declared in include/routepack/experts.h
+EXPERT_EXPORTS = ("routepack_order_workspace", "routepack_order_tokens", "routepack_quantize_mx",
+                  "routepack_dequantize_mx", "routepack_expert_product", "routepack_expert_product_backward",
+                  "routepack_combine_tokens", "routepack_combine_backward")
 # measurement aid declared in include/routepack_probe.h (not part of the method),
 # built as its own library
 PROBE_EXPORTS = ("routepack_probe_lds_read",)
@@ -66,6 +70,17 @@ class _Rows(C.Structure):
                 ("layer_stride", C.c_int64)]
 
 
+class _Matrix(C.Structure):
+    """routepack_matrix."""
+    _fields_ = [("data", C.c_void_p), ("type", C.c_int32), ("n_rows", C.c_int64), ("n_cols", C.c_int64),
+                ("row_stride", C.c_int64)]
+
+
+class _MxMatrix(C.Structure):
+    """routepack_mx."""
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("n_rows", C.c_int64), ("n_cols", C.c_int64)]
+
+
 _lib = None
 
 
@@ -95,14 +110,25 @@ def load_library():
         lib.routepack_balance_workspace.argtypes = [P, i64, i32]
         lib.routepack_balance_loss.argtypes = [P, R, i32, vp, vp, i32, i32, vp, vp, vp, i64, vp]
         lib.routepack_route_backward.argtypes = [P, R, R, vp, i32, f32, i32, vp, vp, i32, vp, i32, vp, vp]
+        lib.routepack_route_grouped.argtypes = [P, R, vp, i32, i32, i32, i32, i32, f32, vp, vp, vp]
+        M, X = C.POINTER(_Matrix), C.POINTER(_MxMatrix)
+        lib.routepack_order_workspace.argtypes = [P, i64]
+        lib.routepack_order_tokens.argtypes = [P, R, vp, vp, vp, vp, vp, i64, vp]
+        lib.routepack_quantize_mx.argtypes = [M, vp, i32, X, vp]
+        lib.routepack_dequantize_mx.argtypes = [X, M, vp]
+        lib.routepack_expert_product.argtypes = [X, X, i32, vp, M, vp]
+        lib.routepack_expert_product_backward.argtypes = [M, X, X, i32, vp, M, M, vp]
+        lib.routepack_combine_tokens.argtypes = [M, R, i32, vp, i64, M, vp]
+        lib.routepack_combine_backward.argtypes = [M, M, vp, R, i32, vp, i64, M, vp, vp]
         lib.routepack_strerror.argtypes = [C.c_int]
         lib.routepack_strerror.restype = C.c_char_p
         for f in EXPORTS:
             if f != "routepack_strerror":
                 getattr(lib, f).restype = C.c_int
-        for f in ROUTER_EXPORTS:
+        for f in ROUTER_EXPORTS + EXPERT_EXPORTS:
             getattr(lib, f).restype = C.c_int
         lib.routepack_balance_workspace.restype = C.c_int64
+        lib.routepack_order_workspace.restype = C.c_int64
         _lib = lib
     return _lib
 
@@ -468,8 +494,9 @@ def _functions():
 
     class Gates(torch.autograd.Function):
         @staticmethod
-        def forward(ctx, logits, prob, ids, bias, score, normalize, scale):
-            out, gates = route_tokens(prob, logits, ids=ids, bias=bias, score=score, normalize=normalize, scale=scale)
+        def forward(ctx, logits, prob, ids, bias, score, normalize, scale, groups, keep, group_top):
+            out, gates = route_tokens(prob, logits, ids=ids, bias=bias, score=score, normalize=normalize, scale=scale,
+                                      groups=groups, keep=keep, group_top=group_top)
             ctx.save_for_backward(logits, out)
             ctx.set_materialize_grads(False)
             ctx.args = prob, dict(score=score, normalize=normalize, scale=scale)
@@ -485,7 +512,7 @@ def _functions():
             if grads[-1] is not None:
                 (logits, ids), (prob, how) = ctx.saved_tensors, ctx.args
                 dz = route_backward(prob, logits, ids=ids, dgates=grads[-1].contiguous(), **how)
-            return dz, None, None, None, None, None, None
+            return (dz,) + (None,) * 9
 
     class Loss(torch.autograd.Function):
         @staticmethod
@@ -511,7 +538,8 @@ def _functions():
     return _FUNCTIONS
 
 
-def route_tokens(prob: Problem, logits, *, ids=None, bias=None, score="softmax", normalize=True, scale=1.0):
+def route_tokens(prob: Problem, logits, *, ids=None, bias=None, score="softmax", normalize=True, scale=1.0, groups=None,
+                 keep=None, group_top=1):
     """The router's gates: (ids, gates), each [T][L][k] (or [T][k] for logits
     [T][E]), k = prob.top_k.
 
@@ -522,6 +550,11 @@ def route_tokens(prob: Problem, logits, *, ids=None, bias=None, score="softmax",
     (uint8, int16, int32 or int64; a replayed record) the gates are those of
     the recorded experts, and `ids` is returned as it is.  score: "softmax"
     or "sigmoid"; normalize: divide by the sum over the token's choices.
+
+    With `groups` (not with `ids`) the choice is among the experts of the
+    `keep` best of that many groups of adjacent experts, by the sum of each
+    group's `group_top` (1 or 2) largest keys, which are the scores with the
+    bias added.
 
     Where the logits require a gradient, autograd records the gates: their
     backward pass is route_backward's with the ids as constants (none reaches
@@ -534,8 +567,12 @@ def route_tokens(prob: Problem, logits, *, ids=None, bias=None, score="softmax",
     call = _Call("routepack_route_tokens", torch)
     shape, z = call.rows("logits", logits, floats, prob.n_layers, prob.n_experts)
     if logits.requires_grad and torch.is_grad_enabled():
-        out = _functions()[0].apply(logits, prob, ids, bias, score, normalize, scale)
+        out = _functions()[0].apply(logits, prob, ids, bias, score, normalize, scale, groups, keep, group_top)
         return out if ids is None else (ids, out)
+    if (groups is None) != (keep is None):
+        raise ValueError(f"{call.fn}: groups and keep go together")
+    if groups is not None and ids is not None:
+        raise ValueError(f"{call.fn}: recorded ids are not chosen among groups")
     shape = (*shape[:-1], prob.top_k)
     b = bias
     if bias is not None:
@@ -549,6 +586,11 @@ def route_tokens(prob: Problem, logits, *, ids=None, bias=None, score="softmax",
     else:
         out = torch.empty(shape, dtype=torch.int32, device=call.device)
     gates = torch.empty(shape, dtype=torch.float32, device=call.device)
+    if groups is not None:
+        call.fn = "routepack_route_grouped"
+        call.run(lib.routepack_route_grouped, prob.ref, C.byref(z), b, groups, keep, group_top, _score(call.fn, score),
+                 1 if normalize else 0, scale, out.data_ptr(), gates.data_ptr())
+        return out, gates
     call.run(lib.routepack_route_tokens, prob.ref, C.byref(z), rec, b, _score(call.fn, score), 1 if normalize else 0,
              scale, out.data_ptr() if ids is None else None, gates.data_ptr())
     return out, gates
@@ -639,3 +681,343 @@ def route_backward(prob: Problem, logits, *, ids=None, dgates=None, normalize=Tr
     call.run(lib.routepack_route_backward, prob.ref, C.byref(z), rec, dg, 1 if normalize else 0, scale, G, off, n,
              n_type, dl, _score(call.fn, score), dz.data_ptr())
     return dz
+
+
+# -- the experts' operators (include/routepack/experts.h) ----------------------
+
+class Order:
+    """The order of (token, choice) pairs by slot, of order_tokens: pair t k + j
+    is token t's choice j.
+
+    rows    int32 [P], P = T k: the pair in each row, -1 behind the last one made
+    offsets int64 [E + 1]: slot s has the rows [offsets[s], offsets[s + 1])
+    places  int32 [T][k]: the row of each pair, -1 where no choice was made
+
+    For L layers rows is [L][P], offsets [L][E + 1] and places [T][L][k]; `layer`
+    gives one layer's, which is what the other operators take."""
+
+    __slots__ = ("rows", "offsets", "places")
+
+    def __init__(self, rows, offsets, places):
+        self.rows, self.offsets, self.places = rows, offsets, places
+
+    def layer(self, l):
+        return Order(self.rows[l], self.offsets[l], self.places[:, l])
+
+
+class Mx:
+    """A matrix [...][rows][columns] in microscaled 4-bit floating point (OCP
+    MXFP4): blocks of 32 columns with a common power of two.
+
+    codes  uint8 [...][rows][64 n], n = ceil(columns / 128): two values a byte, the
+           even column in the low half; sign, two bits of exponent, one of mantissa
+    scales uint8 [...][rows][4 n]: the blocks' exponents plus 127, 255 for NaN
+
+    Columns behind the last are zero codes with scale 0."""
+
+    __slots__ = ("codes", "scales", "columns")
+
+    def __init__(self, codes, scales, columns):
+        self.codes, self.scales, self.columns = codes, scales, int(columns)
+
+    @property
+    def shape(self):
+        return (*self.codes.shape[:-1], self.columns)
+
+
+class _ExpertCall(_Call):
+    __slots__ = ()
+
+    def mx(self, name, q, dims):
+        """An Mx of `dims` axes, or of that many and more: (its shape, the
+        description of its rows)."""
+        torch = self.torch
+        if not isinstance(q, Mx):
+            raise TypeError(f"{self.fn}: {name} must be an Mx, got {type(q).__name__}")
+        codes = self.tensor(f"{name}.codes", q.codes, (torch.uint8,))
+        scales = self.tensor(f"{name}.scales", q.scales, (torch.uint8,))
+        n, shape = (q.columns + 127) // 128, codes.shape
+        if len(shape) != dims or q.columns < 0 or shape[-1] != 64 * n or scales.shape != (*shape[:-1], 4 * n):
+            raise ValueError(f"{self.fn}: {name} has codes {tuple(shape)} and scales {tuple(scales.shape)} for "
+                             f"{q.columns} columns, expected {dims} axes, the last {64 * n} and {4 * n}")
+        if not codes.is_contiguous() or not scales.is_contiguous():
+            raise ValueError(f"{self.fn}: {name} must be contiguous")
+        rows = shape[0] if dims == 2 else shape[0] * shape[1]
+        return shape, _MxMatrix(codes.data_ptr(), scales.data_ptr(), rows, q.columns)
+
+    def matrix(self, name, x, types):
+        """[rows][columns] with adjacent columns."""
+        self.tensor(name, x, types)
+        shape, stride = x.shape, x.stride()
+        if len(shape) != 2:
+            raise ValueError(f"{self.fn}: {name} has shape {tuple(shape)}, expected [rows][columns]")
+        if shape[1] > 1 and stride[1] != 1 and shape[0] > 0:
+            raise ValueError(f"{self.fn}: the columns of {name} must be adjacent in memory")
+        return shape, _Matrix(x.data_ptr(), types[x.dtype], shape[0], shape[1], stride[0])
+
+    def out(self, rows, cols, dtype, types, lead=None):
+        x = self.torch.empty((rows, cols) if lead is None else (lead, rows, cols), dtype=dtype, device=self.device)
+        return x, _Matrix(x.data_ptr(), types[dtype], rows * (lead or 1) if lead != 0 else 0, cols, cols)
+
+    def offsets(self, order, n_slots):
+        off = order.offsets if isinstance(order, Order) else order
+        return self.dense("offsets", off, (self.torch.int64,), (n_slots + 1,)).data_ptr()
+
+    def places(self, order):
+        if not isinstance(order, Order):
+            raise TypeError(f"{self.fn}: order must be an Order, got {type(order).__name__}")
+        p = self.tensor("order.places", order.places, (self.torch.int32,))
+        if p.dim() != 2 or p.shape[1] < 1 or (p.shape[1] > 1 and p.stride(1) != 1 and p.shape[0] > 0):
+            raise ValueError(f"{self.fn}: order.places has shape {tuple(p.shape)}, expected [T][k], choices adjacent")
+        return p.shape, _Rows(p.data_ptr(), 5, p.shape[0], p.stride(0), 0)
+
+    def gates(self, gates, shape):
+        if gates is None:
+            return None, 0
+        g = self.tensor("gates", gates, (self.torch.float32,), shape)
+        if g.shape[1] > 1 and g.stride(1) != 1 and g.shape[0] > 0:
+            raise ValueError(f"{self.fn}: a token's gates must be adjacent in memory")
+        return g.data_ptr(), g.stride(0)
+
+
+def order_tokens(prob: Problem, ids, *, slots=None):
+    """The Order of the pairs of tokens and chosen experts: by slot, and by pair
+    within a slot.
+
+    ids [T][L][k] (or [T][k] where L is 1) uint8, int16, int32 or int64, any
+    strides over tokens and layers; ids outside [0, E) are no choices.  slots:
+    int32 [L][E], place_experts' slot of each expert; without it the experts
+    are the slots.  For ids [T][k] the order is one layer's; for [T][L][k] it
+    has a layer axis (`Order.layer`)."""
+    lib, torch, _, ints = _router()
+    call = _Call("routepack_order_tokens", torch)
+    shape, x = call.rows("ids", ids, ints, prob.n_layers, prob.top_k)
+    L, E, at = prob.n_layers, prob.n_experts, call.device
+    s = None if slots is None else call.dense("slots", slots, (torch.int32,), (L, E)).data_ptr()
+    lead = () if len(shape) == 2 else (L,)
+    rows = torch.empty((*lead, shape[0] * prob.top_k), dtype=torch.int32, device=at)
+    offsets = torch.empty((*lead, E + 1), dtype=torch.int64, device=at)
+    places = torch.empty(shape, dtype=torch.int32, device=at)
+    size = lib.routepack_order_workspace(prob.ref, shape[0])
+    work = torch.empty(max(size, 16), dtype=torch.uint8, device=at)
+    call.run(lib.routepack_order_tokens, prob.ref, C.byref(x), s, rows.data_ptr(), offsets.data_ptr(),
+             places.data_ptr(), work.data_ptr(), size)
+    return Order(rows, offsets, places)
+
+
+def quantize_mx(x, *, order=None):
+    """x [rows][columns] (or [n][rows][columns], contiguous) fp32, bf16 or fp16,
+    any stride over rows, as an Mx.  With `order` the result's rows are the
+    order's pairs: row r holds the token of pair rows[r] (zeros behind the
+    last)."""
+    lib, torch, floats, _ = _router()
+    call = _ExpertCall("routepack_quantize_mx", torch)
+    call.tensor("x", x, floats)
+    lead = x.shape[:-1]
+    if x.dim() == 3 and order is None and x.is_contiguous():
+        x = x.view(-1, x.shape[-1]) if x.numel() else x.reshape(lead[0] * lead[1], x.shape[-1])
+    shape, m = call.matrix("x", x, floats)
+    rows, per = None, 1
+    if order is not None:
+        places, _ = call.places(order)
+        if places[0] != shape[0]:
+            raise ValueError(f"{call.fn}: the order has {places[0]} tokens, x {shape[0]} rows")
+        lead = (places[0] * places[1],)
+        rows, per = call.dense("order.rows", order.rows, (torch.int32,), lead).data_ptr(), places[1]
+    n = (shape[1] + 127) // 128
+    codes = torch.empty((*lead, 64 * n), dtype=torch.uint8, device=call.device)
+    scales = torch.empty((*lead, 4 * n), dtype=torch.uint8, device=call.device)
+    q = _MxMatrix(codes.data_ptr(), scales.data_ptr(), shape[0] if order is None else lead[0], shape[1])
+    call.run(lib.routepack_quantize_mx, C.byref(m), rows, per, C.byref(q))
+    return Mx(codes, scales, shape[1])
+
+
+def dequantize_mx(q: Mx, dtype=None):
+    """The values of an Mx as a tensor of its shape (bf16 unless `dtype` is
+    given; exact in fp32 and bf16)."""
+    lib, torch, floats, _ = _router()
+    call = _ExpertCall("routepack_dequantize_mx", torch)
+    dtype = torch.bfloat16 if dtype is None else dtype
+    if dtype not in floats:
+        raise ValueError(f"{call.fn}: dtype is {dtype}")
+    shape, m = call.mx("q", q, 3 if isinstance(q, Mx) and q.codes.dim() == 3 else 2)
+    x = torch.empty(q.shape, dtype=dtype, device=call.device)
+    out = _Matrix(x.data_ptr(), floats[dtype], m.n_rows, q.columns, q.columns)
+    call.run(lib.routepack_dequantize_mx, C.byref(m), C.byref(out))
+    return x
+
+
+def expert_product(x, w, order, *, dtype=None):
+    """y [P][N]: each slot's rows of x times its matrix,
+    y[r] = w[s] x[r] for r in [offsets[s], offsets[s + 1]), 0 in rows of no slot.
+
+    x: Mx [P][C]; w: Mx [E][N][C]; order: an Order, or its offsets (int64
+    [E + 1]).  Either may be a tensor (fp32, bf16, fp16) instead, which the call
+    quantizes.  y has type `dtype`, by default x's type if that is a tensor, else
+    bf16.  Where such tensors require a gradient, autograd records the product;
+    the gradient passes the quantization as if it were the identity, and is
+    expert_product_backward's."""
+    lib, torch, floats, _ = _router()
+    call = _ExpertCall("routepack_expert_product", torch)
+    tensors = [t for t in (x, w) if isinstance(t, torch.Tensor)]
+    if dtype is None:
+        dtype = x.dtype if isinstance(x, torch.Tensor) else torch.bfloat16
+    if dtype not in floats:
+        raise ValueError(f"{call.fn}: dtype is {dtype}")
+    if any(t.requires_grad for t in tensors) and torch.is_grad_enabled():
+        return _expert_functions()[0].apply(x, w, order, dtype)
+    if isinstance(x, torch.Tensor):
+        x = quantize_mx(x)
+    if isinstance(w, torch.Tensor):
+        w = quantize_mx(w)
+    got, xm = call.mx("x", x, 2)
+    shape, wm = call.mx("w", w, 3)
+    if x.columns != w.columns:
+        raise ValueError(f"{call.fn}: x has {x.columns} columns, w {w.columns}")
+    off = call.offsets(order, shape[0])
+    y, ym = call.out(got[0], shape[1], dtype, floats)
+    call.run(lib.routepack_expert_product, C.byref(xm), C.byref(wm), shape[0], off, C.byref(ym))
+    return y
+
+
+def expert_product_backward(dy, x, w, order, *, need=(True, True)):
+    """(dx [P][C], dw [E][N][C]), both of dy's type, of expert_product's y given
+    its gradient dy [P][N] (fp32, bf16 or fp16, any stride over rows); None for
+    what `need` leaves out.  x and w are the Mx of the product (x may be None
+    where dw is not needed, and w where dx is not, but for its shape: then give
+    (E, N, columns))."""
+    lib, torch, floats, _ = _router()
+    call = _ExpertCall("routepack_expert_product_backward", torch)
+    got, dm = call.matrix("dy", dy, floats)
+    if not any(need):
+        raise ValueError(f"{call.fn}: neither gradient is needed")
+    if isinstance(w, Mx):
+        shape, wm = call.mx("w", w, 3)
+        E, N, cols = shape[0], shape[1], w.columns
+    elif need[0]:
+        raise TypeError(f"{call.fn}: w must be an Mx, got {type(w).__name__}")
+    else:
+        E, N, cols = w
+        wm = _MxMatrix(None, None, E * N, cols)
+    if isinstance(x, Mx):
+        xs, xm = call.mx("x", x, 2)
+        if xs[0] != got[0] or x.columns != cols:
+            raise ValueError(f"{call.fn}: x has {xs[0]} rows of {x.columns}, dy {got[0]} rows, w {cols} columns")
+    elif need[1]:
+        raise TypeError(f"{call.fn}: x must be an Mx, got {type(x).__name__}")
+    else:
+        xm = _MxMatrix(None, None, got[0], cols)
+    if got[1] != N:
+        raise ValueError(f"{call.fn}: dy has {got[1]} columns, w {N} rows a slot")
+    off = call.offsets(order, E)
+    dx = dw = dxm = dwm = None
+    if need[0]:
+        dx, dxm = call.out(got[0], cols, dy.dtype, floats)
+        dxm = C.byref(dxm)
+    if need[1]:
+        dw, dwm = call.out(N, cols, dy.dtype, floats, lead=E)
+        dwm = C.byref(dwm)
+    call.run(lib.routepack_expert_product_backward, C.byref(dm), C.byref(xm), C.byref(wm), E, off, dxm, dwm)
+    return dx, dw
+
+
+def combine_tokens(y, order, gates=None):
+    """out [T][C] = sum over a token's choices of gate times row: y [P][C] fp32,
+    bf16 or fp16, any stride over rows; gates float32 [T][k], any stride over
+    tokens (ones if None); order: one layer's Order.  Sums run in 32 bits in the
+    order of the choices; out has y's type.  Where y or the gates require a
+    gradient, autograd records the sum; its backward pass is combine_backward's."""
+    lib, torch, floats, _ = _router()
+    call = _ExpertCall("routepack_combine_tokens", torch)
+    got, ym = call.matrix("y", y, floats)
+    shape, p = call.places(order)
+    g, stride = call.gates(gates, shape)
+    if (y.requires_grad or (gates is not None and gates.requires_grad)) and torch.is_grad_enabled():
+        return _expert_functions()[1].apply(y, gates, order)
+    out, om = call.out(shape[0], got[1], y.dtype, floats)
+    call.run(lib.routepack_combine_tokens, C.byref(ym), C.byref(p), shape[1], g, stride, C.byref(om))
+    return out
+
+
+def combine_backward(dout, y, order, gates=None, *, need=(True, True)):
+    """(dy [P][C] of y's type, dgates float32 [T][k]) of combine_tokens' sum given
+    its gradient dout [T][C] of y's type; None for what `need` leaves out."""
+    lib, torch, floats, _ = _router()
+    call = _ExpertCall("routepack_combine_backward", torch)
+    got, ym = call.matrix("y", y, floats)
+    dshape, dm = call.matrix("dout", dout, {y.dtype: floats[y.dtype]})
+    shape, p = call.places(order)
+    g, stride = call.gates(gates, shape)
+    if tuple(dshape) != (shape[0], got[1]):
+        raise ValueError(f"{call.fn}: dout has shape {tuple(dshape)}, expected {(shape[0], got[1])}")
+    if not any(need):
+        raise ValueError(f"{call.fn}: neither gradient is needed")
+    dy = dgates = dym = rows = None
+    if need[0]:
+        rows = call.dense("order.rows", order.rows, (torch.int32,), (got[0],)).data_ptr()
+        dy, dym = call.out(got[0], got[1], y.dtype, floats)
+        dym = C.byref(dym)
+    if need[1]:
+        dgates = torch.empty(tuple(shape), dtype=torch.float32, device=call.device)
+        if dy is None and shape[0] == 0:  # (no token: nothing to write, and no address to pass)
+            return None, dgates
+    call.run(lib.routepack_combine_backward, C.byref(dm), C.byref(ym), rows, C.byref(p), shape[1], g, stride, dym,
+             None if dgates is None else dgates.data_ptr())
+    return dy, dgates
+
+
+_EXPERT_FUNCTIONS = None
+
+
+def _expert_functions():
+    """(product, sum) as functions that autograd records."""
+    global _EXPERT_FUNCTIONS
+    if _EXPERT_FUNCTIONS is not None:
+        return _EXPERT_FUNCTIONS
+    torch = _router()[1]
+    once_differentiable = torch.autograd.function.once_differentiable
+
+    class Product(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, w, order, dtype):
+            qx = quantize_mx(x) if isinstance(x, torch.Tensor) else x
+            qw = quantize_mx(w) if isinstance(w, torch.Tensor) else w
+            off = order.offsets if isinstance(order, Order) else order
+            # (the packed matrices are kept, a quarter of the tensors in bf16)
+            need = ctx.needs_input_grad
+            none = qx.codes.new_empty(0)
+            ctx.save_for_backward(qx.codes if need[1] else none, qx.scales if need[1] else none,
+                                  qw.codes if need[0] else none, qw.scales if need[0] else none, off)
+            ctx.sizes = (*qw.shape[:2], qw.columns), [t.dtype if isinstance(t, torch.Tensor) else None for t in (x, w)]
+            return expert_product(qx, qw, off, dtype=dtype)
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, dy):
+            xc, xs, wc, ws, off = ctx.saved_tensors
+            sizes, types = ctx.sizes
+            need = tuple(ctx.needs_input_grad[:2])
+            if dy.dim() == 2 and dy.stride(1) != 1:
+                dy = dy.contiguous()
+            dx, dw = expert_product_backward(dy, Mx(xc, xs, sizes[2]) if need[1] else None,
+                                             Mx(wc, ws, sizes[2]) if need[0] else sizes, off, need=need)
+            return None if dx is None else dx.to(types[0]), None if dw is None else dw.to(types[1]), None, None
+
+    class Sum(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, y, gates, order):
+            ctx.save_for_backward(y, gates, order.rows, order.places)
+            return combine_tokens(y, order, gates)
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, dout):
+            y, gates, rows, places = ctx.saved_tensors
+            if dout.stride(1) != 1:
+                dout = dout.contiguous()
+            dy, dgates = combine_backward(dout, y, Order(rows, None, places), gates,
+                                          need=tuple(ctx.needs_input_grad[:2]))
+            return dy, dgates, None
+
+    _EXPERT_FUNCTIONS = Product, Sum
+    return _EXPERT_FUNCTIONS

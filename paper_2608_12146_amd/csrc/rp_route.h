@@ -380,6 +380,13 @@ __device__ inline float value32(uint32_t o) {
     return __uint_as_float(o >> 31 ? o ^ 0x80000000u : ~o);
 }
 
+// A double's order as an unsigned number (-0 equals +0); 0 stands for "not
+// available".
+__device__ inline uint64_t order64(double x) {
+    const uint64_t u = (uint64_t)__double_as_longlong(x + 0.0);
+    return u >> 63 ? ~u : u | (uint64_t)1 << 63;
+}
+
 // 16-bit logits: their 32-bit form has at most 19 significant leading bits
 // (bf16 16, fp16 1 + 8 + 10), so 21 bits of order and 11 of index are one
 // 32-bit word.

@@ -4,6 +4,7 @@
 
 #include "rp_internal.h"
 #include "rp_route.h"
+#include "rp_route_groups.h"
 
 namespace rp {
 
@@ -12,6 +13,10 @@ namespace rp {
 int choose_f32(const RouteArgs &a, hipStream_t stream);
 int choose_bf16(const RouteArgs &a, hipStream_t stream);
 int choose_f16(const RouteArgs &a, hipStream_t stream);
+
+int choose_groups_f32(const GroupArgs &a, hipStream_t stream);
+int choose_groups_bf16(const GroupArgs &a, hipStream_t stream);
+int choose_groups_f16(const GroupArgs &a, hipStream_t stream);
 
 // Gates of recorded experts that need no more of a row than the experts'
 // logits: a group of G >= k lanes a token, a choice a lane.
@@ -105,6 +110,32 @@ extern "C" int routepack_route_tokens(const routepack_problem *prob, const route
         if (a.k <= 16) return go(k_replay_chosen<T, 16>, 16);
         return go(k_replay_chosen<T, 32>, 32);
     });
+}
+
+extern "C" int routepack_route_grouped(const routepack_problem *prob, const routepack_logits *logits, const float *bias,
+                                       int32_t n_groups, int32_t keep, int32_t group_top, int32_t score,
+                                       int32_t normalize, float scale, int32_t *ids, float *gates, hipStream_t stream) {
+    RP_TRY(check_logits(prob, logits, score));
+    const int32_t E = prob->n_experts, k = prob->top_k;
+    if (k < 1 || k > E || !isfinite(scale)) return ROUTEPACK_E_INVALID;
+    if (n_groups < 1 || E % n_groups != 0 || keep < 1 || keep > n_groups || group_top < 1 || group_top > 2)
+        return ROUTEPACK_E_INVALID;
+    if (k > keep * (E / n_groups)) return ROUTEPACK_E_INVALID;
+    if (k > kMaxChoices || E > 1024 || n_groups > 64) return ROUTEPACK_E_UNSUPPORTED;
+    if (logits->n_tokens * prob->n_layers == 0) return ROUTEPACK_OK;
+    if (!gates || !ids) return ROUTEPACK_E_INVALID;
+    GroupArgs a = {};
+    a.r = {logits->data, logits->token_stride, logits->layer_stride, logits->n_tokens, prob->n_layers, E, k, nullptr, 0,
+           0, 0, bias, score, normalize != 0, scale, ids, gates};
+    a.groups = n_groups;
+    a.keep = keep;
+    a.top = group_top;
+    a.size = E / n_groups;
+    switch (logits->type) {
+        case ROUTEPACK_F32: return choose_groups_f32(a, stream);
+        case ROUTEPACK_BF16: return choose_groups_bf16(a, stream);
+        default: return choose_groups_f16(a, stream);
+    }
 }
 
 extern "C" int routepack_route_backward(const routepack_problem *prob, const routepack_logits *logits,

@@ -126,13 +126,6 @@ __global__ void __launch_bounds__(256) k_route(RouteArgs a) {
     }
 }
 
-// A double's order as an unsigned number (-0 equals +0); 0 stands for "not
-// available".
-__device__ inline uint64_t order64(double x) {
-    const uint64_t u = (uint64_t)__double_as_longlong(x + 0.0);
-    return u >> 63 ? ~u : u | (uint64_t)1 << 63;
-}
-
 // One round of a maximum over (key, -index) across the G lanes.
 template <int G, int D = 2>
 __device__ inline void group_first(uint64_t &key, uint32_t &at) {

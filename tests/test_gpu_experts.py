@@ -1,0 +1,512 @@
+"""The experts' operators (include/routepack/experts.h) and the router's grouped
+choice (router.h) against the oracle in 64 bits: masks, ties, missing choices,
+slots without rows, odd sizes, strides, every type, gradients, and the whole
+sequence as a trainer runs it.
+
+Tolerances, u = 2^-24 (half a step of rounding in 32 bits):
+- Gates: as derived for the router's operators, (3.3 D + 80) u of themselves
+  with D the range of the logits; a grouped choice sums over more lanes, 6
+  exchanges and at most 32 values a lane, fewer than counted there.
+- The matrix instructions form products of 4-bit values and powers of two, and of
+  bf16 values, exactly and add them in 32 bits, each addition off by at most a
+  whole step (2 u) of the magnitudes' sum where the hardware truncates.  A sum of
+  n terms: at most 2 n u of the sum of magnitudes; n = C, N or the slot's rows,
+  times the parts of dy (bf16 1, fp16 2, fp32 3), plus 8 for joining four waves'
+  sums and the padded columns' zeros.
+- combine: k products and additions, 2 k u of the magnitudes; a gate's gradient:
+  C of them and 9 exchanges.
+Rounding to the output's type adds half a step, finfo.eps / 2 of the value, or
+half of the smallest subnormal number.
+"""
+import numpy as np
+import pytest
+
+from oracle import experts as X
+from oracle import router as O
+
+gpu = pytest.mark.gpu
+U = 2.0 ** -24
+TINY = 2.0 ** -125
+
+
+def _log(msg):
+    print(f"[experts] {msg}", flush=True)
+
+
+def _problem(L, E, k):
+    import paper_2608_12146_amd as rp
+    return rp.Problem(1, L, E, k, 1, 1, 1, [0], 1 << 20, [1], [0])
+
+
+def _type(name):
+    import torch
+    return {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16, "u8": torch.uint8,
+            "i16": torch.int16, "i32": torch.int32, "i64": torch.int64}[name]
+
+
+def _host(x):
+    import torch
+    x = x.detach().cpu()
+    return x.double().numpy() if x.is_floating_point() else x.to(torch.int64).numpy()
+
+
+def _floats(seed, shape, dtype, gap=0, scale=1.0):
+    """Normal values; `gap` elements between one row and the next."""
+    import torch
+    g = torch.Generator().manual_seed(seed)
+    x = (torch.randn((*shape[:-1], shape[-1] + gap), generator=g) * scale).to(_type(dtype)).cuda()
+    return x[..., :shape[-1]]
+
+
+def _near(got, want, tol, what):
+    """Within tol, which counts 32-bit errors, and the output type's rounding."""
+    import torch
+    info = torch.finfo(got.dtype)
+    got = _host(got)
+    assert got.shape == want.shape, what
+    tol = tol + np.abs(want) * (info.eps / 2) * (1 + 2.0 ** -10) + info.tiny * info.eps / 2 + TINY
+    nan = np.isnan(want)
+    assert np.array_equal(np.isnan(got), nan), what
+    bad = ~(np.abs(got - want) <= tol) & ~nan
+    assert not bad.any(), (what, int(bad.sum()), got[bad][:4], want[bad][:4], np.broadcast_to(tol, want.shape)[bad][:4])
+
+
+# -- the choice among groups ---------------------------------------------------
+
+GROUPS = [  # T, L, E, k, groups, keep
+    (1, 1, 1, 1, 1, 1), (1, 1, 256, 8, 8, 4), (5, 2, 6, 2, 3, 1), (33, 1, 16, 3, 2, 1), (17, 3, 60, 6, 4, 2),
+    (70, 1, 256, 8, 8, 4), (37, 1, 250, 9, 5, 3), (64, 2, 64, 8, 64, 20), (9, 1, 1024, 32, 2, 1), (19, 1, 512, 8, 16, 3),
+    (11, 1, 1023, 17, 33, 5), (13, 1, 1020, 10, 17, 17), (40, 1, 40, 32, 8, 7), (21, 1, 12, 12, 1, 1), (6, 1, 300, 4, 12, 2),
+]
+
+
+def _logits(seed, T, L, E, dtype, mask, gap=0):
+    import torch
+    z = _floats(seed, (T, L, E), dtype, gap, 2.0)
+    if mask:
+        g = torch.Generator().manual_seed(seed + 1)
+        z[(torch.rand((T, L, E), generator=g) < mask).cuda()] = -np.inf
+        row = torch.rand((T, L), generator=g).cuda()
+        z[row < 0.1] = -np.inf
+        z[row > 0.9] = torch.finfo(z.dtype).min
+    return z
+
+
+def _gates_near(gates, z, ids, score, normalize, scale, what):
+    want = O.gates(z, ids, score, normalize, scale)
+    with np.errstate(invalid="ignore"):
+        d = z.max(axis=-1, keepdims=True) - z
+    d = np.concatenate([d[np.isfinite(d)].ravel(), np.abs(z[np.isfinite(z)]).ravel(), [0.0]])
+    _near(gates, want, (3.3 * d[d <= 104.0].max() + 80) * U * np.abs(want) + abs(scale) * TINY, what)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_choice_among_groups(dtype, score):
+    import torch
+    import paper_2608_12146_amd as rp
+    for n, (T, L, E, k, groups, keep) in enumerate(GROUPS):
+        for top, biased, mask in ((1, False, 0.0), (1, False, 0.5), (2, False, 0.0), (2, True, 0.3), (1, True, 0.0)):
+            z = _logits(100 * n, T, L, E, dtype, mask, gap=n % 3)
+            bias = None
+            if biased:
+                bias = torch.randn((L, E), generator=torch.Generator().manual_seed(n)) * 0.3
+                if mask:
+                    bias[:, ::5] = -np.inf
+                    bias[:, 1::7] = np.nan
+            what = (dtype, score, T, L, E, k, groups, keep, top, biased, mask)
+            _log(what)
+            for normalize, scale in ((True, 2.5), (False, 1.0)):
+                ids, gates = rp.route_tokens(_problem(L, E, k), z, bias=None if bias is None else bias.cuda(),
+                                             score=score, normalize=normalize, scale=scale, groups=groups, keep=keep,
+                                             group_top=top)
+                want = X.choose_groups(_host(z), k, groups, keep, top, None if bias is None else _host(bias), score)
+                assert np.array_equal(_host(ids), want), what
+                _gates_near(gates, _host(z), want, score, normalize, scale, what)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_groups_of_equal_keys(dtype):
+    """Ties go to the lowest group and expert; one group of all experts is the
+    choice without groups; NaN takes no part."""
+    import torch
+    import paper_2608_12146_amd as rp
+    for E, k, groups, keep in ((12, 3, 4, 2), (256, 8, 8, 3), (510, 20, 17, 4)):
+        z = torch.zeros((6, 1, E), dtype=_type(dtype))
+        z[1, :, ::2] = -0.0
+        z[2] = torch.randint(-1, 2, (1, E), generator=torch.Generator().manual_seed(E)).to(z.dtype)
+        z[3] = torch.finfo(z.dtype).min
+        z[4] = -np.inf
+        z[4, :, E // 2:] = torch.finfo(z.dtype).min
+        z[5, :, 1::3] = np.nan
+        z[5, :, 2] = np.inf
+        for top in (1, 2):
+            for bias in (None, torch.full((1, E), 0.25)):
+                for score in ("softmax", "sigmoid"):
+                    ids, _ = rp.route_tokens(_problem(1, E, k), z.cuda(), bias=None if bias is None else bias.cuda(),
+                                             score=score, groups=groups, keep=keep, group_top=top)
+                    want = X.choose_groups(_host(z), k, groups, keep, top, None if bias is None else _host(bias), score)
+                    assert np.array_equal(_host(ids), want), (dtype, E, top, bias is None, score)
+        one, _ = rp.route_tokens(_problem(1, E, k), z.cuda(), groups=1, keep=1)
+        plain, _ = rp.route_tokens(_problem(1, E, k), z.cuda())
+        assert torch.equal(one, plain)
+
+
+@gpu
+def test_scores_close_to_each_other_in_groups():
+    """Keys that 32 bits do not tell apart."""
+    import torch
+    import paper_2608_12146_amd as rp
+    T, E, k, groups, keep = 64, 64, 6, 8, 3
+    z = _floats(5, (T, 1, E), "fp32", scale=1.0)
+    for score in ("softmax", "sigmoid"):
+        zh = _host(z)[0]
+        s = np.exp(zh - zh.max(-1, keepdims=True))
+        s = s / s.sum(-1, keepdims=True) if score == "softmax" else 1 / (1 + np.exp(-zh))
+        bias = torch.as_tensor(0.5 - s).float()
+        one = z[:1].expand(T, 1, E).contiguous()
+        for x in (z, one):
+            ids, _ = rp.route_tokens(_problem(1, E, k), x, bias=bias.cuda(), score=score, groups=groups, keep=keep,
+                                     group_top=2)
+            want = X.choose_groups(_host(x), k, groups, keep, 2, _host(bias), score)
+            assert np.array_equal(_host(ids), want), score
+
+
+@gpu
+def test_grouped_gates_have_gradients():
+    import torch
+    import paper_2608_12146_amd as rp
+    z = _floats(3, (40, 1, 64), "fp32").requires_grad_()
+    prob = _problem(1, 64, 4)
+    ids, gates = rp.route_tokens(prob, z, groups=8, keep=2, group_top=2, score="sigmoid", scale=1.5)
+    dg = _floats(4, (40, 1, 4), "fp32")
+    (dz,) = torch.autograd.grad(gates, z, dg)
+    want = rp.route_backward(prob, z.detach(), ids=ids, dgates=dg, score="sigmoid", scale=1.5)
+    assert torch.equal(dz, want)
+
+
+# -- the order -----------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("itype", ["u8", "i16", "i32", "i64"])
+def test_order(itype):
+    import torch
+    import paper_2608_12146_amd as rp
+    for n, (T, L, E, k) in enumerate([(0, 1, 5, 2), (1, 1, 1, 1), (1, 1, 256, 8), (3, 2, 7, 3), (61, 1, 256, 8), (65, 3, 16, 2),
+                                      (700, 2, 60, 6), (512, 1, 2048, 8), (513, 1, 100, 8), (2500, 2, 33, 7)]):
+        if itype == "u8" and E > 255:
+            E = 200
+        for missing, placed, same in ((0.0, False, False), (0.2, True, False), (0.0, False, True), (1.0, False, False)):
+            g = torch.Generator().manual_seed(n)
+            ids = torch.randint(0, E, (T, L, k), generator=g)
+            if same:
+                ids[:] = E - 1
+            gone = torch.rand((T, L, k), generator=g) < missing
+            ids[gone] = 255 if itype == "u8" else -1
+            wide = torch.zeros((T, L, k + 3), dtype=_type(itype))
+            wide[:, :, :k] = ids
+            x = wide.cuda()[:, :, :k] if n % 2 else wide[:, :, :k].contiguous().cuda()
+            if n % 3 == 2 and T:  # layers outermost
+                x = x.transpose(0, 1).contiguous().transpose(0, 1)
+            slots = None
+            if placed:
+                slots = torch.stack([torch.randperm(E, generator=g) for _ in range(L)]).to(torch.int32)
+                if E > 3:
+                    slots[:, 2] = -1  # an expert that is nowhere
+            what = (itype, T, L, E, k, missing, placed, same)
+            _log(what)
+            got = rp.order_tokens(_problem(L, E, k), x, slots=None if slots is None else slots.cuda())
+            rows, off, places = X.order(ids.numpy(), E, None if slots is None else slots.numpy())
+            assert np.array_equal(_host(got.offsets), off), what
+            assert np.array_equal(_host(got.rows), rows) and np.array_equal(_host(got.places), places), what
+            one = got.layer(L - 1)
+            assert torch.equal(one.rows, got.rows[L - 1]) and torch.equal(one.places, got.places[:, L - 1])
+
+
+@gpu
+@pytest.mark.parametrize("T,E,k,L", [(40000, 256, 8, 1), (131072, 64, 6, 2), (300000, 2048, 10, 1)])
+def test_order_of_many_chunks(T, E, k, L):
+    import torch
+    import paper_2608_12146_amd as rp
+    g = torch.Generator(device="cuda").manual_seed(T)
+    ids = (torch.rand((T, L, k), device="cuda", generator=g) ** 3 * (E + 1)).long()  # (E: no choice)
+    got = rp.order_tokens(_problem(L, E, k), ids)
+    for l in range(L):
+        key = ids[:, l].reshape(-1)
+        by, rows = torch.sort(key, stable=True)
+        made = int((key < E).sum())
+        assert torch.equal(got.rows[l, :made].long(), rows[:made]) and bool((got.rows[l, made:] == -1).all())
+        assert torch.equal(got.offsets[l], torch.searchsorted(by, torch.arange(E + 1, device="cuda")))
+        place = torch.full((T * k,), -1, dtype=torch.int64, device="cuda")
+        place[rows[:made]] = torch.arange(made, device="cuda")
+        assert torch.equal(got.places[:, l].reshape(-1).long(), place)
+
+
+# -- matrices in 4 bits --------------------------------------------------------
+
+def _blocks(seed, rows, cols, dtype):
+    """Values of every exponent, ties, zeros, and blocks with NaN or infinities."""
+    import torch
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn((rows, cols), generator=g)
+    if rows > 4:
+        lo, hi = {"fp32": (-149, 126), "bf16": (-133, 126), "fp16": (-24, 14)}[dtype]
+        e = torch.randint(lo, hi, (rows, 1), generator=g).double()
+        x = (x.double().clamp(-1.9, 1.9) * 2.0 ** e)
+        x[1] = torch.tensor(X.STEPS)[torch.randint(0, 8, (cols,), generator=g)] * 1.25
+        x[2] = torch.randint(-32, 33, (cols,), generator=g) / 4.0
+        x[3] = 0.0
+        x[4, ::2] = -0.0
+    x = x.to(_type(dtype))
+    if rows > 7:
+        x[5, cols // 2], x[6, cols - 1], x[7, 0] = np.nan, np.inf, -np.inf
+    return x
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_blocks_of_four_bits(dtype):
+    import torch
+    import paper_2608_12146_amd as rp
+    for n, (rows, cols, gap) in enumerate([(1, 1, 0), (9, 31, 1), (33, 128, 0), (300, 100, 3), (17, 1000, 0), (70, 129, 8), (8, 2048, 2)]):
+        x = _blocks(n, rows, cols, dtype)
+        wide = torch.zeros((rows, cols + gap), dtype=x.dtype)
+        wide[:, :cols] = x
+        what = (dtype, rows, cols, gap)
+        _log(what)
+        q = rp.quantize_mx(wide.cuda()[:, :cols])
+        codes, scales = X.quantize(_host(x))
+        assert q.shape == (rows, cols)
+        assert np.array_equal(_host(q.scales), scales), what
+        assert np.array_equal(_host(q.codes), codes), what
+        for back in ("fp32", "bf16", "fp16"):
+            v = rp.dequantize_mx(q, _type(back))
+            with np.errstate(over="ignore"):
+                want = torch.as_tensor(X.values(codes, scales, cols)).to(_type(back))
+            got = v.cpu()
+            assert torch.equal(torch.isnan(got), torch.isnan(want)), what
+            assert torch.equal(torch.nan_to_num(got, nan=0.0), torch.nan_to_num(want, nan=0.0)), (what, back)
+
+
+@gpu
+def test_every_code_and_scale_back():
+    import torch
+    import paper_2608_12146_amd as rp
+    codes = torch.arange(16, dtype=torch.uint8).repeat(256, 8)[:, ::2] * 17  # (both halves of a byte alike)
+    scales = torch.arange(256, dtype=torch.uint8)[:, None].repeat(1, 4)
+    q = rp.Mx(codes.contiguous().cuda(), scales.contiguous().cuda(), 128)
+    want = X.values(codes.numpy(), scales.numpy(), 128)
+    for dtype in ("fp32", "bf16"):
+        got = _host(rp.dequantize_mx(q, _type(dtype)))
+        assert np.array_equal(np.isnan(got), np.isnan(want))
+        assert np.array_equal(got[:255], torch.as_tensor(want[:255]).to(_type(dtype)).double().numpy()), dtype
+
+
+@gpu
+def test_rows_gathered_as_they_are_quantized():
+    import torch
+    import paper_2608_12146_amd as rp
+    T, E, k, cols = 50, 7, 3, 200
+    ids = torch.randint(-1, E, (T, k), generator=torch.Generator().manual_seed(1)).cuda()
+    order = rp.order_tokens(_problem(1, E, k), ids)
+    x = _floats(2, (T, cols), "bf16", gap=5)
+    q = rp.quantize_mx(x, order=order)
+    rows = _host(order.rows)
+    want = np.where((rows >= 0)[:, None], _host(x)[np.maximum(rows, 0) // k], 0.0)
+    codes, scales = X.quantize(want)
+    assert np.array_equal(_host(q.codes), codes) and np.array_equal(_host(q.scales), scales)
+    # rows outside the tokens are rows of zeros
+    order.rows[3], order.rows[4] = T * k, 2 ** 31 - 1
+    q = rp.quantize_mx(x, order=order)
+    assert not q.codes[3:5].any() and not q.scales[3:5].any()
+    # weights: three axes
+    w = _floats(3, (4, 9, cols), "fp32")
+    q = rp.quantize_mx(w)
+    codes, scales = X.quantize(_host(w).reshape(36, cols))
+    assert q.shape == (4, 9, cols) and np.array_equal(_host(q.codes).reshape(36, -1), codes)
+    assert np.array_equal(_host(rp.dequantize_mx(q, torch.float32)), X.values(codes, scales, cols).reshape(4, 9, cols))
+
+
+# -- the experts' products -----------------------------------------------------
+
+def _random_mx(seed, shape, cols, spread=6):
+    import torch
+    import paper_2608_12146_amd as rp
+    g = torch.Generator().manual_seed(seed)
+    n = (cols + 127) // 128
+    codes = torch.randint(0, 256, (*shape, 64 * n), generator=g).to(torch.uint8)
+    scales = (torch.randint(0, spread, (*shape, 4 * n), generator=g) + 127 - spread // 2).to(torch.uint8)
+    # columns behind the last: zero codes, scale 0
+    half = codes.view(*shape, 64 * n)
+    half[..., (cols + 1) // 2:] = 0
+    if cols % 2:
+        half[..., cols // 2] &= 15
+    scales[..., (cols + 31) // 32:] = 0
+    return rp.Mx(codes.cuda(), scales.cuda(), cols)
+
+
+def _values(q):
+    return X.values(_host(q.codes).astype(np.uint8), _host(q.scales).astype(np.uint8), q.columns)
+
+
+def _offsets(counts, start=0):
+    import torch
+    return torch.as_tensor(np.concatenate([[start], start + np.cumsum(counts)]).astype(np.int64)).cuda()
+
+
+PRODUCTS = [  # rows of each slot, rows before, rows behind, N, C
+    ([1], 0, 0, 1, 1), ([0], 0, 3, 5, 40), ([3, 0, 17, 1], 0, 0, 20, 128), ([16, 33, 0, 0, 5], 2, 9, 33, 160),
+    ([0, 0, 1, 0], 0, 0, 64, 2048), ([40, 100, 7], 0, 1, 130, 385), ([300], 0, 0, 257, 96), ([129, 128, 127, 0, 1], 0, 0, 128, 256),
+    ([64] * 9, 1, 0, 96, 640), ([5, 500, 2], 0, 60, 200, 1000), ([1] * 70, 0, 0, 48, 300), ([700, 0, 350], 3, 2, 384, 512),
+    ([260, 250], 0, 0, 520, 2176),
+]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+def test_products(dtype):
+    import paper_2608_12146_amd as rp
+    for n, (counts, before, behind, N, C) in enumerate(PRODUCTS):
+        what = (dtype, counts[:5], len(counts), before, behind, N, C)
+        _log(what)
+        R = before + sum(counts) + behind
+        x, w, off = _random_mx(n, (R,), C), _random_mx(n + 50, (len(counts), N), C), _offsets(counts, before)
+        y = rp.expert_product(x, w, off, dtype=_type(dtype))
+        want, mag = X.product(_values(x), _values(w), _host(off))
+        _near(y, want, 2 * (C + 136) * U * mag, what)
+
+
+@gpu
+def test_products_of_extreme_scales():
+    """Powers of two far apart, a block of NaN, and a slot's last row next to
+    another slot's NaN."""
+    import torch
+    import paper_2608_12146_amd as rp
+    for rows in ([5, 4], [150, 140]):
+        x, w = _random_mx(1, (sum(rows),), 200, 60), _random_mx(2, (2, 40), 200, 60)
+        x.scales[rows[0], 3] = 255
+        w.scales[0, 7, 0] = 255
+        off = _offsets(rows)
+        y = rp.expert_product(x, w, off, dtype=torch.float32)
+        want, mag = X.product(_values(x), _values(w), _host(off))
+        # (a padded block's NaN scale is no part of the product: none is set)
+        _near(y, want, 2 * (200 + 136) * U * np.nan_to_num(mag, nan=0.0), rows)
+
+
+@gpu
+def test_offsets_that_are_wrong_stay_within_the_arrays():
+    """Undefined values, but nothing outside the arrays: slots that overlap,
+    decrease, or leave the rows."""
+    import torch
+    import paper_2608_12146_amd as rp
+    for off in ([-5, 3, 900], [20, 10, 4], [0, 64, 64], [64, 64, 64], [2 ** 62, -2 ** 62, 1]):
+        o = torch.tensor(off, device="cuda")
+        x, w = _random_mx(1, (64,), 100), _random_mx(2, (2, 30), 100)
+        y = rp.expert_product(x, w, o)
+        assert y.shape == (64, 30)
+        dx, dw = rp.expert_product_backward(y, x, w, o)
+        assert dx.shape == (64, 100) and dw.shape == (2, 30, 100)
+    torch.cuda.synchronize()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+def test_product_gradients(dtype):
+    import paper_2608_12146_amd as rp
+    parts = {"bf16": 1, "fp16": 2, "fp32": 3}[dtype]
+    for n, (counts, before, behind, N, C) in enumerate(PRODUCTS):
+        what = (dtype, counts[:5], len(counts), before, behind, N, C)
+        _log(what)
+        R = before + sum(counts) + behind
+        x, w, off = _random_mx(n, (R,), C), _random_mx(n + 50, (len(counts), N), C), _offsets(counts, before)
+        dy = _floats(n + 70, (R, N), dtype, gap=n % 4, scale=0.3)
+        dx, dw = rp.expert_product_backward(dy, x, w, off)
+        (wx, mx), (ww, mw) = X.product_backward(_host(dy), _values(x), _values(w), _host(off))
+        _near(dx, wx, 2 * (parts * N + 136) * U * mx, what)
+        _near(dw, ww, 2 * (parts * max(counts) + 136) * U * mw, what)
+        one, none = rp.expert_product_backward(dy, None, w, off, need=(True, False))
+        assert none is None and bool((one == dx).all())
+        none, one = rp.expert_product_backward(dy, x, (len(counts), N, C), off, need=(False, True))
+        assert none is None and bool((one == dw).all())
+
+
+@gpu
+def test_product_gradients_of_infinities():
+    import torch
+    import paper_2608_12146_amd as rp
+    for dtype in ("bf16", "fp16", "fp32"):
+        dy = _floats(1, (40, 50), dtype)
+        dy[3, 4], dy[7, 9], dy[8, 0] = np.inf, np.nan, torch.finfo(dy.dtype).max
+        x, w, off = _random_mx(1, (40,), 70), _random_mx(2, (2, 50), 70), _offsets([20, 20])
+        dx, dw = rp.expert_product_backward(dy, x, w, off)
+        with np.errstate(invalid="ignore", over="ignore"):
+            (wx, _), (ww, _) = X.product_backward(_host(dy), _values(x), _values(w), _host(off))
+            wx = torch.as_tensor(wx).to(dy.dtype).double().numpy()
+        dx, dw = _host(dx), _host(dw)
+        assert np.array_equal(np.isnan(dx[3]), np.isnan(wx[3])) and np.array_equal(dx[3][np.isinf(wx[3])], wx[3][np.isinf(wx[3])])
+        assert np.isnan(dx[7]).all() and not np.isnan(dx[[0, 1, 2, 4, 5, 6] + list(range(9, 40))]).any()
+        assert np.isnan(dw[0, 9]).all() and not np.isnan(dw[1]).any() and not np.isnan(dw[0, [1, 2, 3, 5]]).any()
+
+
+# -- the sum under the gates ---------------------------------------------------
+
+COMBINES = [(0, 3, 4, 40), (1, 1, 1, 1), (1, 8, 256, 2048), (33, 2, 5, 7), (50, 3, 7, 100), (17, 6, 60, 1447), (20, 9, 16, 513),
+            (7, 32, 40, 264), (300, 4, 8, 64), (9, 5, 8, 4096)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_sum_and_gradients(dtype):
+    import torch
+    import paper_2608_12146_amd as rp
+    for n, (T, k, E, C) in enumerate(COMBINES):
+        for missing, ones in ((0.0, False), (0.3, False), (0.1, True), (1.0, False)):
+            what = (dtype, T, k, E, C, missing, ones)
+            _log(what)
+            g = torch.Generator().manual_seed(n)
+            ids = torch.randint(0, E, (T, 2, k), generator=g)
+            ids[torch.rand((T, 2, k), generator=g) < missing] = -1
+            order = rp.order_tokens(_problem(2, E, k), ids.cuda()).layer(1)
+            y = _floats(n, (T * k, C), dtype, gap=n % 3)
+            gates = None if ones else _floats(n + 1, (T, k), "fp32", gap=n % 2)
+            if T * k > 4 and missing:
+                y[int(order.offsets[-1]):] = np.nan  # rows of no pair are not read
+            places, rows = _host(order.places), _host(order.rows)
+            gh = np.ones((T, k)) if ones else _host(gates)
+            yh = _host(y)
+            out = rp.combine_tokens(y, order, gates)
+            want, mag = X.combine(yh, places, gh)
+            _near(out, want, 2 * k * U * mag, what)
+            dout = _floats(n + 2, (T, C), dtype, gap=n % 2)
+            dy, dgates = rp.combine_backward(dout, y, order, gates)
+            wy, (wg, mg) = X.combine_backward(_host(dout), yh, rows, places, gh)
+            _near(dy, wy, 2 * U * np.abs(wy), what)
+            _near(dgates, wg, 2 * (C + 9) * U * mg, what)
+            only, none = rp.combine_backward(dout, y, order, gates, need=(True, False))
+            assert none is None and torch.equal(only, dy)
+            none, only = rp.combine_backward(dout, y, order, gates, need=(False, True))
+            assert none is None and torch.equal(only, dgates)
+
+
+@gpu
+def test_orders_that_are_wrong_stay_within_the_arrays():
+    """Places and rows outside their range are no rows and no pairs; a row that
+    two pairs name belongs to the one that it names."""
+    import torch
+    import paper_2608_12146_amd as rp
+    T, k, C = 12, 2, 40
+    places = torch.randint(-3, 40, (T, k), generator=torch.Generator().manual_seed(1)).to(torch.int32)
+    places[0] = 5
+    rows = torch.randint(-5, 60, (24,), generator=torch.Generator().manual_seed(2)).to(torch.int32)
+    rows[5] = 1
+    order = rp.Order(rows.cuda(), None, places.cuda())
+    y, gates, dout = _floats(1, (24, C), "fp32"), _floats(2, (T, k), "fp32"), _floats(3, (T, C), "fp32")
+    out = rp.combine_tokens(y, order, gates)
+    want, mag = X.combine(_host(y), places.numpy(), _host(gates))
+    _near(out, want, 2 * k * U * mag, "out")
+    dy, dgates = rp.combine_backward(dout, y, order, gates)
+    wy, (wg, mg) = X.combine_backward(_host(dout), _host(y), rows.numpy(), places.numpy(), _host(gates))
+    _near(dy, wy, 2 * U * np.abs(wy), "dy")
+    _near(dgates, wg, 2 * (C + 9) * U * mg, "dgates")
