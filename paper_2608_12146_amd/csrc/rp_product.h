@@ -11,6 +11,12 @@ typedef int int8_ __attribute__((ext_vector_type(8)));
 typedef float float4_ __attribute__((ext_vector_type(4)));
 typedef float float16_ __attribute__((ext_vector_type(16)));
 
+// A value that all lanes of a wave have.
+__device__ inline int64_t uniform64(int64_t v) {
+    return (int64_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 |
+           (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v);
+}
+
 struct Segment {
     int64_t begin, end;
 };
@@ -45,20 +51,20 @@ __device__ inline int32_t slot_of_tile(const int64_t *offsets, int32_t n_slots, 
         const int64_t v = __shfl_up((long long)upto, d, kWave);
         upto += lane >= d ? v : 0;
     }
-    total = __shfl((long long)upto, kWave - 1, kWave);
+    total = uniform64(__shfl((long long)upto, kWave - 1, kWave));
     if (index >= total) return -1;
     const uint64_t past = __ballot(upto > index);
     const int owner = __builtin_ctzll(past);
-    int64_t at = __shfl((long long)(upto - mine), owner, kWave);
+    int64_t at = uniform64(__shfl((long long)(upto - mine), owner, kWave));
     // the owner's run, by all lanes alike
-    int32_t s = owner * per;
+    int32_t s = __builtin_amdgcn_readfirstlane(owner) * per;
     for (;; ++s) {
         const int64_t n = tiles(s);
         if (index < at + n || s + 1 >= n_slots) break;
         at += n;
     }
     before = index - at;
-    return __builtin_amdgcn_readfirstlane(s);
+    return s;
 }
 
 // Zeros in the rows of no slot: piece `index` of `pieces` of them.
