@@ -115,6 +115,28 @@ __device__ inline void wait_and_meet() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(N) : "memory");
 }
 
+// A wave's LDS accesses before are done before those after.
+__device__ inline void wave_meet() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// 16 bytes of values from column c on, as many as the row has.
+template <class T>
+__device__ inline void store_cols(T *row, int32_t cols, int32_t c, int4_ v) {
+    constexpr int W = 16 / (int)sizeof(T);
+    typedef int four __attribute__((ext_vector_type(4), aligned(2)));
+    if (c + W <= cols) {
+        *reinterpret_cast<four *>(row + c) = v;
+    } else {
+        typedef T values __attribute__((ext_vector_type(W)));
+        const values x = __builtin_bit_cast(values, v);
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+            if (c + i < cols) row[c + i] = x[i];
+    }
+}
+
 template <class T, int WM, int WN, int MT, int NT, int S>
 __global__ void __launch_bounds__(256, 2) k_product_many(ProductArgs a) {
     using G = Shape<WM, WN, MT, NT, S>;
@@ -242,19 +264,35 @@ __global__ void __launch_bounds__(256, 2) k_product_many(ProductArgs a) {
         }
         if (step % kUnit == kUnit - 1 && step + 1 < steps) store_scales(unit + 1);
     }
-    // a value's row is lane % 32 of x, its column 8 (i / 4) + 4 (lane / 32) + i % 4 of w
+    // A value's row is lane % 32 of x, its column 8 (i / 4) + 4 (lane / 32) + i % 4
+    // of w: 32 rows at a time go through this wave's part of LDS, to leave as
+    // whole lines.
+    wait_and_meet<0>();
+    constexpr int kCols = NT * 32, kPitch = kCols * (int)sizeof(T) + 16, kVec = 16 / (int)sizeof(T);
+    constexpr int kLanes = kCols / kVec, kRowsAtOnce = kWave / kLanes;
+    static_assert(4 * 32 * kPitch <= G::kLds, "the waves' parts fit");
+    char *mine = lds + wave * 32 * kPitch;
     T *y = static_cast<T *>(a.y);
+    const int32_t c0 = n0 + wn - G::TM;
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-        const int64_t r = r0 + wm + m * 32 + r32;
-        if (r >= seg.end) continue;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int32_t c = n0 + wn - G::TM + n * 32 + 8 * (i >> 2) + 4 * half + (i & 3);
-                if (c < a.N) y[r * a.N + c] = (T)sum[m][n][i];
+            for (int g = 0; g < 4; ++g) {
+                typedef T four __attribute__((ext_vector_type(4)));
+                const four v = {(T)sum[m][n][4 * g], (T)sum[m][n][4 * g + 1], (T)sum[m][n][4 * g + 2], (T)sum[m][n][4 * g + 3]};
+                *reinterpret_cast<four *>(mine + r32 * kPitch + (n * 32 + 8 * g + 4 * half) * sizeof(T)) = v;
             }
+        wave_meet();
+#pragma unroll
+        for (int i = 0; i < 32 / kRowsAtOnce; ++i) {
+            const int row = i * kRowsAtOnce + lane / kLanes, c = (lane % kLanes) * kVec;
+            const int4_ v = *reinterpret_cast<const int4_ *>(mine + row * kPitch + c * sizeof(T));
+            const int64_t r = r0 + wm + m * 32 + row;
+            if (r < seg.end) store_cols<T>(y + r * a.N, a.N, c0 + c, v);
+        }
+        wave_meet();
     }
 }
 
