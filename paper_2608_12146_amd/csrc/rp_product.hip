@@ -77,23 +77,20 @@ __global__ void __launch_bounds__(256) k_product_few(ProductArgs a) {
     }
 }
 
-// Many rows a slot: tiles of TM rows by TN of N, four waves of MT x NT matrix
-// tiles of 32 x 32, 128 columns (64 bytes a row) a step.
+// Many rows a slot: tiles of 256 rows by 256 of N, eight waves of 4 x 2 matrix
+// tiles of 32 x 32, 256 columns (128 bytes a row) a step.
 //
-// The codes go from memory to LDS without passing registers, S - 1 steps ahead;
-// a row's four pieces of 16 bytes are exchanged by the row (the sources are, as
-// a wave's 64 pieces land one after the other), so that the 32 rows of a fragment
-// stand in different banks.  The scales of kUnit steps are loaded together and
-// turned in LDS to a word a row and step.
-constexpr int kUnit = 2;  // steps whose scales are loaded together
-
-template <int WM, int WN, int MT, int NT, int S>
-struct Shape {
-    static constexpr int TM = WM * MT * 32, TN = WN * NT * 32, kRows = TM + TN;
-    static constexpr int kStage = kRows * 64, kLds = S * kStage + 2 * kUnit * kRows * 4;
-    static constexpr int kLoads = kRows / 64;  // a wave's loads of 1 KiB a step
-    static_assert(kRows % 64 == 0 && TM % 16 == 0, "whole loads");
-};
+// A wave's blocks of 32 rows alternate with its neighbour's, and blocks that
+// the slot's rows leave empty are not multiplied: a part-filled tile costs both
+// waves of a SIMD alike, in steps of 32 rows (2).
+// The codes go from memory to LDS without passing registers, a step ahead; a
+// row's eight pieces of 16 bytes are exchanged by the row (the sources are, as a
+// wave's 64 pieces land one after the other), so that the 32 rows of a fragment
+// stand in different banks.  The scales of two steps are loaded together and
+// turned in LDS to words by row.
+constexpr int kTileRows = 256, kTileCols = 256, kBoth = kTileRows + kTileCols;
+constexpr int kStage = kBoth * 128, kWords = 4;  // of scales, two steps
+constexpr int kManyLds = 2 * kStage + 2 * kWords * kBoth * 4;
 
 __device__ inline uint32_t lds_address(const void *p) {
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)p;
@@ -108,12 +105,9 @@ __device__ inline void load_to_lds(const uint8_t *base, uint32_t offset, uint32_
                  : "=&s"(m0) : "s"(to), "v"(offset), "s"(base) : "memory");
 }
 
-// All but this wave's last N loads have ended, and its LDS accesses; then the
+// All of this wave's loads have ended, and its LDS accesses; then the
 // workgroup's barrier.
-template <int N>
-__device__ inline void wait_and_meet() {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(N) : "memory");
-}
+__device__ inline void wait_and_meet() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // A wave's LDS accesses before are done before those after.
 __device__ inline void wave_meet() {
@@ -137,9 +131,8 @@ __device__ inline void store_cols(T *row, int32_t cols, int32_t c, int4_ v) {
     }
 }
 
-template <class T, int WM, int WN, int MT, int NT, int S>
-__global__ void __launch_bounds__(256, 2) k_product_many(ProductArgs a) {
-    using G = Shape<WM, WN, MT, NT, S>;
+template <class T>
+__global__ void __launch_bounds__(512, 1) k_product_many(ProductArgs a) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int64_t id = group_index();
     if (id >= a.tiles) {
@@ -149,135 +142,132 @@ __global__ void __launch_bounds__(256, 2) k_product_many(ProductArgs a) {
     // Workgroups go to the eight XCDs in turn: each XCD gets a run of adjacent
     // tiles, the row tiles of a slot's piece of N next to each other.
     int64_t before, total;
-    slot_of_tile<false>(a.offsets, a.n_slots, a.R, G::TM, INT64_MAX, before, total);
+    slot_of_tile<false>(a.offsets, a.n_slots, a.R, kTileRows, INT64_MAX, before, total);
     const int64_t all = total * a.n_tiles, run = (all + 7) / 8, index = (id & 7) * run + (id >> 3);
     if ((id >> 3) >= run || index >= all) return;
     // (a slot's tiles: its row tiles times n_tiles)
-    const int32_t s = slot_of_tile<false>(a.offsets, a.n_slots, a.R, G::TM, index / a.n_tiles, before, total);
+    const int32_t s = slot_of_tile<false>(a.offsets, a.n_slots, a.R, kTileRows, index / a.n_tiles, before, total);
     if (s < 0) return;
     const Segment seg = segment_of(a.offsets, s, a.R);
-    const int64_t m_tiles = (seg.end - seg.begin + G::TM - 1) / G::TM;
-    // index - (the slot's first) = before * n_tiles + index % n_tiles
-    const int64_t within = before * a.n_tiles + index % a.n_tiles;
+    const int64_t m_tiles = (seg.end - seg.begin + kTileRows - 1) / kTileRows;
+    const int64_t within = before * a.n_tiles + index % a.n_tiles;  // index less the slot's first
     const int32_t nt = (int32_t)(within / m_tiles), mt = (int32_t)(within - nt * m_tiles);
-    const int64_t r0 = seg.begin + (int64_t)mt * G::TM;
-    const int32_t n0 = nt * G::TN;
+    const int64_t r0 = seg.begin + (int64_t)mt * kTileRows;
+    const int32_t n0 = nt * kTileCols;
+    const int32_t rows = seg.end - r0 < kTileRows ? (int32_t)(seg.end - r0) : kTileRows;
+    const int32_t cols = a.N - n0 < kTileCols ? a.N - n0 : kTileCols;
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int64_t code_row = (int64_t)a.groups * 64, scale_row = (int64_t)a.groups * 4;
-    // tile row i: x row r0 + i, then w row n0 + (i - TM); past the ends the last one again
-    auto x_row = [&](int i) { return r0 + i < seg.end ? i : (int)(seg.end - 1 - r0); };
-    auto w_row = [&](int i) { return n0 + i < a.N ? i : a.N - 1 - n0; };
     const uint8_t *xbase = a.xc + r0 * code_row, *wbase = a.wc + ((int64_t)s * a.N + n0) * code_row;
-    uint32_t from[G::kLoads];
+    // Load i of a wave brings 8 rows, of x (i < 4) or w; rows past the end are the
+    // last one again, loads of none but those are left out.
+    const int piece = (lane & 7) ^ (lane >> 3);
+    uint32_t from[8], from_last[8];
+    int n_x = 0, n_w = 0;
+    const bool odd = a.groups & 1;  // the last step has four pieces a row
 #pragma unroll
-    for (int i = 0; i < G::kLoads; ++i) {
-        const int row = ((wave + 4 * i) * 16) + (lane >> 2), piece = (lane & 3) ^ ((row >> 1) & 3);
-        const int real = row < G::TM ? x_row(row) : w_row(row - G::TM);
-        from[i] = (uint32_t)(real * code_row + piece * 16);
+    for (int i = 0; i < 8; ++i) {
+        const int first = ((i & 3) * 8 + wave) * 8, row = first + (lane >> 3), most = (i < 4 ? rows : cols) - 1;
+        const uint32_t at = (uint32_t)((row < most ? row : most) * code_row);
+        from[i] = at + piece * 16;
+        from_last[i] = at + (odd ? piece & 3 : piece) * 16;
+        if (first <= most) (i < 4 ? n_x : n_w) += 1;
     }
     const uint32_t lds0 = lds_address(lds);
-    const int32_t steps = a.groups;
+    const int32_t steps = (a.groups + 1) / 2;
     auto issue = [&](int32_t step) {
-        const uint32_t to = lds0 + (uint32_t)(step % S) * G::kStage;
+        const uint32_t to = lds0 + (step & 1) * kStage + wave * 1024;
+        const uint8_t *x = xbase + (int64_t)step * 128, *w = wbase + (int64_t)step * 128;
+        const bool last = step + 1 == steps;
 #pragma unroll
-        for (int i = 0; i < G::kLoads; ++i) {
-            const int load = wave + 4 * i;
-            const uint8_t *base = (load * 16 < G::TM ? xbase : wbase) + (int64_t)step * 64;
-            load_to_lds(base, from[i], to + load * 1024);
-        }
+        for (int i = 0; i < 4; ++i)
+            if (i < n_x) load_to_lds(x, last ? from_last[i] : from[i], to + i * 8192);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < n_w) load_to_lds(w, last ? from_last[4 + i] : from[4 + i], to + (4 + i) * 8192);
     };
-    // scales: a row's word of each step of a unit
-    constexpr int kMine = (G::kRows + 255) / 256;
-    uint32_t *turned = reinterpret_cast<uint32_t *>(lds + S * G::kStage);
-    uint32_t sc[kMine][kUnit];
+    // scales: a row's words of two steps a thread
+    uint32_t *turned = reinterpret_cast<uint32_t *>(lds + 2 * kStage);
+    uint32_t sc[kWords];
+    const int srow = t < kTileRows ? (t < rows ? t : rows - 1) : (t - kTileRows < cols ? t - kTileRows : cols - 1);
+    const uint32_t *scales = reinterpret_cast<const uint32_t *>(
+        t < kTileRows ? a.xs + (r0 + srow) * scale_row : a.ws + ((int64_t)s * a.N + n0 + srow) * scale_row);
     auto fetch_scales = [&](int32_t unit) {
+        if ((unit + 1) * kWords <= a.groups) {
+            load16<false>(scales + unit * kWords, sc);
+        } else {
 #pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-            const int row = t + 256 * i;
-            if (row >= G::kRows) continue;
-            const uint8_t *p = row < G::TM ? a.xs + (r0 + x_row(row)) * scale_row
-                                           : a.ws + ((int64_t)s * a.N + n0 + w_row(row - G::TM)) * scale_row;
-            typedef uint32_t words __attribute__((ext_vector_type(kUnit), aligned(4)));
-            const uint32_t *w = reinterpret_cast<const uint32_t *>(p) + unit * kUnit;
-            if ((unit + 1) * kUnit <= steps) {
-                const words v = *reinterpret_cast<const words *>(w);
-#pragma unroll
-                for (int k = 0; k < kUnit; ++k) sc[i][k] = v[k];
-            } else {
-#pragma unroll
-                for (int k = 0; k < kUnit; ++k) sc[i][k] = unit * kUnit + k < steps ? w[k] : 0;
-            }
+            for (int k = 0; k < kWords; ++k) sc[k] = unit * kWords + k < a.groups ? scales[unit * kWords + k] : 0;
         }
     };
     auto store_scales = [&](int32_t unit) {
-        uint32_t *to = turned + (unit & 1) * kUnit * G::kRows;
 #pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-            const int row = t + 256 * i;
-            if (row >= G::kRows) continue;
-#pragma unroll
-            for (int k = 0; k < kUnit; ++k) to[k * G::kRows + row] = sc[i][k];
-        }
+        for (int k = 0; k < kWords; ++k) turned[((unit & 1) * kWords + k) * kBoth + t] = sc[k];
     };
-    const int wm = (wave / WN) * MT * 32, wn = G::TM + (wave % WN) * NT * 32, half = lane >> 5, r32 = lane & 31;
-    float16_ sum[MT][NT] = {};
-    fetch_scales(0);
-#pragma unroll
-    for (int i = 0; i < S - 1; ++i)
-        if (i < steps) issue(i);
-    store_scales(0);
+    // this wave's blocks: rows (2 m + wm) 32, columns wn + 32 n
+    const int wm = wave >> 2, wn = (wave & 3) * 64, half = lane >> 5, r32 = lane & 31;
+    const int blocks = (rows + 31) / 32, live = wn < cols ? (blocks - wm + 1) / 2 : 0;
+    T *y = static_cast<T *>(a.y);
+    // The whole of it for a number of blocks (the accumulators stay where they
+    // are): every wave meets the others as often, whatever its number.
+    auto multiply = [&](auto live_) {
+    constexpr int kLive = decltype(live_)::value;
+    float16_ sum[kLive ? kLive : 1][2] = {};
     for (int32_t step = 0; step < steps; ++step) {
-        // (this step's loads: the oldest of those in flight)
-        if (step + S - 2 < steps) wait_and_meet<(S - 2) * G::kLoads>();
-        else wait_and_meet<0>();
-        if (step + S - 1 < steps) issue(step + S - 1);
-        const int32_t unit = step / kUnit;
-        if (step % kUnit == 0 && (unit + 1) * kUnit < steps) fetch_scales(unit + 1);
-        const char *tile = lds + (step % S) * G::kStage;
-        const uint32_t *scale = turned + ((unit & 1) * kUnit + step % kUnit) * G::kRows + r32;
-        uint32_t xs[MT], ws[NT];
+        wait_and_meet();
+        if (step + 1 < steps) issue(step + 1);
+        const int32_t unit = step >> 1;
+        const bool more = (unit + 1) * kWords < a.groups;
+        if ((step & 1) == 0 && more) fetch_scales(unit + 1);
+        const char *tile = lds + (step & 1) * kStage;
+        const uint32_t *scale = turned + (((step >> 1) & 1) * kWords + (step & 1) * 2) * kBoth + r32;
+        const int groups = step + 1 == steps && odd ? 1 : 2;
 #pragma unroll
-        for (int m = 0; m < MT; ++m) xs[m] = scale[wm + m * 32] >> (8 * half);
+        for (int g = 0; g < 2; ++g) {
+            if (kLive == 0 || g >= groups) break;
+            uint32_t xs[kLive ? kLive : 1], ws[2];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) ws[n] = scale[wn + n * 32] >> (8 * half);
+            for (int m = 0; m < kLive; ++m) xs[m] = scale[g * kBoth + (2 * m + wm) * 32] >> (8 * half);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            auto fragment = [&](int first) {
-                const int row = first + r32, piece = (2 * k + half) ^ ((row >> 1) & 3);
-                const int4_ v = *reinterpret_cast<const int4_ *>(tile + row * 64 + piece * 16);
-                return int8_{v[0], v[1], v[2], v[3], 0, 0, 0, 0};
-            };
-            int8_ x[MT], w[NT];
+            for (int n = 0; n < 2; ++n) ws[n] = scale[g * kBoth + kTileRows + wn + n * 32] >> (8 * half);
 #pragma unroll
-            for (int m = 0; m < MT; ++m) x[m] = fragment(wm + m * 32);
+            for (int k = 0; k < 2; ++k) {
+                auto fragment = [&](int first) {
+                    const int row = first + r32, at = (4 * g + 2 * k + half) ^ (row & 7);
+                    const int4_ v = *reinterpret_cast<const int4_ *>(tile + row * 128 + at * 16);
+                    return int8_{v[0], v[1], v[2], v[3], 0, 0, 0, 0};
+                };
+                int8_ x[kLive ? kLive : 1], w[2];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) w[n] = fragment(wn + n * 32);
+                for (int n = 0; n < 2; ++n) w[n] = fragment(kTileRows + wn + n * 32);
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+                for (int m = 0; m < kLive; ++m) x[m] = fragment((2 * m + wm) * 32);
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    if (k == 0)
-                        sum[m][n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w[n], x[m], sum[m][n], 4, 4, 0, (int)ws[n], 0, (int)xs[m]);
-                    else
-                        sum[m][n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w[n], x[m], sum[m][n], 4, 4, 2, (int)ws[n], 2, (int)xs[m]);
-                }
+                for (int m = 0; m < kLive; ++m)
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
+                        if (k == 0)
+                            sum[m][n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w[n], x[m], sum[m][n], 4, 4, 0, (int)ws[n], 0, (int)xs[m]);
+                        else
+                            sum[m][n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w[n], x[m], sum[m][n], 4, 4, 2, (int)ws[n], 2, (int)xs[m]);
+                    }
+            }
         }
-        if (step % kUnit == kUnit - 1 && step + 1 < steps) store_scales(unit + 1);
+        if ((step & 1) == 1 && more) store_scales(unit + 1);
     }
     // A value's row is lane % 32 of x, its column 8 (i / 4) + 4 (lane / 32) + i % 4
     // of w: 32 rows at a time go through this wave's part of LDS, to leave as
     // whole lines.
-    wait_and_meet<0>();
-    constexpr int kCols = NT * 32, kPitch = kCols * (int)sizeof(T) + 16, kVec = 16 / (int)sizeof(T);
-    constexpr int kLanes = kCols / kVec, kRowsAtOnce = kWave / kLanes;
-    static_assert(4 * 32 * kPitch <= G::kLds, "the waves' parts fit");
+    wait_and_meet();
+    constexpr int kPitch = 64 * (int)sizeof(T) + 16, kVec = 16 / (int)sizeof(T);
+    constexpr int kLanes = 64 / kVec, kRowsAtOnce = kWave / kLanes;
+    static_assert(8 * 32 * kPitch <= kManyLds, "the waves' parts fit");
     char *mine = lds + wave * 32 * kPitch;
-    T *y = static_cast<T *>(a.y);
-    const int32_t c0 = n0 + wn - G::TM;
+    const int32_t c0 = n0 + wn;
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
+    for (int m = 0; m < kLive; ++m) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < 2; ++n)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 typedef T four __attribute__((ext_vector_type(4)));
@@ -289,10 +279,23 @@ __global__ void __launch_bounds__(256, 2) k_product_many(ProductArgs a) {
         for (int i = 0; i < 32 / kRowsAtOnce; ++i) {
             const int row = i * kRowsAtOnce + lane / kLanes, c = (lane % kLanes) * kVec;
             const int4_ v = *reinterpret_cast<const int4_ *>(mine + row * kPitch + c * sizeof(T));
-            const int64_t r = r0 + wm + m * 32 + row;
-            if (r < seg.end) store_cols<T>(y + r * a.N, a.N, c0 + c, v);
+            const int r = (2 * m + wm) * 32 + row;
+            if (r < rows) store_cols<T>(y + (r0 + r) * a.N, a.N, c0 + c, v);
         }
         wave_meet();
+    }
+    };
+    if (steps > 0) {
+        fetch_scales(0);
+        issue(0);
+        store_scales(0);
+    }
+    switch (live) {
+        case 4: multiply(Int<4>()); break;
+        case 3: multiply(Int<3>()); break;
+        case 2: multiply(Int<2>()); break;
+        case 1: multiply(Int<1>()); break;
+        default: multiply(Int<0>());
     }
 }
 
@@ -327,15 +330,14 @@ extern "C" int routepack_expert_product(const routepack_mx *x, const routepack_m
     return by_type(y->type, [&](auto tag) -> int {
         using T = decltype(tag);
         if (a.R >= 32 * (int64_t)n_slots) {
-            using G = Shape<2, 2, 2, 4, 3>;
-            const auto kern = k_product_many<T, 2, 2, 2, 4, 3>;
-            a.n_tiles = (int32_t)((N + G::TN - 1) / G::TN);
+            const auto kern = k_product_many<T>;
+            a.n_tiles = (int32_t)((N + kTileCols - 1) / kTileCols);
             // (each slot may have a tile that is not full; eight runs of equal length)
-            a.tiles = ((a.R / G::TM + most) * a.n_tiles + 7) / 8 * 8;
+            a.tiles = ((a.R / kTileRows + most) * a.n_tiles + 7) / 8 * 8;
             if (hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                    G::kLds) != hipSuccess)
+                                    kManyLds) != hipSuccess)
                 return ROUTEPACK_E_DEVICE;
-            hipLaunchKernelGGL(kern, grid_of(a.tiles + a.clears), dim3(256), G::kLds, stream, a);
+            hipLaunchKernelGGL(kern, grid_of(a.tiles + a.clears), dim3(512), kManyLds, stream, a);
             return launched();
         }
         a.n_tiles = (int32_t)((N + 15) / 16);
