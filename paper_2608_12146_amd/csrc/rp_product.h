@@ -29,43 +29,73 @@ __device__ inline Segment segment_of(const int64_t *offsets, int32_t s, int64_t 
     return {b, e};
 }
 
-// The slot that holds tile `index` of a row of tiles, where a slot of n rows has
-// ceil(n / tile) of them (at most one where ONE), and the number of its tiles
-// before.  Every wave of a workgroup searches by itself: a lane counts a run of
-// adjacent slots.  Returns -1 behind the last tile; `total` is their number.
-template <bool ONE>
-__device__ inline int32_t slot_of_tile(const int64_t *offsets, int32_t n_slots, int64_t R, int32_t tile, int64_t index,
-                                       int64_t &before, int64_t &total) {
-    const int lane = threadIdx.x & (kWave - 1);
-    const int32_t per = (n_slots + kWave - 1) / kWave, s0 = lane * per;
-    auto tiles = [&](int32_t s) -> int64_t {
-        if (s >= n_slots) return 0;
-        const Segment g = segment_of(offsets, s, R);
-        if (ONE) return g.end > g.begin ? 1 : 0;
-        return (g.end - g.begin + tile - 1) / tile;
-    };
-    int64_t mine = 0;
-    for (int32_t i = 0; i < per; ++i) mine += tiles(s0 + i);
-    int64_t upto = mine;
-    for (int d = 1; d < kWave; d <<= 1) {
-        const int64_t v = __shfl_up((long long)upto, d, kWave);
-        upto += lane >= d ? v : 0;
+// Which slot's segment a tile lies in, where a slot of n rows has ceil(n / tile)
+// tiles (one, if any, where tile is 0).  Every wave of a workgroup searches by
+// itself: a lane counts a run of adjacent slots, whose offsets it keeps.
+struct TileMap {
+    static constexpr int kKeep = 4;  // slots of a lane whose offsets stay in registers
+    int32_t per;
+    int64_t mine, upto;              // tiles of this lane's run, and up to its end
+    int64_t total;
+    Segment kept[kKeep];
+
+    static __device__ int64_t tiles(const Segment &g, int32_t tile) {
+        const int64_t n = g.end - g.begin;
+        return tile ? (n + tile - 1) / tile : n > 0;
     }
-    total = uniform64(__shfl((long long)upto, kWave - 1, kWave));
-    if (index >= total) return -1;
-    const uint64_t past = __ballot(upto > index);
-    const int owner = __builtin_ctzll(past);
-    int64_t at = uniform64(__shfl((long long)(upto - mine), owner, kWave));
-    // the owner's run, by all lanes alike
-    int32_t s = __builtin_amdgcn_readfirstlane(owner) * per;
-    for (;; ++s) {
-        const int64_t n = tiles(s);
-        if (index < at + n || s + 1 >= n_slots) break;
-        at += n;
+    __device__ TileMap(const int64_t *offsets, int32_t n_slots, int64_t R, int32_t tile) {
+        const int lane = threadIdx.x & (kWave - 1);
+        per = (n_slots + kWave - 1) / kWave;
+        mine = 0;
+#pragma unroll
+        for (int i = 0; i < kKeep; ++i) {
+            const int32_t s = lane * per + i;
+            kept[i] = {0, 0};
+            if (i < per && s < n_slots) kept[i] = segment_of(offsets, s, R);
+        }
+#pragma unroll
+        for (int i = 0; i < kKeep; ++i) mine += tiles(kept[i], tile);
+        for (int i = kKeep; i < per; ++i)
+            if (lane * per + i < n_slots) mine += tiles(segment_of(offsets, lane * per + i, R), tile);
+        upto = mine;
+        for (int d = 1; d < kWave; d <<= 1) {
+            const int64_t v = __shfl_up((long long)upto, d, kWave);
+            upto += lane >= d ? v : 0;
+        }
+        total = uniform64(__shfl((long long)upto, kWave - 1, kWave));
     }
-    before = index - at;
-    return s;
-}
+    // The slot of tile `index` < total, its segment, and the number of its tiles
+    // before.  All results are uniform.
+    __device__ int32_t find(int64_t index, const int64_t *offsets, int32_t n_slots, int64_t R, int32_t tile, Segment &g,
+                            int64_t &before) const {
+        const int owner = __builtin_amdgcn_readfirstlane(__builtin_ctzll(__ballot(upto > index)));
+        int64_t at = uniform64(__shfl((long long)(upto - mine), owner, kWave));
+        const int32_t s0 = owner * per;
+        int32_t s = s0;
+        bool found = false;
+#pragma unroll
+        for (int i = 0; i < kKeep; ++i) {
+            const Segment k = {uniform64(__shfl((long long)kept[i].begin, owner, kWave)),
+                               uniform64(__shfl((long long)kept[i].end, owner, kWave))};
+            const int64_t n = tiles(k, tile);
+            if (!found && index < at + n) {
+                found = true;
+                s = s0 + i;
+                g = k;
+            }
+            at += found ? 0 : n;
+        }
+        if (!found)
+            for (s = s0 + kKeep;; ++s) {
+                g = segment_of(offsets, s, R);
+                const int64_t n = tiles(g, tile);
+                if (index < at + n || s + 1 >= n_slots) break;
+                at += n;
+            }
+        before = index - at;
+        return s;
+    }
+};
 
 // Zeros in the rows of no slot: piece `index` of `pieces` of them.
 template <class T>

@@ -29,10 +29,11 @@ __global__ void __launch_bounds__(256) k_product_few(ProductArgs a) {
     }
     const int64_t index = id / a.n_tiles;
     const int32_t n0 = (int32_t)(id - index * a.n_tiles) * 16;
-    int64_t before, total;
-    const int32_t s = slot_of_tile<true>(a.offsets, a.n_slots, a.R, 0, index, before, total);
-    if (s < 0) return;
-    const Segment seg = segment_of(a.offsets, s, a.R);
+    const TileMap map(a.offsets, a.n_slots, a.R, 0);
+    if (index >= map.total) return;
+    Segment seg;
+    int64_t before;
+    const int32_t s = map.find(index, a.offsets, a.n_slots, a.R, 0, seg, before);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane >> 4, i16 = lane & 15;
     const int32_t n = n0 + i16 < a.N ? n0 + i16 : a.N - 1;
     const int64_t row = (int64_t)s * a.N + n;
@@ -140,18 +141,19 @@ __global__ void __launch_bounds__(512, 1) k_product_many(ProductArgs a) {
         return;
     }
     // Workgroups go to the eight XCDs in turn: each XCD gets a run of adjacent
-    // tiles, the row tiles of a slot's piece of N next to each other.
-    int64_t before, total;
-    slot_of_tile<false>(a.offsets, a.n_slots, a.R, kTileRows, INT64_MAX, before, total);
-    const int64_t all = total * a.n_tiles, run = (all + 7) / 8, index = (id & 7) * run + (id >> 3);
+    // tiles, and within a slot four tiles of N next to each other for each of its
+    // row tiles, so that those at work together share both operands.
+    const TileMap map(a.offsets, a.n_slots, a.R, kTileRows);
+    const int64_t all = map.total * a.n_tiles, run = (all + 7) / 8, index = (id & 7) * run + (id >> 3);
     if ((id >> 3) >= run || index >= all) return;
-    // (a slot's tiles: its row tiles times n_tiles)
-    const int32_t s = slot_of_tile<false>(a.offsets, a.n_slots, a.R, kTileRows, index / a.n_tiles, before, total);
-    if (s < 0) return;
-    const Segment seg = segment_of(a.offsets, s, a.R);
+    Segment seg;
+    int64_t before;
+    const int32_t s = map.find(index / a.n_tiles, a.offsets, a.n_slots, a.R, kTileRows, seg, before);
     const int64_t m_tiles = (seg.end - seg.begin + kTileRows - 1) / kTileRows;
     const int64_t within = before * a.n_tiles + index % a.n_tiles;  // index less the slot's first
-    const int32_t nt = (int32_t)(within / m_tiles), mt = (int32_t)(within - nt * m_tiles);
+    const int32_t group = (int32_t)(within / (m_tiles * 4)), n_left = a.n_tiles - group * 4;
+    const int32_t rest = (int32_t)(within - group * (m_tiles * 4)), n_here = n_left < 4 ? n_left : 4;
+    const int32_t mt = rest / n_here, nt = group * 4 + rest - mt * n_here;
     const int64_t r0 = seg.begin + (int64_t)mt * kTileRows;
     const int32_t n0 = nt * kTileCols;
     const int32_t rows = seg.end - r0 < kTileRows ? (int32_t)(seg.end - r0) : kTileRows;
@@ -161,7 +163,7 @@ __global__ void __launch_bounds__(512, 1) k_product_many(ProductArgs a) {
     const uint8_t *xbase = a.xc + r0 * code_row, *wbase = a.wc + ((int64_t)s * a.N + n0) * code_row;
     // Load i of a wave brings 8 rows, of x (i < 4) or w; rows past the end are the
     // last one again, loads of none but those are left out.
-    const int piece = (lane & 7) ^ (lane >> 3);
+    const int piece = (lane & 7) ^ ((wave * 4 + (lane >> 4)) & 7);
     uint32_t from[8], from_last[8];
     int n_x = 0, n_w = 0;
     const bool odd = a.groups & 1;  // the last step has four pieces a row
@@ -233,7 +235,7 @@ __global__ void __launch_bounds__(512, 1) k_product_many(ProductArgs a) {
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 auto fragment = [&](int first) {
-                    const int row = first + r32, at = (4 * g + 2 * k + half) ^ (row & 7);
+                    const int row = first + r32, at = (4 * g + 2 * k + half) ^ ((row >> 1) & 7);
                     const int4_ v = *reinterpret_cast<const int4_ *>(tile + row * 128 + at * 16);
                     return int8_{v[0], v[1], v[2], v[3], 0, 0, 0, 0};
                 };

@@ -120,10 +120,10 @@ __global__ void __launch_bounds__(256) k_product_back(BackProductArgs a) {
         }
         const int64_t index = id / a.c_tiles;
         ct = (int32_t)(id - index * a.c_tiles);
-        int64_t before, total;
-        s = slot_of_tile<false>(a.offsets, a.n_slots, a.R, kTile, index, before, total);
-        if (s < 0) return;
-        seg = segment_of(a.offsets, s, a.R);
+        int64_t before;
+        const TileMap map(a.offsets, a.n_slots, a.R, kTile);
+        if (index >= map.total) return;
+        s = map.find(index, a.offsets, a.n_slots, a.R, kTile, seg, before);
         m0 = seg.begin + before * kTile;
     }
     const int c0 = ct * kTile, t = threadIdx.x, lane = t & 63, wave = t >> 6;
