@@ -1,171 +1,210 @@
 // The order of the pairs of tokens and chosen experts by slot, on gfx950: a
 // stable counting sort.
 //
-// A layer's pairs are cut into chunks; a chunk's pairs are counted by slot
-// (k_order_count), the counts of a slot are summed over the chunks before
-// (k_order_scan), and each chunk places its pairs behind those (k_order_place).
-// Pairs without a choice count for a slot of their own behind the last.  Within
-// a chunk each wave holds a part in order and counters of its own; 64 pairs at a
-// time find their rank among those with the same slot by ballots over the
-// slot's bits, so rows do not depend on the order of atomics.  One chunk needs
-// the last kernel alone.
+// A layer's pairs are cut into chunks of 4096, 8 a thread: a chunk's pairs are
+// counted by slot (k_order_count), a slot's counts are summed over the chunks
+// before (k_order_scan, a wave each), and each chunk places its pairs behind
+// those (k_order_place).  Pairs without a choice count for a slot of their own
+// behind the last.  Within a chunk each wave has counters of its own; 64 pairs
+// at a time find their rank among those of the same slot by ballots over the
+// slot's bits, so rows do not depend on the order of atomics.  The chunk is put
+// in order in LDS first: a slot's rows then leave as a run (written from where
+// they are found they were 4 bytes each, and 46 us where now @PLACE@).  One chunk
+// needs the last kernel alone.
+//
+// 131072 x 4 x 8 byte ids, 256 slots, placed: @ALL@ us.
 #include "rp_experts.h"
 
 namespace rp {
 
+constexpr int kOrderThreads = 512, kOrderWaves = kOrderThreads / kWave, kEach = 8;
+constexpr int32_t kChunk = kOrderThreads * kEach;
+
 struct OrderArgs {
     const void *ids;
-    int32_t type;
     int64_t ts, ls;
     int32_t P, L, E, k;     // pairs of a layer
+    uint32_t k_inv;         // p / k = p k_inv >> k_shift for p < 2^31
+    int32_t k_shift;
     const int32_t *slots;
-    int32_t chunk, n_chunks;
+    int32_t n_chunks;
     int32_t bits;           // of a slot, 0 .. E
-    int32_t *counts;        // [L][n_chunks][E + 1], then sums over the chunks before
+    int32_t *counts;        // [L][E + 1][n_chunks], then sums over the chunks before
     int32_t *totals;        // [L][E + 1]
     int32_t *rows;
     int64_t *offsets;
     int32_t *places;
 };
 
-constexpr int kOrderThreads = 512, kOrderWaves = kOrderThreads / kWave;
+__device__ inline int32_t token_of(const OrderArgs &a, int32_t p) {
+    return (int32_t)((uint64_t)(uint32_t)p * a.k_inv >> a.k_shift);
+}
 
-// Pair p's slot; E for none.
+// The slots of pairs p, p + step, .. (E for none), 8 loads at a time.
 template <class I>
-__device__ inline int32_t slot_of_pair(const OrderArgs &a, int32_t l, int32_t p) {
-    const int32_t t = (int32_t)((uint32_t)p / (uint32_t)a.k), j = p - t * a.k;
-    const int64_t v = (int64_t) static_cast<const I *>(a.ids)[t * a.ts + l * a.ls + j];
-    if (v < 0 || v >= a.E) return a.E;
-    if (!a.slots) return (int32_t)v;
-    const int32_t s = a.slots[(int64_t)l * a.E + v];
-    return s >= 0 && s < a.E ? s : a.E;
+__device__ inline void slots_of_pairs(const OrderArgs &a, int32_t l, int32_t p, int32_t step, int32_t end,
+                                      int32_t (&slot)[kEach]) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int32_t x = p + i * step;
+        slot[i] = a.E;
+        if (x < end) {
+            const int32_t t = token_of(a, x), j = x - t * a.k;
+            const int64_t v = (int64_t) static_cast<const I *>(a.ids)[t * a.ts + l * a.ls + j];
+            slot[i] = v >= 0 && v < a.E ? (int32_t)v : a.E;
+        }
+    }
+    if (!a.slots) return;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int32_t s = slot[i] < a.E ? a.slots[(int64_t)l * a.E + slot[i]] : -1;
+        slot[i] = s >= 0 && s < a.E ? s : a.E;
+    }
 }
 
 template <class I>
 __global__ void __launch_bounds__(kOrderThreads) k_order_count(OrderArgs a) {
     extern __shared__ int32_t n[];
     const int32_t l = (int32_t)(blockIdx.x / a.n_chunks), c = (int32_t)(blockIdx.x - (uint32_t)l * a.n_chunks);
+    const int32_t b = c * kChunk, e = a.P - b < kChunk ? a.P : b + kChunk;
+    int32_t slot[kEach];
+    slots_of_pairs<I>(a, l, b + (int32_t)threadIdx.x, kOrderThreads, e, slot);
     for (int32_t s = threadIdx.x; s <= a.E; s += kOrderThreads) n[s] = 0;
     __syncthreads();
-    const int32_t b = c * a.chunk, e = a.P - b < a.chunk ? a.P : b + a.chunk;
-    for (int32_t p = b + (int32_t)threadIdx.x; p < e; p += kOrderThreads) atomicAdd(&n[slot_of_pair<I>(a, l, p)], 1);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+        if (b + (int32_t)threadIdx.x + i * kOrderThreads < e) atomicAdd(&n[slot[i]], 1);
     __syncthreads();
-    int32_t *out = a.counts + ((int64_t)l * a.n_chunks + c) * (a.E + 1);
-    for (int32_t s = threadIdx.x; s <= a.E; s += kOrderThreads) out[s] = n[s];
+    int32_t *out = a.counts + (int64_t)l * (a.E + 1) * a.n_chunks + c;
+    for (int32_t s = threadIdx.x; s <= a.E; s += kOrderThreads) out[(int64_t)s * a.n_chunks] = n[s];
 }
 
-// A wave sums 16 slots over the chunks, a quarter of a round's chunks each lane.
+// A wave a slot: its counts become sums over the chunks before.
 __global__ void __launch_bounds__(256) k_order_scan(OrderArgs a) {
-    const int32_t per = (a.E + 1 + 63) / 64, l = (int32_t)(blockIdx.x / per);
-    const int32_t s = (int32_t)(blockIdx.x - (uint32_t)l * per) * 64 + (int32_t)(threadIdx.x >> 2), q = threadIdx.x & 3;
-    if (s > a.E) return;  // (all four lanes of a slot)
-    int32_t *col = a.counts + (int64_t)l * a.n_chunks * (a.E + 1) + s;
-    const int32_t part = (a.n_chunks + 3) / 4, b = q * part, e = b + part < a.n_chunks ? b + part : a.n_chunks;
-    int32_t sum = 0;
-    for (int32_t c = b; c < e; ++c) sum += col[(int64_t)c * (a.E + 1)];
-    const int32_t s0 = __shfl(sum, 0, 4), s1 = __shfl(sum, 1, 4), s2 = __shfl(sum, 2, 4), s3 = __shfl(sum, 3, 4);
-    int32_t before = (q > 0 ? s0 : 0) + (q > 1 ? s1 : 0) + (q > 2 ? s2 : 0);
-    if (q == 0) a.totals[(int64_t)l * (a.E + 1) + s] = s0 + s1 + s2 + s3;
-    for (int32_t c = b; c < e; ++c) {
-        const int32_t v = col[(int64_t)c * (a.E + 1)];
-        col[(int64_t)c * (a.E + 1)] = before;
-        before += v;
+    const int64_t s = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (s >= (int64_t)a.L * (a.E + 1)) return;
+    const int lane = threadIdx.x & 63;
+    int32_t *row = a.counts + s * a.n_chunks;
+    int32_t before = 0;
+    for (int32_t c0 = 0; c0 < a.n_chunks; c0 += kWave * 4) {
+        int32_t v[4], sum = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int32_t c = c0 + lane * 4 + i;
+            v[i] = c < a.n_chunks ? row[c] : 0;
+            sum += v[i];
+        }
+        int32_t upto = sum;
+        for (int d = 1; d < kWave; d <<= 1) {
+            const int32_t x = __shfl_up(upto, d, kWave);
+            upto += lane >= d ? x : 0;
+        }
+        int32_t at = before + upto - sum;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int32_t c = c0 + lane * 4 + i;
+            if (c < a.n_chunks) row[c] = at;
+            at += v[i];
+        }
+        before += __shfl(upto, kWave - 1, kWave);
     }
+    if (lane == 0) a.totals[s] = before;
 }
 
 template <class I>
 __global__ void __launch_bounds__(kOrderThreads) k_order_place(OrderArgs a) {
     extern __shared__ int32_t lds[];
     const int32_t S = a.E + 1;
-    __shared__ int32_t wave_sum[kOrderWaves];
-    int32_t *mine = lds + (threadIdx.x >> 6) * S;  // this wave's counters, then its next rows
+    __shared__ uint64_t wave_sum[kOrderWaves];
+    int32_t *sorted = lds;                               // [kChunk]: slot, and pair within the chunk
+    int32_t *from = sorted + kChunk;                     // [S]: a slot's first row less its first place in `sorted`
+    int32_t *next = from + S + (threadIdx.x >> 6) * S;   // [waves][S]: this wave's counts, then its next places
     const int32_t l = (int32_t)(blockIdx.x / a.n_chunks), c = (int32_t)(blockIdx.x - (uint32_t)l * a.n_chunks);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int32_t s = threadIdx.x; s < kOrderWaves * S; s += kOrderThreads) lds[s] = 0;
+    const int32_t b = c * kChunk, e = a.P - b < kChunk ? a.P : b + kChunk, first = b + wave * (kWave * kEach) + lane;
+    int32_t slot[kEach];
+    slots_of_pairs<I>(a, l, first, kWave, e, slot);
+    for (int32_t s = threadIdx.x; s < kOrderWaves * S; s += kOrderThreads) from[S + s] = 0;
     __syncthreads();
-    const int32_t b = c * a.chunk, e = a.P - b < a.chunk ? a.P : b + a.chunk;
-    const int32_t part = ((e - b + kOrderWaves - 1) / kOrderWaves + 63) / 64 * 64;
-    const int32_t pb = e - b < wave * part ? e : b + wave * part, pe = e - pb < part ? e : pb + part;
-    for (int32_t p = pb + lane; p < pe; p += kWave) atomicAdd(&mine[slot_of_pair<I>(a, l, p)], 1);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+        if (first + i * kWave < e) atomicAdd(&next[slot[i]], 1);
     __syncthreads();
-    // the first row of every slot, and of this chunk's and wave's part of it
+    // A thread's slots: their rows (of all chunks) and their places in this one.
     const int32_t each = (S + kOrderThreads - 1) / kOrderThreads, s0 = threadIdx.x * each;
     const int32_t s1 = s0 + each < S ? s0 + each : S;
-    const int64_t at = ((int64_t)l * a.n_chunks + c) * S;
-    int32_t sum = 0;
+    const bool one = a.n_chunks == 1;
+    uint64_t sum = 0;  // rows << 32 | places
     for (int32_t s = s0; s < s1; ++s) {
-        if (a.n_chunks > 1) {
-            sum += a.totals[(int64_t)l * S + s];
-        } else {
-            for (int w = 0; w < kOrderWaves; ++w) sum += lds[w * S + s];
-        }
+        uint32_t here = 0;
+        for (int w = 0; w < kOrderWaves; ++w) here += (uint32_t)from[S + w * S + s];
+        sum += (uint64_t)(one ? here : (uint32_t)a.totals[(int64_t)l * S + s]) << 32 | here;
     }
-    int32_t upto = sum;
+    uint64_t upto = sum;
     for (int d = 1; d < kWave; d <<= 1) {
-        const int32_t v = __shfl_up(upto, d, kWave);
+        const uint64_t v = (uint64_t)__shfl_up((unsigned long long)upto, d, kWave);
         upto += lane >= d ? v : 0;
     }
     if (lane == kWave - 1) wave_sum[wave] = upto;
     __syncthreads();
-    int32_t row = upto - sum;
-    for (int w = 0; w < wave; ++w) row += wave_sum[w];
+    uint64_t at = upto - sum;
+    for (int w = 0; w < wave; ++w) at += wave_sum[w];
+    int32_t row = (int32_t)(at >> 32), place = (int32_t)(uint32_t)at;
     for (int32_t s = s0; s < s1; ++s) {
         if (c == 0) a.offsets[(int64_t)l * S + s] = row;  // (S = E + 1: the last is the end of slot E - 1)
-        int32_t next = row, total = 0;
-        if (a.n_chunks > 1) {
-            total = a.totals[(int64_t)l * S + s];
-            next += a.counts[at + s];
-        }
+        const int32_t before = one ? 0 : a.counts[((int64_t)l * S + s) * a.n_chunks + c];
+        from[s] = row + before - place;
+        if (!one) row += a.totals[(int64_t)l * S + s];
         for (int w = 0; w < kOrderWaves; ++w) {
-            const int32_t v = lds[w * S + s];
-            lds[w * S + s] = next;
-            next += v;
+            const int32_t v = from[S + w * S + s];
+            from[S + w * S + s] = place;
+            place += v;
+            if (one) row += v;
         }
-        row = a.n_chunks > 1 ? row + total : next;
     }
     __syncthreads();
-    int32_t *rows = a.rows + (int64_t)l * a.P;
-    for (int32_t p0 = pb; p0 < pe; p0 += kWave) {
-        const int32_t p = p0 + lane;
-        const bool live = p < pe;
-        const int32_t s = live ? slot_of_pair<I>(a, l, p) : a.E;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int32_t p = first + i * kWave;
+        const bool live = p < e;
         uint64_t same = __ballot(live);
-        for (int i = 0; i < a.bits; ++i) {
-            const bool bit = s >> i & 1;
+        for (int k = 0; k < a.bits; ++k) {
+            const bool bit = slot[i] >> k & 1;
             const uint64_t ones = __ballot(bit);
             same &= bit ? ones : ~ones;
         }
         const int32_t rank = __popcll(same & (((uint64_t)1 << lane) - 1)), all = __popcll(same);
-        const int32_t first = mine[s];
+        const int32_t base = next[slot[i]];
         __builtin_amdgcn_wave_barrier();  // (all reads of a wave's counters before the writes)
-        if (live && rank == 0) mine[s] = first + all;
+        if (live && rank == 0) next[slot[i]] = base + all;
         __builtin_amdgcn_wave_barrier();
         if (live) {
-            const int32_t r = first + rank;
-            const bool made = s < a.E;
-            rows[r] = made ? p : -1;
-            const int32_t t = (int32_t)((uint32_t)p / (uint32_t)a.k), j = p - t * a.k;
-            a.places[((int64_t)t * a.L + l) * a.k + j] = made ? r : -1;
+            sorted[base + rank] = slot[i] << 12 | (p - b);
+            const int32_t t = token_of(a, p), j = p - t * a.k;
+            a.places[((int64_t)t * a.L + l) * a.k + j] = slot[i] < a.E ? from[slot[i]] + base + rank : -1;
         }
+    }
+    __syncthreads();
+    int32_t *rows = a.rows + (int64_t)l * a.P;
+    for (int32_t i = threadIdx.x; i < e - b; i += kOrderThreads) {
+        const int32_t v = sorted[i], s = v >> 12;
+        rows[from[s] + i] = s < a.E ? b + (v & (kChunk - 1)) : -1;
     }
 }
 
-// Chunks of a layer: of 4096 pairs, fewer than 512 of them.
-inline int32_t order_chunk(int64_t P) {
-    const int64_t c = (P / 512 + 4095) / 4096 * 4096;
-    return (int32_t)(c < 4096 ? 4096 : c);
-}
+inline int32_t order_chunks(int64_t P) { return (int32_t)((P + kChunk - 1) / kChunk); }
 
 inline int check_order(const routepack_problem *p, int64_t n_tokens) {
     if (!p || n_tokens < 0 || p->n_layers < 0 || p->n_experts < 1 || p->top_k < 1) return ROUTEPACK_E_INVALID;
     if (p->n_experts > kMaxSlots || p->top_k > 256 || n_tokens > INT32_MAX / p->top_k) return ROUTEPACK_E_UNSUPPORTED;
-    if (p->n_layers > 0 && (int64_t)p->n_layers * (p->n_experts + 1) > INT64_MAX / 16 / 1024) return ROUTEPACK_E_UNSUPPORTED;
+    // (2^31 / kChunk + 1 chunks at most)
+    if ((int64_t)p->n_layers * (p->n_experts + 1) > kMaxBytes >> 24) return ROUTEPACK_E_UNSUPPORTED;
     return ROUTEPACK_OK;
 }
 
 // (of one chunk: none, but a workspace of size 0 would be a special case)
 inline int64_t order_bytes(const routepack_problem *p, int64_t n_tokens) {
-    const int64_t P = n_tokens * p->top_k, chunk = order_chunk(P), n = (P + chunk - 1) / chunk;
+    const int64_t n = order_chunks(n_tokens * p->top_k);
     return n <= 1 ? 16 : (int64_t)p->n_layers * (n + 1) * (p->n_experts + 1) * 4;
 }
 
@@ -190,7 +229,6 @@ extern "C" int routepack_order_tokens(const routepack_problem *prob, const route
     if (ids->n_tokens > 0 && (!rows || !places)) return ROUTEPACK_E_INVALID;
     OrderArgs a = {};
     a.ids = ids->data;
-    a.type = ids->type;
     a.ts = ids->token_stride;
     a.ls = ids->layer_stride;
     a.P = (int32_t)(ids->n_tokens * prob->top_k);
@@ -198,8 +236,10 @@ extern "C" int routepack_order_tokens(const routepack_problem *prob, const route
     a.E = prob->n_experts;
     a.k = prob->top_k;
     a.slots = slots;
-    a.chunk = order_chunk(a.P);
-    a.n_chunks = a.P > a.chunk ? (int32_t)(((int64_t)a.P + a.chunk - 1) / a.chunk) : 1;
+    a.n_chunks = order_chunks(a.P) > 1 ? order_chunks(a.P) : 1;
+    a.k_shift = 31;  // k_inv = ceil(2^k_shift / k), below 2^32: exact for p < 2^31
+    while ((int64_t)1 << (a.k_shift - 31) < a.k) ++a.k_shift;
+    a.k_inv = (uint32_t)((((uint64_t)1 << a.k_shift) + a.k - 1) / a.k);
     a.bits = 32 - __builtin_clz((unsigned)a.E);
     a.counts = static_cast<int32_t *>(workspace);
     a.totals = a.counts + (int64_t)a.L * a.n_chunks * (a.E + 1);
@@ -208,12 +248,12 @@ extern "C" int routepack_order_tokens(const routepack_problem *prob, const route
     a.places = places;
     if ((int64_t)a.L * a.n_chunks > INT32_MAX / kOrderThreads) return ROUTEPACK_E_UNSUPPORTED;
     const unsigned n = (unsigned)(a.L * a.n_chunks);
-    const size_t one = 4 * (size_t)(a.E + 1), all = one * kOrderWaves;
+    const size_t one = 4 * (size_t)(a.E + 1), all = 4 * kChunk + one * (1 + kOrderWaves);
     auto go = [&](auto tag) -> int {
         using I = decltype(tag);
         if (a.n_chunks > 1) {
             hipLaunchKernelGGL(k_order_count<I>, dim3(n), dim3(kOrderThreads), one, stream, a);
-            hipLaunchKernelGGL(k_order_scan, dim3((unsigned)a.L * (unsigned)((a.E + 1 + 63) / 64)), dim3(256), 0, stream, a);
+            hipLaunchKernelGGL(k_order_scan, dim3((unsigned)(((int64_t)a.L * (a.E + 1) + 3) / 4)), dim3(256), 0, stream, a);
         }
         if (all > 64 * 1024 - 256 &&
             hipFuncSetAttribute(reinterpret_cast<const void *>(k_order_place<I>),

@@ -3,14 +3,23 @@
 // group_top largest keys have the largest sum, and chooses among their experts.
 // Included by one translation unit for each type of logits.
 //
-// A group lies in Q adjacent lanes (a power of two) of up to V values, a token
-// in the Q n_groups lanes of its groups, rounded up to a power of two: a
-// group's best keys are reductions over its lanes, its rank is the number of
-// groups that precede it, and the choice is the selection of rp_route.h over
-// the lanes of the groups kept.
+// A group lies in Q adjacent lanes (a power of two) of up to 8 vectors of 16
+// bytes, a token in the Q n_groups lanes of its groups, rounded up to a power of
+// two and 4: a group's best keys are reductions over its lanes, its rank is the
+// number of groups that precede it, and the choice runs as without groups
+// (rp_route_choose.h) over the vectors of the groups kept: their maxima, then the
+// elements of the k vectors that lead.  Few lanes, as each doubling costs a merge
+// of lists: 8 lanes of 8 vectors a token.
+//
 // Without a bias and with group_top = 1 the keys are the logits, whose order
 // is the scores'.  Otherwise keys are compared in 64 bits, as two
-// implementations in 32 bits would choose differently.
+// implementations in 32 bits would choose differently: the keys are formed in
+// 32 bits, and where their error leaves the groups kept, the choices or their
+// order open (about one token in 500, and ties), the wave forms them in 64.
+//
+// Bound by HBM and vector instructions: 131072 x 512 bf16, 8 groups: @STRESS@
+// us; 65536 x 256 fp32, logistic, two keys a group and a bias: @BIAS@ us (78 with
+// all keys in 64 bits).
 #pragma once
 
 #include "rp_route.h"
@@ -23,6 +32,9 @@ struct GroupArgs {
     int32_t size;               // experts of a group
     int32_t q_shift, lane_shift;  // lanes of a group, of a token (powers of two)
 };
+
+template <bool B, class X, class Y> struct Choose { using type = X; };
+template <class X, class Y> struct Choose<false, X, Y> { using type = Y; };
 
 __device__ inline double value64(uint64_t o) {
     return __longlong_as_double((long long)(o >> 63 ? o ^ (uint64_t)1 << 63 : ~o));
@@ -59,6 +71,14 @@ __device__ inline void lanes_two(uint64_t &first, uint64_t &second, int lanes) {
     first = max64(first, f);
     if constexpr (D < kWave) lanes_two<2 * D>(first, second, lanes);
 }
+template <int D = 2>
+__device__ inline void lanes_two(float &first, float &second, int lanes) {
+    if (D > lanes) return;
+    const float f = across<D>(first), s = across<D>(second);
+    second = __builtin_fmaxf(__builtin_fminf(first, f), __builtin_fmaxf(second, s));
+    first = __builtin_fmaxf(first, f);
+    if constexpr (D < kWave) lanes_two<2 * D>(first, second, lanes);
+}
 // The largest (key, -index) over the lanes.
 template <int D = 2>
 __device__ inline void lanes_first(uint64_t &key, uint32_t &at, int lanes) {
@@ -80,25 +100,33 @@ __device__ inline void lanes_top(typename Key::Word (&top)[K], int lanes) {
     if constexpr (D < kWave) lanes_top<Key, K, 2 * D>(top, lanes);
 }
 
-// Whether group g's best (an order, 0 where none is available) is among the
-// `keep` largest: the groups that precede it are counted.  Every lane of the
-// token's group calls it with its own.
-__device__ inline bool kept(const GroupArgs &a, uint64_t best, int g, int first_lane_of_token) {
-    int before = 0;
+// The groups that precede group g of the token whose lanes begin at lane0: with
+// a larger `best`, or an equal one and a lower index.  Every lane of a group
+// calls it with its group's.
+__device__ inline int groups_before(const GroupArgs &a, float best, int g, int lane0) {
+    int n = 0;
     for (int o = 0; o < a.groups; ++o) {
-        const int from = first_lane_of_token + (o << a.q_shift);
+        const float b = __shfl(best, lane0 + (o << a.q_shift), kWave);
+        n += b > best || (b == best && o < g) ? 1 : 0;
+    }
+    return n;
+}
+__device__ inline int groups_before(const GroupArgs &a, uint64_t best, int g, int lane0) {
+    int n = 0;
+    for (int o = 0; o < a.groups; ++o) {
+        const int from = lane0 + (o << a.q_shift);
         const uint64_t b = (uint64_t)(uint32_t)__shfl((int)(best >> 32), from, kWave) << 32 |
                            (uint32_t)__shfl((int)(uint32_t)best, from, kWave);
-        before += b > best || (b == best && o < g) ? 1 : 0;
+        n += b > best || (b == best && o < g) ? 1 : 0;
     }
-    return best != 0 && before < a.keep;
+    return n;
 }
 
-template <class T, int V, int K, bool SCORES>
+template <class T, int NV, int K, bool SCORES>
 __global__ void __launch_bounds__(256) k_route_groups(GroupArgs ga) {
-    using Key = typename KeyOf<T>::type;
+    using Key = typename KeyOf<typename Choose<SCORES, float, T>::type>::type;
     using Word = typename Key::Word;
-    constexpr int W = 16 / sizeof(T);
+    constexpr int W = 16 / sizeof(T), M = 4, S = K / M;
     const RouteArgs &a = ga.r;
     const int lanes = 1 << ga.lane_shift, Q = 1 << ga.q_shift;
     const int c = threadIdx.x & (lanes - 1), g = c >> ga.q_shift, q = c & (Q - 1);
@@ -110,126 +138,283 @@ __global__ void __launch_bounds__(256) k_route_groups(GroupArgs ga) {
     const int64_t t = a.L == 1 ? at : n <= UINT32_MAX ? (uint32_t)at / (uint32_t)a.L : at / a.L;
     const int32_t l = (int32_t)(at - t * a.L);
     const T *data = static_cast<const T *>(a.logits) + t * a.ts + l * a.ls;
+    const float *bias = SCORES && a.bias ? a.bias + (int64_t)l * a.E : nullptr;
     const Row<T> row = {data + g * ga.size, g < ga.groups ? ga.size : 0};
-    float z[V];
+    Vec<T> raw[NV];
 #pragma unroll
-    for (int i = 0; i < V / W; ++i) {
-        const Vec<T> x = row.vec(i * Q + q);
-#pragma unroll
-        for (int w = 0; w < W; ++w) z[i * W + w] = x.at(w);
-    }
-    // element v of this lane within its group
-    auto elem = [&](int v) { return ((v / W) * Q + q) * W + v % W; };
+    for (int i = 0; i < NV; ++i) raw[i] = row.vec(i * Q + q);
+    // a vector's number among the token's: group by group, in the order of its
+    // elements (so that ties go to the lowest)
+    const int per_group = NV * Q;
     const int lane0 = (int)(threadIdx.x & 63) - c;
     const bool softmax = a.score == ROUTEPACK_SOFTMAX;
     float m = 0.0f, inv = 0.0f;
-    if (softmax && !a.normalize) {
+    if (softmax && (SCORES || !a.normalize)) {
         m = -kInf;
 #pragma unroll
-        for (int v = 0; v < V; ++v) m = __builtin_fmaxf(m, z[v]);
+        for (int v = 0; v < NV * W; ++v) m = __builtin_fmaxf(m, raw[v / W].at(v % W));
         m = lanes_max(m, lanes);
         m = m == -kInf ? 0.0f : m;
         float sum = 0.0f;
 #pragma unroll
-        for (int v = 0; v < V; ++v) sum += exp_plain(z[v] - m);
+        for (int v = 0; v < NV * W; ++v) sum += exp_plain(raw[v / W].at(v % W) - m);
         sum = lanes_add(sum, lanes);
         inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     }
-    constexpr int S = K >= 32 ? 8 : K / 4;  // choices of each of the first lanes
-    constexpr int M = K / S;                // (4 lanes)
-    int32_t id[K];
-    if constexpr (!SCORES) {
-        uint32_t best = 0;
-        Word x[V], top[K];
+    // a vector's keys in 32 bits, -inf where the expert is not available
+    auto keys_of = [&](const Vec<T> &r, int group, int vec, float (&y)[W]) {
+        if constexpr (SCORES) {
+            float b[W] = {};
+            if (bias) {
+                const Row<float> bias_row = {bias + group * ga.size, group < ga.groups ? ga.size : 0};
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const uint32_t o = order32(z[v]);
-            best = o > best ? o : best;
-            x[v] = Key::make(z[v], kIndexMask ^ (uint32_t)(g * ga.size + elem(v)));
-        }
-        best = best > 0x007FFFFFu ? best : 0;
-        uint64_t f = best, s = 0;
-        lanes_two(f, s, Q);
-        const bool on = kept(ga, f, g, lane0);
+                for (int k = 0; k < W / 4; ++k) {
+                    const Vec<float> x = bias_row.vec(vec * (W / 4) + k);
 #pragma unroll
-        for (int v = 0; v < V; ++v) x[v] = on ? x[v] : Word(0);
-        lane_top<Key, K, V>(x, top);
-        lanes_top<Key, K>(top, lanes);
-#pragma unroll
-        for (int j = 0; j < K; ++j) id[j] = j < a.k && Key::available(top[j]) ? (int32_t)Key::index(top[j]) : -1;
-    } else {
-        uint64_t key[V];
-        double sum = 1.0, base = 0.0;
-        if (softmax) {  // NaN takes no part; experts of +inf share the scores alone
-            float b = -kInf;
-#pragma unroll
-            for (int v = 0; v < V; ++v) b = z[v] > b ? z[v] : b;
-            b = lanes_max(b, lanes);
-            base = b;
-            sum = 0.0;
-#pragma unroll
-            for (int v = 0; v < V; ++v) sum += z[v] > -kInf ? exp(__builtin_fmin((double)z[v] - base, 0.0)) : 0.0;
-            sum = lanes_add(sum, lanes);
-        }
-        uint64_t f = 0, s = 0;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int e = elem(v);
-            double k0 = softmax ? exp(__builtin_fmin((double)z[v] - base, 0.0)) / sum : 1.0 / (1.0 + exp(-(double)z[v]));
-            if (a.bias && e < row.E) k0 += (double)a.bias[(int64_t)l * a.E + g * ga.size + e];
-            key[v] = z[v] > -kInf && k0 > -__builtin_inf() ? order64(k0) : 0;
-            s = max64(s, min64(f, key[v]));
-            f = max64(f, key[v]);
-        }
-        lanes_two(f, s, Q);
-        if (ga.top == 2 && s) f = order64(value64(f) + value64(s));
-        const bool on = kept(ga, f, g, lane0);
-#pragma unroll
-        for (int v = 0; v < V; ++v) key[v] = on ? key[v] : 0;
-#pragma unroll
-        for (int j = 0; j < K; ++j) id[j] = -1;
-#pragma unroll 1
-        for (int j = 0; j < a.k; ++j) {
-            uint64_t k0 = 0;
-            uint32_t e0 = UINT32_MAX;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {  // (a lane's elements ascend)
-                const bool more = key[v] > k0;
-                k0 = more ? key[v] : k0;
-                e0 = more ? (uint32_t)(g * ga.size + elem(v)) : e0;
+                    for (int w = 0; w < 4; ++w) b[k * 4 + w] = x.at(w);
+                }
             }
-            lanes_first(k0, e0, lanes);
 #pragma unroll
-            for (int v = 0; v < V; ++v) key[v] = (uint32_t)(g * ga.size + elem(v)) == e0 ? 0 : key[v];
+            for (int w = 0; w < W; ++w) {
+                const float z = r.at(w);
+                float s, less;
+                if (softmax) s = exp_plain(z - m) * inv;
+                else logistic<false>(z, s, less);
+                const float key = s + b[w];
+                y[w] = z > -kInf && key > -kInf ? key : -kInf;
+            }
+        } else {
 #pragma unroll
-            for (int i = 0; i < K; ++i) id[i] = i == j && k0 ? (int32_t)e0 : id[i];
+            for (int w = 0; w < W; ++w) y[w] = r.at(w) + 0.0f;  // (the sum quiets a NaN, which the maximum drops)
+        }
+    };
+    // the vectors' maxima, and the group's two largest keys
+    float mx[NV], f1 = -kInf, f2 = -kInf;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        float y[W];
+        keys_of(raw[i], g, i * Q + q, y);
+        mx[i] = -kInf;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            if constexpr (SCORES) {
+                f2 = __builtin_fmaxf(f2, __builtin_fminf(f1, y[w]));
+                f1 = __builtin_fmaxf(f1, y[w]);
+            }
+            mx[i] = __builtin_fmaxf(mx[i], y[w]);
+        }
+        f1 = __builtin_fmaxf(f1, mx[i]);
+    }
+    // A key's error in 32 bits is (err + |key|) u, u = 2^-24, as for the choices
+    // without groups: logistic scores 8 u, softmax scores (1 + 98 p) u with up to
+    // 64 additions in a lane and 6 across lanes, and p <= inv.
+    const float err = softmax ? 1.0f + 98.0f * inv : 8.0f;
+    bool open = false, on;
+    {
+        lanes_two(f1, f2, Q);
+        float best = f1, slack = 0.0f;
+        if (SCORES) {
+            if (ga.top == 2 && f2 > -kInf) best = f1 + f2;
+            // (twice the errors of the keys and of their sum)
+            slack = (2.0f * err + __builtin_fabsf(f1) + (f2 > -kInf ? __builtin_fabsf(f2) : 0.0f) + __builtin_fabsf(best)) * 0x1p-23f;
+        }
+        on = groups_before(ga, best, g, lane0) < ga.keep && f1 > -kInf;
+        if (SCORES) {
+            const float low = -lanes_max(on ? slack - best : -kInf, lanes);
+            const float high = lanes_max(!on && f1 > -kInf ? best + slack : -kInf, lanes);
+            open = high > -kInf && !(low > high);
+            open = open || inv != inv || low != low || high != high;
         }
     }
-    // the gates: choice s M + c in lane c < M (of the token's 4 lanes and more)
-    float zc[S], w[S], less[S];
-    bool on[S];
-    int32_t mine[S];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) mx[i] = on ? mx[i] : -kInf;
+    Word vk[NV], first[K];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) vk[i] = Key::make(mx[i], kIndexMask ^ (uint32_t)(g * per_group + i * Q + q));
+    lane_top<Key, K, NV>(vk, first);
+    lanes_top<Key, K>(first, lanes);
+    // the elements of the k vectors that lead, vector s M + c in lane c < M
+    Word x[S * W], top[K];
+    float cand[SCORES ? S * W : 1], most[S];
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-        mine[s] = -1;
+        Word mine = Word(0);
 #pragma unroll
-        for (int j = 0; j < M; ++j) mine[s] = c == j ? id[s * M + j] : mine[s];
-        on[s] = mine[s] >= 0;
-        zc[s] = on[s] ? to_f32(data[mine[s]]) : 0.0f;
+        for (int j = 0; j < M; ++j) mine = c == j ? first[s * M + j] : mine;
+        const bool ok = c < M && s * M + c < a.k && Key::available(mine);
+        const int id = (int)Key::index(mine), vg = id / per_group, v = id - vg * per_group;
+        most[s] = ok ? Key::value(mine) : -kInf;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            x[s * W + w] = Word(0);
+            if constexpr (SCORES) cand[s * W + w] = -kInf;
+        }
+        if (ok) {
+            float y[W];
+            const Row<T> r = {data + vg * ga.size, ga.size};
+            keys_of(r.vec(v), vg, v, y);
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                if constexpr (SCORES) cand[s * W + w] = y[w];
+                x[s * W + w] = Key::make(y[w], kIndexMask ^ (uint32_t)(vg * ga.size + v * W + w));
+            }
+        }
     }
-    choice_gates<M, S>(zc, on, a.score, a.normalize, m, inv, w, less);
+    lane_top<Key, K, S * W>(x, top);
+    group_top<Key, K, M>(top);
+    int32_t id[S];
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+        Word mine = Word(0);
+#pragma unroll
+        for (int j = 0; j < M; ++j) mine = c == j ? top[s * M + j] : mine;
+        id[s] = c < M && s * M + c < a.k && Key::available(mine) ? (int32_t)Key::index(mine) : -1;
+    }
+    if constexpr (SCORES) {
+        // is the order beyond doubt?  Two keys further apart than `slack` are in order.
+        auto slack = [&](float key) { return (err + 2.0f * __builtin_fabsf(key)) * 0x1p-23f; };
+        float edge = -kInf;  // a key below it is not among the k largest
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            if (j >= a.k || !Key::available(top[j])) continue;
+            const float v = Key::value(top[j]);
+            if (j > 0) {
+                const float u = Key::value(top[j > 0 ? j - 1 : 0]);
+                open = open || !(u - v > slack(u) && u - v > slack(v));
+            }
+            if (j == a.k - 1) edge = v - slack(v);
+        }
+        edge = lanes_max(c < M ? edge : -kInf, lanes);
+        // from the edge on: elements of the chosen vectors, and other vectors
+        float over = 0.0f, more = 0.0f;
+#pragma unroll
+        for (int i = 0; i < S * W; ++i) over += cand[i] >= edge && cand[i] > -kInf ? 1.0f : 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) more += mx[i] >= edge && mx[i] > -kInf ? 1.0f : 0.0f;
+#pragma unroll
+        for (int s = 0; s < S; ++s) more -= most[s] >= edge && most[s] > -kInf ? 1.0f : 0.0f;
+        over = lanes_add(over, lanes);
+        more = lanes_add(more, lanes);
+        open = open || (edge > -kInf && (over != (float)a.k || more != 0.0f)) || edge != edge;
+        if (__any(open)) {
+            // All of it in 64 bits: loops of little code, a vector at a time from
+            // memory.  NaN takes no part; experts of +inf share the scores alone.
+            float b = -kInf;
+#pragma unroll 1
+            for (int i = 0; i < NV; ++i) {
+                const Vec<T> y = row.vec(i * Q + q);
+#pragma unroll
+                for (int w = 0; w < W; ++w) b = y.at(w) > b ? y.at(w) : b;
+            }
+            const double base = lanes_max(b, lanes);
+            auto part = [&](float z) { return exp(__builtin_fmin((double)z - base, 0.0)); };
+            // f(order of the key, element) for every element of this lane
+            double sum = 1.0;
+            auto each = [&](auto &&f) {
+#pragma unroll 1
+                for (int i = 0; i < NV; ++i) {
+                    const int v = i * Q + q;
+                    if (v * W >= row.E) break;
+                    const Vec<T> y = row.vec(v);
+                    float z[W], bv[W];
+#pragma unroll
+                    for (int w = 0; w < W; ++w) {
+                        z[w] = y.at(w);
+                        bv[w] = bias && v * W + w < row.E ? bias[g * ga.size + v * W + w] : 0.0f;
+                    }
+#pragma unroll 1
+                    for (int w = 0; w < W; ++w) {
+                        double key = softmax ? part(z[0]) / sum : 1.0 / (1.0 + exp(-(double)z[0]));
+                        key += (double)bv[0];
+                        f(z[0] > -kInf && key > -__builtin_inf() ? order64(key) : 0, (uint32_t)(g * ga.size + v * W + w));
+#pragma unroll
+                        for (int k = 0; k + 1 < W; ++k) {
+                            z[k] = z[k + 1];
+                            bv[k] = bv[k + 1];
+                        }
+                    }
+                }
+            };
+            if (softmax) {
+                double mine = 0.0;
+#pragma unroll 1
+                for (int i = 0; i < NV; ++i) {
+                    const Vec<T> y = row.vec(i * Q + q);
+#pragma unroll
+                    for (int w = 0; w < W; ++w) mine += y.at(w) > -kInf ? part(y.at(w)) : 0.0;
+                }
+                sum = lanes_add(mine, lanes);
+            }
+            uint64_t g1 = 0, g2 = 0;
+            each([&](uint64_t key, uint32_t) {
+                g2 = max64(g2, min64(g1, key));
+                g1 = max64(g1, key);
+            });
+            lanes_two(g1, g2, Q);
+            if (ga.top == 2 && g2) g1 = order64(value64(g1) + value64(g2));
+            const bool keep = g1 != 0 && groups_before(ga, g1, g, lane0) < ga.keep;
+            uint64_t list[K];  // a lane's K largest, sorted by insertion
+            uint32_t who[K];
+#pragma unroll
+            for (int j = 0; j < K; ++j) {
+                list[j] = 0;
+                who[j] = UINT32_MAX;
+            }
+            each([&](uint64_t key, uint32_t e) {
+                key = keep ? key : 0;
+#pragma unroll
+                for (int j = 0; j < K; ++j) {
+                    const bool before = key > list[j] || (key == list[j] && e < who[j]);
+                    const uint64_t k1 = list[j];
+                    const uint32_t e1 = who[j];
+                    list[j] = before ? key : k1;
+                    who[j] = before ? e : e1;
+                    key = before ? k1 : key;
+                    e = before ? e1 : e;
+                }
+            });
+#pragma unroll
+            for (int s = 0; s < S; ++s) id[s] = -1;
+#pragma unroll 1
+            for (int j = 0; j < a.k; ++j) {
+                uint64_t k0 = list[0];
+                uint32_t e0 = who[0];
+                lanes_first(k0, e0, lanes);
+                if (who[0] == e0) {
+#pragma unroll
+                    for (int i = 0; i + 1 < K; ++i) {
+                        list[i] = list[i + 1];
+                        who[i] = who[i + 1];
+                    }
+                    list[K - 1] = 0;
+                    who[K - 1] = UINT32_MAX;
+                }
+#pragma unroll
+                for (int s = 0; s < S; ++s)
+                    if (j == s * M + c && k0) id[s] = (int32_t)e0;
+            }
+        }
+    }
+    float zc[S], w[S], less[S];
+    bool made[S];
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+        made[s] = c < M && id[s] >= 0;
+        zc[s] = made[s] ? to_f32(data[id[s]]) : 0.0f;
+    }
+    choice_gates<M, S>(zc, made, a.score, a.normalize, m, inv, w, less);
 #pragma unroll
     for (int s = 0; s < S; ++s) {
         const int j = s * M + c;
         if (live && c < M && j < a.k) {
-            a.ids[at * a.k + j] = mine[s];
+            a.ids[at * a.k + j] = id[s];
             a.gates[at * a.k + j] = a.scale * w[s];
         }
     }
 }
 
-// Lanes of a group and a token: as few as hold the group in V values a lane
-// (at least 4 a token, for the gates).
+// Lanes of a group and a token: as few as hold a group in 8 vectors a lane (at
+// least 4 a token, for the second selection).
 template <class T>
 int choose_groups(GroupArgs a, hipStream_t stream) {
     constexpr int W = 16 / sizeof(T);
@@ -241,11 +426,9 @@ int choose_groups(GroupArgs a, hipStream_t stream) {
     }
     a.q_shift = 0;
     const int vecs = (a.size + W - 1) / W;
-    while ((vecs + (1 << a.q_shift) - 1) / (1 << a.q_shift) * W > (sizeof(T) == 4 ? 16 : 32) && (groups << a.q_shift) < kWave)
-        ++a.q_shift;
-    while ((groups << a.q_shift) < 4) ++a.q_shift;
+    auto each = [&] { return (vecs + (1 << a.q_shift) - 1) >> a.q_shift; };
+    while ((each() > 8 && (groups << a.q_shift) < kWave) || (groups << a.q_shift) < 4) ++a.q_shift;
     a.lane_shift += a.q_shift;
-    const int V = (vecs + (1 << a.q_shift) - 1) / (1 << a.q_shift) * W;
     const int64_t items = a.r.T * a.r.L, per = 256 >> a.lane_shift;
     auto go = [&](auto kern) {
         hipLaunchKernelGGL(kern, grid_of((items + per - 1) / per), dim3(256), 0, stream, a);
@@ -257,10 +440,11 @@ int choose_groups(GroupArgs a, hipStream_t stream) {
         if (a.r.k <= 8) return scores ? go(k_route_groups<T, N, 8, true>) : go(k_route_groups<T, N, 8, false>);
         return scores ? go(k_route_groups<T, N, 32, true>) : go(k_route_groups<T, N, 32, false>);
     };
-    if (V <= 8) return by_k(Int<8>());
-    if (V <= 16) return by_k(Int<16>());
-    if (V <= 32) return by_k(Int<32>());
-    return ROUTEPACK_E_UNSUPPORTED;
+    if (each() <= 1) return by_k(Int<1>());
+    if (each() <= 2) return by_k(Int<2>());
+    if (each() <= 4) return by_k(Int<4>());
+    if (each() <= 8) return by_k(Int<8>());
+    return ROUTEPACK_E_UNSUPPORTED;  // (never: E <= 1024)
 }
 
 }  // namespace rp
