@@ -24,19 +24,6 @@
 
 namespace rp {
 
-// The largest of a vector's elements; NaN where it holds one (the instruction
-// that drops a quiet NaN returns a signalling one, and the next would drop that
-// with the elements before it).
-__device__ inline float max3(float a, float b, float c) {
-    float d;
-    asm("v_maximum3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
-    return d;
-}
-__device__ inline float most_of(const float (&x)[4]) { return max3(max3(x[0], x[1], x[2]), x[3], x[3]); }
-__device__ inline float most_of(const float (&x)[8]) {
-    return max3(max3(max3(x[0], x[1], x[2]), x[3], x[4]), max3(x[5], x[6], x[7]), x[7]);
-}
-
 template <class T, int G, int NV, int K>
 __global__ void __launch_bounds__(256) k_route(RouteArgs a) {
     using Key = typename KeyOf<T>::type;

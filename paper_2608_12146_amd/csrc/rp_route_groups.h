@@ -103,18 +103,18 @@ __device__ inline void lanes_top(typename Key::Word (&top)[K], int lanes) {
 // The groups that precede group g of the token whose lanes begin at lane0: with
 // a larger `best`, or an equal one and a lower index.  Every lane of a group
 // calls it with its group's.
-__device__ inline int groups_before(const GroupArgs &a, float best, int g, int lane0) {
+__device__ inline int groups_before(int groups, int q_shift, float best, int g, int lane0) {
     int n = 0;
-    for (int o = 0; o < a.groups; ++o) {
-        const float b = __shfl(best, lane0 + (o << a.q_shift), kWave);
+    for (int o = 0; o < groups; ++o) {
+        const float b = __shfl(best, lane0 + (o << q_shift), kWave);
         n += b > best || (b == best && o < g) ? 1 : 0;
     }
     return n;
 }
-__device__ inline int groups_before(const GroupArgs &a, uint64_t best, int g, int lane0) {
+__device__ inline int groups_before(int groups, int q_shift, uint64_t best, int g, int lane0) {
     int n = 0;
-    for (int o = 0; o < a.groups; ++o) {
-        const int from = lane0 + (o << a.q_shift);
+    for (int o = 0; o < groups; ++o) {
+        const int from = lane0 + (o << q_shift);
         const uint64_t b = (uint64_t)(uint32_t)__shfl((int)(best >> 32), from, kWave) << 32 |
                            (uint32_t)__shfl((int)(uint32_t)best, from, kWave);
         n += b > best || (b == best && o < g) ? 1 : 0;
@@ -149,11 +149,30 @@ __global__ void __launch_bounds__(256) k_route_groups(GroupArgs ga) {
     const int lane0 = (int)(threadIdx.x & 63) - c;
     const bool softmax = a.score == ROUTEPACK_SOFTMAX;
     float m = 0.0f, inv = 0.0f;
-    if (softmax && (SCORES || !a.normalize)) {
-        m = -kInf;
+    float mx[NV], f1 = -kInf, f2 = -kInf;  // the vectors' largest logits, then keys
+    if (!SCORES || softmax) {
+        bool odd = false;
 #pragma unroll
-        for (int v = 0; v < NV * W; ++v) m = __builtin_fmaxf(m, raw[v / W].at(v % W));
-        m = lanes_max(m, lanes);
+        for (int i = 0; i < NV; ++i) {
+            float x[W];
+#pragma unroll
+            for (int w = 0; w < W; ++w) x[w] = raw[i].at(w);
+            mx[i] = most_of(x);
+            odd = odd || mx[i] != mx[i];
+        }
+        if (__any(odd)) {  // NaN takes no part (the sum quiets it, the maximum drops it)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                mx[i] = -kInf;
+#pragma unroll
+                for (int w = 0; w < W; ++w) mx[i] = __builtin_fmaxf(mx[i], raw[i].at(w) + 0.0f);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) f1 = __builtin_fmaxf(f1, mx[i]);
+    }
+    if (softmax && (SCORES || !a.normalize)) {
+        m = lanes_max(f1, lanes);
         m = m == -kInf ? 0.0f : m;
         float sum = 0.0f;
 #pragma unroll
@@ -185,25 +204,24 @@ __global__ void __launch_bounds__(256) k_route_groups(GroupArgs ga) {
             }
         } else {
 #pragma unroll
-            for (int w = 0; w < W; ++w) y[w] = r.at(w) + 0.0f;  // (the sum quiets a NaN, which the maximum drops)
+            for (int w = 0; w < W; ++w) y[w] = r.at(w);
         }
     };
-    // the vectors' maxima, and the group's two largest keys
-    float mx[NV], f1 = -kInf, f2 = -kInf;
+    // the vectors' largest keys, and the group's two
+    if constexpr (SCORES) {
+        f1 = -kInf;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        float y[W];
-        keys_of(raw[i], g, i * Q + q, y);
-        mx[i] = -kInf;
+        for (int i = 0; i < NV; ++i) {
+            float y[W];
+            keys_of(raw[i], g, i * Q + q, y);
+            mx[i] = -kInf;
 #pragma unroll
-        for (int w = 0; w < W; ++w) {
-            if constexpr (SCORES) {
+            for (int w = 0; w < W; ++w) {
                 f2 = __builtin_fmaxf(f2, __builtin_fminf(f1, y[w]));
                 f1 = __builtin_fmaxf(f1, y[w]);
+                mx[i] = __builtin_fmaxf(mx[i], y[w]);
             }
-            mx[i] = __builtin_fmaxf(mx[i], y[w]);
         }
-        f1 = __builtin_fmaxf(f1, mx[i]);
     }
     // A key's error in 32 bits is (err + |key|) u, u = 2^-24, as for the choices
     // without groups: logistic scores 8 u, softmax scores (1 + 98 p) u with up to
@@ -218,7 +236,7 @@ __global__ void __launch_bounds__(256) k_route_groups(GroupArgs ga) {
             // (twice the errors of the keys and of their sum)
             slack = (2.0f * err + __builtin_fabsf(f1) + (f2 > -kInf ? __builtin_fabsf(f2) : 0.0f) + __builtin_fabsf(best)) * 0x1p-23f;
         }
-        on = groups_before(ga, best, g, lane0) < ga.keep && f1 > -kInf;
+        on = groups_before(ga.groups, ga.q_shift, best, g, lane0) < ga.keep && f1 > -kInf;
         if (SCORES) {
             const float low = -lanes_max(on ? slack - best : -kInf, lanes);
             const float high = lanes_max(!on && f1 > -kInf ? best + slack : -kInf, lanes);
@@ -296,63 +314,56 @@ __global__ void __launch_bounds__(256) k_route_groups(GroupArgs ga) {
         over = lanes_add(over, lanes);
         more = lanes_add(more, lanes);
         open = open || (edge > -kInf && (over != (float)a.k || more != 0.0f)) || edge != edge;
-        if (__any(open)) {
-            // All of it in 64 bits: loops of little code, a vector at a time from
-            // memory.  NaN takes no part; experts of +inf share the scores alone.
-            float b = -kInf;
-#pragma unroll 1
-            for (int i = 0; i < NV; ++i) {
-                const Vec<T> y = row.vec(i * Q + q);
-#pragma unroll
-                for (int w = 0; w < W; ++w) b = y.at(w) > b ? y.at(w) : b;
-            }
-            const double base = lanes_max(b, lanes);
+        // The tokens in doubt, one at a time by the whole wave, in 64 bits: loops of
+        // little code, an element at a time from memory, a group in as many lanes as
+        // fit 64 (a wave that took them by their own lanes took 15 us, and kept the
+        // rest waiting).  NaN takes no part; experts of +inf share the scores alone.
+        int q_shift = 0;
+        while ((ga.groups << (q_shift + 1)) <= kWave) ++q_shift;
+        for (uint64_t todo = __ballot(open); todo;) {
+            const int from = __builtin_amdgcn_readfirstlane(__builtin_ctzll(todo) & ~(lanes - 1));
+            const uint64_t its = (lanes == kWave ? ~(uint64_t)0 : ((uint64_t)1 << lanes) - 1) << from;
+            todo &= ~its;
+            const int lane = threadIdx.x & 63, group = lane >> q_shift, step = 1 << q_shift;
+            const int64_t where = (int64_t)readlane64((uint64_t)(uintptr_t)data, from);
+            const int64_t what = (int64_t)readlane64((uint64_t)(uintptr_t)bias, from);
+            const int count = group < ga.groups ? ga.size : 0;
+            const T *z_of = reinterpret_cast<const T *>(where) + group * ga.size;
+            const float *b_of = reinterpret_cast<const float *>(what) + group * ga.size;
+            double base = 0.0, sum = 1.0;
             auto part = [&](float z) { return exp(__builtin_fmin((double)z - base, 0.0)); };
-            // f(order of the key, element) for every element of this lane
-            double sum = 1.0;
-            auto each = [&](auto &&f) {
-#pragma unroll 1
-                for (int i = 0; i < NV; ++i) {
-                    const int v = i * Q + q;
-                    if (v * W >= row.E) break;
-                    const Vec<T> y = row.vec(v);
-                    float z[W], bv[W];
-#pragma unroll
-                    for (int w = 0; w < W; ++w) {
-                        z[w] = y.at(w);
-                        bv[w] = bias && v * W + w < row.E ? bias[g * ga.size + v * W + w] : 0.0f;
-                    }
-#pragma unroll 1
-                    for (int w = 0; w < W; ++w) {
-                        double key = softmax ? part(z[0]) / sum : 1.0 / (1.0 + exp(-(double)z[0]));
-                        key += (double)bv[0];
-                        f(z[0] > -kInf && key > -__builtin_inf() ? order64(key) : 0, (uint32_t)(g * ga.size + v * W + w));
-#pragma unroll
-                        for (int k = 0; k + 1 < W; ++k) {
-                            z[k] = z[k + 1];
-                            bv[k] = bv[k + 1];
-                        }
-                    }
-                }
-            };
             if (softmax) {
+                float b = -kInf;
+#pragma unroll 1
+                for (int e = lane & (step - 1); e < count; e += step) {
+                    const float z = to_f32(z_of[e]);
+                    b = z > b ? z : b;
+                }
+                base = lanes_max(b, kWave);
                 double mine = 0.0;
 #pragma unroll 1
-                for (int i = 0; i < NV; ++i) {
-                    const Vec<T> y = row.vec(i * Q + q);
-#pragma unroll
-                    for (int w = 0; w < W; ++w) mine += y.at(w) > -kInf ? part(y.at(w)) : 0.0;
+                for (int e = lane & (step - 1); e < count; e += step) {
+                    const float z = to_f32(z_of[e]);
+                    mine += z > -kInf ? part(z) : 0.0;
                 }
-                sum = lanes_add(mine, lanes);
+                sum = lanes_add(mine, kWave);
             }
+            auto key_at = [&](int e) -> uint64_t {
+                const float z = to_f32(z_of[e]);
+                double key = softmax ? part(z) / sum : 1.0 / (1.0 + exp(-(double)z));
+                if (what) key += (double)b_of[e];
+                return z > -kInf && key > -__builtin_inf() ? order64(key) : 0;
+            };
             uint64_t g1 = 0, g2 = 0;
-            each([&](uint64_t key, uint32_t) {
+#pragma unroll 1
+            for (int e = lane & (step - 1); e < count; e += step) {
+                const uint64_t key = key_at(e);
                 g2 = max64(g2, min64(g1, key));
                 g1 = max64(g1, key);
-            });
-            lanes_two(g1, g2, Q);
+            }
+            lanes_two(g1, g2, step);
             if (ga.top == 2 && g2) g1 = order64(value64(g1) + value64(g2));
-            const bool keep = g1 != 0 && groups_before(ga, g1, g, lane0) < ga.keep;
+            const bool keep = g1 != 0 && groups_before(ga.groups, q_shift, g1, group, 0) < ga.keep;
             uint64_t list[K];  // a lane's K largest, sorted by insertion
             uint32_t who[K];
 #pragma unroll
@@ -360,8 +371,10 @@ __global__ void __launch_bounds__(256) k_route_groups(GroupArgs ga) {
                 list[j] = 0;
                 who[j] = UINT32_MAX;
             }
-            each([&](uint64_t key, uint32_t e) {
-                key = keep ? key : 0;
+#pragma unroll 1
+            for (int e0 = lane & (step - 1); e0 < (keep ? count : 0); e0 += step) {
+                uint64_t key = key_at(e0);
+                uint32_t e = (uint32_t)(group * ga.size + e0);
 #pragma unroll
                 for (int j = 0; j < K; ++j) {
                     const bool before = key > list[j] || (key == list[j] && e < who[j]);
@@ -372,14 +385,13 @@ __global__ void __launch_bounds__(256) k_route_groups(GroupArgs ga) {
                     key = before ? k1 : key;
                     e = before ? e1 : e;
                 }
-            });
-#pragma unroll
-            for (int s = 0; s < S; ++s) id[s] = -1;
+            }
+            const bool its_lane = its >> lane & 1;
 #pragma unroll 1
             for (int j = 0; j < a.k; ++j) {
                 uint64_t k0 = list[0];
                 uint32_t e0 = who[0];
-                lanes_first(k0, e0, lanes);
+                lanes_first(k0, e0, kWave);
                 if (who[0] == e0) {
 #pragma unroll
                     for (int i = 0; i + 1 < K; ++i) {
@@ -391,7 +403,7 @@ __global__ void __launch_bounds__(256) k_route_groups(GroupArgs ga) {
                 }
 #pragma unroll
                 for (int s = 0; s < S; ++s)
-                    if (j == s * M + c && k0) id[s] = (int32_t)e0;
+                    if (its_lane && j == s * M + c) id[s] = k0 ? (int32_t)e0 : -1;
             }
         }
     }
