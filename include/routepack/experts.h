@@ -77,13 +77,16 @@ int routepack_order_tokens(const routepack_problem *prob, const routepack_ids *i
  * less 2 (at least -127); its values, divided by that power of two, are rounded
  * to the nearest code, ties to the even one, and end at 6.  A block with NaN or
  * an infinity is NaN (codes 0, scale 255), a block of zeros has scale 0.
- *   rows  NULL, or int32 [q.n_rows]: row r is x's row rows[r] / per_row (the
- *         pairs' tokens, with per_row = k); a negative one gives a row of zeros
+ *   rows, places  NULL, or an order: q's row r is the row of x of the token of
+ *         pair rows[r], where that pair's place is r, else zeros.  rows int32
+ *         [q.n_rows]; places [x.n_rows][1][k] of ROUTEPACK_I32 (the layer stride is
+ *         not looked at)
  * E_INVALID on null pointers, a negative size or stride, an unknown type, other
- * columns in q than in x, other rows without `rows`, per_row < 1 with them, or
- * q misaligned; E_UNSUPPORTED when n_cols > 2^24. */
-int routepack_quantize_mx(const routepack_matrix *x, const int32_t *rows, int32_t per_row,
-                          const routepack_mx *q, hipStream_t stream);
+ * columns in q than in x, one of rows and places, places of other tokens than x's
+ * rows or k < 1 with them, other rows without them, or q misaligned;
+ * E_UNSUPPORTED when n_cols > 2^24, k > 256 or x.n_rows k >= 2^31. */
+int routepack_quantize_mx(const routepack_matrix *x, const int32_t *rows, const routepack_ids *places,
+                          int32_t top_k, const routepack_mx *q, hipStream_t stream);
 
 /* The values of a matrix in 4 bits, in x's type (exact in fp32 and bf16; in
  * fp16 rounded, and infinite beyond its range).  x's row_stride is n_cols.

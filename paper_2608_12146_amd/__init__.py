@@ -114,7 +114,7 @@ def load_library():
         M, X = C.POINTER(_Matrix), C.POINTER(_MxMatrix)
         lib.routepack_order_workspace.argtypes = [P, i64]
         lib.routepack_order_tokens.argtypes = [P, R, vp, vp, vp, vp, vp, i64, vp]
-        lib.routepack_quantize_mx.argtypes = [M, vp, i32, X, vp]
+        lib.routepack_quantize_mx.argtypes = [M, vp, R, i32, X, vp]
         lib.routepack_dequantize_mx.argtypes = [X, M, vp]
         lib.routepack_expert_product.argtypes = [X, X, i32, vp, M, vp]
         lib.routepack_expert_product_backward.argtypes = [M, X, X, i32, vp, M, M, vp]
@@ -817,18 +817,18 @@ def quantize_mx(x, *, order=None):
     if x.dim() == 3 and order is None and x.is_contiguous():
         x = x.view(-1, x.shape[-1]) if x.numel() else x.reshape(lead[0] * lead[1], x.shape[-1])
     shape, m = call.matrix("x", x, floats)
-    rows, per = None, 1
+    rows, p, k = None, None, 1
     if order is not None:
-        places, _ = call.places(order)
-        if places[0] != shape[0]:
-            raise ValueError(f"{call.fn}: the order has {places[0]} tokens, x {shape[0]} rows")
-        lead = (places[0] * places[1],)
-        rows, per = call.dense("order.rows", order.rows, (torch.int32,), lead).data_ptr(), places[1]
+        got, p = call.places(order)
+        if got[0] != shape[0]:
+            raise ValueError(f"{call.fn}: the order has {got[0]} tokens, x {shape[0]} rows")
+        k, lead, p = got[1], (got[0] * got[1],), C.byref(p)
+        rows = call.dense("order.rows", order.rows, (torch.int32,), lead).data_ptr()
     n = (shape[1] + 127) // 128
     codes = torch.empty((*lead, 64 * n), dtype=torch.uint8, device=call.device)
     scales = torch.empty((*lead, 4 * n), dtype=torch.uint8, device=call.device)
     q = _MxMatrix(codes.data_ptr(), scales.data_ptr(), shape[0] if order is None else lead[0], shape[1])
-    call.run(lib.routepack_quantize_mx, C.byref(m), rows, per, C.byref(q))
+    call.run(lib.routepack_quantize_mx, C.byref(m), rows, p, k, C.byref(q))
     return Mx(codes, scales, shape[1])
 
 

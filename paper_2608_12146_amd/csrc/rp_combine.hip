@@ -9,20 +9,16 @@ namespace rp {
 
 struct CombineArgs {
     const void *y;
-    int64_t stride, n_rows;
+    int64_t stride;
     int32_t cols, vecs;        // vectors of 16 bytes a row
     int32_t lt, chunks;        // lanes of a token, vectors / lanes
-    const int32_t *places;
-    int64_t place_stride;
-    int32_t k;
+    OrderView order;           // (rows: of the gradients)
     const float *gates;
     int64_t gate_stride;
-    int64_t T;
     void *out;
     // gradients
     const void *dout;
     int64_t dout_stride;
-    const int32_t *rows;
     void *dy;
     float *dgates;
     int64_t token_groups;      // workgroups of tokens; those behind look for rows of no pair
@@ -54,7 +50,7 @@ __device__ inline void add_rows(const CombineArgs &a, const int32_t *places, con
 #pragma unroll
     for (int j = 0; j < N; ++j) {
         const int64_t r = places[j];
-        on[j] = r >= 0 && r < a.n_rows;
+        on[j] = r >= 0 && r < a.order.n_rows;
         g[j] = gates ? gates[j] : 1.0f;
         x[j] = row_vec<T>(static_cast<const T *>(a.y) + (on[j] ? r : 0) * a.stride, a.cols, c);
     }
@@ -77,29 +73,20 @@ __global__ void __launch_bounds__(256) k_combine(CombineArgs a) {
         t = item <= UINT32_MAX ? (uint32_t)item / (uint32_t)a.chunks : item / a.chunks;
         v += (int32_t)(item - t * a.chunks) * kWave;
     }
-    if (t >= a.T || v >= a.vecs) return;
-    const int32_t *places = a.places + t * a.place_stride;
+    if (t >= a.order.T || v >= a.vecs) return;
+    const int32_t *places = a.order.places + t * a.order.place_stride;
     const float *gates = a.gates ? a.gates + t * a.gate_stride : nullptr;
     float sum[W] = {};
     int j = 0;
-    if (a.n_rows > 0) {
-        for (; j + 4 <= a.k; j += 4) add_rows<T, 4>(a, places + j, gates ? gates + j : nullptr, v * W, sum);
-        if (j + 2 <= a.k) {
+    if (a.order.n_rows > 0) {
+        for (; j + 4 <= a.order.k; j += 4) add_rows<T, 4>(a, places + j, gates ? gates + j : nullptr, v * W, sum);
+        if (j + 2 <= a.order.k) {
             add_rows<T, 2>(a, places + j, gates ? gates + j : nullptr, v * W, sum);
             j += 2;
         }
-        if (j < a.k) add_rows<T, 1>(a, places + j, gates ? gates + j : nullptr, v * W, sum);
+        if (j < a.order.k) add_rows<T, 1>(a, places + j, gates ? gates + j : nullptr, v * W, sum);
     }
     store_vec<T, false>(static_cast<T *>(a.out) + t * a.cols, a.cols, v * W, sum);
-}
-
-// The pair that stands in row r, if its place is r; else -1.
-__device__ inline int64_t pair_of_row(const CombineArgs &a, int64_t r) {
-    const int32_t p = a.rows[r];
-    if (p < 0) return -1;
-    const uint32_t t = (uint32_t)p / (uint32_t)a.k;
-    if (t >= a.T) return -1;
-    return a.places[t * a.place_stride + (p - t * (uint32_t)a.k)] == r ? p : -1;
 }
 
 // The sum over aligned groups of lt lanes.
@@ -108,9 +95,41 @@ __device__ inline float lanes_sum(float v, int lt) {
     return v;
 }
 
-// Gradients of a token: each chunk's dout is held while its k rows are read
-// (for the gates) and written.  NW waves share a token's columns (lt < 64: a
-// wave has several tokens).
+// Rows r[0], .. of N choices j, ..: their products with d are added to dots, and
+// gate times d is written where the row is the pair's.
+template <class T, int N>
+__device__ inline void spread_rows(const CombineArgs &a, const int64_t (&r)[N], const bool (&own)[N], const float (&g)[N],
+                                   int32_t c, const Vec<T> &d, float *dots) {
+    constexpr int W = Vec<T>::W;
+    if (a.dgates) {
+        Vec<T> y[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            y[j] = row_vec<T>(static_cast<const T *>(a.y) + (r[j] >= 0 ? r[j] : 0) * a.stride, a.cols, c);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            float sum = dots[j];
+#pragma unroll
+            for (int w = 0; w < W; ++w) sum = __builtin_fmaf(y[j].at(w), d.at(w), sum);
+            dots[j] = r[j] >= 0 ? sum : dots[j];
+        }
+    }
+    if (a.dy) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            if (!own[j]) continue;
+            float x[W];
+#pragma unroll
+            for (int w = 0; w < W; ++w) x[w] = g[j] * d.at(w);
+            store_vec<T, false>(static_cast<T *>(a.dy) + r[j] * a.cols, a.cols, c, x);
+        }
+    }
+}
+
+// Gradients of a token: each vector of dout is held while the same of its k rows
+// is read (for the gates) and written.  NW > 0: a token has NW waves, which look
+// its rows up once, a lane a choice, and hold them in scalars; NW = 0: a wave has
+// several tokens, of lt lanes.
 template <class T, int K, int NW>
 __global__ void __launch_bounds__(256) k_spread(CombineArgs a) {
     constexpr int W = Vec<T>::W;
@@ -118,7 +137,7 @@ __global__ void __launch_bounds__(256) k_spread(CombineArgs a) {
     if (group_index() >= a.token_groups) {  // rows of no pair: zeros
         const int lane = threadIdx.x & 63;
         const int64_t r0 = (group_index() - a.token_groups) * 256 + (threadIdx.x & ~63);
-        const bool mine = r0 + lane < a.n_rows && pair_of_row(a, r0 + lane) < 0;
+        const bool mine = r0 + lane < a.order.n_rows && a.order.pair_of_row(r0 + lane) < 0;
         for (uint64_t m = __ballot(mine); m; m &= m - 1) {
             T *row = static_cast<T *>(a.dy) + (r0 + __builtin_ctzll(m)) * a.cols;
             const float zero[W] = {};
@@ -126,79 +145,74 @@ __global__ void __launch_bounds__(256) k_spread(CombineArgs a) {
         }
         return;
     }
-    const int lt = NW > 1 ? kWave : a.lt, lane = threadIdx.x & (lt - 1), wave = threadIdx.x >> 6;
-    const int64_t t = NW > 1 ? group_index() * (4 / NW) + wave / NW : group_index() * (256 / lt) + threadIdx.x / lt;
-    const bool live = t < a.T;
+    const int lt = NW ? kWave : a.lt, lane = threadIdx.x & (lt - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t t = NW ? group_index() * (4 / (NW ? NW : 1)) + wave / (NW ? NW : 1) : group_index() * (256 / lt) + threadIdx.x / lt;
+    const bool live = t < a.order.T;
+    const int32_t k = a.order.k;
     float dots[K] = {};
     if (live) {
-        const int32_t *places = a.places + t * a.place_stride;
+        const int32_t *places = a.order.places + t * a.order.place_stride;
         const float *gates = a.gates ? a.gates + t * a.gate_stride : nullptr;
         const T *dout = static_cast<const T *>(a.dout) + t * a.dout_stride;
-        for (int32_t v = lane + wave % NW * kWave; v < a.vecs; v += lt * NW) {
+        auto look_up = [&](int j, bool &own, float &g) -> int {
+            const int32_t r = places[j];
+            const bool on = r >= 0 && r < a.order.n_rows;
+            own = on && a.dy && a.order.rows[r] == t * k + j;
+            g = gates ? gates[j] : 1.0f;
+            return on ? r : -1;
+        };
+        int mine = -1;
+        bool mine_own = false;
+        float mine_gate = 0.0f;
+        if (NW && lane < k) mine = look_up(lane, mine_own, mine_gate);
+        for (int32_t v = lane + (NW ? wave % (NW ? NW : 1) * kWave : 0); v < a.vecs; v += lt * (NW ? NW : 1)) {
             const Vec<T> d = row_vec<T>(dout, a.cols, v * W);
+            auto batch = [&](auto n_, int j0, float *sums) {
+                constexpr int N = decltype(n_)::value;
+                int64_t r[N];
+                bool own[N];
+                float g[N];
 #pragma unroll
-            for (int j0 = 0; j0 < K; j0 += 4) {
-                if (j0 >= a.k) continue;
-                int64_t r[4];
-                bool on[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    r[j] = j0 + j < a.k ? places[j0 + j] : -1;
-                    on[j] = r[j] >= 0 && r[j] < a.n_rows;
-                }
-                if (a.dgates && a.n_rows > 0) {
-                    Vec<T> y[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        y[j] = row_vec<T>(static_cast<const T *>(a.y) + (on[j] ? r[j] : 0) * a.stride, a.cols, v * W);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int w = 0; w < W; ++w)
-                            dots[j0 + j] = on[j] ? __builtin_fmaf(y[j].at(w), d.at(w), dots[j0 + j]) : dots[j0 + j];
-                }
-                if (a.dy) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (!on[j] || a.rows[r[j]] != t * a.k + j0 + j) continue;
-                        const float g = gates ? gates[j0 + j] : 1.0f;
-                        float x[W];
-#pragma unroll
-                        for (int w = 0; w < W; ++w) x[w] = g * d.at(w);
-                        store_vec<T, false>(static_cast<T *>(a.dy) + r[j] * a.cols, a.cols, v * W, x);
+                for (int j = 0; j < N; ++j) {
+                    if (NW) {
+                        r[j] = __builtin_amdgcn_readlane(mine, j0 + j);
+                        own[j] = __builtin_amdgcn_readlane((int)mine_own, j0 + j);
+                        g[j] = __uint_as_float(__builtin_amdgcn_readlane((int)__float_as_uint(mine_gate), j0 + j));
+                    } else {
+                        r[j] = look_up(j0 + j, own[j], g[j]);
                     }
                 }
+                spread_rows<T, N>(a, r, own, g, v * W, d, sums);
+            };
+#pragma unroll
+            for (int j0 = 0; j0 < K; j0 += 4) {
+                const int left = k - j0;
+                if (left >= 4) batch(Int<4>(), j0, dots + j0);
+                else if (left == 3) batch(Int<3>(), j0, dots + j0);
+                else if (left == 2) batch(Int<2>(), j0, dots + j0);
+                else if (left == 1) batch(Int<1>(), j0, dots + j0);
             }
         }
     }
     if (!a.dgates) return;
 #pragma unroll
     for (int j = 0; j < K; ++j)
-        if (j < a.k) dots[j] = lanes_sum(dots[j], lt);
+        if (j < k) dots[j] = lanes_sum(dots[j], lt);
     if (NW > 1) {
         if (lane == 0)
 #pragma unroll
             for (int j = 0; j < K; ++j) part[wave][j] = dots[j];
         __syncthreads();
-        if (wave % NW == 0 && live && lane < a.k) {
+        if (wave % (NW ? NW : 1) == 0 && live && lane < k) {
             float s = 0.0f;
             for (int w = 0; w < NW; ++w) s += part[wave + w][lane];
-            a.dgates[t * a.k + lane] = s;
+            a.dgates[t * k + lane] = s;
         }
     } else if (live && lane == 0) {
 #pragma unroll
         for (int j = 0; j < K; ++j)
-            if (j < a.k) a.dgates[t * a.k + j] = dots[j];
+            if (j < k) a.dgates[t * k + j] = dots[j];
     }
-}
-
-inline int check_places(const routepack_ids *p, int32_t k, int64_t gate_stride) {
-    if (!p || p->type != ROUTEPACK_I32 || p->n_tokens < 0 || p->token_stride < 0 || k < 1 || gate_stride < 0)
-        return ROUTEPACK_E_INVALID;
-    if (k > kMaxChoices || p->n_tokens > INT32_MAX / k || !sizes_fit(p->n_tokens, p->token_stride) ||
-        !sizes_fit(p->n_tokens, gate_stride))
-        return ROUTEPACK_E_UNSUPPORTED;
-    return ROUTEPACK_OK;
 }
 
 inline void geometry(CombineArgs &a, int W) {
@@ -216,7 +230,9 @@ extern "C" int routepack_combine_tokens(const routepack_matrix *y, const routepa
                                         const float *gates, int64_t gate_stride, const routepack_matrix *out,
                                         hipStream_t stream) {
     RP_TRY(check_matrix(y));
-    RP_TRY(check_places(places, top_k, gate_stride));
+    RP_TRY(check_places(places, top_k, kMaxChoices));
+    if (gate_stride < 0) return ROUTEPACK_E_INVALID;
+    if (!sizes_fit(places->n_tokens, gate_stride)) return ROUTEPACK_E_UNSUPPORTED;
     RP_TRY(check_output(out, places->n_tokens, y->n_cols));
     if (out->type != y->type) return ROUTEPACK_E_INVALID;
     if (places->n_tokens == 0 || y->n_cols == 0) return ROUTEPACK_OK;
@@ -224,19 +240,15 @@ extern "C" int routepack_combine_tokens(const routepack_matrix *y, const routepa
     CombineArgs a = {};
     a.y = y->data;
     a.stride = y->row_stride;
-    a.n_rows = y->n_rows;
     a.cols = (int32_t)y->n_cols;
-    a.places = static_cast<const int32_t *>(places->data);
-    a.place_stride = places->token_stride;
-    a.k = top_k;
+    a.order = {nullptr, static_cast<const int32_t *>(places->data), places->token_stride, places->n_tokens, y->n_rows, top_k};
     a.gates = gates;
     a.gate_stride = gate_stride;
-    a.T = places->n_tokens;
     a.out = out->data;
     return by_type(y->type, [&](auto tag) -> int {
         using T = decltype(tag);
         geometry(a, Vec<T>::W);
-        const int64_t items = a.T * a.chunks, per = 256 / a.lt;
+        const int64_t items = a.order.T * a.chunks, per = 256 / a.lt;
         auto kern = a.lt == kWave ? k_combine<T, true> : k_combine<T, false>;
         hipLaunchKernelGGL(kern, grid_of((items + per - 1) / per), dim3(256), 0, stream, a);
         return launched();
@@ -249,7 +261,9 @@ extern "C" int routepack_combine_backward(const routepack_matrix *dout, const ro
                                           hipStream_t stream) {
     RP_TRY(check_matrix(dout));
     RP_TRY(check_matrix(y));
-    RP_TRY(check_places(places, top_k, gate_stride));
+    RP_TRY(check_places(places, top_k, kMaxChoices));
+    if (gate_stride < 0) return ROUTEPACK_E_INVALID;
+    if (!sizes_fit(places->n_tokens, gate_stride)) return ROUTEPACK_E_UNSUPPORTED;
     if (!dy && !dgates) return ROUTEPACK_E_INVALID;
     if (dout->type != y->type || dout->n_rows != places->n_tokens || dout->n_cols != y->n_cols) return ROUTEPACK_E_INVALID;
     if (dy) {
@@ -263,30 +277,29 @@ extern "C" int routepack_combine_backward(const routepack_matrix *dout, const ro
     CombineArgs a = {};
     a.y = y->data;
     a.stride = y->row_stride;
-    a.n_rows = y->n_rows;
     a.cols = (int32_t)y->n_cols;
-    a.places = static_cast<const int32_t *>(places->data);
-    a.place_stride = places->token_stride;
-    a.k = top_k;
+    a.order = {rows, static_cast<const int32_t *>(places->data), places->token_stride, places->n_tokens, y->n_rows, top_k};
     a.gates = gates;
     a.gate_stride = gate_stride;
-    a.T = places->n_tokens;
     a.dout = dout->data;
     a.dout_stride = dout->row_stride;
-    a.rows = rows;
     a.dy = dy && y->n_cols > 0 && y->n_rows > 0 ? dy->data : nullptr;
     a.dgates = dgates;
     return by_type(y->type, [&](auto tag) -> int {
         using T = decltype(tag);
         geometry(a, Vec<T>::W);
-        const int nw = a.chunks > 1 ? 4 : 1;
-        const int64_t per = nw > 1 ? 1 : 256 / a.lt;
-        a.token_groups = (a.T + per - 1) / per;
-        const int64_t n = a.token_groups + (a.dy ? (a.n_rows + 255) / 256 : 0);
+        // A token's waves: few where that fills them (6 vectors of 64: two waves take
+        // three each), four where there are few tokens.
+        const int nw = a.lt < kWave ? 0 : a.chunks == 1 ? 1 : a.chunks % 4 == 0 || a.chunks > 8 || a.order.T < 1024 ? 4 : 2;
+        const int64_t per = nw ? 4 / nw : 256 / a.lt;
+        a.token_groups = (a.order.T + per - 1) / per;
+        const int64_t n = a.token_groups + (a.dy ? (a.order.n_rows + 255) / 256 : 0);
         if (n == 0) return ROUTEPACK_OK;
-        auto few = nw > 1 ? k_spread<T, 8, 4> : k_spread<T, 8, 1>;
-        auto many = nw > 1 ? k_spread<T, 32, 4> : k_spread<T, 32, 1>;
-        hipLaunchKernelGGL(a.k <= 8 ? few : many, grid_of(n), dim3(256), 0, stream, a);
+        auto pick = [&](auto k_) {
+            constexpr int K = decltype(k_)::value;
+            return nw == 4 ? k_spread<T, K, 4> : nw == 2 ? k_spread<T, K, 2> : nw == 1 ? k_spread<T, K, 1> : k_spread<T, K, 0>;
+        };
+        hipLaunchKernelGGL((top_k <= 8 ? pick(Int<8>()) : pick(Int<32>())), grid_of(n), dim3(256), 0, stream, a);
         return launched();
     });
 }

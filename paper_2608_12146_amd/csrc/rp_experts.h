@@ -42,6 +42,34 @@ inline int check_mx(const routepack_mx *q, bool data) {
     return ROUTEPACK_OK;
 }
 
+// The places of an order, [T][1][k]: k <= most.
+inline int check_places(const routepack_ids *p, int32_t k, int32_t most) {
+    if (!p || p->type != ROUTEPACK_I32 || p->n_tokens < 0 || p->token_stride < 0 || k < 1) return ROUTEPACK_E_INVALID;
+    if (k > most || p->n_tokens > INT32_MAX / k || !sizes_fit(p->n_tokens, p->token_stride)) return ROUTEPACK_E_UNSUPPORTED;
+    return ROUTEPACK_OK;
+}
+
+// An order's rows and places, on the device.
+struct OrderView {
+    const int32_t *rows;
+    const int32_t *places;
+    int64_t place_stride, T, n_rows;
+    int32_t k;
+    // The pair that stands in row r, if its place is r; else -1.
+    __device__ int64_t pair_of_row(int64_t r) const {
+        const int32_t p = rows[r];
+        if (p < 0) return -1;
+        const uint32_t t = (uint32_t)p / (uint32_t)k;
+        if (t >= T) return -1;
+        return places[t * place_stride + (p - t * (uint32_t)k)] == r ? p : -1;
+    }
+    // The row of token t's choice j, if it is that row's pair; else -1.
+    __device__ int64_t row_of_pair(int64_t t, int j) const {
+        const int64_t r = places[t * place_stride + j];
+        return r >= 0 && r < n_rows && rows[r] == t * k + j ? r : -1;
+    }
+};
+
 inline int launched() { return hipGetLastError() == hipSuccess ? ROUTEPACK_OK : ROUTEPACK_E_DEVICE; }
 
 // The workgroup's index in a grid of grid_of.

@@ -91,8 +91,8 @@ def test_mx_refusals():
     import paper_2608_12146_amd as rp
     lib = rp.load_library()
 
-    def quant(x, q, rows=None, per=1):
-        return lib.routepack_quantize_mx(_by(x), rows, per, _by(q), None)
+    def quant(x, q, rows=None, places=None, k=2):
+        return lib.routepack_quantize_mx(_by(x), rows, _by(places), k, _by(q), None)
 
     def back(q, x):
         return lib.routepack_dequantize_mx(_by(q), _by(x), None)
@@ -101,7 +101,13 @@ def test_mx_refusals():
         assert quant(x, _mx()) == -1 and back(_mx(), x) == -1
     for q in (None, _mx(rows=-1), _mx(cols=-1), _mx(codes=None), _mx(scales=None), _mx(codes=72), _mx(scales=68)):
         assert quant(_matrix(), q) == -1 and back(q, _matrix()) == -1
-    assert quant(_matrix(), _mx(), SOME, 0) == -1 and back(_mx(), _matrix(stride=41)) == -1
+    assert quant(_matrix(), _mx(8), SOME, None) == -1 and quant(_matrix(), _mx(8), None, _rows()) == -1
+    for bad in (_rows(6), _rows(T=5), _rows(ts=-1), _rows(data=None)):
+        assert quant(_matrix(), _mx(8), SOME, bad) == -1
+    assert quant(_matrix(), _mx(8), SOME, _rows(), k=0) == -1 and quant(_matrix(), _mx(8), SOME, _rows(), k=257) == -8
+    assert quant(_matrix(rows=1 << 30), _mx(8), SOME, _rows(T=1 << 30)) == -8
+    assert quant(_matrix(), _mx(0, codes=None, scales=None), None, _rows()) == 0
+    assert back(_mx(), _matrix(stride=41)) == -1
     big = (1 << 24) + 1
     assert quant(_matrix(cols=big), _mx(cols=big)) == -8
     assert quant(_matrix(rows=1 << 50, cols=1 << 20), _mx(1 << 50, 1 << 20)) == -8

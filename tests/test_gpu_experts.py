@@ -317,10 +317,10 @@ def test_rows_gathered_as_they_are_quantized():
     want = np.where((rows >= 0)[:, None], _host(x)[np.maximum(rows, 0) // k], 0.0)
     codes, scales = X.quantize(want)
     assert np.array_equal(_host(q.codes), codes) and np.array_equal(_host(q.scales), scales)
-    # rows outside the tokens are rows of zeros
-    order.rows[3], order.rows[4] = T * k, 2 ** 31 - 1
+    # rows that name no pair, or one whose place is another, are zeros
+    order.rows[3], order.rows[4], order.rows[5] = T * k, 2 ** 31 - 1, order.rows[6].item()
     q = rp.quantize_mx(x, order=order)
-    assert not q.codes[3:5].any() and not q.scales[3:5].any()
+    assert not q.codes[3:6].any() and not q.scales[3:6].any() and q.codes[6].any()
     # weights: three axes
     w = _floats(3, (4, 9, cols), "fp32")
     q = rp.quantize_mx(w)
