@@ -81,27 +81,34 @@ __device__ inline void split8(const T *row, int32_t from, int32_t end, bool live
         }
 }
 
-// Byte of column c (a multiple of 4) of term row k in a tile of 128 columns:
-// the row's four pieces of 64 bytes are exchanged by the row, so that the 4
-// rows of a transposing load stand in different banks.
-__device__ inline int term_at(int k, int c) { return k * 256 + (((c >> 5) ^ (k & 3)) << 6) + (c & 31) * 2; }
+// Byte of column c (a multiple of 4) of term row k in a tile of COLS columns: each
+// four pieces of 64 bytes of the row, and the four of 16 in each, are exchanged by
+// the row, so that the 4 rows of a transposing load, and the 4 rows that 16 lanes
+// write, stand in different banks.
+template <int COLS>
+__device__ inline int term_at(int k, int c) {
+    return k * COLS * 2 + (((c >> 5) ^ (k & 3)) << 6) + ((((c >> 3) ^ k) & 3) << 4) + (c & 7) * 2;
+}
 
 // The fragment of 32 columns from c0 and 16 terms from k0 on.
+template <int COLS>
 __device__ inline bf16x8 term_fragment(const char *tile, int k0, int c0) {
     const int lane = threadIdx.x & 63, i = (lane >> 2) & 3, k = k0 + (lane >> 5) * 8 + i;
     const int c = c0 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
     typedef __attribute__((address_space(3))) short4_ lds4;
-    const short4_ a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(tile + term_at(k, c)));
-    const short4_ b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(tile + term_at(k + 4, c)));
+    const short4_ a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(tile + term_at<COLS>(k, c)));
+    const short4_ b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(tile + term_at<COLS>(k + 4, c)));
     const short8_ v = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
     return __builtin_bit_cast(bf16x8, v);
 }
 
-template <class T, bool DW>
-__global__ void __launch_bounds__(256) k_product_back(BackProductArgs a) {
+template <class T, bool DW, int NB>
+__global__ void __launch_bounds__(256, 2) k_product_back(BackProductArgs a) {
     constexpr int P = kParts<T>;
-    __shared__ __attribute__((aligned(16))) char As[P][kTile * kTerms * 2];
-    __shared__ __attribute__((aligned(16))) char Bs[kTerms * kTile * 2];
+    constexpr int kCols = 64 * NB;  // a wave has 2 x NB matrix tiles, two waves each way
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    char *const Bs = lds + P * kTile * kTerms * 2;
+    auto As = [&](int p) { return lds + p * kTile * kTerms * 2; };
     const int64_t id = group_index();
     int32_t s, ct;
     int64_t m0;       // first output row: of R (dx), of the slot's N (dw)
@@ -126,15 +133,15 @@ __global__ void __launch_bounds__(256) k_product_back(BackProductArgs a) {
         s = map.find(index, a.offsets, a.n_slots, a.R, kTile, seg, before);
         m0 = seg.begin + before * kTile;
     }
-    const int c0 = ct * kTile, t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    const int wm = (wave >> 1) * 64, wc = (wave & 1) * 64;
+    const int c0 = ct * kCols, t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const int wm = (wave >> 1) * 64, wc = (wave & 1) * 32 * NB;
     // terms [k0, k1), and A's and B's rows of them
     const int64_t k_begin = DW ? seg.begin : 0, k_end = DW ? seg.end : a.N;
     const T *dy = static_cast<const T *>(a.dy);
     const int64_t b_row0 = DW ? 0 : (int64_t)s * a.N;
     int4_ pa[4][P];
-    int4_ pb;
-    uint32_t sb;
+    int4_ pb[NB / 2];
+    uint32_t sb[NB / 2];
     auto fetch = [&](int64_t k0) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -147,14 +154,16 @@ __global__ void __launch_bounds__(256) k_product_back(BackProductArgs a) {
             }
         }
         const int64_t k = k0 + (t >> 2);
-        const int block = ct * 4 + (t & 3);
-        const bool on = k < k_end && block < a.groups * 4;
-        pb = int4_{0, 0, 0, 0};
-        sb = 127;
-        if (on) {
-            const int64_t row = b_row0 + k;
-            pb = *reinterpret_cast<const int4_ *>(a.bc + row * a.groups * 64 + block * 16);
-            sb = a.bs[row * a.groups * 4 + block];
+#pragma unroll
+        for (int i = 0; i < NB / 2; ++i) {
+            const int block = ct * (kCols / 32) + (t & 3) + 4 * i;
+            pb[i] = int4_{0, 0, 0, 0};
+            sb[i] = 127;
+            if (k < k_end && block < a.groups * 4) {
+                const int64_t row = b_row0 + k;
+                pb[i] = *reinterpret_cast<const int4_ *>(a.bc + row * a.groups * 64 + block * 16);
+                sb[i] = a.bs[row * a.groups * 4 + block];
+            }
         }
     };
     auto store = [&]() {
@@ -163,24 +172,25 @@ __global__ void __launch_bounds__(256) k_product_back(BackProductArgs a) {
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 int at;
-                if constexpr (DW) at = term_at((t >> 4) + 16 * i, (t & 15) * 8);
-                else at = ((t >> 3) + 32 * i) * 128 + (((t & 7) ^ ((t >> 3) & 7)) << 4);
-                *reinterpret_cast<int4_ *>(As[p] + at) = pa[i][p];
+                if constexpr (DW) at = term_at<kTile>((t >> 4) + 16 * i, (t & 15) * 8);
+                else at = ((t >> 3) + 32 * i) * 128 + (((t & 7) ^ ((t >> 4) & 7)) << 4);
+                *reinterpret_cast<int4_ *>(As(p) + at) = pa[i][p];
             }
-        const float scale = scale_of(sb);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            bf16x2 v[4];
-            v[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((unsigned)pb[i], scale, 0);
-            v[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((unsigned)pb[i], scale, 1);
-            v[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((unsigned)pb[i], scale, 2);
-            v[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((unsigned)pb[i], scale, 3);
-            const int4_ w = {__builtin_bit_cast(int, v[0]), __builtin_bit_cast(int, v[1]), __builtin_bit_cast(int, v[2]),
-                             __builtin_bit_cast(int, v[3])};
-            *reinterpret_cast<int4_ *>(Bs + term_at(t >> 2, (t & 3) * 32 + i * 8)) = w;
+        for (int b = 0; b < NB / 2; ++b) {
+            const float scale = scale_of(sb[b]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const unsigned w = (unsigned)pb[b][i];
+                const bf16x2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1),
+                                     __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3)};
+                const int4_ x = {__builtin_bit_cast(int, v[0]), __builtin_bit_cast(int, v[1]), __builtin_bit_cast(int, v[2]),
+                                 __builtin_bit_cast(int, v[3])};
+                *reinterpret_cast<int4_ *>(Bs + term_at<kCols>(t >> 2, ((t & 3) + 4 * b) * 32 + i * 8)) = x;
+            }
         }
     };
-    float16_ sum[2][2] = {};
+    float16_ sum[2][NB] = {};
     if (k_begin < k_end) fetch(k_begin);
     for (int64_t k0 = k_begin; k0 < k_end; k0 += kTerms) {
         store();
@@ -188,20 +198,22 @@ __global__ void __launch_bounds__(256) k_product_back(BackProductArgs a) {
         if (k0 + kTerms < k_end) fetch(k0 + kTerms);
 #pragma unroll
         for (int k = 0; k < kTerms; k += 16) {
-            const bf16x8 b[2] = {term_fragment(Bs, k, wc), term_fragment(Bs, k, wc + 32)};
+            bf16x8 b[NB];
+#pragma unroll
+            for (int n = 0; n < NB; ++n) b[n] = term_fragment<kCols>(Bs, k, wc + n * 32);
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
                 for (int p = P - 1; p >= 0; --p) {  // (the smallest parts first)
                     bf16x8 x;
                     if constexpr (DW) {
-                        x = term_fragment(As[p], k, wm + m * 32);
+                        x = term_fragment<kTile>(As(p), k, wm + m * 32);
                     } else {
                         const int row = wm + m * 32 + (lane & 31), chunk = (k >> 3) + (lane >> 5);
-                        x = *reinterpret_cast<const bf16x8 *>(As[p] + row * 128 + ((chunk ^ (row & 7)) << 4));
+                        x = *reinterpret_cast<const bf16x8 *>(As(p) + row * 128 + ((chunk ^ ((row >> 1) & 7)) << 4));
                     }
-                    sum[m][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, b[0], sum[m][0], 0, 0, 0);
-                    sum[m][1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, b[1], sum[m][1], 0, 0, 0);
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) sum[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, b[n], sum[m][n], 0, 0, 0);
                 }
         }
         __syncthreads();
@@ -212,7 +224,7 @@ __global__ void __launch_bounds__(256) k_product_back(BackProductArgs a) {
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int n = 0; n < NB; ++n)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int64_t r = m0 + wm + m * 32 + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3);
@@ -256,11 +268,19 @@ extern "C" int routepack_expert_product_backward(const routepack_matrix *dy, con
     a.N = (int32_t)N;
     a.C = (int32_t)C;
     a.n_slots = n_slots;
-    a.c_tiles = (int32_t)((C + kTile - 1) / kTile);
     a.R = x->n_rows;
     a.offsets = offsets;
     return by_type(dy->type, [&](auto tag) -> int {
         using T = decltype(tag);
+        constexpr int NB = kParts<T> == 3 ? 2 : 4, lds = kParts<T> * kTile * kTerms * 2 + kTerms * NB * 64 * 2;
+        a.c_tiles = (int32_t)((C + NB * 64 - 1) / (NB * 64));
+        auto go = [&](auto kern, int64_t n, const BackProductArgs &b) -> int {
+            if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(kern),
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
+                return ROUTEPACK_E_DEVICE;
+            hipLaunchKernelGGL(kern, grid_of(n), dim3(256), lds, stream, b);
+            return launched();
+        };
         if (do_x) {
             BackProductArgs b = a;
             b.bc = static_cast<const uint8_t *>(w->codes);
@@ -271,8 +291,7 @@ extern "C" int routepack_expert_product_backward(const routepack_matrix *dy, con
             b.tiles = (a.R / kTile + slots) * a.c_tiles;
             const int64_t pieces = (a.R * C + 65535) / 65536;
             b.clears = pieces < 256 ? pieces : 256;
-            hipLaunchKernelGGL((k_product_back<T, false>), grid_of(b.tiles + b.clears), dim3(256), 0, stream, b);
-            RP_TRY(launched());
+            RP_TRY(go(k_product_back<T, false, NB>, b.tiles + b.clears, b));
         }
         if (do_w) {
             BackProductArgs b = a;
@@ -281,8 +300,7 @@ extern "C" int routepack_expert_product_backward(const routepack_matrix *dy, con
             b.out = dw->data;
             b.m_tiles = (int32_t)((N + kTile - 1) / kTile);
             b.tiles = (int64_t)n_slots * b.m_tiles * a.c_tiles;
-            hipLaunchKernelGGL((k_product_back<T, true>), grid_of(b.tiles), dim3(256), 0, stream, b);
-            RP_TRY(launched());
+            RP_TRY(go(k_product_back<T, true, NB>, b.tiles, b));
         }
         return ROUTEPACK_OK;
     });
