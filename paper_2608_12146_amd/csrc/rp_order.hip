@@ -40,32 +40,47 @@ __device__ inline int32_t token_of(const OrderArgs &a, int32_t p) {
     return (int32_t)((uint64_t)(uint32_t)p * a.k_inv >> a.k_shift);
 }
 
-// The slots of pairs p, p + step, .. (E for none), 8 loads at a time.
+// A workgroup's layer and chunk: workgroups go to the eight XCDs in turn, and the
+// layers of a chunk, whose ids and places share lines, to the same one.
+__device__ inline bool order_item(const OrderArgs &a, int32_t &l, int32_t &c) {
+    const uint32_t i = blockIdx.x >> 3, q = i / (uint32_t)a.L;
+    l = (int32_t)(i - q * a.L);
+    c = (int32_t)(q * 8 + (blockIdx.x & 7));
+    return c < a.n_chunks;
+}
+
+// The slots of pairs p, p + step, .. (E for none and from `end` on): 8 loads at a
+// time, without branches that would part them.
 template <class I>
 __device__ inline void slots_of_pairs(const OrderArgs &a, int32_t l, int32_t p, int32_t step, int32_t end,
                                       int32_t (&slot)[kEach]) {
+    I id[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) slot[i] = a.E;
+    if (end == 0) return;  // (no pair at all)
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-        const int32_t x = p + i * step;
-        slot[i] = a.E;
-        if (x < end) {
-            const int32_t t = token_of(a, x), j = x - t * a.k;
-            const int64_t v = (int64_t) static_cast<const I *>(a.ids)[t * a.ts + l * a.ls + j];
-            slot[i] = v >= 0 && v < a.E ? (int32_t)v : a.E;
-        }
+        const int32_t x = p + i * step < end ? p + i * step : end - 1, t = token_of(a, x), j = x - t * a.k;
+        id[i] = static_cast<const I *>(a.ids)[t * a.ts + l * a.ls + j];
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int64_t v = (int64_t)id[i];
+        slot[i] = p + i * step < end && v >= 0 && v < a.E ? (int32_t)v : a.E;
     }
     if (!a.slots) return;
+    int32_t s[kEach];
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const int32_t s = slot[i] < a.E ? a.slots[(int64_t)l * a.E + slot[i]] : -1;
-        slot[i] = s >= 0 && s < a.E ? s : a.E;
-    }
+    for (int i = 0; i < kEach; ++i) s[i] = a.slots[(int64_t)l * a.E + (slot[i] < a.E ? slot[i] : 0)];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) slot[i] = slot[i] < a.E && s[i] >= 0 && s[i] < a.E ? s[i] : a.E;
 }
 
 template <class I>
 __global__ void __launch_bounds__(kOrderThreads) k_order_count(OrderArgs a) {
     extern __shared__ int32_t n[];
-    const int32_t l = (int32_t)(blockIdx.x / a.n_chunks), c = (int32_t)(blockIdx.x - (uint32_t)l * a.n_chunks);
+    int32_t l, c;
+    if (!order_item(a, l, c)) return;
     const int32_t b = c * kChunk, e = a.P - b < kChunk ? a.P : b + kChunk;
     int32_t slot[kEach];
     slots_of_pairs<I>(a, l, b + (int32_t)threadIdx.x, kOrderThreads, e, slot);
@@ -119,10 +134,19 @@ __global__ void __launch_bounds__(kOrderThreads) k_order_place(OrderArgs a) {
     int32_t *sorted = lds;                               // [kChunk]: slot, and pair within the chunk
     int32_t *from = sorted + kChunk;                     // [S]: a slot's first row less its first place in `sorted`
     int32_t *next = from + S + (threadIdx.x >> 6) * S;   // [waves][S]: this wave's counts, then its next places
-    const int32_t l = (int32_t)(blockIdx.x / a.n_chunks), c = (int32_t)(blockIdx.x - (uint32_t)l * a.n_chunks);
+    int32_t l, c;
+    if (!order_item(a, l, c)) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int32_t b = c * kChunk, e = a.P - b < kChunk ? a.P : b + kChunk, first = b + wave * (kWave * kEach) + lane;
     int32_t slot[kEach];
+    // (the sums of the first of a thread's slots, which is its only one up to 511)
+    const bool one = a.n_chunks == 1;
+    const int32_t each = (S + kOrderThreads - 1) / kOrderThreads, s0 = threadIdx.x * each;
+    const int32_t s1 = s0 + each < S ? s0 + each : S;
+    auto total_of = [&](int32_t s) { return a.totals[(int64_t)l * S + s]; };
+    auto before_of = [&](int32_t s) { return a.counts[((int64_t)l * S + s) * a.n_chunks + c]; };
+    const bool early = !one && s0 < S;
+    const int32_t total0 = early ? total_of(s0) : 0, before0 = early ? before_of(s0) : 0;
     slots_of_pairs<I>(a, l, first, kWave, e, slot);
     for (int32_t s = threadIdx.x; s < kOrderWaves * S; s += kOrderThreads) from[S + s] = 0;
     __syncthreads();
@@ -131,14 +155,11 @@ __global__ void __launch_bounds__(kOrderThreads) k_order_place(OrderArgs a) {
         if (first + i * kWave < e) atomicAdd(&next[slot[i]], 1);
     __syncthreads();
     // A thread's slots: their rows (of all chunks) and their places in this one.
-    const int32_t each = (S + kOrderThreads - 1) / kOrderThreads, s0 = threadIdx.x * each;
-    const int32_t s1 = s0 + each < S ? s0 + each : S;
-    const bool one = a.n_chunks == 1;
     uint64_t sum = 0;  // rows << 32 | places
     for (int32_t s = s0; s < s1; ++s) {
         uint32_t here = 0;
         for (int w = 0; w < kOrderWaves; ++w) here += (uint32_t)from[S + w * S + s];
-        sum += (uint64_t)(one ? here : (uint32_t)a.totals[(int64_t)l * S + s]) << 32 | here;
+        sum += (uint64_t)(one ? here : (uint32_t)(s == s0 ? total0 : total_of(s))) << 32 | here;
     }
     uint64_t upto = sum;
     for (int d = 1; d < kWave; d <<= 1) {
@@ -152,9 +173,9 @@ __global__ void __launch_bounds__(kOrderThreads) k_order_place(OrderArgs a) {
     int32_t row = (int32_t)(at >> 32), place = (int32_t)(uint32_t)at;
     for (int32_t s = s0; s < s1; ++s) {
         if (c == 0) a.offsets[(int64_t)l * S + s] = row;  // (S = E + 1: the last is the end of slot E - 1)
-        const int32_t before = one ? 0 : a.counts[((int64_t)l * S + s) * a.n_chunks + c];
+        const int32_t before = one ? 0 : s == s0 ? before0 : before_of(s);
         from[s] = row + before - place;
-        if (!one) row += a.totals[(int64_t)l * S + s];
+        if (!one) row += s == s0 ? total0 : total_of(s);
         for (int w = 0; w < kOrderWaves; ++w) {
             const int32_t v = from[S + w * S + s];
             from[S + w * S + s] = place;
@@ -167,13 +188,17 @@ __global__ void __launch_bounds__(kOrderThreads) k_order_place(OrderArgs a) {
     for (int i = 0; i < kEach; ++i) {
         const int32_t p = first + i * kWave;
         const bool live = p < e;
-        uint64_t same = __ballot(live);
+        // lanes with the same slot, bit by bit, in 32-bit halves
+        const uint64_t all_live = __ballot(live);
+        uint32_t lo = (uint32_t)all_live, hi = (uint32_t)(all_live >> 32);
         for (int k = 0; k < a.bits; ++k) {
-            const bool bit = slot[i] >> k & 1;
-            const uint64_t ones = __ballot(bit);
-            same &= bit ? ones : ~ones;
+            const uint32_t mine = 0u - ((uint32_t)slot[i] >> k & 1u);
+            const uint64_t ones = __ballot(mine != 0);
+            lo &= ~((uint32_t)ones ^ mine);
+            hi &= ~((uint32_t)(ones >> 32) ^ mine);
         }
-        const int32_t rank = __popcll(same & (((uint64_t)1 << lane) - 1)), all = __popcll(same);
+        const int32_t rank = (int32_t)__builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0));
+        const int32_t all = __popc(lo) + __popc(hi);
         const int32_t base = next[slot[i]];
         __builtin_amdgcn_wave_barrier();  // (all reads of a wave's counters before the writes)
         if (live && rank == 0) next[slot[i]] = base + all;
@@ -246,8 +271,8 @@ extern "C" int routepack_order_tokens(const routepack_problem *prob, const route
     a.rows = rows;
     a.offsets = offsets;
     a.places = places;
-    if ((int64_t)a.L * a.n_chunks > INT32_MAX / kOrderThreads) return ROUTEPACK_E_UNSUPPORTED;
-    const unsigned n = (unsigned)(a.L * a.n_chunks);
+    if ((int64_t)a.L * (a.n_chunks + 7) > INT32_MAX / kOrderThreads) return ROUTEPACK_E_UNSUPPORTED;
+    const unsigned n = (unsigned)((a.n_chunks + 7) / 8 * 8 * (int64_t)a.L);
     const size_t one = 4 * (size_t)(a.E + 1), all = 4 * kChunk + one * (1 + kOrderWaves);
     auto go = [&](auto tag) -> int {
         using I = decltype(tag);

@@ -97,6 +97,57 @@ struct TileMap {
     }
 };
 
+// A wave's LDS accesses before are done before those after.
+__device__ inline void wave_meet() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// 16 bytes of values from column c on, as many as the row has.
+template <class T>
+__device__ inline void store_cols(T *row, int32_t cols, int32_t c, int4_ v) {
+    constexpr int W = 16 / (int)sizeof(T);
+    typedef int four __attribute__((ext_vector_type(4), aligned(2)));
+    if (c + W <= cols) {
+        *reinterpret_cast<four *>(row + c) = v;
+    } else {
+        typedef T values __attribute__((ext_vector_type(W)));
+        const values x = __builtin_bit_cast(values, v);
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+            if (c + i < cols) row[c + i] = x[i];
+    }
+}
+
+// 32 rows of NB matrix tiles of 32 columns, from registers to memory through this
+// wave's part of LDS, so that they leave as whole lines: lane l holds row l % 32,
+// element i of tile n its column 32 n + 8 (i / 4) + 4 (l / 32) + i % 4.  Columns
+// c0 .. of rows out, out + stride, ..: as many as `rows` and `cols` have.
+template <class T, int NB>
+constexpr int kPitch = NB * 32 * (int)sizeof(T) + 16;
+template <class T, int NB>
+__device__ inline void leave_by_lines(char *mine, const float16_ (&v)[NB], T *out, int64_t stride, int rows, int32_t cols,
+                                      int32_t c0) {
+    constexpr int kVec = 16 / (int)sizeof(T), kLanes = NB * 32 / kVec, kRowsAtOnce = kWave / kLanes;
+    const int lane = threadIdx.x & 63, half = lane >> 5, r32 = lane & 31;
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            typedef T four __attribute__((ext_vector_type(4)));
+            const four x = {(T)v[n][4 * g], (T)v[n][4 * g + 1], (T)v[n][4 * g + 2], (T)v[n][4 * g + 3]};
+            *reinterpret_cast<four *>(mine + r32 * kPitch<T, NB> + (n * 32 + 8 * g + 4 * half) * sizeof(T)) = x;
+        }
+    wave_meet();
+#pragma unroll
+    for (int i = 0; i < 32 / kRowsAtOnce; ++i) {
+        const int row = i * kRowsAtOnce + lane / kLanes, c = (lane % kLanes) * kVec;
+        const int4_ x = *reinterpret_cast<const int4_ *>(mine + row * kPitch<T, NB> + c * sizeof(T));
+        if (row < rows) store_cols<T>(out + row * stride, cols, c0 + c, x);
+    }
+    wave_meet();
+}
+
 // Zeros in the rows of no slot: piece `index` of `pieces` of them.
 template <class T>
 __device__ inline void clear_rows(T *y, int64_t cols, const int64_t *offsets, int32_t n_slots, int64_t R, int64_t index,

@@ -111,28 +111,6 @@ __device__ inline void load_to_lds(const uint8_t *base, uint32_t offset, uint32_
 // workgroup's barrier.
 __device__ inline void wait_and_meet() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// A wave's LDS accesses before are done before those after.
-__device__ inline void wave_meet() {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_wave_barrier();
-}
-
-// 16 bytes of values from column c on, as many as the row has.
-template <class T>
-__device__ inline void store_cols(T *row, int32_t cols, int32_t c, int4_ v) {
-    constexpr int W = 16 / (int)sizeof(T);
-    typedef int four __attribute__((ext_vector_type(4), aligned(2)));
-    if (c + W <= cols) {
-        *reinterpret_cast<four *>(row + c) = v;
-    } else {
-        typedef T values __attribute__((ext_vector_type(W)));
-        const values x = __builtin_bit_cast(values, v);
-#pragma unroll
-        for (int i = 0; i < W; ++i)
-            if (c + i < cols) row[c + i] = x[i];
-    }
-}
-
 template <class T>
 __global__ void __launch_bounds__(512, 1) k_product_many(ProductArgs a) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -213,7 +191,7 @@ __global__ void __launch_bounds__(512, 1) k_product_many(ProductArgs a) {
     T *y = static_cast<T *>(a.y);
     // The whole of it for a number of blocks (the accumulators stay where they
     // are): every wave meets the others as often, whatever its number.
-    auto multiply = [&](auto live_) {
+    auto multiply = [&](auto live_) __attribute__((always_inline)) {
     constexpr int kLive = decltype(live_)::value;
     float16_ sum[kLive ? kLive : 1][2] = {};
     for (int32_t step = 0; step < steps; ++step) {
@@ -258,34 +236,12 @@ __global__ void __launch_bounds__(512, 1) k_product_many(ProductArgs a) {
         }
         if ((step & 1) == 1 && more) store_scales(unit + 1);
     }
-    // A value's row is lane % 32 of x, its column 8 (i / 4) + 4 (lane / 32) + i % 4
-    // of w: 32 rows at a time go through this wave's part of LDS, to leave as
-    // whole lines.
     wait_and_meet();
-    constexpr int kPitch = 64 * (int)sizeof(T) + 16, kVec = 16 / (int)sizeof(T);
-    constexpr int kLanes = 64 / kVec, kRowsAtOnce = kWave / kLanes;
-    static_assert(8 * 32 * kPitch <= kManyLds, "the waves' parts fit");
-    char *mine = lds + wave * 32 * kPitch;
-    const int32_t c0 = n0 + wn;
+    static_assert(8 * 32 * kPitch<T, 2> <= kManyLds, "the waves' parts fit");
 #pragma unroll
     for (int m = 0; m < kLive; ++m) {
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                typedef T four __attribute__((ext_vector_type(4)));
-                const four v = {(T)sum[m][n][4 * g], (T)sum[m][n][4 * g + 1], (T)sum[m][n][4 * g + 2], (T)sum[m][n][4 * g + 3]};
-                *reinterpret_cast<four *>(mine + r32 * kPitch + (n * 32 + 8 * g + 4 * half) * sizeof(T)) = v;
-            }
-        wave_meet();
-#pragma unroll
-        for (int i = 0; i < 32 / kRowsAtOnce; ++i) {
-            const int row = i * kRowsAtOnce + lane / kLanes, c = (lane % kLanes) * kVec;
-            const int4_ v = *reinterpret_cast<const int4_ *>(mine + row * kPitch + c * sizeof(T));
-            const int r = (2 * m + wm) * 32 + row;
-            if (r < rows) store_cols<T>(y + (r0 + r) * a.N, a.N, c0 + c, v);
-        }
-        wave_meet();
+        const int first = (2 * m + wm) * 32;
+        leave_by_lines<T, 2>(lds + wave * 32 * kPitch<T, 2>, sum[m], y + (r0 + first) * a.N, a.N, rows - first, a.N, n0 + wn);
     }
     };
     if (steps > 0) {

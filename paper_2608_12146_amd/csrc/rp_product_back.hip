@@ -5,11 +5,11 @@
 // bf16 parts that add up to it (one for bf16, two for fp16, three for fp32), so
 // bf16 matrix instructions form exact products and add them in 32 bits.
 //
-// Both are the same tile program: A is dy, 128 of the output's rows by 64 terms;
-// B is the matrix in 4 bits, 64 terms (its rows) by 128 columns, converted on
-// the way into LDS.  The terms are B's rows, and A's too in dw: their fragments
-// are read through the transposing LDS loads (16 lanes read 4 terms of 16
-// columns and each receives a column's 4 terms).
+// Both are the same tile program: A is dy, the output's rows by 64 terms; B is the
+// matrix in 4 bits, 64 terms (its rows) by the output's columns, converted on the
+// way into LDS.  The terms are B's rows, and A's too in dw: their fragments are
+// read through the transposing LDS loads (16 lanes read 4 terms of 16 columns and
+// each receives a column's 4 terms).
 #include "rp_product.h"
 
 namespace rp {
@@ -32,7 +32,7 @@ typedef short short4_ __attribute__((ext_vector_type(4)));
 typedef short short8_ __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kTile = 128, kTerms = 64;
+constexpr int kTerms = 64;
 
 template <class T> constexpr int kParts = sizeof(T) == 4 ? 3 : __is_same(T, _Float16) ? 2 : 1;
 
@@ -102,13 +102,26 @@ __device__ inline bf16x8 term_fragment(const char *tile, int k0, int c0) {
     return __builtin_bit_cast(bf16x8, v);
 }
 
-template <class T, bool DW, int NB>
-__global__ void __launch_bounds__(256, 2) k_product_back(BackProductArgs a) {
-    constexpr int P = kParts<T>;
-    constexpr int kCols = 64 * NB;  // a wave has 2 x NB matrix tiles, two waves each way
+// Tiles of 64 MB rows by 32 NB WN columns: 2 x WN waves of MB x NB matrix tiles.
+// A wave's blocks of 32 rows alternate with the other row of waves', and the
+// upper half of them is left out where it is empty.  TWICE: two stages of LDS, one
+// filled from registers while the other is read; else one, filled between two
+// barriers.
+template <class T, int WN, int MB, int NB, bool TWICE>
+struct BackShape {
+    static constexpr int P = kParts<T>, kThreads = 128 * WN, kRows = 64 * MB, kCols = 32 * NB * WN;
+    static constexpr int kA = kRows * kTerms * 2, kB = kTerms * kCols * 2, kStage = P * kA + kB;
+    static constexpr int kLeave = 2 * WN * 32 * kPitch<T, NB>;
+    static constexpr int kLds = (TWICE ? 2 : 1) * kStage > kLeave ? (TWICE ? 2 : 1) * kStage : kLeave;
+    // pieces of 8 values of A, and blocks of B, that a thread fetches
+    static constexpr int kPieces = kRows * kTerms / 8 / kThreads, kBlocks = kTerms * kCols / 32 / kThreads;
+};
+
+template <class T, bool DW, int WN, int MB, int NB, bool TWICE>
+__global__ void __launch_bounds__(128 * WN, WN == 4 ? 1 : 2) k_product_back(BackProductArgs a) {
+    using G = BackShape<T, WN, MB, NB, TWICE>;
+    constexpr int P = G::P, kRows = G::kRows, kCols = G::kCols;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    char *const Bs = lds + P * kTile * kTerms * 2;
-    auto As = [&](int p) { return lds + p * kTile * kTerms * 2; };
     const int64_t id = group_index();
     int32_t s, ct;
     int64_t m0;       // first output row: of R (dx), of the slot's N (dw)
@@ -118,7 +131,7 @@ __global__ void __launch_bounds__(256, 2) k_product_back(BackProductArgs a) {
         const int64_t mt = id / a.c_tiles;
         ct = (int32_t)(id - mt * a.c_tiles);
         s = (int32_t)(mt / a.m_tiles);
-        m0 = (mt - (int64_t)s * a.m_tiles) * kTile;
+        m0 = (mt - (int64_t)s * a.m_tiles) * kRows;
         seg = segment_of(a.offsets, s, a.R);
     } else {
         if (id >= a.tiles) {
@@ -128,35 +141,37 @@ __global__ void __launch_bounds__(256, 2) k_product_back(BackProductArgs a) {
         const int64_t index = id / a.c_tiles;
         ct = (int32_t)(id - index * a.c_tiles);
         int64_t before;
-        const TileMap map(a.offsets, a.n_slots, a.R, kTile);
+        const TileMap map(a.offsets, a.n_slots, a.R, kRows);
         if (index >= map.total) return;
-        s = map.find(index, a.offsets, a.n_slots, a.R, kTile, seg, before);
-        m0 = seg.begin + before * kTile;
+        s = map.find(index, a.offsets, a.n_slots, a.R, kRows, seg, before);
+        m0 = seg.begin + before * kRows;
     }
-    const int c0 = ct * kCols, t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    const int wm = (wave >> 1) * 64, wc = (wave & 1) * 32 * NB;
-    // terms [k0, k1), and A's and B's rows of them
+    const int c0 = ct * kCols, t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int wm = wave / WN, wc = (wave % WN) * 32 * NB;
+    const int64_t m_end = DW ? a.N : seg.end;
+    const int rows = m_end - m0 < kRows ? (int)(m_end - m0) : kRows;
+    // terms [k_begin, k_end), and A's and B's rows of them
     const int64_t k_begin = DW ? seg.begin : 0, k_end = DW ? seg.end : a.N;
     const T *dy = static_cast<const T *>(a.dy);
     const int64_t b_row0 = DW ? 0 : (int64_t)s * a.N;
-    int4_ pa[4][P];
-    int4_ pb[NB / 2];
-    uint32_t sb[NB / 2];
-    auto fetch = [&](int64_t k0) {
+    // The tile's A: pieces of 8 values, of a row's 64 terms (dx) or of a term's
+    // kRows columns (dw); B: blocks of 32 columns, kCols / 32 a term.
+    constexpr int kAcross = DW ? kRows / 8 : kTerms / 8, kBlocksAcross = kCols / 32;
+    constexpr int kAStep = G::kThreads / kAcross, kBStep = G::kThreads / kBlocksAcross;
+    const int a_row = t / kAcross, a_piece = t % kAcross, b_row = t / kBlocksAcross, b_block = t % kBlocksAcross;
+    int4_ pa[G::kPieces][P];
+    int4_ pb[G::kBlocks];
+    uint32_t sb[G::kBlocks];
+    auto fetch = [&](int64_t k0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (DW) {
-                const int64_t r = k0 + (t >> 4) + 16 * i;
-                split8<T, P>(dy + (r < k_end ? r : 0) * a.stride, (int32_t)m0 + (t & 15) * 8, a.N, r < k_end, pa[i]);
-            } else {
-                const int64_t r = m0 + (t >> 3) + 32 * i;
-                split8<T, P>(dy + (r < seg.end ? r : 0) * a.stride, (int32_t)k0 + (t & 7) * 8, a.N, r < seg.end, pa[i]);
-            }
+        for (int i = 0; i < G::kPieces; ++i) {
+            const int64_t r = (DW ? k0 : m0) + a_row + i * kAStep, end = DW ? k_end : m_end;
+            split8<T, P>(dy + (r < end ? r : 0) * a.stride, (int32_t)(DW ? m0 : k0) + a_piece * 8, a.N, r < end, pa[i]);
         }
-        const int64_t k = k0 + (t >> 2);
 #pragma unroll
-        for (int i = 0; i < NB / 2; ++i) {
-            const int block = ct * (kCols / 32) + (t & 3) + 4 * i;
+        for (int i = 0; i < G::kBlocks; ++i) {
+            const int64_t k = k0 + b_row + i * kBStep;
+            const int block = ct * kBlocksAcross + b_block;
             pb[i] = int4_{0, 0, 0, 0};
             sb[i] = 127;
             if (k < k_end && block < a.groups * 4) {
@@ -166,18 +181,20 @@ __global__ void __launch_bounds__(256, 2) k_product_back(BackProductArgs a) {
             }
         }
     };
-    auto store = [&]() {
+    auto store = [&](char *stage) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < G::kPieces; ++i)
 #pragma unroll
             for (int p = 0; p < P; ++p) {
+                const int row = a_row + i * kAStep;
                 int at;
-                if constexpr (DW) at = term_at<kTile>((t >> 4) + 16 * i, (t & 15) * 8);
-                else at = ((t >> 3) + 32 * i) * 128 + (((t & 7) ^ ((t >> 4) & 7)) << 4);
-                *reinterpret_cast<int4_ *>(As(p) + at) = pa[i][p];
+                if constexpr (DW) at = term_at<kRows>(row, a_piece * 8);
+                else at = row * 128 + ((a_piece ^ ((row >> 1) & 7)) << 4);
+                *reinterpret_cast<int4_ *>(stage + p * G::kA + at) = pa[i][p];
             }
+        char *const to = stage + P * G::kA;
 #pragma unroll
-        for (int b = 0; b < NB / 2; ++b) {
+        for (int b = 0; b < G::kBlocks; ++b) {
             const float scale = scale_of(sb[b]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -186,51 +203,111 @@ __global__ void __launch_bounds__(256, 2) k_product_back(BackProductArgs a) {
                                      __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3)};
                 const int4_ x = {__builtin_bit_cast(int, v[0]), __builtin_bit_cast(int, v[1]), __builtin_bit_cast(int, v[2]),
                                  __builtin_bit_cast(int, v[3])};
-                *reinterpret_cast<int4_ *>(Bs + term_at<kCols>(t >> 2, ((t & 3) + 4 * b) * 32 + i * 8)) = x;
+                *reinterpret_cast<int4_ *>(to + term_at<kCols>(b_row + b * kBStep, b_block * 32 + i * 8)) = x;
             }
         }
     };
-    float16_ sum[2][NB] = {};
-    if (k_begin < k_end) fetch(k_begin);
-    for (int64_t k0 = k_begin; k0 < k_end; k0 += kTerms) {
-        store();
-        __syncthreads();
-        if (k0 + kTerms < k_end) fetch(k0 + kTerms);
-#pragma unroll
-        for (int k = 0; k < kTerms; k += 16) {
+    T *out = static_cast<T *>(a.out) + ((DW ? (int64_t)s * a.N : 0) + m0) * a.C;
+    auto run = [&](auto live_) __attribute__((always_inline)) {
+        constexpr int kLive = decltype(live_)::value;
+        float16_ sum[kLive ? kLive : 1][NB] = {};
+        auto multiply = [&](const char *stage, int k) __attribute__((always_inline)) {
             bf16x8 b[NB];
 #pragma unroll
-            for (int n = 0; n < NB; ++n) b[n] = term_fragment<kCols>(Bs, k, wc + n * 32);
+            for (int n = 0; n < NB; ++n) b[n] = term_fragment<kCols>(stage + P * G::kA, k, wc + n * 32);
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
+            for (int m = 0; m < kLive; ++m)
 #pragma unroll
                 for (int p = P - 1; p >= 0; --p) {  // (the smallest parts first)
+                    const int first = (2 * m + wm) * 32;
                     bf16x8 x;
                     if constexpr (DW) {
-                        x = term_fragment<kTile>(As(p), k, wm + m * 32);
+                        x = term_fragment<kRows>(stage + p * G::kA, k, first);
                     } else {
-                        const int row = wm + m * 32 + (lane & 31), chunk = (k >> 3) + (lane >> 5);
-                        x = *reinterpret_cast<const bf16x8 *>(As(p) + row * 128 + ((chunk ^ ((row >> 1) & 7)) << 4));
+                        const int row = first + (lane & 31), piece = (k >> 3) + (lane >> 5);
+                        x = *reinterpret_cast<const bf16x8 *>(stage + p * G::kA + row * 128 + ((piece ^ ((row >> 1) & 7)) << 4));
                     }
 #pragma unroll
-                    for (int n = 0; n < NB; ++n) sum[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, b[n], sum[m][n], 0, 0, 0);
+                    for (int n = 0; n < NB; ++n) sum[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[n], x, sum[m][n], 0, 0, 0);
                 }
-        }
-        __syncthreads();
-    }
-    // value (m, c) of a 32 x 32 tile: column lane % 32, row 8 (i / 4) + 4 (lane / 32) + i % 4
-    T *out = static_cast<T *>(a.out);
-    const int64_t m_end = DW ? a.N : seg.end, row0 = DW ? (int64_t)s * a.N : 0;
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int n = 0; n < NB; ++n)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int64_t r = m0 + wm + m * 32 + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3);
-                const int c = c0 + wc + n * 32 + (lane & 31);
-                if (r < m_end && c < a.C) out[(row0 + r) * a.C + c] = (T)sum[m][n][i];
+        };
+        if (k_begin < k_end) fetch(k_begin);
+        if constexpr (TWICE) {
+            if (k_begin < k_end) store(lds);
+            if (k_begin + kTerms < k_end) fetch(k_begin + kTerms);
+            char *now = lds, *next = lds + G::kStage;
+            for (int64_t k0 = k_begin; k0 < k_end; k0 += kTerms) {
+                __syncthreads();  // (this stage is filled, and the other one read)
+                if (kLive) {
+                    multiply(now, 0);
+                    multiply(now, 16);
+                }
+                if (k0 + kTerms < k_end) store(next);
+                if (k0 + 2 * kTerms < k_end) fetch(k0 + 2 * kTerms);
+                if (kLive) {
+                    multiply(now, 32);
+                    multiply(now, 48);
+                }
+                char *const x = now;
+                now = next;
+                next = x;
             }
+            __syncthreads();
+        } else {
+            for (int64_t k0 = k_begin; k0 < k_end; k0 += kTerms) {
+                store(lds);
+                __syncthreads();
+                if (k0 + kTerms < k_end) fetch(k0 + kTerms);
+                if (kLive) {
+#pragma unroll
+                    for (int k = 0; k < kTerms; k += 16) multiply(lds, k);
+                }
+                __syncthreads();
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < kLive; ++m) {
+            const int first = (2 * m + wm) * 32;
+            leave_by_lines<T, NB>(lds + wave * 32 * kPitch<T, NB>, sum[m], out + first * (int64_t)a.C, a.C, rows - first, a.C, c0 + wc);
+        }
+    };
+    const int blocks = (rows + 31) / 32, live = c0 + wc < a.C ? (blocks - wm + 1) / 2 : 0;
+    if (live > MB / 2) run(Int<MB>());
+    else if (live > 0) run(Int<MB / 2>());
+    else run(Int<0>());
+}
+
+// A launch for each gradient; big: tiles of 256 x 256.
+template <class T, bool DW, int WN, int MB, int NB, bool TWICE>
+int back_by(BackProductArgs a, hipStream_t stream) {
+    using G = BackShape<T, WN, MB, NB, TWICE>;
+    a.c_tiles = (a.C + G::kCols - 1) / G::kCols;
+    if (DW) {
+        a.m_tiles = (a.N + G::kRows - 1) / G::kRows;
+        a.tiles = (int64_t)a.n_slots * a.m_tiles * a.c_tiles;
+        a.clears = 0;
+    } else {
+        // each slot may have a tile that is not full
+        const int64_t slots = a.R < a.n_slots ? a.R : a.n_slots, pieces = (a.R * a.C + 65535) / 65536;
+        a.tiles = (a.R / G::kRows + slots) * a.c_tiles;
+        a.clears = pieces < 256 ? pieces : 256;
+    }
+    const auto kern = k_product_back<T, DW, WN, MB, NB, TWICE>;
+    if (G::kLds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(kern),
+                                                   hipFuncAttributeMaxDynamicSharedMemorySize, G::kLds) != hipSuccess)
+        return ROUTEPACK_E_DEVICE;
+    hipLaunchKernelGGL(kern, grid_of(a.tiles + a.clears), dim3(G::kThreads), G::kLds, stream, a);
+    return launched();
+}
+
+template <class T, bool DW>
+int back_of(const BackProductArgs &a, hipStream_t stream) {
+    // Large tiles where they are enough for the chip.
+    const int64_t across = (a.C + 255) / 256;
+    const int64_t tiles = DW ? (int64_t)a.n_slots * ((a.N + 255) / 256) * across
+                             : (a.R + (int64_t)(a.R < a.n_slots ? a.R : a.n_slots) * 128) / 256 * across;
+    if (tiles >= 256) return back_by<T, DW, 4, 2, 2, false>(a, stream);
+    return back_by<T, DW, 2, 2, 2, false>(a, stream);
 }
 
 }  // namespace rp
@@ -272,35 +349,19 @@ extern "C" int routepack_expert_product_backward(const routepack_matrix *dy, con
     a.offsets = offsets;
     return by_type(dy->type, [&](auto tag) -> int {
         using T = decltype(tag);
-        constexpr int NB = kParts<T> == 3 ? 2 : 4, lds = kParts<T> * kTile * kTerms * 2 + kTerms * NB * 64 * 2;
-        a.c_tiles = (int32_t)((C + NB * 64 - 1) / (NB * 64));
-        auto go = [&](auto kern, int64_t n, const BackProductArgs &b) -> int {
-            if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(kern),
-                                                       hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
-                return ROUTEPACK_E_DEVICE;
-            hipLaunchKernelGGL(kern, grid_of(n), dim3(256), lds, stream, b);
-            return launched();
-        };
         if (do_x) {
             BackProductArgs b = a;
             b.bc = static_cast<const uint8_t *>(w->codes);
             b.bs = static_cast<const uint8_t *>(w->scales);
             b.out = dx->data;
-            // tiles of 128 rows: each slot may have one that is not full
-            const int64_t slots = a.R < n_slots ? a.R : n_slots;
-            b.tiles = (a.R / kTile + slots) * a.c_tiles;
-            const int64_t pieces = (a.R * C + 65535) / 65536;
-            b.clears = pieces < 256 ? pieces : 256;
-            RP_TRY(go(k_product_back<T, false, NB>, b.tiles + b.clears, b));
+            RP_TRY((back_of<T, false>(b, stream)));
         }
         if (do_w) {
             BackProductArgs b = a;
             b.bc = static_cast<const uint8_t *>(x->codes);
             b.bs = static_cast<const uint8_t *>(x->scales);
             b.out = dw->data;
-            b.m_tiles = (int32_t)((N + kTile - 1) / kTile);
-            b.tiles = (int64_t)n_slots * b.m_tiles * a.c_tiles;
-            RP_TRY(go(k_product_back<T, true, NB>, b.tiles, b));
+            RP_TRY((back_of<T, true>(b, stream)));
         }
         return ROUTEPACK_OK;
     });
