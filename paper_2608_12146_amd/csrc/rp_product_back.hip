@@ -72,6 +72,28 @@ __device__ inline void split8(const T *row, int32_t from, int32_t end, bool live
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = live && from + i < end ? to_f32(row[from + i]) : 0.0f;
     }
+    // (all finite: no test a value; what is left of an infinity or NaN is NaN)
+    float left[8], sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        left[i] = v[i] - __uint_as_float(__float_as_uint(v[i]) & 0xFFFF0000u);
+        sum += left[i];
+    }
+    if (P > 1 && sum == sum) {
+        auto top = [](float a, float b) {  // the upper halves, b's above a's
+            return (int)__builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+        };
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            part[0][i] = top(v[2 * i], v[2 * i + 1]);
+            part[P > 1 ? 1 : 0][i] = top(left[2 * i], left[2 * i + 1]);
+            if (P > 2) {
+                const float a = left[2 * i], b = left[2 * i + 1];
+                part[P - 1][i] = top(a - __uint_as_float(__float_as_uint(a) & 0xFFFF0000u), b - __uint_as_float(__float_as_uint(b) & 0xFFFF0000u));
+            }
+        }
+        return;
+    }
 #pragma unroll
     for (int p = 0; p < P; ++p)
 #pragma unroll
@@ -104,22 +126,22 @@ __device__ inline bf16x8 term_fragment(const char *tile, int k0, int c0) {
 
 // Tiles of 64 MB rows by 32 NB WN columns: 2 x WN waves of MB x NB matrix tiles.
 // A wave's blocks of 32 rows alternate with the other row of waves', and the
-// upper half of them is left out where it is empty.  TWICE: two stages of LDS, one
-// filled from registers while the other is read; else one, filled between two
-// barriers.
-template <class T, int WN, int MB, int NB, bool TWICE>
+// upper half of them is left out where it is empty.  One stage of LDS, filled
+// between two barriers: two or three workgroups a CU (WAVES a SIMD) cover each
+// other's phases (two stages with one barrier, one workgroup a CU: @TWICE@).
+template <class T, int WN, int MB, int NB>
 struct BackShape {
     static constexpr int P = kParts<T>, kThreads = 128 * WN, kRows = 64 * MB, kCols = 32 * NB * WN;
     static constexpr int kA = kRows * kTerms * 2, kB = kTerms * kCols * 2, kStage = P * kA + kB;
     static constexpr int kLeave = 2 * WN * 32 * kPitch<T, NB>;
-    static constexpr int kLds = (TWICE ? 2 : 1) * kStage > kLeave ? (TWICE ? 2 : 1) * kStage : kLeave;
+    static constexpr int kLds = kStage > kLeave ? kStage : kLeave;
     // pieces of 8 values of A, and blocks of B, that a thread fetches
     static constexpr int kPieces = kRows * kTerms / 8 / kThreads, kBlocks = kTerms * kCols / 32 / kThreads;
 };
 
-template <class T, bool DW, int WN, int MB, int NB, bool TWICE>
-__global__ void __launch_bounds__(128 * WN, WN == 4 ? 1 : 2) k_product_back(BackProductArgs a) {
-    using G = BackShape<T, WN, MB, NB, TWICE>;
+template <class T, bool DW, int WN, int MB, int NB, int WAVES>
+__global__ void __launch_bounds__(128 * WN, WAVES) k_product_back(BackProductArgs a) {
+    using G = BackShape<T, WN, MB, NB>;
     constexpr int P = G::P, kRows = G::kRows, kCols = G::kCols;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int64_t id = group_index();
@@ -232,38 +254,15 @@ __global__ void __launch_bounds__(128 * WN, WN == 4 ? 1 : 2) k_product_back(Back
                 }
         };
         if (k_begin < k_end) fetch(k_begin);
-        if constexpr (TWICE) {
-            if (k_begin < k_end) store(lds);
-            if (k_begin + kTerms < k_end) fetch(k_begin + kTerms);
-            char *now = lds, *next = lds + G::kStage;
-            for (int64_t k0 = k_begin; k0 < k_end; k0 += kTerms) {
-                __syncthreads();  // (this stage is filled, and the other one read)
-                if (kLive) {
-                    multiply(now, 0);
-                    multiply(now, 16);
-                }
-                if (k0 + kTerms < k_end) store(next);
-                if (k0 + 2 * kTerms < k_end) fetch(k0 + 2 * kTerms);
-                if (kLive) {
-                    multiply(now, 32);
-                    multiply(now, 48);
-                }
-                char *const x = now;
-                now = next;
-                next = x;
+        for (int64_t k0 = k_begin; k0 < k_end; k0 += kTerms) {
+            store(lds);
+            __syncthreads();
+            if (k0 + kTerms < k_end) fetch(k0 + kTerms);
+            if (kLive) {
+#pragma unroll
+                for (int k = 0; k < kTerms; k += 16) multiply(lds, k);
             }
             __syncthreads();
-        } else {
-            for (int64_t k0 = k_begin; k0 < k_end; k0 += kTerms) {
-                store(lds);
-                __syncthreads();
-                if (k0 + kTerms < k_end) fetch(k0 + kTerms);
-                if (kLive) {
-#pragma unroll
-                    for (int k = 0; k < kTerms; k += 16) multiply(lds, k);
-                }
-                __syncthreads();
-            }
         }
 #pragma unroll
         for (int m = 0; m < kLive; ++m) {
@@ -277,10 +276,9 @@ __global__ void __launch_bounds__(128 * WN, WN == 4 ? 1 : 2) k_product_back(Back
     else run(Int<0>());
 }
 
-// A launch for each gradient; big: tiles of 256 x 256.
-template <class T, bool DW, int WN, int MB, int NB, bool TWICE>
+template <class T, bool DW, int WN, int MB, int NB, int WAVES>
 int back_by(BackProductArgs a, hipStream_t stream) {
-    using G = BackShape<T, WN, MB, NB, TWICE>;
+    using G = BackShape<T, WN, MB, NB>;
     a.c_tiles = (a.C + G::kCols - 1) / G::kCols;
     if (DW) {
         a.m_tiles = (a.N + G::kRows - 1) / G::kRows;
@@ -292,7 +290,7 @@ int back_by(BackProductArgs a, hipStream_t stream) {
         a.tiles = (a.R / G::kRows + slots) * a.c_tiles;
         a.clears = pieces < 256 ? pieces : 256;
     }
-    const auto kern = k_product_back<T, DW, WN, MB, NB, TWICE>;
+    const auto kern = k_product_back<T, DW, WN, MB, NB, WAVES>;
     if (G::kLds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(kern),
                                                    hipFuncAttributeMaxDynamicSharedMemorySize, G::kLds) != hipSuccess)
         return ROUTEPACK_E_DEVICE;
@@ -302,12 +300,13 @@ int back_by(BackProductArgs a, hipStream_t stream) {
 
 template <class T, bool DW>
 int back_of(const BackProductArgs &a, hipStream_t stream) {
-    // Large tiles where they are enough for the chip.
-    const int64_t across = (a.C + 255) / 256;
-    const int64_t tiles = DW ? (int64_t)a.n_slots * ((a.N + 255) / 256) * across
-                             : (a.R + (int64_t)(a.R < a.n_slots ? a.R : a.n_slots) * 128) / 256 * across;
-    if (tiles >= 256) return back_by<T, DW, 4, 2, 2, false>(a, stream);
-    return back_by<T, DW, 2, 2, 2, false>(a, stream);
+    // dx: tiles of 128 x 256 where they are enough for the chip.  dw, whose sums are
+    // short, and small problems: of 128 x 128, more of them at a time.
+    const int64_t tiles = (a.R / 128 + (a.R < a.n_slots ? a.R : a.n_slots) / 2) * ((a.C + 255) / 256);
+    constexpr int P = kParts<T>;
+    if constexpr (!DW)
+        if (tiles >= 256) return back_by<T, DW, 4, 2, 2, P == 1 ? 4 : 2>(a, stream);
+    return back_by<T, DW, 2, 2, 2, P == 1 ? 3 : 2>(a, stream);
 }
 
 }  // namespace rp

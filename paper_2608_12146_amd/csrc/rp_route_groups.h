@@ -5,7 +5,7 @@
 //
 // A group lies in Q adjacent lanes (a power of two) of up to 8 vectors of 16
 // bytes, a token in the Q n_groups lanes of its groups, rounded up to a power of
-// two and 4: a group's best keys are reductions over its lanes, its rank is the
+// two and 8: a group's best keys are reductions over its lanes, its rank is the
 // number of groups that precede it, and the choice runs as without groups
 // (rp_route_choose.h) over the vectors of the groups kept: their maxima, then the
 // elements of the k vectors that lead.  Few lanes, as each doubling costs a merge
@@ -90,12 +90,19 @@ __device__ inline void lanes_first(uint64_t &key, uint32_t &at, int lanes) {
     at = take ? oa : at;
     if constexpr (D < kWave) lanes_first<2 * D>(key, at, lanes);
 }
+// The K largest of the lanes' lists, in every lane, in no order: the upper half of
+// the lanes has them the other way round.
 template <class Key, int K, int D = 2>
 __device__ inline void lanes_top(typename Key::Word (&top)[K], int lanes) {
     if (D > lanes) return;
     typename Key::Word y[K];
 #pragma unroll
     for (int i = 0; i < K; ++i) y[i] = across<D>(top[i]);
+    if (D == lanes) {  // (the last step need not sort)
+#pragma unroll
+        for (int i = 0; i < K; ++i) top[i] = Key::max(top[i], y[K - 1 - i]);
+        return;
+    }
     merge_top<Key, K>(top, y);
     if constexpr (D < kWave) lanes_top<Key, K, 2 * D>(top, lanes);
 }
@@ -122,11 +129,12 @@ __device__ inline int groups_before(int groups, int q_shift, uint64_t best, int 
     return n;
 }
 
-template <class T, int NV, int K, bool SCORES>
+// WHOLE: every lane's vectors are whole.
+template <class T, int NV, int K, bool SCORES, bool WHOLE>
 __global__ void __launch_bounds__(256) k_route_groups(GroupArgs ga) {
     using Key = typename KeyOf<typename Choose<SCORES, float, T>::type>::type;
     using Word = typename Key::Word;
-    constexpr int W = 16 / sizeof(T), M = 4, S = K / M;
+    constexpr int W = 16 / sizeof(T), M = 8, S = K / M;
     const RouteArgs &a = ga.r;
     const int lanes = 1 << ga.lane_shift, Q = 1 << ga.q_shift;
     const int c = threadIdx.x & (lanes - 1), g = c >> ga.q_shift, q = c & (Q - 1);
@@ -139,7 +147,7 @@ __global__ void __launch_bounds__(256) k_route_groups(GroupArgs ga) {
     const int32_t l = (int32_t)(at - t * a.L);
     const T *data = static_cast<const T *>(a.logits) + t * a.ts + l * a.ls;
     const float *bias = SCORES && a.bias ? a.bias + (int64_t)l * a.E : nullptr;
-    const Row<T> row = {data + g * ga.size, g < ga.groups ? ga.size : 0};
+    const Row<T, WHOLE> row = {data + g * ga.size, g < ga.groups ? ga.size : 0};
     Vec<T> raw[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) raw[i] = row.vec(i * Q + q);
@@ -185,7 +193,7 @@ __global__ void __launch_bounds__(256) k_route_groups(GroupArgs ga) {
         if constexpr (SCORES) {
             float b[W] = {};
             if (bias) {
-                const Row<float> bias_row = {bias + group * ga.size, group < ga.groups ? ga.size : 0};
+                const Row<float, WHOLE> bias_row = {bias + group * ga.size, group < ga.groups ? ga.size : 0};
 #pragma unroll
                 for (int k = 0; k < W / 4; ++k) {
                     const Vec<float> x = bias_row.vec(vec * (W / 4) + k);
@@ -196,9 +204,8 @@ __global__ void __launch_bounds__(256) k_route_groups(GroupArgs ga) {
 #pragma unroll
             for (int w = 0; w < W; ++w) {
                 const float z = r.at(w);
-                float s, less;
-                if (softmax) s = exp_plain(z - m) * inv;
-                else logistic<false>(z, s, less);
+                // (a logistic score this way keeps the absolute error below, not 1 - s)
+                const float s = softmax ? exp_plain(z - m) * inv : __builtin_amdgcn_rcpf(1.0f + exp_plain(-z));
                 const float key = s + b[w];
                 y[w] = z > -kInf && key > -kInf ? key : -kInf;
             }
@@ -251,15 +258,18 @@ __global__ void __launch_bounds__(256) k_route_groups(GroupArgs ga) {
     for (int i = 0; i < NV; ++i) vk[i] = Key::make(mx[i], kIndexMask ^ (uint32_t)(g * per_group + i * Q + q));
     lane_top<Key, K, NV>(vk, first);
     lanes_top<Key, K>(first, lanes);
-    // the elements of the k vectors that lead, vector s M + c in lane c < M
+    // the elements of the K vectors that lead, one or a few in each lane c < M
     Word x[S * W], top[K];
     float cand[SCORES ? S * W : 1], most[S];
 #pragma unroll
     for (int s = 0; s < S; ++s) {
         Word mine = Word(0);
 #pragma unroll
-        for (int j = 0; j < M; ++j) mine = c == j ? first[s * M + j] : mine;
-        const bool ok = c < M && s * M + c < a.k && Key::available(mine);
+        for (int j = 0; j < M; ++j) {
+            const int up = s * M + j;
+            mine = c == j ? (j >= M / 2 && lanes == M ? first[K - 1 - up] : first[up]) : mine;
+        }
+        const bool ok = c < M && Key::available(mine);
         const int id = (int)Key::index(mine), vg = id / per_group, v = id - vg * per_group;
         most[s] = ok ? Key::value(mine) : -kInf;
 #pragma unroll
@@ -269,7 +279,7 @@ __global__ void __launch_bounds__(256) k_route_groups(GroupArgs ga) {
         }
         if (ok) {
             float y[W];
-            const Row<T> r = {data + vg * ga.size, ga.size};
+            const Row<T, WHOLE> r = {data + vg * ga.size, ga.size};
             keys_of(r.vec(v), vg, v, y);
 #pragma unroll
             for (int w = 0; w < W; ++w) {
@@ -426,7 +436,7 @@ __global__ void __launch_bounds__(256) k_route_groups(GroupArgs ga) {
 }
 
 // Lanes of a group and a token: as few as hold a group in 8 vectors a lane (at
-// least 4 a token, for the second selection).
+// least 8 a token, for the second selection).
 template <class T>
 int choose_groups(GroupArgs a, hipStream_t stream) {
     constexpr int W = 16 / sizeof(T);
@@ -439,7 +449,7 @@ int choose_groups(GroupArgs a, hipStream_t stream) {
     a.q_shift = 0;
     const int vecs = (a.size + W - 1) / W;
     auto each = [&] { return (vecs + (1 << a.q_shift) - 1) >> a.q_shift; };
-    while ((each() > 8 && (groups << a.q_shift) < kWave) || (groups << a.q_shift) < 4) ++a.q_shift;
+    while ((each() > 8 && (groups << a.q_shift) < kWave) || (groups << a.q_shift) < 8) ++a.q_shift;
     a.lane_shift += a.q_shift;
     const int64_t items = a.r.T * a.r.L, per = 256 >> a.lane_shift;
     auto go = [&](auto kern) {
@@ -449,8 +459,12 @@ int choose_groups(GroupArgs a, hipStream_t stream) {
     auto by_k = [&](auto v) {
         constexpr int N = decltype(v)::value;
         const bool scores = a.r.bias || a.top > 1;
-        if (a.r.k <= 8) return scores ? go(k_route_groups<T, N, 8, true>) : go(k_route_groups<T, N, 8, false>);
-        return scores ? go(k_route_groups<T, N, 32, true>) : go(k_route_groups<T, N, 32, false>);
+        // (8 choices at most, whole vectors and no idle lanes: without the checks of
+        // every vector)
+        const bool whole = a.r.k <= 8 && a.size == (N * W) << a.q_shift && a.groups == groups;
+        if (whole) return scores ? go(k_route_groups<T, N, 8, true, true>) : go(k_route_groups<T, N, 8, false, true>);
+        if (a.r.k <= 8) return scores ? go(k_route_groups<T, N, 8, true, false>) : go(k_route_groups<T, N, 8, false, false>);
+        return scores ? go(k_route_groups<T, N, 32, true, false>) : go(k_route_groups<T, N, 32, false, false>);
     };
     if (each() <= 1) return by_k(Int<1>());
     if (each() <= 2) return by_k(Int<2>());
