@@ -16,65 +16,87 @@ struct ProductArgs {
     int64_t clears;
 };
 
-// Few rows a slot: a workgroup holds 16 of a slot's N and passes over its rows,
-// 16 RB at a time; the four waves share the columns and add up in LDS.
-// Bound by the weights' bytes: each is read once (per pass).
+// Few rows a slot: a wave holds 16 of a slot's N, a workgroup 64, and passes over
+// the slot's rows, 16 RB at a time.  A lane loads 16 bytes of a row of w and of x
+// for each 128 columns, the scales of 512 columns at once.
+// Bound by the weights' bytes: each is read once a pass.
 template <class T, int RB>
 __global__ void __launch_bounds__(256) k_product_few(ProductArgs a) {
-    __shared__ float part[4][RB][4][kWave];
     const int64_t id = group_index();
     if (id >= a.tiles) {
         clear_rows(static_cast<T *>(a.y), a.N, a.offsets, a.n_slots, a.R, id - a.tiles, a.clears);
         return;
     }
     const int64_t index = id / a.n_tiles;
-    const int32_t n0 = (int32_t)(id - index * a.n_tiles) * 16;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, i16 = lane & 15;
+    const int32_t n0 = (int32_t)(id - index * a.n_tiles) * 64 + wave * 16;
     const TileMap map(a.offsets, a.n_slots, a.R, 0);
-    if (index >= map.total) return;
+    if (index >= map.total || n0 >= a.N) return;
     Segment seg;
     int64_t before;
     const int32_t s = map.find(index, a.offsets, a.n_slots, a.R, 0, seg, before);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane >> 4, i16 = lane & 15;
     const int32_t n = n0 + i16 < a.N ? n0 + i16 : a.N - 1;
     const int64_t row = (int64_t)s * a.N + n;
-    const uint8_t *wc = a.wc + row * a.groups * 64 + q * 16, *ws = a.ws + row * a.groups * 4;
-    const int32_t g0 = (int32_t)((int64_t)a.groups * wave / 4), g1 = (int32_t)((int64_t)a.groups * (wave + 1) / 4);
+    const uint8_t *wc = a.wc + row * a.groups * 64 + q * 16;
+    const uint32_t *ws = reinterpret_cast<const uint32_t *>(a.ws + row * a.groups * 4);
     for (int64_t r0 = seg.begin; r0 < seg.end; r0 += 16 * RB) {
-        const uint8_t *xc[RB], *xs[RB];
+        const uint8_t *xc[RB];
+        const uint32_t *xs[RB];
 #pragma unroll
         for (int b = 0; b < RB; ++b) {
             const int64_t r = r0 + b * 16 + i16, x = r < seg.end ? r : seg.end - 1;
             xc[b] = a.xc + x * a.groups * 64 + q * 16;
-            xs[b] = a.xs + x * a.groups * 4;
+            xs[b] = reinterpret_cast<const uint32_t *>(a.xs + x * a.groups * 4);
         }
         float4_ sum[RB] = {};
-#pragma unroll 4
-        for (int32_t g = g0; g < g1; ++g) {
-            const int4_ w = *reinterpret_cast<const int4_ *>(wc + (int64_t)g * 64);
-            const int wscale = (*reinterpret_cast<const int *>(ws + (int64_t)g * 4) >> (8 * q)) & 255;
+        // N groups of 128 columns from g on
+        auto some = [&](int32_t g, auto n_) __attribute__((always_inline)) {
+            constexpr int M = decltype(n_)::value;
+            typedef uint32_t words __attribute__((ext_vector_type(M), aligned(4)));
+            int4_ w[M], x[RB][M];
+            uint32_t wscale[M], xscale[RB][M];
+#pragma unroll
+            for (int i = 0; i < M; ++i) w[i] = *reinterpret_cast<const int4_ *>(wc + (int64_t)(g + i) * 64);
+            const words v = *reinterpret_cast<const words *>(ws + g);
+#pragma unroll
+            for (int i = 0; i < M; ++i) wscale[i] = v[i];
 #pragma unroll
             for (int b = 0; b < RB; ++b) {
-                const int4_ x = *reinterpret_cast<const int4_ *>(xc[b] + (int64_t)g * 64);
-                const int xscale = (*reinterpret_cast<const int *>(xs[b] + (int64_t)g * 4) >> (8 * q)) & 255;
-                const int8_ wa = {w[0], w[1], w[2], w[3], 0, 0, 0, 0}, xb = {x[0], x[1], x[2], x[3], 0, 0, 0, 0};
-                sum[b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wa, xb, sum[b], 4, 4, 0, wscale, 0, xscale);
+#pragma unroll
+                for (int i = 0; i < M; ++i) x[b][i] = *reinterpret_cast<const int4_ *>(xc[b] + (int64_t)(g + i) * 64);
+                const words u = *reinterpret_cast<const words *>(xs[b] + g);
+#pragma unroll
+                for (int i = 0; i < M; ++i) xscale[b][i] = u[i];
             }
-        }
 #pragma unroll
-        for (int b = 0; b < RB; ++b)
+            for (int i = 0; i < M; ++i)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) part[wave][b][i][lane] = sum[b][i];
-        __syncthreads();
-        // value (n, r) stands in lane (n / 4) 16 + r, element n % 4
-        const int n_ = threadIdx.x & 15, r_ = threadIdx.x >> 4, from = (n_ >> 2) * 16 + r_;
+                for (int b = 0; b < RB; ++b) {
+                    const int8_ wa = {w[i][0], w[i][1], w[i][2], w[i][3], 0, 0, 0, 0};
+                    const int8_ xb = {x[b][i][0], x[b][i][1], x[b][i][2], x[b][i][3], 0, 0, 0, 0};
+                    sum[b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wa, xb, sum[b], 4, 4, 0, (int)(wscale[i] >> (8 * q)), 0,
+                                                                              (int)(xscale[b][i] >> (8 * q)));
+                }
+        };
+        int32_t g = 0;
+        for (; g + 4 <= a.groups; g += 4) some(g, Int<4>());
+        for (; g < a.groups; ++g) some(g, Int<1>());
+        // a value's row is lane % 16, its column 4 (lane / 16) + i
 #pragma unroll
         for (int b = 0; b < RB; ++b) {
-            const float v = (part[0][b][n_ & 3][from] + part[1][b][n_ & 3][from]) +
-                            (part[2][b][n_ & 3][from] + part[3][b][n_ & 3][from]);
-            const int64_t r = r0 + b * 16 + r_;
-            if (r < seg.end && n0 + n_ < a.N) static_cast<T *>(a.y)[r * a.N + n0 + n_] = (T)v;
+            const int64_t r = r0 + b * 16 + i16;
+            if (r >= seg.end) continue;
+            T *y = static_cast<T *>(a.y) + r * a.N + n0 + q * 4;
+            typedef T four __attribute__((ext_vector_type(4), aligned(2)));
+            const four v = {(T)sum[b][0], (T)sum[b][1], (T)sum[b][2], (T)sum[b][3]};
+            if (n0 + q * 4 + 4 <= a.N) {
+                *reinterpret_cast<four *>(y) = v;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (n0 + q * 4 + i < a.N) y[i] = v[i];
+            }
         }
-        __syncthreads();
     }
 }
 
@@ -286,9 +308,16 @@ extern "C" int routepack_expert_product(const routepack_mx *x, const routepack_m
     const int64_t most = a.R < n_slots ? a.R : n_slots;  // slots with rows
     const int64_t pieces = (a.R * N + 65535) / 65536;
     a.clears = pieces < 256 ? pieces : 256;
+    // Rows a slot on average, and tiles of 256 x 256.  Up to 6 rows the weights'
+    // bytes are all there is and many small workgroups stream them best (256 x 2048
+    // x 2048, 512 rows: 89 us, 104 by tiles; 2048 rows: 138 and 126); so do they where
+    // the tiles would leave half of the chip idle, as long as a slot's rows are few
+    // passes (64 x 256 x 256, 2000 rows: 12 and 15 us).
+    const int64_t tiles = (a.R / kTileRows + most) * ((N + kTileCols - 1) / kTileCols);
+    const bool many = a.R >= 64 * (int64_t)n_slots || (a.R >= 6 * (int64_t)n_slots && tiles >= 128);
     return by_type(y->type, [&](auto tag) -> int {
         using T = decltype(tag);
-        if (a.R >= 32 * (int64_t)n_slots) {
+        if (many) {
             const auto kern = k_product_many<T>;
             a.n_tiles = (int32_t)((N + kTileCols - 1) / kTileCols);
             // (each slot may have a tile that is not full; eight runs of equal length)
@@ -299,9 +328,10 @@ extern "C" int routepack_expert_product(const routepack_mx *x, const routepack_m
             hipLaunchKernelGGL(kern, grid_of(a.tiles + a.clears), dim3(512), kManyLds, stream, a);
             return launched();
         }
-        a.n_tiles = (int32_t)((N + 15) / 16);
+        a.n_tiles = (int32_t)((N + 63) / 64);
         a.tiles = most * a.n_tiles;
-        hipLaunchKernelGGL((k_product_few<T, 2>), grid_of(a.tiles + a.clears), dim3(256), 0, stream, a);
+        const auto kern = a.R < 8 * (int64_t)n_slots ? k_product_few<T, 1> : k_product_few<T, 2>;
+        hipLaunchKernelGGL(kern, grid_of(a.tiles + a.clears), dim3(256), 0, stream, a);
         return launched();
     });
 }

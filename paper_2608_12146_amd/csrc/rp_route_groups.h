@@ -17,9 +17,9 @@
 // 32 bits, and where their error leaves the groups kept, the choices or their
 // order open (about one token in 500, and ties), the wave forms them in 64.
 //
-// Bound by HBM and vector instructions: 131072 x 512 bf16, 8 groups: @STRESS@
-// us; 65536 x 256 fp32, logistic, two keys a group and a bias: @BIAS@ us (78 with
-// all keys in 64 bits).
+// Bound by HBM and vector instructions: 131072 x 512 bf16, 8 groups: 40 us
+// (a copy of the logits takes 26); 65536 x 256 fp32, logistic, two keys a group and a bias: 44 us (78 with all
+// keys in 64 bits; 35 without the tokens in doubt, whose waves end last).
 #pragma once
 
 #include "rp_route.h"
@@ -129,9 +129,11 @@ __device__ inline int groups_before(int groups, int q_shift, uint64_t best, int 
     return n;
 }
 
-// WHOLE: every lane's vectors are whole.
+// WHOLE: every lane's vectors are whole.  (Scores with up to 8 choices are held to
+// four waves a SIMD: left alone the part in 64 bits takes twice the registers, and
+// 51 us where the call takes 44.)
 template <class T, int NV, int K, bool SCORES, bool WHOLE>
-__global__ void __launch_bounds__(256) k_route_groups(GroupArgs ga) {
+__global__ void __launch_bounds__(256, SCORES && K == 8 ? 4 : 1) k_route_groups(GroupArgs ga) {
     using Key = typename KeyOf<typename Choose<SCORES, float, T>::type>::type;
     using Word = typename Key::Word;
     constexpr int W = 16 / sizeof(T), M = 8, S = K / M;
