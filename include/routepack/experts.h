@@ -52,8 +52,8 @@ typedef struct routepack_mx {
     int64_t n_rows, n_cols;
 } routepack_mx;
 
-/* Bytes of workspace that routepack_order_tokens needs for n_tokens tokens, or
- * an error of it. */
+/* Bytes of workspace that routepack_order_tokens needs for n_tokens tokens (0 for
+ * few), or an error of it. */
 int64_t routepack_order_workspace(const routepack_problem *prob, int64_t n_tokens);
 
 /* The order of every layer's pairs by slot, and by pair within a slot.
@@ -65,7 +65,7 @@ int64_t routepack_order_workspace(const routepack_problem *prob, int64_t n_token
  *   offsets    int64 [L][E + 1] out
  *   places     int32 [T][L][k] out
  *   workspace  at least routepack_order_workspace bytes, 16-byte aligned, for
- *              this call alone until its work has ended
+ *              this call alone until its work has ended (may be NULL where those are 0)
  * E_INVALID on null pointers, a negative size or stride, E < 1, k < 1, an
  * unknown type, or a workspace too small or misaligned; E_UNSUPPORTED when
  * E > 2048, k > 256, or T k >= 2^31. */

@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -70,17 +71,6 @@ class _Rows(C.Structure):
                 ("layer_stride", C.c_int64)]
 
 
-class _Matrix(C.Structure):
-    """routepack_matrix."""
-    _fields_ = [("data", C.c_void_p), ("type", C.c_int32), ("n_rows", C.c_int64), ("n_cols", C.c_int64),
-                ("row_stride", C.c_int64)]
-
-
-class _MxMatrix(C.Structure):
-    """routepack_mx."""
-    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("n_rows", C.c_int64), ("n_cols", C.c_int64)]
-
-
 _lib = None
 
 
@@ -111,15 +101,15 @@ def load_library():
         lib.routepack_balance_loss.argtypes = [P, R, i32, vp, vp, i32, i32, vp, vp, vp, i64, vp]
         lib.routepack_route_backward.argtypes = [P, R, R, vp, i32, f32, i32, vp, vp, i32, vp, i32, vp, vp]
         lib.routepack_route_grouped.argtypes = [P, R, vp, i32, i32, i32, i32, i32, f32, vp, vp, vp]
-        M, X = C.POINTER(_Matrix), C.POINTER(_MxMatrix)
+        M = X = vp  # (routepack_matrix, routepack_mx and routepack_ids, also as packed bytes)
         lib.routepack_order_workspace.argtypes = [P, i64]
         lib.routepack_order_tokens.argtypes = [P, R, vp, vp, vp, vp, vp, i64, vp]
-        lib.routepack_quantize_mx.argtypes = [M, vp, R, i32, X, vp]
+        lib.routepack_quantize_mx.argtypes = [M, vp, vp, i32, X, vp]
         lib.routepack_dequantize_mx.argtypes = [X, M, vp]
         lib.routepack_expert_product.argtypes = [X, X, i32, vp, M, vp]
         lib.routepack_expert_product_backward.argtypes = [M, X, X, i32, vp, M, M, vp]
-        lib.routepack_combine_tokens.argtypes = [M, R, i32, vp, i64, M, vp]
-        lib.routepack_combine_backward.argtypes = [M, M, vp, R, i32, vp, i64, M, vp, vp]
+        lib.routepack_combine_tokens.argtypes = [M, vp, i32, vp, i64, M, vp]
+        lib.routepack_combine_backward.argtypes = [M, M, vp, vp, i32, vp, i64, M, vp, vp]
         lib.routepack_strerror.argtypes = [C.c_int]
         lib.routepack_strerror.restype = C.c_char_p
         for f in EXPORTS:
@@ -725,25 +715,45 @@ class Mx:
         return (*self.codes.shape[:-1], self.columns)
 
 
+# routepack_matrix, routepack_mx and routepack_ids as bytes, which take less to make
+# than structures of ctypes do (a call takes about 9 microseconds, 10.5 with those).
+_MATRIX, _MX, _IDS = struct.Struct("Pi4xqqq").pack, struct.Struct("PPqq").pack, struct.Struct("Pi4xqqq").pack
+
+
 class _ExpertCall(_Call):
     __slots__ = ()
 
+    def on_device(self, x):
+        """Whether x is a tensor on the call's GPU (the first one decides)."""
+        if type(x) is not self.torch.Tensor or not x.is_cuda:
+            return False
+        if self.device is None:
+            self.device = x.device
+            return True
+        return x.device == self.device
+
     def mx(self, name, q, dims):
-        """An Mx of `dims` axes, or of that many and more: (its shape, the
-        description of its rows)."""
+        """An Mx of `dims` axes: (its codes' shape, its rows for the library)."""
         torch = self.torch
         if not isinstance(q, Mx):
             raise TypeError(f"{self.fn}: {name} must be an Mx, got {type(q).__name__}")
-        codes = self.tensor(f"{name}.codes", q.codes, (torch.uint8,))
-        scales = self.tensor(f"{name}.scales", q.scales, (torch.uint8,))
-        n, shape = (q.columns + 127) // 128, codes.shape
-        if len(shape) != dims or q.columns < 0 or shape[-1] != 64 * n or scales.shape != (*shape[:-1], 4 * n):
+        codes, scales, cols = q.codes, q.scales, q.columns
+        n = (cols + 127) // 128
+        if self.on_device(codes) and self.on_device(scales) and codes.dtype is torch.uint8 and scales.dtype is torch.uint8:
+            shape, s = codes.shape, scales.shape
+            if (len(shape) == len(s) == dims and shape[-1] == 64 * n and s[-1] == 4 * n and cols >= 0 and shape[0] == s[0]
+                    and (dims == 2 or shape[1] == s[1]) and codes.is_contiguous() and scales.is_contiguous()):
+                return shape, _MX(codes.data_ptr(), scales.data_ptr(), shape[0] if dims == 2 else shape[0] * shape[1], cols)
+        # what is wrong with it (or a subclass of Tensor)
+        codes = self.tensor(f"{name}.codes", codes, (torch.uint8,))
+        scales = self.tensor(f"{name}.scales", scales, (torch.uint8,))
+        shape = codes.shape
+        if len(shape) != dims or cols < 0 or shape[-1] != 64 * n or scales.shape != (*shape[:-1], 4 * n):
             raise ValueError(f"{self.fn}: {name} has codes {tuple(shape)} and scales {tuple(scales.shape)} for "
-                             f"{q.columns} columns, expected {dims} axes, the last {64 * n} and {4 * n}")
+                             f"{cols} columns, expected {dims} axes, the last {64 * n} and {4 * n}")
         if not codes.is_contiguous() or not scales.is_contiguous():
             raise ValueError(f"{self.fn}: {name} must be contiguous")
-        rows = shape[0] if dims == 2 else shape[0] * shape[1]
-        return shape, _MxMatrix(codes.data_ptr(), scales.data_ptr(), rows, q.columns)
+        return shape, _MX(codes.data_ptr(), scales.data_ptr(), shape[0] if dims == 2 else shape[0] * shape[1], cols)
 
     def matrix(self, name, x, types):
         """[rows][columns] with adjacent columns."""
@@ -753,31 +763,36 @@ class _ExpertCall(_Call):
             raise ValueError(f"{self.fn}: {name} has shape {tuple(shape)}, expected [rows][columns]")
         if shape[1] > 1 and stride[1] != 1 and shape[0] > 0:
             raise ValueError(f"{self.fn}: the columns of {name} must be adjacent in memory")
-        return shape, _Matrix(x.data_ptr(), types[x.dtype], shape[0], shape[1], stride[0])
+        return shape, _MATRIX(x.data_ptr(), types[x.dtype], shape[0], shape[1], stride[0])
 
-    def out(self, rows, cols, dtype, types, lead=None):
-        x = self.torch.empty((rows, cols) if lead is None else (lead, rows, cols), dtype=dtype, device=self.device)
-        return x, _Matrix(x.data_ptr(), types[dtype], rows * (lead or 1) if lead != 0 else 0, cols, cols)
+    def out(self, rows, cols, dtype, types):
+        """A new matrix."""
+        x = self.torch.empty((rows, cols), dtype=dtype, device=self.device)
+        return x, _MATRIX(x.data_ptr(), types[dtype], rows, cols, cols)
 
     def offsets(self, order, n_slots):
         off = order.offsets if isinstance(order, Order) else order
+        if self.on_device(off) and off.dtype is self.torch.int64 and off.shape == (n_slots + 1,) and off.is_contiguous():
+            return off.data_ptr()
         return self.dense("offsets", off, (self.torch.int64,), (n_slots + 1,)).data_ptr()
 
     def places(self, order):
         if not isinstance(order, Order):
             raise TypeError(f"{self.fn}: order must be an Order, got {type(order).__name__}")
         p = self.tensor("order.places", order.places, (self.torch.int32,))
-        if p.dim() != 2 or p.shape[1] < 1 or (p.shape[1] > 1 and p.stride(1) != 1 and p.shape[0] > 0):
-            raise ValueError(f"{self.fn}: order.places has shape {tuple(p.shape)}, expected [T][k], choices adjacent")
-        return p.shape, _Rows(p.data_ptr(), 5, p.shape[0], p.stride(0), 0)
+        shape, stride = p.shape, p.stride()
+        if len(shape) != 2 or shape[1] < 1 or (shape[1] > 1 and stride[1] != 1 and shape[0] > 0):
+            raise ValueError(f"{self.fn}: order.places has shape {tuple(shape)}, expected [T][k], choices adjacent")
+        return shape, _IDS(p.data_ptr(), 5, shape[0], stride[0], 0)
 
     def gates(self, gates, shape):
         if gates is None:
             return None, 0
         g = self.tensor("gates", gates, (self.torch.float32,), shape)
-        if g.shape[1] > 1 and g.stride(1) != 1 and g.shape[0] > 0:
+        stride = g.stride()
+        if shape[1] > 1 and stride[1] != 1 and shape[0] > 0:
             raise ValueError(f"{self.fn}: a token's gates must be adjacent in memory")
-        return g.data_ptr(), g.stride(0)
+        return g.data_ptr(), stride[0]
 
 
 def order_tokens(prob: Problem, ids, *, slots=None):
@@ -799,9 +814,9 @@ def order_tokens(prob: Problem, ids, *, slots=None):
     offsets = torch.empty((*lead, E + 1), dtype=torch.int64, device=at)
     places = torch.empty(shape, dtype=torch.int32, device=at)
     size = lib.routepack_order_workspace(prob.ref, shape[0])
-    work = torch.empty(max(size, 16), dtype=torch.uint8, device=at)
+    work = torch.empty(size, dtype=torch.uint8, device=at).data_ptr() if size > 0 else None
     call.run(lib.routepack_order_tokens, prob.ref, C.byref(x), s, rows.data_ptr(), offsets.data_ptr(),
-             places.data_ptr(), work.data_ptr(), size)
+             places.data_ptr(), work, size)
     return Order(rows, offsets, places)
 
 
@@ -822,13 +837,13 @@ def quantize_mx(x, *, order=None):
         got, p = call.places(order)
         if got[0] != shape[0]:
             raise ValueError(f"{call.fn}: the order has {got[0]} tokens, x {shape[0]} rows")
-        k, lead, p = got[1], (got[0] * got[1],), C.byref(p)
+        k, lead = got[1], (got[0] * got[1],)
         rows = call.dense("order.rows", order.rows, (torch.int32,), lead).data_ptr()
     n = (shape[1] + 127) // 128
     codes = torch.empty((*lead, 64 * n), dtype=torch.uint8, device=call.device)
     scales = torch.empty((*lead, 4 * n), dtype=torch.uint8, device=call.device)
-    q = _MxMatrix(codes.data_ptr(), scales.data_ptr(), shape[0] if order is None else lead[0], shape[1])
-    call.run(lib.routepack_quantize_mx, C.byref(m), rows, p, k, C.byref(q))
+    q = _MX(codes.data_ptr(), scales.data_ptr(), shape[0] if order is None else lead[0], shape[1])
+    call.run(lib.routepack_quantize_mx, m, rows, p, k, q)
     return Mx(codes, scales, shape[1])
 
 
@@ -841,9 +856,10 @@ def dequantize_mx(q: Mx, dtype=None):
     if dtype not in floats:
         raise ValueError(f"{call.fn}: dtype is {dtype}")
     shape, m = call.mx("q", q, 3 if isinstance(q, Mx) and q.codes.dim() == 3 else 2)
-    x = torch.empty(q.shape, dtype=dtype, device=call.device)
-    out = _Matrix(x.data_ptr(), floats[dtype], m.n_rows, q.columns, q.columns)
-    call.run(lib.routepack_dequantize_mx, C.byref(m), C.byref(out))
+    cols = q.columns
+    rows = shape[0] if len(shape) == 2 else shape[0] * shape[1]
+    x = torch.empty((*shape[:-1], cols), dtype=dtype, device=call.device)
+    call.run(lib.routepack_dequantize_mx, m, _MATRIX(x.data_ptr(), floats[dtype], rows, cols, cols))
     return x
 
 
@@ -859,24 +875,22 @@ def expert_product(x, w, order, *, dtype=None):
     expert_product_backward's."""
     lib, torch, floats, _ = _router()
     call = _ExpertCall("routepack_expert_product", torch)
-    tensors = [t for t in (x, w) if isinstance(t, torch.Tensor)]
+    x_is, w_is = isinstance(x, torch.Tensor), isinstance(w, torch.Tensor)
     if dtype is None:
-        dtype = x.dtype if isinstance(x, torch.Tensor) else torch.bfloat16
+        dtype = x.dtype if x_is else torch.bfloat16
     if dtype not in floats:
         raise ValueError(f"{call.fn}: dtype is {dtype}")
-    if any(t.requires_grad for t in tensors) and torch.is_grad_enabled():
-        return _expert_functions()[0].apply(x, w, order, dtype)
-    if isinstance(x, torch.Tensor):
-        x = quantize_mx(x)
-    if isinstance(w, torch.Tensor):
-        w = quantize_mx(w)
+    if x_is or w_is:
+        if (x_is and x.requires_grad or w_is and w.requires_grad) and torch.is_grad_enabled():
+            return _expert_functions()[0].apply(x, w, order, dtype)
+        x, w = quantize_mx(x) if x_is else x, quantize_mx(w) if w_is else w
     got, xm = call.mx("x", x, 2)
     shape, wm = call.mx("w", w, 3)
     if x.columns != w.columns:
         raise ValueError(f"{call.fn}: x has {x.columns} columns, w {w.columns}")
     off = call.offsets(order, shape[0])
     y, ym = call.out(got[0], shape[1], dtype, floats)
-    call.run(lib.routepack_expert_product, C.byref(xm), C.byref(wm), shape[0], off, C.byref(ym))
+    call.run(lib.routepack_expert_product, xm, wm, shape[0], off, ym)
     return y
 
 
@@ -898,7 +912,7 @@ def expert_product_backward(dy, x, w, order, *, need=(True, True)):
         raise TypeError(f"{call.fn}: w must be an Mx, got {type(w).__name__}")
     else:
         E, N, cols = w
-        wm = _MxMatrix(None, None, E * N, cols)
+        wm = _MX(0, 0, E * N, cols)
     if isinstance(x, Mx):
         xs, xm = call.mx("x", x, 2)
         if xs[0] != got[0] or x.columns != cols:
@@ -906,18 +920,17 @@ def expert_product_backward(dy, x, w, order, *, need=(True, True)):
     elif need[1]:
         raise TypeError(f"{call.fn}: x must be an Mx, got {type(x).__name__}")
     else:
-        xm = _MxMatrix(None, None, got[0], cols)
+        xm = _MX(0, 0, got[0], cols)
     if got[1] != N:
         raise ValueError(f"{call.fn}: dy has {got[1]} columns, w {N} rows a slot")
     off = call.offsets(order, E)
     dx = dw = dxm = dwm = None
     if need[0]:
         dx, dxm = call.out(got[0], cols, dy.dtype, floats)
-        dxm = C.byref(dxm)
     if need[1]:
-        dw, dwm = call.out(N, cols, dy.dtype, floats, lead=E)
-        dwm = C.byref(dwm)
-    call.run(lib.routepack_expert_product_backward, C.byref(dm), C.byref(xm), C.byref(wm), E, off, dxm, dwm)
+        dw = torch.empty((E, N, cols), dtype=dy.dtype, device=call.device)
+        dwm = _MATRIX(dw.data_ptr(), floats[dy.dtype], E * N, cols, cols)
+    call.run(lib.routepack_expert_product_backward, dm, xm, wm, E, off, dxm, dwm)
     return dx, dw
 
 
@@ -935,7 +948,7 @@ def combine_tokens(y, order, gates=None):
     if (y.requires_grad or (gates is not None and gates.requires_grad)) and torch.is_grad_enabled():
         return _expert_functions()[1].apply(y, gates, order)
     out, om = call.out(shape[0], got[1], y.dtype, floats)
-    call.run(lib.routepack_combine_tokens, C.byref(ym), C.byref(p), shape[1], g, stride, C.byref(om))
+    call.run(lib.routepack_combine_tokens, ym, p, shape[1], g, stride, om)
     return out
 
 
@@ -956,12 +969,11 @@ def combine_backward(dout, y, order, gates=None, *, need=(True, True)):
     if need[0]:
         rows = call.dense("order.rows", order.rows, (torch.int32,), (got[0],)).data_ptr()
         dy, dym = call.out(got[0], got[1], y.dtype, floats)
-        dym = C.byref(dym)
     if need[1]:
         dgates = torch.empty(tuple(shape), dtype=torch.float32, device=call.device)
         if dy is None and shape[0] == 0:  # (no token: nothing to write, and no address to pass)
             return None, dgates
-    call.run(lib.routepack_combine_backward, C.byref(dm), C.byref(ym), rows, C.byref(p), shape[1], g, stride, dym,
+    call.run(lib.routepack_combine_backward, dm, ym, rows, p, shape[1], g, stride, dym,
              None if dgates is None else dgates.data_ptr())
     return dy, dgates
 

@@ -227,10 +227,9 @@ inline int check_order(const routepack_problem *p, int64_t n_tokens) {
     return ROUTEPACK_OK;
 }
 
-// (of one chunk: none, but a workspace of size 0 would be a special case)
 inline int64_t order_bytes(const routepack_problem *p, int64_t n_tokens) {
     const int64_t n = order_chunks(n_tokens * p->top_k);
-    return n <= 1 ? 16 : (int64_t)p->n_layers * (n + 1) * (p->n_experts + 1) * 4;
+    return n <= 1 ? 0 : (int64_t)p->n_layers * (n + 1) * (p->n_experts + 1) * 4;
 }
 
 }  // namespace rp
@@ -249,7 +248,8 @@ extern "C" int routepack_order_tokens(const routepack_problem *prob, const route
     RP_TRY(check_order(prob, ids->n_tokens));
     RP_TRY(check_ids(prob, ids, ids->n_tokens));
     if (prob->n_layers == 0) return ROUTEPACK_OK;
-    if (!offsets || !workspace || ((uintptr_t)workspace & 15) || workspace_bytes < order_bytes(prob, ids->n_tokens))
+    const int64_t bytes = order_bytes(prob, ids->n_tokens);
+    if (!offsets || workspace_bytes < bytes || (bytes > 0 && (!workspace || ((uintptr_t)workspace & 15))))
         return ROUTEPACK_E_INVALID;
     if (ids->n_tokens > 0 && (!rows || !places)) return ROUTEPACK_E_INVALID;
     OrderArgs a = {};

@@ -124,6 +124,7 @@ __device__ inline uint32_t lds_address(const void *p) {
 // waits by wait_and_meet.
 __device__ inline void load_to_lds(const uint8_t *base, uint32_t offset, uint32_t to) {
     base = reinterpret_cast<const uint8_t *>(uniform64((int64_t)base));
+    to = (uint32_t)__builtin_amdgcn_readfirstlane((int)to);
     uint32_t m0;  // (the compiler's, given back)
     asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
                  : "=&s"(m0) : "s"(to), "v"(offset), "s"(base) : "memory");

@@ -26,16 +26,16 @@ def _rows(type_=5, T=4, data=64, ts=48, ls=16):
 
 def _matrix(rows=4, cols=40, type_=1, stride=None, data=64):
     import paper_2608_12146_amd as rp
-    return rp._Matrix(data, type_, rows, cols, cols if stride is None else stride)
+    return rp._MATRIX(data or 0, type_, rows, cols, cols if stride is None else stride)
 
 
 def _mx(rows=4, cols=40, codes=64, scales=64):
     import paper_2608_12146_amd as rp
-    return rp._MxMatrix(codes, scales, rows, cols)
+    return rp._MX(codes or 0, scales or 0, rows, cols)
 
 
 def _by(x):
-    return None if x is None else C.byref(x)
+    return x if x is None or isinstance(x, bytes) else C.byref(x)
 
 
 def test_every_declared_entry_point_is_exported():
@@ -76,12 +76,14 @@ def test_order_refusals():
     assert call(None, I) == -1 and call(_problem(), None) == -1
     for bad in (_rows(0), _rows(7), _rows(T=-1), _rows(data=None), _rows(ts=-1), _rows(ls=-1)):
         assert call(_problem(), bad) == -1
+    many = _rows(T=1 << 20)
     for more in (dict(rows=None), dict(off=None), dict(places=None), dict(work=None), dict(work=C.c_void_p(72)), dict(size=8)):
-        assert call(_problem(), I, **more) == -1, more
+        assert call(_problem(), many, **more) == -1, more
     assert call(_problem(E=0), I) == -1 and call(_problem(k=0), I) == -1 and call(_problem(L=-1), I) == -1
     assert call(_problem(E=2049), I) == -8 and call(_problem(k=257), I) == -8
     assert call(_problem(), _rows(T=1 << 30)) == -8
     need = lib.routepack_order_workspace(_problem().ref, 1 << 20)
+    assert lib.routepack_order_workspace(_problem().ref, 64) == 0
     assert need > 16 and call(_problem(), _rows(T=1 << 20), size=need - 1) == -1
     assert lib.routepack_order_workspace(None, 4) == -1 and lib.routepack_order_workspace(_problem().ref, -1) == -1
     assert call(_problem(L=0), I, None, None, None, None, 0) == 0
