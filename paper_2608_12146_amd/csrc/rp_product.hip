@@ -12,6 +12,7 @@ struct ProductArgs {
     int64_t R;
     const int64_t *offsets;
     void *y;
+    bool whole;       // y's rows are whole vectors of 16 bytes
     int64_t tiles;    // workgroups of tiles; those behind clear rows
     int64_t clears;
 };
@@ -264,7 +265,7 @@ __global__ void __launch_bounds__(512, 1) k_product_many(ProductArgs a) {
 #pragma unroll
     for (int m = 0; m < kLive; ++m) {
         const int first = (2 * m + wm) * 32;
-        leave_by_lines<T, 2>(lds + wave * 32 * kPitch<T, 2>, sum[m], y + (r0 + first) * a.N, a.N, rows - first, a.N, n0 + wn);
+        leave_by_lines<T, 2>(lds + wave * 32 * kPitch<T, 2>, sum[m], y + (r0 + first) * a.N, a.N, rows - first, a.N, n0 + wn, a.whole);
     }
     };
     if (steps > 0) {
@@ -306,6 +307,7 @@ extern "C" int routepack_expert_product(const routepack_mx *x, const routepack_m
     a.R = x->n_rows;
     a.offsets = offsets;
     a.y = y->data;
+    a.whole = N % (y->type == ROUTEPACK_F32 ? 4 : 8) == 0 && ((uintptr_t)y->data & 15) == 0;
     const int64_t most = a.R < n_slots ? a.R : n_slots;  // slots with rows
     const int64_t pieces = (a.R * N + 65535) / 65536;
     a.clears = pieces < 256 ? pieces : 256;

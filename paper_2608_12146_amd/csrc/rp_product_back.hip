@@ -24,6 +24,7 @@ struct BackProductArgs {
     int64_t R;
     const int64_t *offsets;
     void *out;
+    bool whole;                // out's rows are whole vectors of 16 bytes
     int64_t tiles, clears;
 };
 
@@ -267,7 +268,7 @@ __global__ void __launch_bounds__(128 * WN, WAVES) k_product_back(BackProductArg
 #pragma unroll
         for (int m = 0; m < kLive; ++m) {
             const int first = (2 * m + wm) * 32;
-            leave_by_lines<T, NB>(lds + wave * 32 * kPitch<T, NB>, sum[m], out + first * (int64_t)a.C, a.C, rows - first, a.C, c0 + wc);
+            leave_by_lines<T, NB>(lds + wave * 32 * kPitch<T, NB>, sum[m], out + first * (int64_t)a.C, a.C, rows - first, a.C, c0 + wc, a.whole);
         }
     };
     const int blocks = (rows + 31) / 32, live = c0 + wc < a.C ? (blocks - wm + 1) / 2 : 0;
@@ -353,6 +354,7 @@ extern "C" int routepack_expert_product_backward(const routepack_matrix *dy, con
             b.bc = static_cast<const uint8_t *>(w->codes);
             b.bs = static_cast<const uint8_t *>(w->scales);
             b.out = dx->data;
+            b.whole = C % (16 / sizeof(T)) == 0 && ((uintptr_t)dx->data & 15) == 0;
             RP_TRY((back_of<T, false>(b, stream)));
         }
         if (do_w) {
@@ -360,6 +362,7 @@ extern "C" int routepack_expert_product_backward(const routepack_matrix *dy, con
             b.bc = static_cast<const uint8_t *>(x->codes);
             b.bs = static_cast<const uint8_t *>(x->scales);
             b.out = dw->data;
+            b.whole = C % (16 / sizeof(T)) == 0 && ((uintptr_t)dw->data & 15) == 0;
             RP_TRY((back_of<T, true>(b, stream)));
         }
         return ROUTEPACK_OK;
