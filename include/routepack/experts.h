@@ -45,7 +45,8 @@ typedef struct routepack_matrix {
     int64_t n_rows, n_cols, row_stride;
 } routepack_matrix;
 
-/* A matrix in 4 bits, [n_rows][n_cols], dense, 16-byte aligned. */
+/* A matrix in 4 bits, [n_rows][n_cols], dense; codes 16-byte and scales 4-byte
+ * aligned (as runs of a larger matrix's rows are). */
 typedef struct routepack_mx {
     void *codes;   /* uint8 [n_rows][64 ceil(n_cols / 128)] */
     void *scales;  /* uint8 [n_rows][4 ceil(n_cols / 128)] */

@@ -692,6 +692,8 @@ class Order:
         self.rows, self.offsets, self.places = rows, offsets, places
 
     def layer(self, l):
+        if self.rows.dim() != 2:
+            raise ValueError("this Order is one layer's")
         return Order(self.rows[l], self.offsets[l], self.places[:, l])
 
 
@@ -824,7 +826,7 @@ def quantize_mx(x, *, order=None):
     """x [rows][columns] (or [n][rows][columns], contiguous) fp32, bf16 or fp16,
     any stride over rows, as an Mx.  With `order` the result's rows are the
     order's pairs: row r holds the token of pair rows[r] (zeros behind the
-    last)."""
+    last).  The result carries no gradient; expert_product passes one through."""
     lib, torch, floats, _ = _router()
     call = _ExpertCall("routepack_quantize_mx", torch)
     call.tensor("x", x, floats)

@@ -102,10 +102,10 @@ template <class T, int N>
 __device__ inline void spread_rows(const CombineArgs &a, const int64_t (&r)[N], const bool (&own)[N], const float (&g)[N],
                                    int32_t c, const Vec<T> &d, float *dots) {
     constexpr int W = Vec<T>::W;
-    if (a.dgates) {
+    if (a.dgates && a.order.n_rows > 0) {
         Vec<T> y[N];
 #pragma unroll
-        for (int j = 0; j < N; ++j)
+        for (int j = 0; j < N; ++j)  // (no row: the first one, not counted)
             y[j] = row_vec<T>(static_cast<const T *>(a.y) + (r[j] >= 0 ? r[j] : 0) * a.stride, a.cols, c);
 #pragma unroll
         for (int j = 0; j < N; ++j) {

@@ -37,7 +37,7 @@ inline int check_mx(const routepack_mx *q, bool data) {
     if (q->n_cols > kMaxCols || !sizes_fit(q->n_rows, padded_cols(q->n_cols))) return ROUTEPACK_E_UNSUPPORTED;
     if (data && q->n_rows > 0 && q->n_cols > 0) {
         if (!q->codes || !q->scales) return ROUTEPACK_E_INVALID;
-        if (((uintptr_t)q->codes | (uintptr_t)q->scales) & 15) return ROUTEPACK_E_INVALID;
+        if ((uintptr_t)q->codes & 15 || (uintptr_t)q->scales & 3) return ROUTEPACK_E_INVALID;
     }
     return ROUTEPACK_OK;
 }

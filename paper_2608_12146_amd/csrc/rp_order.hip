@@ -50,18 +50,20 @@ __device__ inline bool order_item(const OrderArgs &a, int32_t &l, int32_t &c) {
 }
 
 // The slots of pairs p, p + step, .. (E for none and from `end` on): 8 loads at a
-// time, without branches that would part them.
-template <class I>
+// time, without branches that would part them.  NEAR: a layer's ids and places lie
+// within 2^31 elements of their first.
+template <class I, bool NEAR>
 __device__ inline void slots_of_pairs(const OrderArgs &a, int32_t l, int32_t p, int32_t step, int32_t end,
                                       int32_t (&slot)[kEach]) {
     I id[kEach];
+    const I *ids = static_cast<const I *>(a.ids) + l * a.ls;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) slot[i] = a.E;
     if (end == 0) return;  // (no pair at all)
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
         const int32_t x = p + i * step < end ? p + i * step : end - 1, t = token_of(a, x), j = x - t * a.k;
-        id[i] = static_cast<const I *>(a.ids)[t * a.ts + l * a.ls + j];
+        id[i] = NEAR ? ids[(uint32_t)(t * (int32_t)a.ts + j)] : ids[t * a.ts + j];
     }
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
@@ -70,20 +72,21 @@ __device__ inline void slots_of_pairs(const OrderArgs &a, int32_t l, int32_t p, 
     }
     if (!a.slots) return;
     int32_t s[kEach];
+    const int32_t *slots = a.slots + (int64_t)l * a.E;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) s[i] = a.slots[(int64_t)l * a.E + (slot[i] < a.E ? slot[i] : 0)];
+    for (int i = 0; i < kEach; ++i) s[i] = slots[(uint32_t)(slot[i] < a.E ? slot[i] : 0)];
 #pragma unroll
     for (int i = 0; i < kEach; ++i) slot[i] = slot[i] < a.E && s[i] >= 0 && s[i] < a.E ? s[i] : a.E;
 }
 
-template <class I>
+template <class I, bool NEAR>
 __global__ void __launch_bounds__(kOrderThreads) k_order_count(OrderArgs a) {
     extern __shared__ int32_t n[];
     int32_t l, c;
     if (!order_item(a, l, c)) return;
     const int32_t b = c * kChunk, e = a.P - b < kChunk ? a.P : b + kChunk;
     int32_t slot[kEach];
-    slots_of_pairs<I>(a, l, b + (int32_t)threadIdx.x, kOrderThreads, e, slot);
+    slots_of_pairs<I, NEAR>(a, l, b + (int32_t)threadIdx.x, kOrderThreads, e, slot);
     for (int32_t s = threadIdx.x; s <= a.E; s += kOrderThreads) n[s] = 0;
     __syncthreads();
 #pragma unroll
@@ -96,7 +99,7 @@ __global__ void __launch_bounds__(kOrderThreads) k_order_count(OrderArgs a) {
 
 // A wave a slot: its counts become sums over the chunks before.
 __global__ void __launch_bounds__(256) k_order_scan(OrderArgs a) {
-    const int64_t s = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t s = group_index() * 4 + (threadIdx.x >> 6);
     if (s >= (int64_t)a.L * (a.E + 1)) return;
     const int lane = threadIdx.x & 63;
     int32_t *row = a.counts + s * a.n_chunks;
@@ -126,7 +129,7 @@ __global__ void __launch_bounds__(256) k_order_scan(OrderArgs a) {
     if (lane == 0) a.totals[s] = before;
 }
 
-template <class I>
+template <class I, bool NEAR>
 __global__ void __launch_bounds__(kOrderThreads) k_order_place(OrderArgs a) {
     extern __shared__ int32_t lds[];
     const int32_t S = a.E + 1;
@@ -147,7 +150,7 @@ __global__ void __launch_bounds__(kOrderThreads) k_order_place(OrderArgs a) {
     auto before_of = [&](int32_t s) { return a.counts[((int64_t)l * S + s) * a.n_chunks + c]; };
     const bool early = !one && s0 < S;
     const int32_t total0 = early ? total_of(s0) : 0, before0 = early ? before_of(s0) : 0;
-    slots_of_pairs<I>(a, l, first, kWave, e, slot);
+    slots_of_pairs<I, NEAR>(a, l, first, kWave, e, slot);
     for (int32_t s = threadIdx.x; s < kOrderWaves * S; s += kOrderThreads) from[S + s] = 0;
     __syncthreads();
 #pragma unroll
@@ -205,8 +208,11 @@ __global__ void __launch_bounds__(kOrderThreads) k_order_place(OrderArgs a) {
         __builtin_amdgcn_wave_barrier();
         if (live) {
             sorted[base + rank] = slot[i] << 12 | (p - b);
+            const int32_t place = slot[i] < a.E ? from[slot[i]] + base + rank : -1;
             const int32_t t = token_of(a, p), j = p - t * a.k;
-            a.places[((int64_t)t * a.L + l) * a.k + j] = slot[i] < a.E ? from[slot[i]] + base + rank : -1;
+            int32_t *places = a.places + (int64_t)l * a.k;
+            if (NEAR) places[(uint32_t)(t * (a.L * a.k) + j)] = place;
+            else places[(int64_t)t * a.L * a.k + j] = place;
         }
     }
     __syncthreads();
@@ -274,19 +280,23 @@ extern "C" int routepack_order_tokens(const routepack_problem *prob, const route
     if ((int64_t)a.L * (a.n_chunks + 7) > INT32_MAX / kOrderThreads) return ROUTEPACK_E_UNSUPPORTED;
     const unsigned n = (unsigned)((a.n_chunks + 7) / 8 * 8 * (int64_t)a.L);
     const size_t one = 4 * (size_t)(a.E + 1), all = 4 * kChunk + one * (1 + kOrderWaves);
-    auto go = [&](auto tag) -> int {
+    const int64_t last = ids->n_tokens > 0 ? ids->n_tokens - 1 : 0;
+    const bool near = a.ts <= INT32_MAX && last * a.ts + a.k <= INT32_MAX && (last + 1) * a.L * a.k <= INT32_MAX;
+    auto launch = [&](auto tag, auto near_) -> int {
         using I = decltype(tag);
+        constexpr bool NEAR = decltype(near_)::value != 0;
         if (a.n_chunks > 1) {
-            hipLaunchKernelGGL(k_order_count<I>, dim3(n), dim3(kOrderThreads), one, stream, a);
-            hipLaunchKernelGGL(k_order_scan, dim3((unsigned)(((int64_t)a.L * (a.E + 1) + 3) / 4)), dim3(256), 0, stream, a);
+            hipLaunchKernelGGL((k_order_count<I, NEAR>), dim3(n), dim3(kOrderThreads), one, stream, a);
+            hipLaunchKernelGGL(k_order_scan, grid_of(((int64_t)a.L * (a.E + 1) + 3) / 4), dim3(256), 0, stream, a);
         }
-        if (all > 64 * 1024 - 256 &&
-            hipFuncSetAttribute(reinterpret_cast<const void *>(k_order_place<I>),
-                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)all) != hipSuccess)
+        const auto place = k_order_place<I, NEAR>;
+        if (all > 64 * 1024 - 256 && hipFuncSetAttribute(reinterpret_cast<const void *>(place),
+                                                         hipFuncAttributeMaxDynamicSharedMemorySize, (int)all) != hipSuccess)
             return ROUTEPACK_E_DEVICE;
-        hipLaunchKernelGGL(k_order_place<I>, dim3(n), dim3(kOrderThreads), all, stream, a);
+        hipLaunchKernelGGL(place, dim3(n), dim3(kOrderThreads), all, stream, a);
         return launched();
     };
+    auto go = [&](auto tag) { return near ? launch(tag, Int<1>()) : launch(tag, Int<0>()); };
     switch (ids->type) {
         case ROUTEPACK_U8: return go(uint8_t());
         case ROUTEPACK_I16: return go(int16_t());

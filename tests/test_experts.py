@@ -101,7 +101,7 @@ def test_mx_refusals():
     for x in (None, _matrix(type_=3), _matrix(rows=-1), _matrix(cols=-1), _matrix(stride=-1), _matrix(data=None),
               _matrix(rows=5), _matrix(cols=41)):
         assert quant(x, _mx()) == -1 and back(_mx(), x) == -1
-    for q in (None, _mx(rows=-1), _mx(cols=-1), _mx(codes=None), _mx(scales=None), _mx(codes=72), _mx(scales=68)):
+    for q in (None, _mx(rows=-1), _mx(cols=-1), _mx(codes=None), _mx(scales=None), _mx(codes=72), _mx(scales=66)):
         assert quant(_matrix(), q) == -1 and back(q, _matrix()) == -1
     assert quant(_matrix(), _mx(8), SOME, None) == -1 and quant(_matrix(), _mx(8), None, _rows()) == -1
     for bad in (_rows(6), _rows(T=5), _rows(ts=-1), _rows(data=None)):
@@ -124,7 +124,7 @@ def test_product_refusals():
     def call(x, w, n=3, off=SOME, y=None):
         return lib.routepack_expert_product(_by(x), _by(w), n, off, _by(y), None)
     x, w, y = _mx(), _mx(rows=15), _matrix(cols=5)
-    for bad in (None, _mx(rows=-1), _mx(cols=41), _mx(codes=None), _mx(scales=8), _mx(rows=5)):
+    for bad in (None, _mx(rows=-1), _mx(cols=41), _mx(codes=None), _mx(scales=9), _mx(rows=5)):
         assert call(bad, w, y=y) == -1
     for bad in (None, _mx(rows=16), _mx(rows=15, cols=39), _mx(rows=15, codes=65)):
         assert call(x, bad, y=y) == -1

@@ -491,6 +491,40 @@ def test_sum_and_gradients(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("C", [0, 3, 40, 700, 5000])
+def test_sums_of_no_rows(C):
+    """Tokens whose choices were all not made, over a matrix without rows."""
+    import torch
+    import paper_2608_12146_amd as rp
+    T, k = 5, 3
+    order = rp.Order(torch.empty(0, dtype=torch.int32, device="cuda"), None,
+                     torch.tensor([[-1, 0, 7]] * T, dtype=torch.int32, device="cuda"))
+    y, dout = torch.empty((0, C), device="cuda"), _floats(1, (T, C), "fp32")
+    assert not rp.combine_tokens(y, order).any()
+    dy, dgates = rp.combine_backward(dout, y, order)
+    assert dy.shape == (0, C) and dgates.shape == (T, k) and not dgates.any()
+
+
+@gpu
+def test_runs_of_rows_of_a_matrix_in_4_bits():
+    """A part of the rows of a packed matrix is one (its scales stand on 4 bytes)."""
+    import torch
+    import paper_2608_12146_amd as rp
+    x, w = _random_mx(1, (41,), 100), _random_mx(2, (3, 30), 100)
+    part, some = rp.Mx(x.codes[5:38], x.scales[5:38], 100), rp.Mx(w.codes[1:], w.scales[1:], 100)
+    off = _offsets([20, 13])
+    y = rp.expert_product(part, some, off, dtype=torch.float32)
+    want, mag = X.product(_values(x)[5:38], _values(w)[1:], _host(off))
+    _near(y, want, 2 * (100 + 136) * U * mag, "y")
+    dy = _floats(3, (33, 30), "bf16")
+    dx, dw = rp.expert_product_backward(dy, part, some, off)
+    (wx, mx), (ww, mw) = X.product_backward(_host(dy), _values(x)[5:38], _values(w)[1:], _host(off))
+    _near(dx, wx, 2 * (30 + 136) * U * mx, "dx")
+    _near(dw, ww, 2 * (33 + 136) * U * mw, "dw")
+    assert np.array_equal(_host(rp.dequantize_mx(part, torch.float32)), _values(x)[5:38])
+
+
+@gpu
 def test_orders_that_are_wrong_stay_within_the_arrays():
     """Places and rows outside their range are no rows and no pairs; a row that
     two pairs name belongs to the one that it names."""
@@ -740,6 +774,13 @@ def test_past_two_to_the_32_bytes():
     """Elements and bytes that 32 bits do not count."""
     import torch
     import paper_2608_12146_amd as rp
+    _log("ids 2^31 elements apart")
+    wide = torch.zeros((2 << 31) + 8, dtype=torch.uint8, device="cuda")
+    far = wide.as_strided((3, 1, 4), (1 << 31, 4, 1))
+    far.copy_(torch.tensor([[[3, 0, 255, 1]], [[1, 1, 0, 2]], [[0, 255, 3, 3]]], dtype=torch.uint8))
+    got, want = rp.order_tokens(_problem(1, 4, 4), far), X.order(far.cpu().numpy().astype(np.int64), 4)
+    assert all(np.array_equal(_host(a), b) for a, b in zip((got.rows, got.offsets, got.places), want))
+    del wide, far
     # a broadcast row quantized 2^20 times: 2^33 elements, 2^32 bytes of codes
     row = _floats(1, (1, 8192), "bf16")
     R = (1 << 20) + 3
