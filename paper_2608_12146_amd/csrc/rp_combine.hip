@@ -24,14 +24,14 @@ struct CombineArgs {
     int64_t token_groups;      // workgroups of tokens; those behind look for rows of no pair
 };
 
-// One vector of a row, zeros past its end.  Nothing reads it again: with that hint
-// the gradients of 8192 tokens x 8 of 2048 bf16 take 90 us, 115 without.
-template <class T>
+// One vector of a row, zeros past its end.  WHOLE: there is no such vector, and all
+// stand on 16 bytes.  ONCE: nothing reads it again.
+template <class T, bool WHOLE, bool ONCE>
 __device__ inline Vec<T> row_vec(const T *row, int32_t cols, int32_t c) {
     constexpr int W = Vec<T>::W;
     Vec<T> x;
-    if (c + W <= cols) {
-        load16<true>(row + c, x.w);
+    if (WHOLE || c + W <= cols) {
+        load16<ONCE>(row + c, x.w);
     } else {
         float v[W];
 #pragma unroll
@@ -41,7 +41,7 @@ __device__ inline Vec<T> row_vec(const T *row, int32_t cols, int32_t c) {
     return x;
 }
 
-template <class T, int N>
+template <class T, bool WHOLE, int N>
 __device__ inline void add_rows(const CombineArgs &a, const int32_t *places, const float *gates, int32_t c,
                                 float (&sum)[Vec<T>::W]) {
     constexpr int W = Vec<T>::W;
@@ -53,7 +53,7 @@ __device__ inline void add_rows(const CombineArgs &a, const int32_t *places, con
         const int64_t r = places[j];
         on[j] = r >= 0 && r < a.order.n_rows;
         g[j] = gates ? gates[j] : 1.0f;
-        x[j] = row_vec<T>(static_cast<const T *>(a.y) + (on[j] ? r : 0) * a.stride, a.cols, c);
+        x[j] = row_vec<T, WHOLE, true>(static_cast<const T *>(a.y) + (on[j] ? r : 0) * a.stride, a.cols, c);
     }
 #pragma unroll
     for (int j = 0; j < N; ++j)
@@ -62,7 +62,7 @@ __device__ inline void add_rows(const CombineArgs &a, const int32_t *places, con
 }
 
 // ONE: a wave has one token, whose places and gates are read by scalar loads.
-template <class T, bool ONE>
+template <class T, bool ONE, bool WHOLE>
 __global__ void __launch_bounds__(256) k_combine(CombineArgs a) {
     constexpr int W = Vec<T>::W;
     const int lt = ONE ? kWave : a.lt, lane = threadIdx.x & (lt - 1);
@@ -80,14 +80,14 @@ __global__ void __launch_bounds__(256) k_combine(CombineArgs a) {
     float sum[W] = {};
     int j = 0;
     if (a.order.n_rows > 0) {
-        for (; j + 4 <= a.order.k; j += 4) add_rows<T, 4>(a, places + j, gates ? gates + j : nullptr, v * W, sum);
+        for (; j + 4 <= a.order.k; j += 4) add_rows<T, WHOLE, 4>(a, places + j, gates ? gates + j : nullptr, v * W, sum);
         if (j + 2 <= a.order.k) {
-            add_rows<T, 2>(a, places + j, gates ? gates + j : nullptr, v * W, sum);
+            add_rows<T, WHOLE, 2>(a, places + j, gates ? gates + j : nullptr, v * W, sum);
             j += 2;
         }
-        if (j < a.order.k) add_rows<T, 1>(a, places + j, gates ? gates + j : nullptr, v * W, sum);
+        if (j < a.order.k) add_rows<T, WHOLE, 1>(a, places + j, gates ? gates + j : nullptr, v * W, sum);
     }
-    store_vec<T, false>(static_cast<T *>(a.out) + t * a.cols, a.cols, v * W, sum);
+    store_vec<T, WHOLE>(static_cast<T *>(a.out) + t * a.cols, a.cols, v * W, sum);
 }
 
 // The sum over aligned groups of lt lanes.
@@ -97,8 +97,11 @@ __device__ inline float lanes_sum(float v, int lt) {
 }
 
 // Rows r[0], .. of N choices j, ..: their products with d are added to dots, and
-// gate times d is written where the row is the pair's.
-template <class T, int N>
+// gate times d is written where the row is the pair's.  The hint that y is read
+// and dy written once pays where vectors do not cross lines (8192 tokens x 6 of 1448
+// fp32: 150 -> 133 us), and for loads of 16-bit values (1447: 95 -> 80); else it
+// costs (1447 fp32: 150 -> 162).
+template <class T, bool WHOLE, int N>
 __device__ inline void spread_rows(const CombineArgs &a, const int64_t (&r)[N], const bool (&own)[N], const float (&g)[N],
                                    int32_t c, const Vec<T> &d, float *dots) {
     constexpr int W = Vec<T>::W;
@@ -106,7 +109,7 @@ __device__ inline void spread_rows(const CombineArgs &a, const int64_t (&r)[N], 
         Vec<T> y[N];
 #pragma unroll
         for (int j = 0; j < N; ++j)  // (no row: the first one, not counted)
-            y[j] = row_vec<T>(static_cast<const T *>(a.y) + (r[j] >= 0 ? r[j] : 0) * a.stride, a.cols, c);
+            y[j] = row_vec<T, WHOLE, WHOLE || sizeof(T) == 2>(static_cast<const T *>(a.y) + (r[j] >= 0 ? r[j] : 0) * a.stride, a.cols, c);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             float sum = dots[j];
@@ -122,7 +125,15 @@ __device__ inline void spread_rows(const CombineArgs &a, const int64_t (&r)[N], 
             float x[W];
 #pragma unroll
             for (int w = 0; w < W; ++w) x[w] = g[j] * d.at(w);
-            store_vec<T, false>(static_cast<T *>(a.dy) + r[j] * a.cols, a.cols, c, x);
+            T *const to = static_cast<T *>(a.dy) + r[j] * a.cols;
+            if constexpr (WHOLE) {
+                Vec<T> v;
+                v.set(x);
+                typedef uint32_t four __attribute__((ext_vector_type(4)));
+                __builtin_nontemporal_store(four{v.w[0], v.w[1], v.w[2], v.w[3]}, reinterpret_cast<four *>(to + c));
+            } else {
+                store_vec<T, false>(to, a.cols, c, x);
+            }
         }
     }
 }
@@ -131,7 +142,7 @@ __device__ inline void spread_rows(const CombineArgs &a, const int64_t (&r)[N], 
 // is read (for the gates) and written.  NW > 0: a token has NW waves, which look
 // its rows up once, a lane a choice, and hold them in scalars; NW = 0: a wave has
 // several tokens, of lt lanes.
-template <class T, int K, int NW>
+template <class T, int K, int NW, bool WHOLE>
 __global__ void __launch_bounds__(256) k_spread(CombineArgs a) {
     constexpr int W = Vec<T>::W;
     __shared__ float part[4][K];
@@ -167,7 +178,7 @@ __global__ void __launch_bounds__(256) k_spread(CombineArgs a) {
         float mine_gate = 0.0f;
         if (NW && lane < k) mine = look_up(lane, mine_own, mine_gate);
         for (int32_t v = lane + (NW ? wave % (NW ? NW : 1) * kWave : 0); v < a.vecs; v += lt * (NW ? NW : 1)) {
-            const Vec<T> d = row_vec<T>(dout, a.cols, v * W);
+            const Vec<T> d = row_vec<T, WHOLE, WHOLE || sizeof(T) == 2>(dout, a.cols, v * W);
             auto batch = [&](auto n_, int j0, float *sums) {
                 constexpr int N = decltype(n_)::value;
                 int64_t r[N];
@@ -183,7 +194,7 @@ __global__ void __launch_bounds__(256) k_spread(CombineArgs a) {
                         r[j] = look_up(j0 + j, own[j], g[j]);
                     }
                 }
-                spread_rows<T, N>(a, r, own, g, v * W, d, sums);
+                spread_rows<T, WHOLE, N>(a, r, own, g, v * W, d, sums);
             };
 #pragma unroll
             for (int j0 = 0; j0 < K; j0 += 4) {
@@ -214,6 +225,13 @@ __global__ void __launch_bounds__(256) k_spread(CombineArgs a) {
         for (int j = 0; j < K; ++j)
             if (j < k) a.dgates[t * k + j] = dots[j];
     }
+}
+
+// Rows of whole vectors of 16 bytes, on their boundaries (or none).
+template <class T>
+bool whole_rows(const void *data, int64_t stride, int64_t cols) {
+    constexpr int W = Vec<T>::W;
+    return !data || (((uintptr_t)data & 15) == 0 && stride % W == 0 && cols % W == 0);
 }
 
 inline void geometry(CombineArgs &a, int W) {
@@ -250,7 +268,9 @@ extern "C" int routepack_combine_tokens(const routepack_matrix *y, const routepa
         using T = decltype(tag);
         geometry(a, Vec<T>::W);
         const int64_t items = a.order.T * a.chunks, per = 256 / a.lt;
-        auto kern = a.lt == kWave ? k_combine<T, true> : k_combine<T, false>;
+        const bool whole = whole_rows<T>(y->data, a.stride, a.cols) && whole_rows<T>(a.out, a.cols, a.cols);
+        auto kern = whole ? (a.lt == kWave ? k_combine<T, true, true> : k_combine<T, false, true>)
+                          : (a.lt == kWave ? k_combine<T, true, false> : k_combine<T, false, false>);
         hipLaunchKernelGGL(kern, grid_of((items + per - 1) / per), dim3(256), 0, stream, a);
         return launched();
     });
@@ -298,11 +318,16 @@ extern "C" int routepack_combine_backward(const routepack_matrix *dout, const ro
         a.token_groups = (a.order.T + per - 1) / per;
         const int64_t n = a.token_groups + (a.dy ? (a.order.n_rows + 255) / 256 : 0);
         if (n == 0) return ROUTEPACK_OK;
-        auto pick = [&](auto k_) {
+        const bool whole = whole_rows<T>(a.dgates ? a.y : nullptr, a.stride, a.cols) &&
+                           whole_rows<T>(a.dout, a.dout_stride, a.cols) && whole_rows<T>(a.dy, a.cols, a.cols);
+        auto pick = [&](auto k_, auto whole_) {
             constexpr int K = decltype(k_)::value;
-            return nw == 4 ? k_spread<T, K, 4> : nw == 2 ? k_spread<T, K, 2> : nw == 1 ? k_spread<T, K, 1> : k_spread<T, K, 0>;
+            constexpr bool W = decltype(whole_)::value != 0;
+            return nw == 4 ? k_spread<T, K, 4, W> : nw == 2 ? k_spread<T, K, 2, W> : nw == 1 ? k_spread<T, K, 1, W> : k_spread<T, K, 0, W>;
         };
-        hipLaunchKernelGGL((top_k <= 8 ? pick(Int<8>()) : pick(Int<32>())), grid_of(n), dim3(256), 0, stream, a);
+        // (more than 8 choices: the checks cost little beside them)
+        const auto kern = top_k > 8 ? pick(Int<32>(), Int<0>()) : whole ? pick(Int<8>(), Int<1>()) : pick(Int<8>(), Int<0>());
+        hipLaunchKernelGGL(kern, grid_of(n), dim3(256), 0, stream, a);
         return launched();
     });
 }
