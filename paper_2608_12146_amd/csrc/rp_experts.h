@@ -1,5 +1,5 @@
-// What the experts' operators share: their limits and the checks of their
-// arguments, and the tiles of rows that the slots' segments are cut into.
+// What the experts' operators share: their limits, the checks of their arguments,
+// and the order's view of pairs and rows.
 #pragma once
 
 #include "rp_internal.h"

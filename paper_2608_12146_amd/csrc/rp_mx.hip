@@ -8,7 +8,7 @@
 // to the nearest code, ties to even, ending at 6.
 // Bound by bytes: what is read, and 17/32 of a byte written a value.  Gathered
 // into an order, a token is read and converted once, and written to its k rows
-// (8192 x 2048 bf16, 8 rows each: @QUANT@ us, 70 with a row's conversion each).
+// (8192 x 2048 bf16, 8 rows each: 21 us, 70 with a row's conversion each).
 #include "rp_experts.h"
 
 namespace rp {

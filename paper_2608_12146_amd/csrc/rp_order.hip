@@ -9,10 +9,11 @@
 // at a time find their rank among those of the same slot by ballots over the
 // slot's bits, so rows do not depend on the order of atomics.  The chunk is put
 // in order in LDS first: a slot's rows then leave as a run (written from where
-// they are found they were 4 bytes each, and 46 us where now @PLACE@).  One chunk
+// they are found they were 4 bytes each, and 46 us where now 23).  One chunk
 // needs the last kernel alone.
 //
-// 131072 x 4 x 8 byte ids, 256 slots, placed: @ALL@ us.
+// 131072 x 4 x 8 byte ids, 256 slots, placed: 34 us (9 to count, 5 to scan,
+// 23 to place, each by itself).
 #include "rp_experts.h"
 
 namespace rp {

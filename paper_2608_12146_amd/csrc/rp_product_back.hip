@@ -129,7 +129,8 @@ __device__ inline bf16x8 term_fragment(const char *tile, int k0, int c0) {
 // A wave's blocks of 32 rows alternate with the other row of waves', and the
 // upper half of them is left out where it is empty.  One stage of LDS, filled
 // between two barriers: two or three workgroups a CU (WAVES a SIMD) cover each
-// other's phases (two stages with one barrier, one workgroup a CU: @TWICE@).
+// other's phases (24558 rows, 60 x 1408 x 1984, both gradients: 465 us when this
+// was chosen, 517 with two stages, one barrier and one workgroup a CU).
 template <class T, int WN, int MB, int NB>
 struct BackShape {
     static constexpr int P = kParts<T>, kThreads = 128 * WN, kRows = 64 * MB, kCols = 32 * NB * WN;
@@ -140,12 +141,10 @@ struct BackShape {
     static constexpr int kPieces = kRows * kTerms / 8 / kThreads, kBlocks = kTerms * kCols / 32 / kThreads;
 };
 
-template <class T, bool DW, int WN, int MB, int NB, int WAVES>
-__global__ void __launch_bounds__(128 * WN, WAVES) k_product_back(BackProductArgs a) {
+template <class T, bool DW, int WN, int MB, int NB>
+__device__ __forceinline__ void back_tile(const BackProductArgs &a, int64_t id, char *lds) {
     using G = BackShape<T, WN, MB, NB>;
     constexpr int P = G::P, kRows = G::kRows, kCols = G::kCols;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int64_t id = group_index();
     int32_t s, ct;
     int64_t m0;       // first output row: of R (dx), of the slot's N (dw)
     Segment seg;
@@ -278,8 +277,24 @@ __global__ void __launch_bounds__(128 * WN, WAVES) k_product_back(BackProductArg
 }
 
 template <class T, bool DW, int WN, int MB, int NB, int WAVES>
-int back_by(BackProductArgs a, hipStream_t stream) {
-    using G = BackShape<T, WN, MB, NB>;
+__global__ void __launch_bounds__(128 * WN, WAVES) k_product_back(BackProductArgs a) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    back_tile<T, DW, WN, MB, NB>(a, group_index(), lds);
+}
+
+// Both gradients of a small problem in one launch (100 tokens x 8, 64 x 512 x 512:
+// 29 us for both; 31 and 13 in launches of their own).
+template <class T, int WN, int MB, int NB, int WAVES>
+__global__ void __launch_bounds__(128 * WN, WAVES) k_product_back_both(BackProductArgs x, BackProductArgs w) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int64_t id = group_index(), n = x.tiles + x.clears;
+    if (id < n) back_tile<T, false, WN, MB, NB>(x, id, lds);
+    else back_tile<T, true, WN, MB, NB>(w, id - n, lds);
+}
+
+// The tiles of a gradient.
+template <class G, bool DW>
+void cut(BackProductArgs &a) {
     a.c_tiles = (a.C + G::kCols - 1) / G::kCols;
     if (DW) {
         a.m_tiles = (a.N + G::kRows - 1) / G::kRows;
@@ -291,23 +306,39 @@ int back_by(BackProductArgs a, hipStream_t stream) {
         a.tiles = (a.R / G::kRows + slots) * a.c_tiles;
         a.clears = pieces < 256 ? pieces : 256;
     }
-    const auto kern = k_product_back<T, DW, WN, MB, NB, WAVES>;
+}
+
+template <class G, class Kernel, class... Args>
+int launch_back(Kernel kern, int64_t groups, hipStream_t stream, const Args &...args) {
     if (G::kLds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(kern),
                                                    hipFuncAttributeMaxDynamicSharedMemorySize, G::kLds) != hipSuccess)
         return ROUTEPACK_E_DEVICE;
-    hipLaunchKernelGGL(kern, grid_of(a.tiles + a.clears), dim3(G::kThreads), G::kLds, stream, a);
+    hipLaunchKernelGGL(kern, grid_of(groups), dim3(G::kThreads), G::kLds, stream, args...);
     return launched();
 }
 
-template <class T, bool DW>
-int back_of(const BackProductArgs &a, hipStream_t stream) {
-    // dx: tiles of 128 x 256 where they are enough for the chip.  dw, whose sums are
-    // short, and small problems: of 128 x 128, more of them at a time.
-    const int64_t tiles = (a.R / 128 + (a.R < a.n_slots ? a.R : a.n_slots) / 2) * ((a.C + 255) / 256);
-    constexpr int P = kParts<T>;
-    if constexpr (!DW)
-        if (tiles >= 256) return back_by<T, DW, 4, 2, 2, P == 1 ? 4 : 2>(a, stream);
-    return back_by<T, DW, 2, 2, 2, P == 1 ? 3 : 2>(a, stream);
+// dx: tiles of 128 x 256 where they are enough for the chip.  dw, whose sums are
+// short, and small problems: of 128 x 128, more of them at a time.
+template <class T>
+int back_of(BackProductArgs *x, BackProductArgs *w, hipStream_t stream) {
+    using Large = BackShape<T, 4, 2, 2>;
+    using Small = BackShape<T, 2, 2, 2>;
+    constexpr int kWaves = kParts<T> == 1 ? 3 : 2;
+    if (w) cut<Small, true>(*w);
+    if (x) {
+        const int64_t tiles = (x->R / 128 + (x->R < x->n_slots ? x->R : x->n_slots) / 2) * ((x->C + 255) / 256);
+        if (tiles >= 256) {
+            cut<Large, false>(*x);
+            RP_TRY(launch_back<Large>(k_product_back<T, false, 4, 2, 2, kParts<T> == 1 ? 4 : 2>, x->tiles + x->clears, stream, *x));
+        } else {
+            cut<Small, false>(*x);
+            const int64_t n = x->tiles + x->clears;
+            if (w) return launch_back<Small>(k_product_back_both<T, 2, 2, 2, kWaves>, n + w->tiles, stream, *x, *w);
+            return launch_back<Small>(k_product_back<T, false, 2, 2, 2, kWaves>, n, stream, *x);
+        }
+    }
+    if (w) RP_TRY(launch_back<Small>(k_product_back<T, true, 2, 2, 2, kWaves>, w->tiles, stream, *w));
+    return ROUTEPACK_OK;
 }
 
 }  // namespace rp
@@ -349,22 +380,19 @@ extern "C" int routepack_expert_product_backward(const routepack_matrix *dy, con
     a.offsets = offsets;
     return by_type(dy->type, [&](auto tag) -> int {
         using T = decltype(tag);
+        BackProductArgs bx = a, bw = a;
         if (do_x) {
-            BackProductArgs b = a;
-            b.bc = static_cast<const uint8_t *>(w->codes);
-            b.bs = static_cast<const uint8_t *>(w->scales);
-            b.out = dx->data;
-            b.whole = C % (16 / sizeof(T)) == 0 && ((uintptr_t)dx->data & 15) == 0;
-            RP_TRY((back_of<T, false>(b, stream)));
+            bx.bc = static_cast<const uint8_t *>(w->codes);
+            bx.bs = static_cast<const uint8_t *>(w->scales);
+            bx.out = dx->data;
+            bx.whole = C % (16 / sizeof(T)) == 0 && ((uintptr_t)dx->data & 15) == 0;
         }
         if (do_w) {
-            BackProductArgs b = a;
-            b.bc = static_cast<const uint8_t *>(x->codes);
-            b.bs = static_cast<const uint8_t *>(x->scales);
-            b.out = dw->data;
-            b.whole = C % (16 / sizeof(T)) == 0 && ((uintptr_t)dw->data & 15) == 0;
-            RP_TRY((back_of<T, true>(b, stream)));
+            bw.bc = static_cast<const uint8_t *>(x->codes);
+            bw.bs = static_cast<const uint8_t *>(x->scales);
+            bw.out = dw->data;
+            bw.whole = C % (16 / sizeof(T)) == 0 && ((uintptr_t)dw->data & 15) == 0;
         }
-        return ROUTEPACK_OK;
+        return back_of<T>(do_x ? &bx : nullptr, do_w ? &bw : nullptr, stream);
     });
 }

@@ -18,8 +18,9 @@
 // order open (about one token in 500, and ties), the wave forms them in 64.
 //
 // Bound by HBM and vector instructions: 131072 x 512 bf16, 8 groups: 40 us
-// (a copy of the logits takes 26); 65536 x 256 fp32, logistic, two keys a group and a bias: 44 us (78 with all
-// keys in 64 bits; 35 without the tokens in doubt, whose waves end last).
+// (a copy of the logits takes 26); 65536 x 256 fp32, logistic, two keys a group
+// and a bias: 44 us (78 with all keys in 64 bits; 35 without the tokens in doubt,
+// whose waves end last).
 #pragma once
 
 #include "rp_route.h"
