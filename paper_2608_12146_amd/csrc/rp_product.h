@@ -43,7 +43,7 @@ struct TileMap {
         const int64_t n = g.end - g.begin;
         return tile ? (n + tile - 1) / tile : n > 0;
     }
-    __device__ TileMap(const int64_t *offsets, int32_t n_slots, int64_t R, int32_t tile) {
+    __device__ __forceinline__ TileMap(const int64_t *offsets, int32_t n_slots, int64_t R, int32_t tile) {
         const int lane = threadIdx.x & (kWave - 1);
         per = (n_slots + kWave - 1) / kWave;
         mine = 0;
@@ -66,7 +66,7 @@ struct TileMap {
     }
     // The slot of tile `index` < total, its segment, and the number of its tiles
     // before.  All results are uniform.
-    __device__ int32_t find(int64_t index, const int64_t *offsets, int32_t n_slots, int64_t R, int32_t tile, Segment &g,
+    __device__ __forceinline__ int32_t find(int64_t index, const int64_t *offsets, int32_t n_slots, int64_t R, int32_t tile, Segment &g,
                             int64_t &before) const {
         const int owner = __builtin_amdgcn_readfirstlane(__builtin_ctzll(__ballot(upto > index)));
         int64_t at = uniform64(__shfl((long long)(upto - mine), owner, kWave));

@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(512, 1) k_product_many(ProductArgs a) {
     }
     const uint32_t lds0 = lds_address(lds);
     const int32_t steps = (a.groups + 1) / 2;
-    auto issue = [&](int32_t step) {
+    auto issue = [&](int32_t step) __attribute__((always_inline)) {
         const uint32_t to = lds0 + (step & 1) * kStage + wave * 1024;
         const uint8_t *x = xbase + (int64_t)step * 128, *w = wbase + (int64_t)step * 128;
         const bool last = step + 1 == steps;
@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(512, 1) k_product_many(ProductArgs a) {
     const int srow = t < kTileRows ? (t < rows ? t : rows - 1) : (t - kTileRows < cols ? t - kTileRows : cols - 1);
     const uint32_t *scales = reinterpret_cast<const uint32_t *>(
         t < kTileRows ? a.xs + (r0 + srow) * scale_row : a.ws + ((int64_t)s * a.N + n0 + srow) * scale_row);
-    auto fetch_scales = [&](int32_t unit) {
+    auto fetch_scales = [&](int32_t unit) __attribute__((always_inline)) {
         if ((unit + 1) * kWords <= a.groups) {
             load16<false>(scales + unit * kWords, sc);
         } else {
@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(512, 1) k_product_many(ProductArgs a) {
             for (int k = 0; k < kWords; ++k) sc[k] = unit * kWords + k < a.groups ? scales[unit * kWords + k] : 0;
         }
     };
-    auto store_scales = [&](int32_t unit) {
+    auto store_scales = [&](int32_t unit) __attribute__((always_inline)) {
 #pragma unroll
         for (int k = 0; k < kWords; ++k) turned[((unit & 1) * kWords + k) * kBoth + t] = sc[k];
     };
@@ -220,10 +220,13 @@ __global__ void __launch_bounds__(512, 1) k_product_many(ProductArgs a) {
     float16_ sum[kLive ? kLive : 1][2] = {};
     for (int32_t step = 0; step < steps; ++step) {
         wait_and_meet();
-        if (step + 1 < steps) issue(step + 1);
         const int32_t unit = step >> 1;
-        const bool more = (unit + 1) * kWords < a.groups;
-        if ((step & 1) == 0 && more) fetch_scales(unit + 1);
+        if ((unit + 1) * kWords < a.groups) {
+            // (before the codes' loads, which a wait for the scales would wait for)
+            if (step & 1) store_scales(unit + 1);
+            else fetch_scales(unit + 1);
+        }
+        if (step + 1 < steps) issue(step + 1);
         const char *tile = lds + (step & 1) * kStage;
         const uint32_t *scale = turned + (((step >> 1) & 1) * kWords + (step & 1) * 2) * kBoth + r32;
         const int groups = step + 1 == steps && odd ? 1 : 2;
@@ -258,7 +261,6 @@ __global__ void __launch_bounds__(512, 1) k_product_many(ProductArgs a) {
                     }
             }
         }
-        if ((step & 1) == 1 && more) store_scales(unit + 1);
     }
     wait_and_meet();
     static_assert(8 * 32 * kPitch<T, 2> <= kManyLds, "the waves' parts fit");
