@@ -92,20 +92,31 @@ __device__ inline void lanes_first(uint64_t &key, uint32_t &at, int lanes) {
     if constexpr (D < kWave) lanes_first<2 * D>(key, at, lanes);
 }
 // The K largest of the lanes' lists, in every lane, in no order: the upper half of
-// the lanes has them the other way round.
-template <class Key, int K, int D = 2>
-__device__ inline void lanes_top(typename Key::Word (&top)[K], int lanes) {
-    if (D > lanes) return;
-    typename Key::Word y[K];
+// the lanes has them the other way round.  (A loop over the steps: one network for
+// all of them, where a network for each took twice the registers.)
+template <int D, class T, int K>
+__device__ inline void all_across(const T (&x)[K], T (&y)[K]) {
 #pragma unroll
-    for (int i = 0; i < K; ++i) y[i] = across<D>(top[i]);
-    if (D == lanes) {  // (the last step need not sort)
+    for (int i = 0; i < K; ++i) y[i] = across<D>(x[i]);
+}
+template <class Key, int K>
+__device__ inline void lanes_top(typename Key::Word (&top)[K], int lanes) {
+#pragma unroll 1
+    for (int d = 2;; d *= 2) {
+        typename Key::Word y[K];
+        switch (d) {
+            case 2: all_across<2>(top, y); break;
+            case 4: all_across<4>(top, y); break;
+            case 8: all_across<8>(top, y); break;
+            case 16: all_across<16>(top, y); break;
+            case 32: all_across<32>(top, y); break;
+            default: all_across<64>(top, y);
+        }
 #pragma unroll
         for (int i = 0; i < K; ++i) top[i] = Key::max(top[i], y[K - 1 - i]);
-        return;
+        if (d >= lanes) break;  // (the last step need not sort)
+        bitonic_sort<Key, 0, K>(top);
     }
-    merge_top<Key, K>(top, y);
-    if constexpr (D < kWave) lanes_top<Key, K, 2 * D>(top, lanes);
 }
 
 // The groups that precede group g of the token whose lanes begin at lane0: with
@@ -130,11 +141,9 @@ __device__ inline int groups_before(int groups, int q_shift, uint64_t best, int 
     return n;
 }
 
-// WHOLE: every lane's vectors are whole.  (Scores with up to 8 choices are held to
-// four waves a SIMD: left alone the part in 64 bits takes twice the registers, and
-// 51 us where the call takes 44.)
+// WHOLE: every lane's vectors are whole.
 template <class T, int NV, int K, bool SCORES, bool WHOLE>
-__global__ void __launch_bounds__(256, SCORES && K == 8 ? 4 : 1) k_route_groups(GroupArgs ga) {
+__global__ void __launch_bounds__(256, K == 8 ? 4 : 1) k_route_groups(GroupArgs ga) {
     using Key = typename KeyOf<typename Choose<SCORES, float, T>::type>::type;
     using Word = typename Key::Word;
     constexpr int W = 16 / sizeof(T), M = 8, S = K / M;
@@ -330,7 +339,10 @@ __global__ void __launch_bounds__(256, SCORES && K == 8 ? 4 : 1) k_route_groups(
         // The tokens in doubt, one at a time by the whole wave, in 64 bits: loops of
         // little code, an element at a time from memory, a group in as many lanes as
         // fit 64 (a wave that took them by their own lanes took 15 us, and kept the
-        // rest waiting).  NaN takes no part; experts of +inf share the scores alone.
+        // rest waiting).  A lane's keys stand in LDS, where it alone reads them: they
+        // cost the calls without doubt no registers.  NaN takes no part; experts of +inf share the scores alone.
+        extern __shared__ uint64_t keys_of_waves[];
+        uint64_t *const keys = keys_of_waves + (threadIdx.x >> 6) * a.E;
         int q_shift = 0;
         while ((ga.groups << (q_shift + 1)) <= kWave) ++q_shift;
         for (uint64_t todo = __ballot(open); todo;) {
@@ -371,48 +383,35 @@ __global__ void __launch_bounds__(256, SCORES && K == 8 ? 4 : 1) k_route_groups(
 #pragma unroll 1
             for (int e = lane & (step - 1); e < count; e += step) {
                 const uint64_t key = key_at(e);
+                keys[group * ga.size + e] = key;
                 g2 = max64(g2, min64(g1, key));
                 g1 = max64(g1, key);
             }
             lanes_two(g1, g2, step);
             if (ga.top == 2 && g2) g1 = order64(value64(g1) + value64(g2));
             const bool keep = g1 != 0 && groups_before(ga.groups, q_shift, g1, group, 0) < ga.keep;
-            uint64_t list[K];  // a lane's K largest, sorted by insertion
-            uint32_t who[K];
-#pragma unroll
-            for (int j = 0; j < K; ++j) {
-                list[j] = 0;
-                who[j] = UINT32_MAX;
-            }
+            uint64_t best;  // of what this lane still has
+            uint32_t who;
+            auto look = [&] {
+                best = 0;
+                who = UINT32_MAX;
 #pragma unroll 1
-            for (int e0 = lane & (step - 1); e0 < (keep ? count : 0); e0 += step) {
-                uint64_t key = key_at(e0);
-                uint32_t e = (uint32_t)(group * ga.size + e0);
-#pragma unroll
-                for (int j = 0; j < K; ++j) {
-                    const bool before = key > list[j] || (key == list[j] && e < who[j]);
-                    const uint64_t k1 = list[j];
-                    const uint32_t e1 = who[j];
-                    list[j] = before ? key : k1;
-                    who[j] = before ? e : e1;
-                    key = before ? k1 : key;
-                    e = before ? e1 : e;
+                for (int e = lane & (step - 1); e < (keep ? count : 0); e += step) {
+                    const uint64_t key = keys[group * ga.size + e];
+                    who = key > best ? (uint32_t)(group * ga.size + e) : who;
+                    best = key > best ? key : best;
                 }
-            }
+            };
+            look();
             const bool its_lane = its >> lane & 1;
 #pragma unroll 1
             for (int j = 0; j < a.k; ++j) {
-                uint64_t k0 = list[0];
-                uint32_t e0 = who[0];
+                uint64_t k0 = best;
+                uint32_t e0 = who;
                 lanes_first(k0, e0, kWave);
-                if (who[0] == e0) {
-#pragma unroll
-                    for (int i = 0; i + 1 < K; ++i) {
-                        list[i] = list[i + 1];
-                        who[i] = who[i + 1];
-                    }
-                    list[K - 1] = 0;
-                    who[K - 1] = UINT32_MAX;
+                if (k0 && who == e0) {
+                    keys[e0] = 0;
+                    look();
                 }
 #pragma unroll
                 for (int s = 0; s < S; ++s)
@@ -438,8 +437,10 @@ __global__ void __launch_bounds__(256, SCORES && K == 8 ? 4 : 1) k_route_groups(
     }
 }
 
-// Lanes of a group and a token: as few as hold a group in 8 vectors a lane (at
-// least 8 a token, for the second selection).
+// Lanes of a group and a token: as few as hold a group in 8 vectors a lane, keys
+// other than the logits in 32 elements (at least 8 a token, for the second
+// selection).
+constexpr int kScoresALane = 32;
 template <class T>
 int choose_groups(GroupArgs a, hipStream_t stream) {
     constexpr int W = 16 / sizeof(T);
@@ -451,23 +452,33 @@ int choose_groups(GroupArgs a, hipStream_t stream) {
     }
     a.q_shift = 0;
     const int vecs = (a.size + W - 1) / W;
+    const bool scores = a.r.bias || a.top > 1;
+    const int most = scores ? kScoresALane / W : 8;  // (E <= 1024: 64 lanes never need more)
     auto each = [&] { return (vecs + (1 << a.q_shift) - 1) >> a.q_shift; };
-    while ((each() > 8 && (groups << a.q_shift) < kWave) || (groups << a.q_shift) < 8) ++a.q_shift;
+    while ((each() > most && (groups << a.q_shift) < kWave) || (groups << a.q_shift) < 8) ++a.q_shift;
     a.lane_shift += a.q_shift;
     const int64_t items = a.r.T * a.r.L, per = 256 >> a.lane_shift;
+    const size_t lds = scores ? 4 * (size_t)a.r.E * sizeof(uint64_t) : 0;
     auto go = [&](auto kern) {
-        hipLaunchKernelGGL(kern, grid_of((items + per - 1) / per), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL(kern, grid_of((items + per - 1) / per), dim3(256), lds, stream, a);
         return hipGetLastError() == hipSuccess ? ROUTEPACK_OK : ROUTEPACK_E_DEVICE;
     };
     auto by_k = [&](auto v) {
         constexpr int N = decltype(v)::value;
-        const bool scores = a.r.bias || a.top > 1;
         // (8 choices at most, whole vectors and no idle lanes: without the checks of
         // every vector)
         const bool whole = a.r.k <= 8 && a.size == (N * W) << a.q_shift && a.groups == groups;
-        if (whole) return scores ? go(k_route_groups<T, N, 8, true, true>) : go(k_route_groups<T, N, 8, false, true>);
-        if (a.r.k <= 8) return scores ? go(k_route_groups<T, N, 8, true, false>) : go(k_route_groups<T, N, 8, false, false>);
-        return scores ? go(k_route_groups<T, N, 32, true, false>) : go(k_route_groups<T, N, 32, false, false>);
+        auto by_keys = [&](auto scores_) {
+            constexpr bool SCORES = decltype(scores_)::value != 0;
+            if (whole) return go(k_route_groups<T, N, 8, SCORES, true>);
+            if (a.r.k <= 8) return go(k_route_groups<T, N, 8, SCORES, false>);
+            if (a.r.k <= 16) return go(k_route_groups<T, N, 16, SCORES, false>);
+            return go(k_route_groups<T, N, 32, SCORES, false>);
+        };
+        if constexpr (N * W <= kScoresALane) {
+            if (scores) return by_keys(Int<1>());
+        }
+        return by_keys(Int<0>());
     };
     if (each() <= 1) return by_k(Int<1>());
     if (each() <= 2) return by_k(Int<2>());
