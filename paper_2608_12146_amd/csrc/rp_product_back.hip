@@ -160,12 +160,14 @@ __device__ __forceinline__ void back_tile(const BackProductArgs &a, int64_t id, 
             clear_rows(static_cast<T *>(a.out), a.C, a.offsets, a.n_slots, a.R, id - a.tiles, a.clears);
             return;
         }
-        const int64_t index = id / a.c_tiles;
-        ct = (int32_t)(id - index * a.c_tiles);
         int64_t before;
         const TileMap map(a.offsets, a.n_slots, a.R, kRows);
-        if (index >= map.total) return;
-        s = map.find(index, a.offsets, a.n_slots, a.R, kRows, seg, before);
+        // (workgroups go to the eight XCDs in turn: each XCD gets a run of adjacent tiles)
+        const int64_t all = map.total * a.c_tiles, run = (all + 7) / 8, index = (id & 7) * run + (id >> 3);
+        if ((id >> 3) >= run || index >= all) return;
+        const int64_t tile = index / a.c_tiles;
+        ct = (int32_t)(index - tile * a.c_tiles);
+        s = map.find(tile, a.offsets, a.n_slots, a.R, kRows, seg, before);
         m0 = seg.begin + before * kRows;
     }
     const int c0 = ct * kCols, t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -301,9 +303,9 @@ void cut(BackProductArgs &a) {
         a.tiles = (int64_t)a.n_slots * a.m_tiles * a.c_tiles;
         a.clears = 0;
     } else {
-        // each slot may have a tile that is not full
+        // each slot may have a tile that is not full; eight runs of equal length
         const int64_t slots = a.R < a.n_slots ? a.R : a.n_slots, pieces = (a.R * a.C + 65535) / 65536;
-        a.tiles = (a.R / G::kRows + slots) * a.c_tiles;
+        a.tiles = ((a.R / G::kRows + slots) * a.c_tiles + 7) / 8 * 8;
         a.clears = pieces < 256 ? pieces : 256;
     }
 }
