@@ -49,29 +49,48 @@ __device__ inline uint32_t take_part(float &v) {
     return u >> 16;
 }
 
+// 8 values of dy, in their own type.
+template <class T> constexpr int kRaw = 8 * (int)sizeof(T) / 4;
+template <class T>
+__device__ inline void raw8(const char *at, uint32_t (&raw)[kRaw<T>]) {
+#pragma unroll
+    for (int i = 0; i < kRaw<T> / 4; ++i) {
+        uint32_t w[4];
+        load16<false>(at + 16 * i, w);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) raw[4 * i + j] = w[j];
+    }
+}
+// Those of a row from `from` on, zeros from `end` > 0 on and where the row is not live.
+template <class T>
+__device__ inline void raw8_cut(const T *row, int32_t from, int32_t end, bool live, uint32_t (&raw)[kRaw<T>]) {
+    uint32_t b[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const bool ok = live && from + i < end;
+        b[i] = bits_of(row + (ok ? from + i : 0));
+        b[i] = ok ? b[i] : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < kRaw<T>; ++i) raw[i] = sizeof(T) == 4 ? b[i] : b[2 * i % 8] | b[(2 * i + 1) % 8] << 16;
+}
+
 // 8 values of dy as P vectors of bf16 parts.
 template <class T, int P>
-__device__ inline void split8(const T *row, int32_t from, int32_t end, bool live, int4_ (&part)[P]) {
-    // (a row whose terms do not count is zeros)
-    if (P == 1 && live && from + 8 <= end) {
-        uint32_t w[4];
-        load16<false>(row + from, w);
-        part[0] = int4_{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+__device__ inline void split8(const uint32_t (&raw)[kRaw<T>], int4_ (&part)[P]) {
+    if constexpr (P == 1) {
+        part[0] = int4_{(int)raw[0], (int)raw[1], (int)raw[2], (int)raw[3]};
         return;
     }
+    constexpr int W = Vec<T>::W;
     float v[8];
-    if (live && from + 8 <= end) {
-        constexpr int W = Vec<T>::W;
 #pragma unroll
-        for (int i = 0; i < 8 / W; ++i) {
-            Vec<T> x;
-            load16<false>(row + from + i * W, x.w);
+    for (int i = 0; i < 8 / W; ++i) {
+        Vec<T> x;
 #pragma unroll
-            for (int j = 0; j < W; ++j) v[i * W + j] = x.at(j);
-        }
-    } else {
+        for (int j = 0; j < 4; ++j) x.w[j] = raw[4 * i + j];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = live && from + i < end ? to_f32(row[from + i]) : 0.0f;
+        for (int j = 0; j < W; ++j) v[i * W + j] = x.at(j);
     }
     // (all finite: no test a value; what is left of an infinity or NaN is NaN)
     float left[8], sum = 0.0f;
@@ -179,43 +198,75 @@ __device__ __forceinline__ void back_tile(const BackProductArgs &a, int64_t id, 
     const T *dy = static_cast<const T *>(a.dy);
     const int64_t b_row0 = DW ? 0 : (int64_t)s * a.N;
     // The tile's A: pieces of 8 values, of a row's 64 terms (dx) or of a term's
-    // kRows columns (dw); B: blocks of 32 columns, kCols / 32 a term.
+    // kRows columns (dw); B: blocks of 32 columns, kCols / 32 a term (16 lanes write
+    // 4 of 4 terms each to LDS, in different banks).
     constexpr int kAcross = DW ? kRows / 8 : kTerms / 8, kBlocksAcross = kCols / 32;
     constexpr int kAStep = G::kThreads / kAcross, kBStep = G::kThreads / kBlocksAcross;
-    const int a_row = t / kAcross, a_piece = t % kAcross, b_row = t / kBlocksAcross, b_block = t % kBlocksAcross;
-    int4_ pa[G::kPieces][P];
+    const int a_row = t / kAcross, a_piece = t % kAcross;
+    const int b_row = ((t >> 2) & 3) + 4 * (t / (4 * kBlocksAcross)), b_block = (t & 3) + 4 * ((t >> 4) % (kBlocksAcross / 4));
+    // What a thread fetches stands at fixed distances from a step's first term, in 32
+    // bits (rows and pieces past the output's end are its last ones again: nothing of
+    // them is kept).  Elsewhere (N ends inside a piece, far rows) values go one by one.
+    const bool near = a.stride <= 1 << 22 && (!DW || a.N % 8 == 0 || m0 + kRows <= a.N);
+    const int a_col = DW && m0 + a_piece * 8 > a.N - 8 ? a.N - 8 : (DW ? (int)m0 : 0) + a_piece * 8;
+    const uint32_t code_row = (uint32_t)a.groups * 64, scale_row = (uint32_t)a.groups * 4;
+    const int block = ct * kBlocksAcross + b_block < a.groups * 4 ? ct * kBlocksAcross + b_block : a.groups * 4 - 1;
+    uint32_t a_at[G::kPieces];
+#pragma unroll
+    for (int i = 0; i < G::kPieces; ++i) {
+        const int row = a_row + i * kAStep, r = DW || row < rows ? row : rows - 1;
+        a_at[i] = (uint32_t)((r * a.stride + a_col) * (int)sizeof(T));
+    }
+    uint32_t raw[G::kPieces][kRaw<T>];
     int4_ pb[G::kBlocks];
     uint32_t sb[G::kBlocks];
     auto fetch = [&](int64_t k0) __attribute__((always_inline)) {
+        const int last = k_end - k0 < kTerms ? (int)(k_end - k0) - 1 : kTerms - 1;  // (term)
+        const T *first = dy + (DW ? k0 * a.stride : m0 * a.stride + k0);
+        const uint8_t *codes = a.bc + (b_row0 + k0) * code_row, *scales = a.bs + (b_row0 + k0) * scale_row;
+        if (near && last == kTerms - 1) {
 #pragma unroll
-        for (int i = 0; i < G::kPieces; ++i) {
-            const int64_t r = (DW ? k0 : m0) + a_row + i * kAStep, end = DW ? k_end : m_end;
-            split8<T, P>(dy + (r < end ? r : 0) * a.stride, (int32_t)(DW ? m0 : k0) + a_piece * 8, a.N, r < end, pa[i]);
+            for (int i = 0; i < G::kPieces; ++i) raw8<T>(reinterpret_cast<const char *>(first) + a_at[i], raw[i]);
+        } else if (near && (DW || a.N % 8 == 0)) {
+#pragma unroll
+            for (int i = 0; i < G::kPieces; ++i) {
+                const int row = a_row + i * kAStep;
+                const bool ok = DW ? row <= last : a_piece * 8 <= last;
+                const uint32_t to = DW ? (uint32_t)((last * a.stride + a_col) * (int)sizeof(T)) : a_at[i] - a_piece * 8 * (int)sizeof(T);
+                raw8<T>(reinterpret_cast<const char *>(first) + (ok ? a_at[i] : to), raw[i]);
+#pragma unroll
+                for (int j = 0; j < kRaw<T>; ++j) raw[i][j] = ok ? raw[i][j] : 0;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < G::kPieces; ++i) {
+                const int64_t r = (DW ? k0 : m0) + a_row + i * kAStep, end = DW ? k_end : m_end;
+                raw8_cut<T>(dy + (r < end ? r : end - 1) * a.stride, (int32_t)(DW ? m0 : k0) + a_piece * 8, a.N, r < end, raw[i]);
+            }
         }
 #pragma unroll
         for (int i = 0; i < G::kBlocks; ++i) {
-            const int64_t k = k0 + b_row + i * kBStep;
-            const int block = ct * kBlocksAcross + b_block;
-            pb[i] = int4_{0, 0, 0, 0};
-            sb[i] = 127;
-            if (k < k_end && block < a.groups * 4) {
-                const int64_t row = b_row0 + k;
-                pb[i] = *reinterpret_cast<const int4_ *>(a.bc + row * a.groups * 64 + block * 16);
-                sb[i] = a.bs[row * a.groups * 4 + block];
+            const int row = b_row + i * kBStep, k = row < last ? row : last;
+            pb[i] = *reinterpret_cast<const int4_ *>(codes + (k * code_row + block * 16));
+            sb[i] = scales[k * scale_row + block];
+            if (row > last) {
+                pb[i] = int4_{0, 0, 0, 0};
+                sb[i] = 127;
             }
         }
     };
     auto store = [&](char *stage) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < G::kPieces; ++i)
+        for (int i = 0; i < G::kPieces; ++i) {
+            int4_ part[P];
+            split8<T, P>(raw[i], part);
+            const int row = a_row + i * kAStep;
+            int at;
+            if constexpr (DW) at = term_at<kRows>(row, a_piece * 8);
+            else at = row * 128 + ((a_piece ^ ((row >> 1) & 7)) << 4);
 #pragma unroll
-            for (int p = 0; p < P; ++p) {
-                const int row = a_row + i * kAStep;
-                int at;
-                if constexpr (DW) at = term_at<kRows>(row, a_piece * 8);
-                else at = row * 128 + ((a_piece ^ ((row >> 1) & 7)) << 4);
-                *reinterpret_cast<int4_ *>(stage + p * G::kA + at) = pa[i][p];
-            }
+            for (int p = 0; p < P; ++p) *reinterpret_cast<int4_ *>(stage + p * G::kA + at) = part[p];
+        }
         char *const to = stage + P * G::kA;
 #pragma unroll
         for (int b = 0; b < G::kBlocks; ++b) {
@@ -255,15 +306,15 @@ __device__ __forceinline__ void back_tile(const BackProductArgs &a, int64_t id, 
                     for (int n = 0; n < NB; ++n) sum[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[n], x, sum[m][n], 0, 0, 0);
                 }
         };
-        if (k_begin < k_end) fetch(k_begin);
-        for (int64_t k0 = k_begin; k0 < k_end; k0 += kTerms) {
-            store(lds);
-            __syncthreads();
-            if (k0 + kTerms < k_end) fetch(k0 + kTerms);
-            if (kLive) {
+        for (int64_t k0 = k_begin;; k0 += kTerms) {  // (fetches what follows what is multiplied)
+            if (k0 < k_end) fetch(k0);
+            if (kLive && k0 > k_begin) {
 #pragma unroll
                 for (int k = 0; k < kTerms; k += 16) multiply(lds, k);
             }
+            __syncthreads();
+            if (k0 >= k_end) break;
+            store(lds);
             __syncthreads();
         }
 #pragma unroll
