@@ -370,27 +370,47 @@ int launch_back(Kernel kern, int64_t groups, hipStream_t stream, const Args &...
     return launched();
 }
 
-// dx: tiles of 128 x 256 where they are enough for the chip.  dw, whose sums are
-// short, and small problems: of 128 x 128, more of them at a time.
+// Tiles of 128 x 256 where they fill the chip, on four waves of 64 x 128, which read
+// least of LDS; dx of bf16 on eight of 64 x 64, which wait less (24558 rows, 60 x
+// 1408 x 1984: dx 194 us, 209 on four waves, with fp16 396 and 311; dw 271 and 207,
+// with fp16 378 and 346).  Else tiles of 128 x 128, more of them at a time: for dw,
+// whose sums are short, up to several rounds of the chip (those rows: 226 us; 60000,
+// 128 x 256 x 256: 59 and 85 by the wide ones).
 template <class T>
 int back_of(BackProductArgs *x, BackProductArgs *w, hipStream_t stream) {
-    using Large = BackShape<T, 4, 2, 2>;
-    using Small = BackShape<T, 2, 2, 2>;
     constexpr int kWaves = kParts<T> == 1 ? 3 : 2;
-    if (w) cut<Small, true>(*w);
-    if (x) {
-        const int64_t tiles = (x->R / 128 + (x->R < x->n_slots ? x->R : x->n_slots) / 2) * ((x->C + 255) / 256);
-        if (tiles >= 256) {
-            cut<Large, false>(*x);
-            RP_TRY(launch_back<Large>(k_product_back<T, false, 4, 2, 2, kParts<T> == 1 ? 4 : 2>, x->tiles + x->clears, stream, *x));
+    using Small = BackShape<T, 2, 2, 2>;
+    using Wide = BackShape<T, 2, 2, 4>;
+    const BackProductArgs &any = x ? *x : *w;
+    const int64_t across = (any.C + 255) / 256, slots = any.R < any.n_slots ? any.R : any.n_slots;
+    const bool wide_x = x && any.C > 128 && (any.R / 128 + slots / 2) * across >= 256;
+    const bool wide_w = w && any.C > 128 && (any.N + 127) / 128 * any.n_slots * across >= 4096;
+    if (wide_x) {
+        if constexpr (kParts<T> == 1) {
+            using Eight = BackShape<T, 4, 2, 2>;
+            cut<Eight, false>(*x);
+            RP_TRY(launch_back<Eight>(k_product_back<T, false, 4, 2, 2, 4>, x->tiles + x->clears, stream, *x));
         } else {
-            cut<Small, false>(*x);
-            const int64_t n = x->tiles + x->clears;
-            if (w) return launch_back<Small>(k_product_back_both<T, 2, 2, 2, kWaves>, n + w->tiles, stream, *x, *w);
-            return launch_back<Small>(k_product_back<T, false, 2, 2, 2, kWaves>, n, stream, *x);
+            cut<Wide, false>(*x);
+            RP_TRY(launch_back<Wide>(k_product_back<T, false, 2, 2, 4, 2>, x->tiles + x->clears, stream, *x));
         }
+    } else if (x) {
+        cut<Small, false>(*x);
+        const int64_t n = x->tiles + x->clears;
+        if (w) {
+            cut<Small, true>(*w);
+            return launch_back<Small>(k_product_back_both<T, 2, 2, 2, kWaves>, n + w->tiles, stream, *x, *w);
+        }
+        return launch_back<Small>(k_product_back<T, false, 2, 2, 2, kWaves>, n, stream, *x);
     }
-    if (w) RP_TRY(launch_back<Small>(k_product_back<T, true, 2, 2, 2, kWaves>, w->tiles, stream, *w));
+    if (wide_w) {
+        cut<Wide, true>(*w);
+        return launch_back<Wide>(k_product_back<T, true, 2, 2, 4, 2>, w->tiles, stream, *w);
+    }
+    if (w) {
+        cut<Small, true>(*w);
+        return launch_back<Small>(k_product_back<T, true, 2, 2, 2, kWaves>, w->tiles, stream, *w);
+    }
     return ROUTEPACK_OK;
 }
 
