@@ -370,12 +370,13 @@ int launch_back(Kernel kern, int64_t groups, hipStream_t stream, const Args &...
     return launched();
 }
 
-// Tiles of 128 x 256 where they fill the chip, on four waves of 64 x 128, which read
-// least of LDS; dx of bf16 on eight of 64 x 64, which wait less (24558 rows, 60 x
-// 1408 x 1984: dx 194 us, 209 on four waves, with fp16 396 and 311; dw 271 and 207,
-// with fp16 378 and 346).  Else tiles of 128 x 128, more of them at a time: for dw,
-// whose sums are short, up to several rounds of the chip (those rows: 226 us; 60000,
-// 128 x 256 x 256: 59 and 85 by the wide ones).
+// Tiles of 128 x 256 where they fill the chip: with parts to multiply on four waves
+// of 64 x 128, which read least of LDS (24558 rows, 60 x 1408 x 1984 fp16: dx 396 us
+// by eight waves of 64 x 64, 311; dw 384 by tiles of 128 x 128, 341), dx of bf16 on
+// eight of 64 x 64, which wait less (194 us, 209 on four).  Else tiles of 128 x 128,
+// more of them at a time: for dw, whose sums are short, up to several rounds of the
+// chip, and always with bf16 (those rows: 220 us either way; 60000 rows, 128 x 256 x
+// 256: 59 us, 85 by the wide ones).
 template <class T>
 int back_of(BackProductArgs *x, BackProductArgs *w, hipStream_t stream) {
     constexpr int kWaves = kParts<T> == 1 ? 3 : 2;
@@ -384,7 +385,6 @@ int back_of(BackProductArgs *x, BackProductArgs *w, hipStream_t stream) {
     const BackProductArgs &any = x ? *x : *w;
     const int64_t across = (any.C + 255) / 256, slots = any.R < any.n_slots ? any.R : any.n_slots;
     const bool wide_x = x && any.C > 128 && (any.R / 128 + slots / 2) * across >= 256;
-    const bool wide_w = w && any.C > 128 && (any.N + 127) / 128 * any.n_slots * across >= 4096;
     if (wide_x) {
         if constexpr (kParts<T> == 1) {
             using Eight = BackShape<T, 4, 2, 2>;
@@ -403,9 +403,11 @@ int back_of(BackProductArgs *x, BackProductArgs *w, hipStream_t stream) {
         }
         return launch_back<Small>(k_product_back<T, false, 2, 2, 2, kWaves>, n, stream, *x);
     }
-    if (wide_w) {
-        cut<Wide, true>(*w);
-        return launch_back<Wide>(k_product_back<T, true, 2, 2, 4, 2>, w->tiles, stream, *w);
+    if constexpr (kParts<T> > 1) {
+        if (w && any.C > 128 && (any.N + 127) / 128 * any.n_slots * across >= 4096) {
+            cut<Wide, true>(*w);
+            return launch_back<Wide>(k_product_back<T, true, 2, 2, 4, 2>, w->tiles, stream, *w);
+        }
     }
     if (w) {
         cut<Small, true>(*w);
