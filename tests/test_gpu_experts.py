@@ -11,8 +11,8 @@ Tolerances, u = 2^-24 (half a step of rounding in 32 bits):
   bf16 values, exactly and add them in 32 bits, each addition off by at most a
   whole step (2 u) of the magnitudes' sum where the hardware truncates.  A sum of
   n terms: at most 2 n u of the sum of magnitudes; n = C, N or the slot's rows,
-  times the parts of dy (bf16 1, fp16 2, fp32 3), plus 8 for joining four waves'
-  sums and the padded columns' zeros.
+  times the parts of dy (bf16 1, fp16 2, fp32 3), plus 8 for the padded columns'
+  zeros.
 - combine: k products and additions, 2 k u of the magnitudes; a gate's gradient:
   C of them and 9 exchanges.
 Rounding to the output's type adds half a step, finfo.eps / 2 of the value, or
