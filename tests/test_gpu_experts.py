@@ -433,6 +433,41 @@ def test_product_gradients(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+def test_product_gradients_by_wide_tiles(dtype):
+    """Enough tiles for those of 128 x 256, of dx and of dw; N that ends inside a
+    step, inside a piece of 8, and before one."""
+    import torch
+    import paper_2608_12146_amd as rp
+    parts = {"bf16": 1, "fp16": 2, "fp32": 3}[dtype]
+    few = torch.randint(0, 3, (2048,), generator=torch.Generator().manual_seed(1)).tolist()
+    few[7], few[2000] = 200, 65
+    for n, (counts, N, C) in enumerate([([8000, 0, 300], 72, 1030), ([8001, 5, 290], 61, 1100), (few, 8, 300), (few, 3, 257)]):
+        R = sum(counts)
+        _log((dtype, R, len(counts), N, C))
+        x, w, off = _random_mx(n, (R,), C), _random_mx(n + 50, (len(counts), N), C), _offsets(counts)
+        dy = _floats(n + 70, (R, N), dtype, gap=n % 2, scale=0.3)
+        dx, dw = rp.expert_product_backward(dy, x, w, off)
+        (wx, mx), (ww, mw) = X.product_backward(_host(dy), _values(x), _values(w), _host(off))
+        _near(dx, wx, 2 * (parts * N + 136) * U * mx, (dtype, R, N, C))
+        _near(dw, ww, 2 * (parts * max(counts) + 136) * U * mw, (dtype, R, N, C))
+
+
+@gpu
+def test_product_gradients_of_far_rows():
+    """Rows of dy further apart than 32 bits of bytes reach over a tile."""
+    import torch
+    import paper_2608_12146_amd as rp
+    N, C, counts, stride = 24, 40, [69, 1, 2], (1 << 22) + 8
+    dy = torch.empty(72 * stride, dtype=torch.bfloat16, device="cuda").as_strided((72, N), (stride, 1))
+    near = _floats(1, (72, N), "bf16")
+    dy.copy_(near)
+    x, w, off = _random_mx(1, (72,), C), _random_mx(2, (3, N), C), _offsets(counts)
+    for got, want in zip(rp.expert_product_backward(dy, x, w, off), rp.expert_product_backward(near, x, w, off)):
+        assert torch.equal(got, want)
+
+
+@gpu
 def test_product_gradients_of_infinities():
     import torch
     import paper_2608_12146_amd as rp
