@@ -69,7 +69,8 @@ int64_t routepack_order_workspace(const routepack_problem *prob, int64_t n_token
  *              this call alone until its work has ended (may be NULL where those are 0)
  * E_INVALID on null pointers, a negative size or stride, E < 1, k < 1, an
  * unknown type, or a workspace too small or misaligned; E_UNSUPPORTED when
- * E > 2048, k > 256, or T k >= 2^31. */
+ * E > 2048, k > 256, T k >= 2^31, or the layers' pairs, each layer's in chunks of
+ * 4096 and seven more, make 2^22 chunks. */
 int routepack_order_tokens(const routepack_problem *prob, const routepack_ids *ids, const int32_t *slots,
                            int32_t *rows, int64_t *offsets, int32_t *places, void *workspace,
                            int64_t workspace_bytes, hipStream_t stream);
