@@ -11,16 +11,17 @@
 // elements of the k vectors that lead.  Few lanes, as each doubling costs a merge
 // of lists: 8 lanes of 8 vectors a token.
 //
-// Without a bias and with group_top = 1 the keys are the logits, whose order
-// is the scores'.  Otherwise keys are compared in 64 bits, as two
-// implementations in 32 bits would choose differently: the keys are formed in
-// 32 bits, and where their error leaves the groups kept, the choices or their
-// order open (about one token in 500, and ties), the wave forms them in 64.
+// Without a bias the keys' order is the logits', and only sums of two scores
+// rank groups.  Scores are compared in 64 bits, as two implementations in 32
+// bits would choose differently: they are formed in 32 bits, and where their
+// error leaves the groups kept, the choices or their order open (about one token
+// in 500 in fp32; with a bias ties too), the wave forms them in 64.
 //
 // Bound by HBM and vector instructions: 131072 x 512 bf16, 8 groups: 40 us
 // (a copy of the logits takes 26); 65536 x 256 fp32, logistic, two keys a group
-// and a bias: 44 us (78 with all keys in 64 bits; 35 without the tokens in doubt,
-// whose waves end last).
+// and a bias: 39 us (78 with all keys in 64 bits); 48255 x 352 bf16 in 16 groups,
+// softmax, two keys a group: 53 us (105 with scores as the experts' keys, where
+// equal logits left a third of the tokens in doubt).
 #pragma once
 
 #include "rp_route.h"
@@ -141,10 +142,14 @@ __device__ inline int groups_before(int groups, int q_shift, uint64_t best, int 
     return n;
 }
 
-// WHOLE: every lane's vectors are whole.
-template <class T, int NV, int K, bool SCORES, bool WHOLE>
+// What the keys are: the logits, whose order is the scores' (kLogits); the same for
+// the experts, while groups go by the sum of two scores (kSums); scores with a bias
+// (kBiased).  WHOLE: every lane's vectors are whole.
+enum { kLogits, kSums, kBiased };
+template <class T, int NV, int K, int KEYS, bool WHOLE>
 __global__ void __launch_bounds__(256, K == 8 ? 4 : 1) k_route_groups(GroupArgs ga) {
-    using Key = typename KeyOf<typename Choose<SCORES, float, T>::type>::type;
+    constexpr bool BIASED = KEYS == kBiased, SCORES = KEYS != kLogits;
+    using Key = typename KeyOf<typename Choose<BIASED, float, T>::type>::type;
     using Word = typename Key::Word;
     constexpr int W = 16 / sizeof(T), M = 8, S = K / M;
     const RouteArgs &a = ga.r;
@@ -158,7 +163,7 @@ __global__ void __launch_bounds__(256, K == 8 ? 4 : 1) k_route_groups(GroupArgs 
     const int64_t t = a.L == 1 ? at : n <= UINT32_MAX ? (uint32_t)at / (uint32_t)a.L : at / a.L;
     const int32_t l = (int32_t)(at - t * a.L);
     const T *data = static_cast<const T *>(a.logits) + t * a.ts + l * a.ls;
-    const float *bias = SCORES && a.bias ? a.bias + (int64_t)l * a.E : nullptr;
+    const float *bias = BIASED ? a.bias + (int64_t)l * a.E : nullptr;
     const Row<T, WHOLE> row = {data + g * ga.size, g < ga.groups ? ga.size : 0};
     Vec<T> raw[NV];
 #pragma unroll
@@ -170,7 +175,7 @@ __global__ void __launch_bounds__(256, K == 8 ? 4 : 1) k_route_groups(GroupArgs 
     const bool softmax = a.score == ROUTEPACK_SOFTMAX;
     float m = 0.0f, inv = 0.0f;
     float mx[NV], f1 = -kInf, f2 = -kInf;  // the vectors' largest logits, then keys
-    if (!SCORES || softmax) {
+    if (!BIASED || softmax) {
         bool odd = false;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -200,25 +205,23 @@ __global__ void __launch_bounds__(256, K == 8 ? 4 : 1) k_route_groups(GroupArgs 
         sum = lanes_add(sum, lanes);
         inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     }
+    // (a logistic score this way keeps the absolute error below, not 1 - s)
+    auto score = [&](float z) { return softmax ? exp_plain(z - m) * inv : __builtin_amdgcn_rcpf(1.0f + exp_plain(-z)); };
     // a vector's keys in 32 bits, -inf where the expert is not available
     auto keys_of = [&](const Vec<T> &r, int group, int vec, float (&y)[W]) {
-        if constexpr (SCORES) {
-            float b[W] = {};
-            if (bias) {
-                const Row<float, WHOLE> bias_row = {bias + group * ga.size, group < ga.groups ? ga.size : 0};
+        if constexpr (BIASED) {
+            float b[W];
+            const Row<float, WHOLE> bias_row = {bias + group * ga.size, group < ga.groups ? ga.size : 0};
 #pragma unroll
-                for (int k = 0; k < W / 4; ++k) {
-                    const Vec<float> x = bias_row.vec(vec * (W / 4) + k);
+            for (int k = 0; k < W / 4; ++k) {
+                const Vec<float> x = bias_row.vec(vec * (W / 4) + k);
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) b[k * 4 + w] = x.at(w);
-                }
+                for (int w = 0; w < 4; ++w) b[k * 4 + w] = x.at(w);
             }
 #pragma unroll
             for (int w = 0; w < W; ++w) {
                 const float z = r.at(w);
-                // (a logistic score this way keeps the absolute error below, not 1 - s)
-                const float s = softmax ? exp_plain(z - m) * inv : __builtin_amdgcn_rcpf(1.0f + exp_plain(-z));
-                const float key = s + b[w];
+                const float key = score(z) + b[w];
                 y[w] = z > -kInf && key > -kInf ? key : -kInf;
             }
         } else {
@@ -227,7 +230,16 @@ __global__ void __launch_bounds__(256, K == 8 ? 4 : 1) k_route_groups(GroupArgs 
         }
     };
     // the vectors' largest keys, and the group's two
-    if constexpr (SCORES) {
+    if constexpr (KEYS == kSums) {
+        f1 = -kInf;
+#pragma unroll
+        for (int v = 0; v < NV * W; ++v) {
+            const float x = raw[v / W].at(v % W), z = x > -kInf ? x : -kInf;  // (NaN too)
+            f2 = __builtin_fmaxf(f2, __builtin_fminf(f1, z));
+            f1 = __builtin_fmaxf(f1, z);
+        }
+    }
+    if constexpr (BIASED) {
         f1 = -kInf;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -249,14 +261,28 @@ __global__ void __launch_bounds__(256, K == 8 ? 4 : 1) k_route_groups(GroupArgs 
     bool open = false, on;
     {
         lanes_two(f1, f2, Q);
-        float best = f1, slack = 0.0f;
-        if (SCORES) {
-            if (ga.top == 2 && f2 > -kInf) best = f1 + f2;
-            // (twice the errors of the keys and of their sum)
-            slack = (2.0f * err + __builtin_fabsf(f1) + (f2 > -kInf ? __builtin_fabsf(f2) : 0.0f) + __builtin_fabsf(best)) * 0x1p-23f;
-        }
+        const bool two = SCORES && ga.top == 2 && f2 > -kInf;
+        const float k1 = KEYS == kSums && f1 > -kInf ? score(f1) : f1, k2 = KEYS == kSums && two ? score(f2) : f2;
+        const float best = two ? k1 + k2 : k1;
+        // (twice the errors of the keys and of their sum)
+        const float slack = (2.0f * err + __builtin_fabsf(k1) + (f2 > -kInf ? __builtin_fabsf(k2) : 0.0f) + __builtin_fabsf(best)) * 0x1p-23f;
         on = groups_before(ga.groups, ga.q_shift, best, g, lane0) < ga.keep && f1 > -kInf;
-        if (SCORES) {
+        if constexpr (KEYS == kSums) {
+            // Groups of the same two logits as the last one kept are equal, whatever the
+            // error: others must be clearly above those left out and those equal ones, and
+            // the equal ones clearly above the others left out.
+            const float last = -lanes_max(on ? -best : -kInf, lanes);
+            const float l1 = lanes_max(on && best == last ? f1 : -kInf, lanes);
+            const float l2 = lanes_max(on && best == last && f1 == l1 ? f2 : -kInf, lanes);
+            const bool same = f1 == l1 && f2 == l2;
+            const float low = -lanes_max(on && !same ? slack - best : -kInf, lanes);
+            const float low_same = -lanes_max(on && same ? slack - best : -kInf, lanes);
+            const float high = lanes_max(!on && !same && f1 > -kInf ? best + slack : -kInf, lanes);
+            const float high_same = lanes_max(!on && same && f1 > -kInf ? best + slack : -kInf, lanes);
+            open = (high > -kInf && !(low > high && low_same > high)) || (high_same > -kInf && !(low > high_same));
+            open = open || inv != inv || best != best;
+        }
+        if constexpr (BIASED) {
             const float low = -lanes_max(on ? slack - best : -kInf, lanes);
             const float high = lanes_max(!on && f1 > -kInf ? best + slack : -kInf, lanes);
             open = high > -kInf && !(low > high);
@@ -272,7 +298,7 @@ __global__ void __launch_bounds__(256, K == 8 ? 4 : 1) k_route_groups(GroupArgs 
     lanes_top<Key, K>(first, lanes);
     // the elements of the K vectors that lead, one or a few in each lane c < M
     Word x[S * W], top[K];
-    float cand[SCORES ? S * W : 1], most[S];
+    float cand[BIASED ? S * W : 1], most[S];
 #pragma unroll
     for (int s = 0; s < S; ++s) {
         Word mine = Word(0);
@@ -287,7 +313,7 @@ __global__ void __launch_bounds__(256, K == 8 ? 4 : 1) k_route_groups(GroupArgs 
 #pragma unroll
         for (int w = 0; w < W; ++w) {
             x[s * W + w] = Word(0);
-            if constexpr (SCORES) cand[s * W + w] = -kInf;
+            if constexpr (BIASED) cand[s * W + w] = -kInf;
         }
         if (ok) {
             float y[W];
@@ -295,7 +321,7 @@ __global__ void __launch_bounds__(256, K == 8 ? 4 : 1) k_route_groups(GroupArgs 
             keys_of(r.vec(v), vg, v, y);
 #pragma unroll
             for (int w = 0; w < W; ++w) {
-                if constexpr (SCORES) cand[s * W + w] = y[w];
+                if constexpr (BIASED) cand[s * W + w] = y[w];
                 x[s * W + w] = Key::make(y[w], kIndexMask ^ (uint32_t)(vg * ga.size + v * W + w));
             }
         }
@@ -310,9 +336,36 @@ __global__ void __launch_bounds__(256, K == 8 ? 4 : 1) k_route_groups(GroupArgs 
         for (int j = 0; j < M; ++j) mine = c == j ? top[s * M + j] : mine;
         id[s] = c < M && s * M + c < a.k && Key::available(mine) ? (int32_t)Key::index(mine) : -1;
     }
-    if constexpr (SCORES) {
-        // is the order beyond doubt?  Two keys further apart than `slack` are in order.
-        auto slack = [&](float key) { return (err + 2.0f * __builtin_fabsf(key)) * 0x1p-23f; };
+    // is the order beyond doubt?  Two keys further apart than `slack` are in order.
+    auto slack = [&](float key) { return (err + 2.0f * __builtin_fabsf(key)) * 0x1p-23f; };
+    if constexpr (KEYS == kSums) {
+        // Equal logits have equal scores.  Different ones that are next to each other
+        // among the chosen, and the largest one below them, must differ clearly.
+        float before = 0.0f, s_before = 0.0f, edge = 0.0f, z_last = -kInf;
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            if (j >= a.k || !Key::available(top[j])) continue;
+            const float z = Key::value(top[j]), s = score(z);
+            open = open || (j > 0 && z != before && !(s_before - s > slack(s_before) && s_before - s > slack(s)));
+            before = z;
+            s_before = s;
+            if (j == a.k - 1) {
+                edge = s - slack(s);
+                z_last = z;
+            }
+        }
+        const float z_k = lanes_max(c < M ? z_last : -kInf, lanes);
+        edge = lanes_max(c < M && z_last > -kInf ? edge : -kInf, lanes);
+        float below = -kInf;
+#pragma unroll
+        for (int v = 0; v < NV * W; ++v) {
+            const float x = raw[v / W].at(v % W);
+            below = on && x < z_k ? __builtin_fmaxf(below, x) : below;
+        }
+        below = lanes_max(below, lanes);
+        open = open || (below > -kInf && !(score(below) < edge));
+    }
+    if constexpr (BIASED) {
         float edge = -kInf;  // a key below it is not among the k largest
 #pragma unroll
         for (int j = 0; j < K; ++j) {
@@ -336,6 +389,8 @@ __global__ void __launch_bounds__(256, K == 8 ? 4 : 1) k_route_groups(GroupArgs 
         over = lanes_add(over, lanes);
         more = lanes_add(more, lanes);
         open = open || (edge > -kInf && (over != (float)a.k || more != 0.0f)) || edge != edge;
+    }
+    if constexpr (SCORES) {
         // The tokens in doubt, one at a time by the whole wave, in 64 bits: loops of
         // little code, an element at a time from memory, a group in as many lanes as
         // fit 64 (a wave that took them by their own lanes took 15 us, and kept the
@@ -437,9 +492,8 @@ __global__ void __launch_bounds__(256, K == 8 ? 4 : 1) k_route_groups(GroupArgs 
     }
 }
 
-// Lanes of a group and a token: as few as hold a group in 8 vectors a lane, keys
-// other than the logits in 32 elements (at least 8 a token, for the second
-// selection).
+// Lanes of a group and a token: as few as hold a group in 8 vectors a lane, where
+// scores are keys in 32 elements (at least 8 a token, for the second selection).
 constexpr int kScoresALane = 32;
 template <class T>
 int choose_groups(GroupArgs a, hipStream_t stream) {
@@ -452,13 +506,13 @@ int choose_groups(GroupArgs a, hipStream_t stream) {
     }
     a.q_shift = 0;
     const int vecs = (a.size + W - 1) / W;
-    const bool scores = a.r.bias || a.top > 1;
-    const int most = scores ? kScoresALane / W : 8;  // (E <= 1024: 64 lanes never need more)
+    const int keys = a.r.bias ? kBiased : a.top > 1 ? kSums : kLogits;
+    const int most = keys != kLogits ? kScoresALane / W : 8;  // (E <= 1024: 64 lanes never need more)
     auto each = [&] { return (vecs + (1 << a.q_shift) - 1) >> a.q_shift; };
     while ((each() > most && (groups << a.q_shift) < kWave) || (groups << a.q_shift) < 8) ++a.q_shift;
     a.lane_shift += a.q_shift;
     const int64_t items = a.r.T * a.r.L, per = 256 >> a.lane_shift;
-    const size_t lds = scores ? 4 * (size_t)a.r.E * sizeof(uint64_t) : 0;
+    const size_t lds = keys != kLogits ? 4 * (size_t)a.r.E * sizeof(uint64_t) : 0;
     auto go = [&](auto kern) {
         hipLaunchKernelGGL(kern, grid_of((items + per - 1) / per), dim3(256), lds, stream, a);
         return hipGetLastError() == hipSuccess ? ROUTEPACK_OK : ROUTEPACK_E_DEVICE;
@@ -468,17 +522,18 @@ int choose_groups(GroupArgs a, hipStream_t stream) {
         // (8 choices at most, whole vectors and no idle lanes: without the checks of
         // every vector)
         const bool whole = a.r.k <= 8 && a.size == (N * W) << a.q_shift && a.groups == groups;
-        auto by_keys = [&](auto scores_) {
-            constexpr bool SCORES = decltype(scores_)::value != 0;
-            if (whole) return go(k_route_groups<T, N, 8, SCORES, true>);
-            if (a.r.k <= 8) return go(k_route_groups<T, N, 8, SCORES, false>);
-            if (a.r.k <= 16) return go(k_route_groups<T, N, 16, SCORES, false>);
-            return go(k_route_groups<T, N, 32, SCORES, false>);
+        auto by_keys = [&](auto keys_) {
+            constexpr int KEYS = decltype(keys_)::value;
+            if (whole) return go(k_route_groups<T, N, 8, KEYS, true>);
+            if (a.r.k <= 8) return go(k_route_groups<T, N, 8, KEYS, false>);
+            if (a.r.k <= 16) return go(k_route_groups<T, N, 16, KEYS, false>);
+            return go(k_route_groups<T, N, 32, KEYS, false>);
         };
         if constexpr (N * W <= kScoresALane) {
-            if (scores) return by_keys(Int<1>());
+            if (keys == kBiased) return by_keys(Int<kBiased>());
+            if (keys == kSums) return by_keys(Int<kSums>());
         }
-        return by_keys(Int<0>());
+        return by_keys(Int<kLogits>());
     };
     if (each() <= 1) return by_k(Int<1>());
     if (each() <= 2) return by_k(Int<2>());

@@ -175,6 +175,28 @@ def test_scores_close_to_each_other_in_groups():
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_sums_of_scores_that_meet(dtype):
+    """Different logits whose scores, or sums of them, are equal in 64 bits go by
+    the lowest index; equal pairs of logits in several groups."""
+    import torch
+    import paper_2608_12146_amd as rp
+    sets = {"sigmoid": [-100.0, -40.0, -3.0, 0.0, 0.25, 17.0, 20.0, 25.0, 30.0, 40.0, 45.0, 100.0],
+            "softmax": [0.0, -0.5, -1.0, -50.0, -100.0, -700.0, -800.0, -1000.0]}
+    for E, k, groups, keep in ((16, 3, 8, 3), (64, 8, 8, 3), (352, 8, 16, 12), (512, 12, 8, 2), (60, 20, 4, 2)):
+        for score, values in sets.items():
+            g = torch.Generator().manual_seed(E)
+            z = torch.as_tensor(values)[torch.randint(0, len(values), (65, 1, E), generator=g)]
+            few = torch.as_tensor(values)[torch.randint(0, 2, (65, 1, E), generator=g) * (len(values) - 1)]
+            z[32:] = torch.where(torch.rand((33, 1, E), generator=g) < 0.9, few[32:], z[32:])
+            z = z.to(_type(dtype)).cuda()
+            _log((dtype, E, k, groups, keep, score))
+            ids, _ = rp.route_tokens(_problem(1, E, k), z, score=score, groups=groups, keep=keep, group_top=2)
+            want = X.choose_groups(_host(z), k, groups, keep, 2, None, score)
+            assert np.array_equal(_host(ids), want), (dtype, E, score)
+
+
+@gpu
 def test_grouped_gates_have_gradients():
     import torch
     import paper_2608_12146_amd as rp
