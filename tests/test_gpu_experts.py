@@ -476,6 +476,30 @@ def test_product_gradients_by_wide_tiles(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+def test_product_gradients_keep_to_their_slots(dtype):
+    """NaN in rows of no slot, or of another one, stays there; one row of dy for
+    all of them (stride 0)."""
+    import torch
+    import paper_2608_12146_amd as rp
+    N, C, R = 72, 300, 400
+    x, w = _random_mx(1, (R,), C), _random_mx(2, (4, N), C)
+    dy = _floats(3, (R, N), dtype)
+    off = torch.tensor([11, 80, 150, 150, 290], device="cuda")
+    clean = rp.expert_product_backward(dy, x, w, off)
+    dy[:11] = dy[290:] = np.nan
+    for got, want in zip(rp.expert_product_backward(dy, x, w, off), clean):
+        assert torch.equal(got, want)
+    dy[80] = np.nan  # the second slot's first row
+    dx, dw = rp.expert_product_backward(dy, x, w, off)
+    assert dx[80].isnan().all() and torch.equal(dx[:80], clean[0][:80]) and torch.equal(dx[81:], clean[0][81:])
+    assert dw[1].isnan().all() and all(torch.equal(dw[s], clean[1][s]) for s in (0, 2, 3))
+    one = _floats(4, (1, N), dtype).expand(R, N)
+    for got, want in zip(rp.expert_product_backward(one, x, w, off), rp.expert_product_backward(one.contiguous(), x, w, off)):
+        assert torch.equal(got, want)
+
+
+@gpu
 def test_product_gradients_of_far_rows():
     """Rows of dy further apart than 32 bits of bytes reach over a tile."""
     import torch
