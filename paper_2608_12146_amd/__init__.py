@@ -816,9 +816,10 @@ def order_tokens(prob: Problem, ids, *, slots=None):
     offsets = torch.empty((*lead, E + 1), dtype=torch.int64, device=at)
     places = torch.empty(shape, dtype=torch.int32, device=at)
     size = lib.routepack_order_workspace(prob.ref, shape[0])
-    work = torch.empty(size, dtype=torch.uint8, device=at).data_ptr() if size > 0 else None
+    # (kept until the kernels stand in the stream: only then may another thread's call have it)
+    work = torch.empty(size, dtype=torch.uint8, device=at) if size > 0 else None
     call.run(lib.routepack_order_tokens, prob.ref, C.byref(x), s, rows.data_ptr(), offsets.data_ptr(),
-             places.data_ptr(), work, size)
+             places.data_ptr(), None if work is None else work.data_ptr(), size)
     return Order(rows, offsets, places)
 
 

@@ -214,3 +214,88 @@ def test_oracle_blocks():
     # the packed order: the even column in the low half, two's exponent 2 less
     codes, scales = X.quantize(np.array([[1.0, -2.0]]))
     assert codes[0, 0] == (4 + 16 * 14) and scales[0, 0] == 126
+
+
+# -- the binding without a GPU --------------------------------------------------
+
+class _FakeTensor:
+    """As much of a tensor on a GPU as the binding looks at; addresses are its own."""
+
+    next_address = 1 << 20
+    is_cuda, requires_grad = True, False
+
+    def __init__(self, shape, dtype, device="gpu"):
+        self.shape, self.dtype, self.device = tuple(shape), dtype, device
+        self.address = _FakeTensor.next_address
+        _FakeTensor.next_address += 1 << 20
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return int(np.prod(self.shape))
+
+    def stride(self):
+        return tuple(int(np.prod(self.shape[i + 1:])) for i in range(len(self.shape)))
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return self.address
+
+
+def _without_gpu(monkeypatch, during):
+    """Lets the binding run on _FakeTensors: `during` gets a call's name, its
+    arguments and the live tensors' addresses, in place of the library."""
+    import types
+    import weakref
+
+    import torch
+
+    import paper_2608_12146_amd as rp
+    live = weakref.WeakValueDictionary()
+
+    def tensor(shape, dtype, device="gpu"):
+        x = _FakeTensor((shape,) if isinstance(shape, int) else shape, dtype, device)
+        live[x.address] = x
+        return x
+    names = ("uint8", "int16", "int32", "int64", "float32", "bfloat16", "float16", "is_grad_enabled")
+    fake = types.SimpleNamespace(Tensor=_FakeTensor, empty=tensor, **{n: getattr(torch, n) for n in names})
+    real = rp.load_library()
+
+    class Library:
+        routepack_order_workspace = real.routepack_order_workspace
+
+        def __getattr__(self, name):
+            def call(*args):
+                during(name, args, dict(live))
+                return 0
+            return call
+
+    def run(self, f, *args):
+        assert f(*args, None) == 0
+    floats = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    ints = {torch.uint8: 3, torch.int16: 4, torch.int32: 5, torch.int64: 6}
+    monkeypatch.setattr(rp, "_router", lambda: (Library(), fake, floats, ints))
+    monkeypatch.setattr(rp._Call, "run", run)
+    return tensor
+
+
+def test_workspaces_live_through_the_call(monkeypatch):
+    """Memory of the binding's own goes back to the allocator after the call's
+    kernels stand in the stream: another thread's call on that stream could else
+    be given it while they are being launched."""
+    import torch
+
+    import paper_2608_12146_amd as rp
+    seen = []
+
+    def during(name, args, live):
+        # rows, offsets, places and the workspace of routepack_order_tokens
+        seen.append((name, args[7], [a in live for a in args[3:7]]))
+    tensor = _without_gpu(monkeypatch, during)
+    rp.order_tokens(_problem(L=1, E=256, k=8), tensor((9000, 1, 8), torch.int32))
+    (name, size, alive), = seen
+    assert name == "routepack_order_tokens" and size > 0
+    assert alive == [True] * 4

@@ -944,3 +944,32 @@ def test_binding_refusals():
     for n, kw in enumerate((dict(groups=3, keep=1), dict(groups=2, keep=3), dict(groups=8, keep=1), dict(groups=2, keep=1, group_top=3))):
         with pytest.raises(rp.RoutepackError):
             rp.route_tokens(prob, z, **kw)
+
+
+@gpu
+def test_two_threads_on_one_stream():
+    """Orders that need a workspace, from two threads at once on the same stream:
+    each call's is its own until its kernels stand in the stream."""
+    import threading
+    import torch
+    import paper_2608_12146_amd as rp
+    T, E, k = 3000, 64, 4
+    prob = _problem(1, E, k)
+    ids = [torch.randint(0, E, (T, k), generator=torch.Generator().manual_seed(s), dtype=torch.int32).cuda() for s in (1, 2)]
+    want = [rp.order_tokens(prob, x) for x in ids]
+    torch.cuda.synchronize()
+    got = [[], []]
+
+    def work(i):
+        for _ in range(40):
+            got[i].append(rp.order_tokens(prob, ids[i]))
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for w, results in zip(want, got):
+        assert len(results) == 40
+        for r in results:
+            assert torch.equal(r.rows, w.rows) and torch.equal(r.offsets, w.offsets) and torch.equal(r.places, w.places)
