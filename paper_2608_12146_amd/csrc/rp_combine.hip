@@ -149,6 +149,8 @@ __global__ void __launch_bounds__(256) k_spread(CombineArgs a) {
     constexpr int W = Vec<T>::W;
     __shared__ float part[4][K];
     if (group_index() >= a.token_groups) {  // rows of no pair: zeros
+        // (without dy these are the groups that fill the grid's last row: there may be no `rows` either)
+        if (!a.dy) return;
         const int lane = threadIdx.x & 63;
         const int64_t r0 = (group_index() - a.token_groups) * 256 + (threadIdx.x & ~63);
         const bool mine = r0 + lane < a.order.n_rows && a.order.pair_of_row(r0 + lane) < 0;

@@ -973,3 +973,35 @@ def test_two_threads_on_one_stream():
         assert len(results) == 40
         for r in results:
             assert torch.equal(r.rows, w.rows) and torch.equal(r.offsets, w.offsets) and torch.equal(r.places, w.places)
+
+
+@gpu
+def test_gradients_of_the_gates_of_many_tokens():
+    """More workgroups than one dimension of the grid has: those that fill its last
+    row have no token, and where dy is not asked for no row to clear either."""
+    import torch
+    import paper_2608_12146_amd as rp
+    T, C = (1 << 22) + 1, 2048  # (a workgroup a token)
+    y, d = _floats(1, (1, C), "bf16"), _floats(2, (1, C), "bf16")
+    dout = d.expand(T, C)
+    places = torch.zeros((1, 1), dtype=torch.int32, device="cuda").expand(T, 1)
+    mag = 2 * (C + 9) * U * np.abs(_host(y) * _host(d)).sum(axis=1, keepdims=True)
+    want = (_host(y) * _host(d)).sum(axis=1, keepdims=True)
+    for row in (0, -1):  # the one row is the first pair's, or no pair's
+        rows = torch.full((1,), row, dtype=torch.int32, device="cuda")
+        order = rp.Order(rows, None, places)
+        _log(("gates alone", T, C, row))
+        none, dgates = rp.combine_backward(dout, y, order, need=(False, True))
+        assert none is None and dgates.shape == (T, 1)
+        _near(dgates[:1], want, mag, "dgates")
+        assert bool((dgates == dgates[0]).all())
+        _log("with rows, but without dy")
+        again = torch.zeros_like(dgates)
+        rc = rp.load_library().routepack_combine_backward(
+            rp._MATRIX(dout.data_ptr(), 1, T, C, 0), rp._MATRIX(y.data_ptr(), 1, 1, C, C), rows.data_ptr(),
+            rp._IDS(places.data_ptr(), 5, T, 0, 0), 1, None, 0, None, again.data_ptr(),
+            torch.cuda.current_stream().cuda_stream)
+        assert rc == 0 and torch.equal(again, dgates)
+        _log("both")
+        dy, again = rp.combine_backward(dout, y, order)
+        assert torch.equal(again, dgates) and torch.equal(dy, d if row == 0 else torch.zeros_like(d))
