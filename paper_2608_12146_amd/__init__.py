@@ -389,14 +389,16 @@ SCORES = {"softmax": 0, "sigmoid": 1}
 
 
 _ROUTER = None
+_FORWARD = None  # torch.autograd.forward_ad
 
 
 def _router():
     """(the library, torch, types of logits, types of ids), looked up once:
     the smallest calls take a few microseconds."""
-    global _ROUTER
+    global _ROUTER, _FORWARD
     if _ROUTER is None:
         lib, torch = load_library(), _torch()
+        _FORWARD = torch.autograd.forward_ad
         _ROUTER = (lib, torch, {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2},
                    {torch.uint8: 3, torch.int16: 4, torch.int32: 5, torch.int64: 6})
     return _ROUTER
@@ -430,6 +432,9 @@ class _Call:
             raise ValueError(f"{self.fn}: {name} has type {x.dtype}")
         if shape is not None and tuple(x.shape) != tuple(shape):
             raise ValueError(f"{self.fn}: {name} has shape {tuple(x.shape)}, expected {tuple(shape)}")
+        # (outside of forward mode the level is below 0; where torch hides it, each tensor is asked)
+        if _FORWARD is not None and getattr(_FORWARD, "_current_level", 0) >= 0 and _FORWARD.unpack_dual(x).tangent is not None:
+            raise NotImplementedError(f"{self.fn}: {name} has a tangent; gradients are formed in reverse mode alone")
         return x
 
     def dense(self, name, x, dtypes, shape):

@@ -1005,3 +1005,39 @@ def test_gradients_of_the_gates_of_many_tokens():
         _log("both")
         dy, again = rp.combine_backward(dout, y, order)
         assert torch.equal(again, dgates) and torch.equal(dy, d if row == 0 else torch.zeros_like(d))
+
+
+@gpu
+def test_forward_mode_is_refused():
+    """A tensor with a tangent: no call may drop it without a word."""
+    import torch
+    import torch.autograd.forward_ad as fw
+    import paper_2608_12146_amd as rp
+    prob = _problem(1, 8, 2)
+    z, x = _floats(1, (4, 8), "fp32"), _floats(2, (4, 64), "bf16")
+    ids, gates = rp.route_tokens(prob, z, groups=2, keep=1)
+    order = rp.order_tokens(prob, ids)
+    rows, w, y = _floats(3, (8, 64), "bf16"), _floats(4, (8, 16, 64), "bf16"), _floats(5, (8, 16), "fp32")
+    counts, off = torch.ones((1, 1, 8), dtype=torch.int32, device="cuda"), torch.tensor([0, 4], device="cuda")
+    qx, qw = rp.quantize_mx(rows), rp.quantize_mx(w)
+    calls = {
+        "gates": (z, lambda v: rp.route_tokens(prob, v)), "replayed": (z, lambda v: rp.route_tokens(prob, v, ids=ids)),
+        "grouped": (z, lambda v: rp.route_tokens(prob, v, groups=2, keep=1)),
+        "loss": (z, lambda v: rp.balance_loss(prob, v, counts, off)),
+        "dlogits": (gates, lambda v: rp.route_backward(prob, z, ids=ids, dgates=v)),
+        "quantize": (x, lambda v: rp.quantize_mx(v)), "gathered": (x, lambda v: rp.quantize_mx(v, order=order)),
+        "product x": (rows, lambda v: rp.expert_product(v, qw, order)), "product w": (w, lambda v: rp.expert_product(qx, v, order)),
+        "dy": (y, lambda v: rp.expert_product_backward(v, qx, qw, order)),
+        "sum y": (y, lambda v: rp.combine_tokens(v, order, gates)), "sum gates": (gates, lambda v: rp.combine_tokens(y, order, v)),
+        "dout": (y[:4], lambda v: rp.combine_backward(v, y, order, gates)),
+    }
+    for name, (v, f) in calls.items():
+        for grad in (False, True):
+            with fw.dual_level():
+                dual = fw.make_dual(v.clone().requires_grad_(grad), torch.ones_like(v))
+                with pytest.raises(NotImplementedError):
+                    f(dual)
+                    _log(f"{name} was not refused")
+            f(v.clone().requires_grad_(grad))
+    with fw.dual_level():  # (tensors without a tangent are as anywhere)
+        assert torch.equal(rp.combine_tokens(y, order, gates), rp.combine_tokens(y, order, gates))
