@@ -710,12 +710,15 @@ class Mx:
            even column in the low half; sign, two bits of exponent, one of mantissa
     scales uint8 [...][rows][4 n]: the blocks' exponents plus 127, 255 for NaN
 
-    Columns behind the last are zero codes with scale 0."""
+    Columns behind the last are zero codes with scale 0.  What quantize_mx made
+    of a tensor that requires a gradient leads autograd back to it (`link`, a
+    tensor of this shape whose values mean nothing); other matrices, runs of its
+    rows too, are constants."""
 
-    __slots__ = ("codes", "scales", "columns")
+    __slots__ = ("codes", "scales", "columns", "link")
 
-    def __init__(self, codes, scales, columns):
-        self.codes, self.scales, self.columns = codes, scales, int(columns)
+    def __init__(self, codes, scales, columns, link=None):
+        self.codes, self.scales, self.columns, self.link = codes, scales, int(columns), link
 
     @property
     def shape(self):
@@ -832,10 +835,18 @@ def quantize_mx(x, *, order=None):
     """x [rows][columns] (or [n][rows][columns], contiguous) fp32, bf16 or fp16,
     any stride over rows, as an Mx.  With `order` the result's rows are the
     order's pairs: row r holds the token of pair rows[r] (zeros behind the
-    last).  The result carries no gradient; expert_product passes one through."""
+    last).
+
+    Where x requires a gradient, autograd records the quantization as if it were
+    the identity: expert_product and dequantize_mx pass x's gradient back through
+    the result, with `order` (of at most 32 choices) as the sum of a token's
+    rows, which is combine_tokens'."""
     lib, torch, floats, _ = _router()
     call = _ExpertCall("routepack_quantize_mx", torch)
     call.tensor("x", x, floats)
+    if x.requires_grad and torch.is_grad_enabled():
+        codes, scales, link = _expert_functions()[2].apply(x, order)
+        return Mx(codes, scales, x.shape[-1], link)
     lead = x.shape[:-1]
     if x.dim() == 3 and order is None and x.is_contiguous():
         x = x.view(-1, x.shape[-1]) if x.numel() else x.reshape(lead[0] * lead[1], x.shape[-1])
@@ -863,6 +874,8 @@ def dequantize_mx(q: Mx, dtype=None):
     dtype = torch.bfloat16 if dtype is None else dtype
     if dtype not in floats:
         raise ValueError(f"{call.fn}: dtype is {dtype}")
+    if isinstance(q, Mx) and q.link is not None and torch.is_grad_enabled():
+        return _expert_functions()[3].apply(q.link, q, dtype)
     shape, m = call.mx("q", q, 3 if isinstance(q, Mx) and q.codes.dim() == 3 else 2)
     cols = q.columns
     rows = shape[0] if len(shape) == 2 else shape[0] * shape[1]
@@ -878,9 +891,11 @@ def expert_product(x, w, order, *, dtype=None):
     x: Mx [P][C]; w: Mx [E][N][C]; order: an Order, or its offsets (int64
     [E + 1]).  Either may be a tensor (fp32, bf16, fp16) instead, which the call
     quantizes.  y has type `dtype`, by default x's type if that is a tensor, else
-    bf16.  Where such tensors require a gradient, autograd records the product;
-    the gradient passes the quantization as if it were the identity, and is
-    expert_product_backward's."""
+    bf16.  Where such tensors, or those that an Mx was quantized from, require a
+    gradient, autograd records the product; the gradient passes the quantization
+    as if it were the identity, and is expert_product_backward's: formed in y's
+    type, and only then brought to the tensor's (a gradient in fp32 of fp32
+    weights asks for dtype=torch.float32)."""
     lib, torch, floats, _ = _router()
     call = _ExpertCall("routepack_expert_product", torch)
     x_is, w_is = isinstance(x, torch.Tensor), isinstance(w, torch.Tensor)
@@ -888,9 +903,12 @@ def expert_product(x, w, order, *, dtype=None):
         dtype = x.dtype if x_is else torch.bfloat16
     if dtype not in floats:
         raise ValueError(f"{call.fn}: dtype is {dtype}")
-    if x_is or w_is:
-        if (x_is and x.requires_grad or w_is and w.requires_grad) and torch.is_grad_enabled():
-            return _expert_functions()[0].apply(x, w, order, dtype)
+    # what the gradients go to
+    x_to, w_to = x if x_is else getattr(x, "link", None), w if w_is else getattr(w, "link", None)
+    if x_to is not None or w_to is not None:
+        if ((x_to is not None and x_to.requires_grad or w_to is not None and w_to.requires_grad)
+                and torch.is_grad_enabled()):
+            return _expert_functions()[0].apply(x_to, w_to, None if x_is else x, None if w_is else w, order, dtype)
         x, w = quantize_mx(x) if x_is else x, quantize_mx(w) if w_is else w
     got, xm = call.mx("x", x, 2)
     shape, wm = call.mx("w", w, 3)
@@ -990,7 +1008,7 @@ _EXPERT_FUNCTIONS = None
 
 
 def _expert_functions():
-    """(product, sum) as functions that autograd records."""
+    """(product, sum, quantization, values) as functions that autograd records."""
     global _EXPERT_FUNCTIONS
     if _EXPERT_FUNCTIONS is not None:
         return _EXPERT_FUNCTIONS
@@ -999,16 +1017,15 @@ def _expert_functions():
 
     class Product(torch.autograd.Function):
         @staticmethod
-        def forward(ctx, x, w, order, dtype):
-            qx = quantize_mx(x) if isinstance(x, torch.Tensor) else x
-            qw = quantize_mx(w) if isinstance(w, torch.Tensor) else w
+        def forward(ctx, x_to, w_to, x, w, order, dtype):
+            qx, qw = quantize_mx(x_to) if x is None else x, quantize_mx(w_to) if w is None else w
             off = order.offsets if isinstance(order, Order) else order
             # (the packed matrices are kept, a quarter of the tensors in bf16)
             need = ctx.needs_input_grad
             none = qx.codes.new_empty(0)
             ctx.save_for_backward(qx.codes if need[1] else none, qx.scales if need[1] else none,
                                   qw.codes if need[0] else none, qw.scales if need[0] else none, off)
-            ctx.sizes = (*qw.shape[:2], qw.columns), [t.dtype if isinstance(t, torch.Tensor) else None for t in (x, w)]
+            ctx.sizes = (*qw.shape[:2], qw.columns), [None if t is None else t.dtype for t in (x_to, w_to)]
             return expert_product(qx, qw, off, dtype=dtype)
 
         @staticmethod
@@ -1021,7 +1038,7 @@ def _expert_functions():
                 dy = dy.contiguous()
             dx, dw = expert_product_backward(dy, Mx(xc, xs, sizes[2]) if need[1] else None,
                                              Mx(wc, ws, sizes[2]) if need[0] else sizes, off, need=need)
-            return None if dx is None else dx.to(types[0]), None if dw is None else dw.to(types[1]), None, None
+            return (None if dx is None else dx.to(types[0]), None if dw is None else dw.to(types[1])) + (None,) * 4
 
     class Sum(torch.autograd.Function):
         @staticmethod
@@ -1039,5 +1056,42 @@ def _expert_functions():
                                           need=tuple(ctx.needs_input_grad[:2]))
             return dy, dgates, None
 
-    _EXPERT_FUNCTIONS = Product, Sum
+    class Quantize(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, order):
+            q = quantize_mx(x, order=order)
+            if order is not None and order.places.shape[1] > 32:  # (combine_tokens' limit)
+                raise ValueError(f"routepack_quantize_mx: x requires a gradient, and the order has {order.places.shape[1]} "
+                                 "choices, more than 32")
+            ctx.gathered = order is not None
+            if ctx.gathered:
+                ctx.save_for_backward(order.places)
+            ctx.mark_non_differentiable(q.codes, q.scales)
+            ctx.set_materialize_grads(False)
+            # (one element for all: only its shape, type and place in the graph count)
+            link = torch.empty_strided(q.shape, (0,) * len(q.shape), dtype=x.dtype, device=x.device)
+            return q.codes, q.scales, link
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, _, __, dlink):
+            if dlink is None or not ctx.gathered:
+                return dlink, None
+            (places,) = ctx.saved_tensors
+            if dlink.stride(1) != 1:
+                dlink = dlink.contiguous()
+            return combine_tokens(dlink, Order(None, None, places)), None
+
+    class Values(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, link, q, dtype):
+            ctx.type = link.dtype
+            return dequantize_mx(q, dtype)
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, dx):
+            return dx.to(ctx.type), None, None
+
+    _EXPERT_FUNCTIONS = Product, Sum, Quantize, Values
     return _EXPERT_FUNCTIONS

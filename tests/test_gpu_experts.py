@@ -1041,3 +1041,105 @@ def test_forward_mode_is_refused():
             f(v.clone().requires_grad_(grad))
     with fw.dual_level():  # (tensors without a tangent are as anywhere)
         assert torch.equal(rp.combine_tokens(y, order, gates), rp.combine_tokens(y, order, gates))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+def test_gradients_through_the_quantization(dtype):
+    """A matrix quantized (and gathered) outside of the product passes the gradient
+    on to what it was made of: a token's is the sum of its rows', 2 k u of their
+    magnitudes and half a step of the type."""
+    import torch
+    import paper_2608_12146_amd as rp
+    T, E, k, C, N = 70, 9, 4, 160, 96
+    ids = torch.randint(-1, E, (T, k), generator=torch.Generator().manual_seed(1)).cuda()
+    order = rp.order_tokens(_problem(1, E, k), ids)
+    x, w = _floats(2, (T, C), dtype).requires_grad_(), _floats(3, (E, N, C), dtype, scale=0.1).requires_grad_()
+    dy = _floats(4, (T * k, N), dtype)
+    q, qw = rp.quantize_mx(x, order=order), rp.quantize_mx(w)
+    y = rp.expert_product(q, qw, order, dtype=_type(dtype))
+    gx, gw = torch.autograd.grad(y, (x, w), dy, retain_graph=True)
+    with torch.no_grad():
+        plain, plain_w = rp.quantize_mx(x, order=order), rp.quantize_mx(w)
+        assert plain.link is None and not rp.expert_product(q, qw, order).requires_grad
+        assert torch.equal(plain.codes, q.codes) and torch.equal(plain.scales, q.scales)
+        assert torch.equal(rp.expert_product(plain, plain_w, order, dtype=_type(dtype)), y)
+        dx, dw = rp.expert_product_backward(dy, plain, plain_w, order)
+    assert torch.equal(gw, dw)
+    want, mag = X.combine(_host(dx), _host(order.places), np.ones((T, k)))
+    _near(gx, want, 2 * k * U * mag, "x")
+    assert gx.dtype == x.dtype and gx.any()
+    # either alone, next to a constant or a tensor
+    for f, leaf, g in ((lambda: rp.expert_product(q, plain_w, order, dtype=_type(dtype)), x, gx),
+                       (lambda: rp.expert_product(plain, qw, order, dtype=_type(dtype)), w, gw),
+                       (lambda: rp.expert_product(q, w, order, dtype=_type(dtype)), x, gx),
+                       (lambda: rp.expert_product(q, w, order, dtype=_type(dtype)), w, gw)):
+        (got,) = torch.autograd.grad(f(), leaf, dy, retain_graph=True)
+        assert torch.equal(got, g)
+    # one quantization, two uses: gradients add up
+    (both,) = torch.autograd.grad((y, rp.expert_product(q, qw, order, dtype=_type(dtype))), w, (dy, dy),
+                                  retain_graph=True)
+    assert torch.equal(both, (gw.float() * 2).to(gw.dtype))
+    # its values (the quantization alone keeps nothing that a backward pass uses up)
+    (got,) = torch.autograd.grad(rp.dequantize_mx(qw, torch.float32), w, torch.ones((E, N, C), device="cuda"))
+    assert torch.equal(got, torch.ones_like(w))
+    (got,) = torch.autograd.grad(rp.dequantize_mx(q).sum(), x, retain_graph=True)
+    assert torch.equal(got, (order.places >= 0).sum(dim=1, keepdim=True).expand(T, C).to(got.dtype))
+    # a product in another type: its gradient comes in the leaf's
+    for t in ("fp32", "bf16"):
+        (got,) = torch.autograd.grad(rp.expert_product(q, qw, order, dtype=_type(t)).sum(), x, retain_graph=True)
+        assert got.dtype == x.dtype and got.any()
+
+
+@gpu
+def test_gradients_of_a_gather_of_many_choices_are_refused():
+    import torch
+    import paper_2608_12146_amd as rp
+    for k in (32, 33):
+        ids = torch.randint(0, 40, (5, k), generator=torch.Generator().manual_seed(k)).cuda()
+        order = rp.order_tokens(_problem(1, 40, k), ids)
+        x = _floats(1, (5, 64), "fp32").requires_grad_()
+        if k == 32:
+            (got,) = torch.autograd.grad(rp.dequantize_mx(rp.quantize_mx(x, order=order), torch.float32).sum(), x)
+            assert torch.equal(got, torch.full_like(got, 32.0))
+        else:
+            with pytest.raises(ValueError):
+                rp.quantize_mx(x, order=order)
+        with torch.no_grad():
+            assert rp.quantize_mx(x, order=order).shape == (5 * k, 64)
+
+
+@gpu
+def test_a_captured_backward_pass_of_a_gather():
+    """The gather, the product and their gradients recorded into a graph."""
+    import torch
+    import paper_2608_12146_amd as rp
+    E, k, T, C, N = 8, 2, 64, 128, 64
+    ids = torch.randint(0, E, (T, k), generator=torch.Generator().manual_seed(1)).cuda()
+    order = rp.order_tokens(_problem(1, E, k), ids)
+    x, w = _floats(2, (T, C), "bf16").requires_grad_(), _floats(3, (E, N, C), "bf16", scale=0.1).requires_grad_()
+    gates, dout = _floats(4, (T, k), "fp32").requires_grad_(), _floats(5, (T, N), "bf16")
+
+    def step():
+        y = rp.expert_product(rp.quantize_mx(x, order=order), rp.quantize_mx(w), order)
+        return torch.autograd.grad(rp.combine_tokens(y, order, gates), (x, w, gates), dout)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = step()
+    for n in range(4):
+        with torch.no_grad():
+            x.copy_(_floats(20 + n, (T, C), "bf16"))
+            dout.copy_(_floats(40 + n, (T, N), "bf16"))
+        for t in got:
+            t.detach().zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        leaves = [t.detach().clone().requires_grad_() for t in (x, w, gates)]
+        y = rp.expert_product(rp.quantize_mx(leaves[0], order=order), rp.quantize_mx(leaves[1]), order)
+        want = torch.autograd.grad(rp.combine_tokens(y, order, leaves[2]), leaves, dout)
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), n
