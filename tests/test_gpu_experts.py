@@ -1143,3 +1143,34 @@ def test_a_captured_backward_pass_of_a_gather():
         y = rp.expert_product(rp.quantize_mx(leaves[0], order=order), rp.quantize_mx(leaves[1]), order)
         want = torch.autograd.grad(rp.combine_tokens(y, order, leaves[2]), leaves, dout)
         assert all(torch.equal(a, b) for a, b in zip(got, want)), n
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp32", "fp16", "bf16"])
+def test_product_gradients_keep_every_bit(dtype):
+    """One value of dy a row, of full precision, by matrices of powers of two: each
+    output is one product, which fits the type, plus zeros.  A part of dy that was
+    left out would show.  By small tiles and by wide ones of dx and dw."""
+    import torch
+    import paper_2608_12146_amd as rp
+    # (2048 slots by 300 columns: dx and dw by wide tiles, one row a slot)
+    for slots, N, C in ((5, 20, 100), (3, 64, 128), (2048, 8, 300), (2048, 13, 257)):
+        g = torch.Generator().manual_seed(slots + N)
+        step = torch.finfo(_type(dtype)).eps
+        # mantissas 1 + an odd number of steps: the last bit is set
+        odd = 2 * torch.randint(0, int(0.5 / step), (slots,), generator=g) + 1
+        value = ((1.0 + odd.double() * step) * torch.where(torch.rand(slots, generator=g) < 0.5, 1.0, -1.0).double()).to(_type(dtype))
+        dy = torch.zeros((slots, N), dtype=_type(dtype))
+        dy[torch.arange(slots), torch.randint(0, N, (slots,), generator=g)] = value
+        # codes of 0.5, 1, 2 and 4 of either sign (and zeros behind the last column)
+        x, w = _random_mx(slots, (slots,), C, 4), _random_mx(slots + 1, (slots, N), C, 4)
+        powers = torch.tensor([1, 2, 4, 6, 9, 10, 12, 14], dtype=torch.uint8, device="cuda")
+        for q in (x, w):
+            column = 2 * torch.arange(q.codes.shape[-1], device="cuda")
+            low = powers[(q.codes & 7).long()] * (column < C).to(torch.uint8)
+            q.codes = low | (powers[(q.codes >> 4 & 7).long()] * (column + 1 < C).to(torch.uint8)) << 4
+        off = _offsets([1] * slots)
+        dx, dw = rp.expert_product_backward(dy.cuda(), x, w, off)
+        (wx, _), (ww, _) = X.product_backward(_host(dy), _values(x), _values(w), _host(off))
+        assert np.array_equal(wx, torch.as_tensor(wx).to(_type(dtype)).double().numpy())  # (they fit)
+        assert np.array_equal(_host(dx), wx) and np.array_equal(_host(dw), ww), (dtype, slots, N, C)
