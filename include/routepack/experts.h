@@ -109,8 +109,9 @@ int routepack_expert_product(const routepack_mx *x, const routepack_mx *w, int32
  * row_stride):
  *   dx[r][c]    = sum_n dy[r][n] w[s][n][c]               n_rows x C out, or NULL
  *   dw[s][n][c] = sum over slot s's r of dy[r][n] x[r][c]   (n_slots N) x C out, or NULL
- * both of dy's type, row_stride C; not both NULL.  The products are exact (dy is
- * split into bf16 parts).  x is read for dw alone (else its pointers may be
+ * both of dy's type, row_stride C; not both NULL.  The products are exact: dy is
+ * split into bf16 parts (fp32 values below 2^-110 are cut to multiples of 2^-133,
+ * where bf16 ends).  x is read for dw alone (else its pointers may be
  * null), w for dx alone.
  * Errors as routepack_expert_product. */
 int routepack_expert_product_backward(const routepack_matrix *dy, const routepack_mx *x, const routepack_mx *w,

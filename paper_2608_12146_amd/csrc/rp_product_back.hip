@@ -3,7 +3,8 @@
 //   dw[s][n][c] = sum_r dy[r][n] x[r][c]      over the rows r of slot s.
 // A 4-bit value times its power of two is exact in bf16, and dy is split into
 // bf16 parts that add up to it (one for bf16, two for fp16, three for fp32), so
-// bf16 matrix instructions form exact products and add them in 32 bits.
+// bf16 matrix instructions form exact products and add them in 32 bits.  (bf16 ends
+// at multiples of 2^-133, and parts of fp32 values below 2^-110 with it.)
 //
 // Both are the same tile program: A is dy, the output's rows by 64 terms; B is the
 // matrix in 4 bits, 64 terms (its rows) by the output's columns, converted on the

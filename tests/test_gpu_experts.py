@@ -1174,3 +1174,26 @@ def test_product_gradients_keep_every_bit(dtype):
         (wx, _), (ww, _) = X.product_backward(_host(dy), _values(x), _values(w), _host(off))
         assert np.array_equal(wx, torch.as_tensor(wx).to(_type(dtype)).double().numpy())  # (they fit)
         assert np.array_equal(_host(dx), wx) and np.array_equal(_host(dw), ww), (dtype, slots, N, C)
+
+
+@gpu
+def test_product_gradients_of_tiny_values():
+    """bf16 ends at multiples of 2^-133: dy is exact from 2^-110 on in fp32 (24 bits
+    above that), and cut there below; in bf16 it is exact down to its last number."""
+    import torch
+    import paper_2608_12146_amd as rp
+    N, C = 12, 40
+    x, w = _random_mx(1, (9,), C), _random_mx(2, (2, N), C)
+    w.scales[:, :, :2] += 60
+    x.scales[:, :2] += 60
+    off = _offsets([4, 5])
+    for dtype, exponent in (("fp32", -110), ("fp32", -118), ("fp32", -126), ("fp32", -140), ("bf16", -126), ("bf16", -130)):
+        m = 1.0 + torch.rand((9, N), generator=torch.Generator().manual_seed(3), dtype=torch.float64)
+        dy = (m * 2.0 ** exponent).to(_type(dtype)).cuda()
+        dx, dw = rp.expert_product_backward(dy, x, w, off)
+        (wx, mx), (ww, mw) = X.product_backward(_host(dy), _values(x), _values(w), _host(off))
+        (cx, _), (cw, _) = X.product_backward(np.full(dy.shape, 2.0 ** -133 if dtype == "fp32" and exponent < -110 else 0.0),
+                                              np.abs(_values(x)), np.abs(_values(w)), _host(off))
+        parts = 3 if dtype == "fp32" else 1
+        _near(dx, wx, 2 * (parts * N + 136) * U * mx + cx, (dtype, exponent, "dx"))
+        _near(dw, ww, 2 * (parts * 5 + 136) * U * mw + cw, (dtype, exponent, "dw"))
