@@ -1197,3 +1197,72 @@ def test_product_gradients_of_tiny_values():
         parts = 3 if dtype == "fp32" else 1
         _near(dx, wx, 2 * (parts * N + 136) * U * mx + cx, (dtype, exponent, "dx"))
         _near(dw, ww, 2 * (parts * 5 + 136) * U * mw + cw, (dtype, exponent, "dw"))
+
+
+class _Guarded:
+    """A dense output between margins that no call may write: `skew` elements past
+    a vector's boundary."""
+
+    def __init__(self, rows, cols, dtype, skew=0):
+        import torch
+        self.rows, self.cols, self.n = rows, cols, rows * cols
+        self.first = 4096 + skew
+        self.data = torch.full((self.n + self.first + 4096,), 7.0, dtype=_type(dtype), device="cuda")
+        self.type = {"fp32": 0, "bf16": 1, "fp16": 2}[dtype]
+
+    def matrix(self):
+        import paper_2608_12146_amd as rp
+        return rp._MATRIX(self.data.data_ptr() + self.first * self.data.element_size(), self.type, self.rows, self.cols, self.cols)
+
+    def inside(self):
+        return self.data[self.first:self.first + self.n].view(self.rows, self.cols)
+
+    def check(self, what):
+        assert bool((self.data[:self.first] == 7.0).all()) and bool((self.data[self.first + self.n:] == 7.0).all()), what
+
+
+def _packed_args(q):
+    import paper_2608_12146_amd as rp
+    rows = q.codes.shape[0] if q.codes.dim() == 2 else q.codes.shape[0] * q.codes.shape[1]
+    return rp._MX(q.codes.data_ptr(), q.scales.data_ptr(), rows, q.columns)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_outputs_keep_to_their_arrays(dtype):
+    """The products and their gradients write y, dx and dw and nothing next to them:
+    by every kernel, sizes that end inside a tile, outputs off a vector's boundary,
+    and offsets that overlap, decrease or leave the rows."""
+    import torch
+    import paper_2608_12146_amd as rp
+    lib, stream = rp.load_library(), torch.cuda.current_stream().cuda_stream
+    big = 1 << 62
+    cases = [  # offsets, rows, N, C
+        ([0, 1], 1, 1, 1), ([3, 20, 37], 40, 33, 130), ([0, 300, 301, 450], 460, 257, 385), ([0, 64, 200], 210, 520, 100),
+        ([-5, 3, 900], 64, 30, 100), ([20, 10, 4], 64, 30, 100), ([64, 64, 64], 64, 30, 100), ([big, -big, 1], 64, 30, 100),
+        ([-5, 250, 90000], 300, 261, 130), ([200, 100, 40], 300, 261, 130), ([0, 300, 0, 300], 300, 258, 129),
+        ([0, 8000, 3, 8290], 8300, 61, 1030), ([-1, 9000, 9000], 8300, 72, 1026),
+    ]
+    for off, R, N, C in cases:
+        S = len(off) - 1
+        o = torch.tensor(off, device="cuda")
+        x, w = _random_mx(1, (R,), C), _random_mx(2, (S, N), C)
+        dy = _floats(3, (R, N), dtype)
+        d = rp._MATRIX(dy.data_ptr(), {"fp32": 0, "bf16": 1, "fp16": 2}[dtype], R, N, N)
+        lies = off[0] < 0 or off[-1] > R or any(a > b for a, b in zip(off, off[1:]))
+        for skew in (0, 1):
+            what = (dtype, off, R, N, C, skew)
+            _log(what)
+            y, dx, dw = _Guarded(R, N, dtype, skew), _Guarded(R, C, dtype, skew), _Guarded(S * N, C, dtype, skew)
+            assert lib.routepack_expert_product(_packed_args(x), _packed_args(w), S, o.data_ptr(), y.matrix(), stream) == 0
+            assert lib.routepack_expert_product_backward(d, _packed_args(x), _packed_args(w), S, o.data_ptr(), dx.matrix(),
+                                                         dw.matrix(), stream) == 0
+            only = _Guarded(S * N, C, dtype, skew)  # (a launch of its own)
+            assert lib.routepack_expert_product_backward(d, _packed_args(x), _packed_args(w), S, o.data_ptr(), None,
+                                                         only.matrix(), stream) == 0
+            for g in (y, dx, dw, only):
+                g.check(what)
+            if not lies:
+                assert torch.equal(y.inside(), rp.expert_product(x, w, o, dtype=_type(dtype))), what
+                for g, want in zip((dx, dw, only), [*(r := rp.expert_product_backward(dy, x, w, o)), r[1]]):
+                    assert torch.equal(g.inside(), want.view(g.rows, g.cols)), what
