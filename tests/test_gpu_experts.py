@@ -1266,3 +1266,39 @@ def test_outputs_keep_to_their_arrays(dtype):
                 assert torch.equal(y.inside(), rp.expert_product(x, w, o, dtype=_type(dtype))), what
                 for g, want in zip((dx, dw, only), [*(r := rp.expert_product_backward(dy, x, w, o)), r[1]]):
                     assert torch.equal(g.inside(), want.view(g.rows, g.cols)), what
+
+
+@gpu
+def test_large_calls_recorded_into_a_graph():
+    """The kernels of many chunks, many rows and wide tiles, which ask for more LDS
+    than a launch has by itself, captured and replayed with eager calls between."""
+    import torch
+    import paper_2608_12146_amd as rp
+    prob = _problem(1, 2048, 4)
+    ids = torch.randint(0, 2048, (3000, 4), generator=torch.Generator().manual_seed(1)).cuda()
+    R, N, C, S = 32768, 136, 300, 8
+    x, w = _random_mx(1, (R,), C), _random_mx(2, (S, N), C)
+    off = _offsets([4000, 0, 5000, 3001, 7000, 6000, 3999, 3768])
+    dys = [_floats(3, (R, N), t, scale=0.1) for t in ("bf16", "fp16", "fp32")]
+
+    def step():
+        order = rp.order_tokens(prob, ids)
+        out = [order.rows, order.offsets, order.places, rp.expert_product(x, w, off)]
+        for dy in dys:
+            out += rp.expert_product_backward(dy, x, w, off)
+        return out
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = step()
+    for n in range(4):
+        ids.copy_(torch.randint(0, 2048, (3000, 4), generator=torch.Generator().manual_seed(10 + n)))
+        dys[n % 3].copy_(_floats(20 + n, (R, N), "fp32", scale=0.1))
+        want = step()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), n
