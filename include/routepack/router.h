@@ -112,7 +112,9 @@ int routepack_route_tokens(const routepack_problem *prob, const routepack_logits
  *   gates    float [T][L][k] out
  * Errors as there, and E_INVALID when n_groups < 1 does not divide E, keep is
  * outside [1, n_groups], group_top is neither 1 nor 2, or k exceeds the experts
- * of `keep` groups; E_UNSUPPORTED when E > 1024 or n_groups > 64. */
+ * of `keep` groups; E_UNSUPPORTED when E > 1024 or n_groups > 64 (a wave holds a
+ * token in lanes of whole groups, with their number rounded up to a power of two:
+ * of 2048 experts that may be twice what it has room for). */
 int routepack_route_grouped(const routepack_problem *prob, const routepack_logits *logits, const float *bias,
                             int32_t n_groups, int32_t keep, int32_t group_top, int32_t score,
                             int32_t normalize, float scale, int32_t *ids, float *gates,

@@ -3,10 +3,11 @@
 A thin ctypes layer over the C-ABI in include/routepack.h and, for the
 router's and the experts' operators, include/routepack/router.h and experts.h
 (libroutepack.so).  It only marshals arguments (and lets autograd record the
-router's gates and loss, the experts' products and their sums): torch supplies device memory and the current HIP stream, and every step
-of the path runs in the library's HIP kernels.  There is no CPU fallback:
-importing works without a GPU, but every call raises if the library or a GPU
-is missing.
+router's gates and loss, quantized matrices, the experts' products and their
+sums, in reverse mode): torch supplies device memory and the current HIP stream,
+and every step of the path runs in the library's HIP kernels.  There is no CPU
+fallback: importing works without a GPU, but every call raises if the library or
+a GPU is missing.
 """
 from __future__ import annotations
 

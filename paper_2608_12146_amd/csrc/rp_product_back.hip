@@ -12,9 +12,9 @@
 // read through the transposing LDS loads (16 lanes read 4 terms of 16 columns and
 // each receives a column's 4 terms).
 //
-// 24558 rows, 60 x 1408 x 1984 bf16: dx 190 us, dw 215 (1.37e11 operations each,
-// 110 us at a large bf16 product's rate).  Bound by LDS (about 80 us of cycles each)
-// and by the waits between its two phases.
+// 24558 rows, 60 x 1408 x 1984 bf16: dx 174 us, dw 207 (1.37e11 operations each,
+// 110 us at a large bf16 product's rate).  Bound by LDS (77 and 88 us of its cycles,
+// 57 and 59 of the matrix cores') and by the waits between its two phases.
 #include "rp_product.h"
 
 namespace rp {
@@ -340,8 +340,8 @@ __global__ void __launch_bounds__(128 * WN, WAVES) k_product_back(BackProductArg
     back_tile<T, DW, WN, MB, NB>(a, group_index(), lds);
 }
 
-// Both gradients of a small problem in one launch (100 tokens x 8, 64 x 512 x 512:
-// 29 us for both; 31 and 13 in launches of their own).
+// Both gradients of a small problem in one launch (100 tokens x 8, 64 x 512 x 512
+// bf16: 13.2 us for both; 10.7 and 10.4 in launches of their own).
 template <class T, int WN, int MB, int NB, int WAVES>
 __global__ void __launch_bounds__(128 * WN, WAVES) k_product_back_both(BackProductArgs x, BackProductArgs w) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -381,7 +381,8 @@ int launch_back(Kernel kern, int64_t groups, hipStream_t stream, const Args &...
 // eight of 64 x 64, which wait less (194 us, 209 on four).  Else tiles of 128 x 128,
 // more of them at a time: for dw, whose sums are short, up to several rounds of the
 // chip, and always with bf16 (those rows: 220 us either way; 60000 rows, 128 x 256 x
-// 256: 59 us, 85 by the wide ones).
+// 256: 59 us, 85 by the wide ones).  The wide kernels with parts hold all 256
+// registers; dw spills 26 (fp16) and 21 (fp32) to scratch, dx one (fp32).
 template <class T>
 int back_of(BackProductArgs *x, BackProductArgs *w, hipStream_t stream) {
     constexpr int kWaves = kParts<T> == 1 ? 3 : 2;

@@ -14,8 +14,12 @@
 // Without a bias the keys' order is the logits', and only sums of two scores
 // rank groups.  Scores are compared in 64 bits, as two implementations in 32
 // bits would choose differently: they are formed in 32 bits, and where their
-// error leaves the groups kept, the choices or their order open (about one token
-// in 500 in fp32; with a bias ties too), the wave forms them in 64.
+// error leaves the groups kept, the choices or their order open, the wave forms
+// them in 64.  With a bias that is one token in 200 at most, and ties.  Without one
+// the error is absolute while the scores of wide logits crowd at 0 (or 1), and it
+// grows with the logits' deviation: of 256 experts in 8 groups, 8 choices, at 1.5, 5
+// and 8 softmax leaves 0.3, 8 and 37% of the tokens open (65536 fp32: 44, 72, 145 us)
+// and logistic scores 0.1, 56 and 100% (34, 143, 176 us).
 //
 // Bound by HBM and vector instructions: 131072 x 512 bf16, 8 groups: 40 us
 // (a copy of the logits takes 26); 65536 x 256 fp32, logistic, two keys a group
